@@ -388,6 +388,103 @@ int32_t dl_sparse_attn_decode_fp8_layers(dl_ctx* ctx, int32_t L, const void* q_t
                                          const float* v_scales, int32_t* cache_len, const uint8_t* keep, int32_t B,
                                          int32_t cap, float scale, void* out, int32_t commit, void* stream);
 
+/* ---- extension, NOT in the paper: whole prompts, packed ----------------------------------- */
+
+/* Causal attention over whole prompts of different lengths, packed one behind the other, with grouped heads: what the
+ * layers in front of the token selection compute (Eq. 1 on every token), before any cache exists.
+ *   Row i of sequence b (packed row starts[b] + i) attends rows 0..i of the same sequence; query head h reads K/V head
+ *   h / (n_heads / n_kv_heads).
+ *   q [total][n_heads][D], k, v [total][n_kv_heads][D] dev bf16; q_stride, kv_stride: elements from one token's row to the
+ *   next (0: dense), multiples of 8, so that q, k and v may be parts of one projection's output;
+ *   starts dev [B + 1]: starts[b] <= starts[b + 1] <= total; equal ones make an empty sequence;
+ *   max_rows HOST: no sequence is longer (rows behind it are not computed);
+ *   out dev [total][n_heads][D] dense; rows of no sequence are left as they were.
+ * A list of starts that breaks these rules records DL_ERR_INVALID_ARG with the sequence (if there is a workspace); nothing
+ * is read or written outside the tensors.  A NaN or an infinity in v of a token may reach every row of its sequence that
+ * shares a block of 128 keys with it, earlier ones too (0 * NaN in a matrix product).
+ * bf16 models only (DL_ERR_UNSUPPORTED otherwise).  No workspace needed. */
+int32_t dl_attn_prefill_packed(dl_ctx* ctx, const void* q, const void* k, const void* v, int64_t q_stride,
+                               int64_t kv_stride, const int32_t* starts, int32_t B, int32_t n_kv_heads, int32_t total,
+                               int32_t max_rows, float scale, void* out, void* stream);
+
+/* ---- extension, NOT in the paper: caches in pages ------------------------------------------- */
+
+/* The books of a paged cache.  All pointers dev, caller-owned.  Sequence b's rows [i * page_rows, (i + 1) * page_rows) are
+ * in page table[b][i] of every pool (one pool per layer, say) that goes by these books. */
+typedef struct {
+  int32_t B;           /* sequences (slots), up to 2048 */
+  int32_t n_pages;     /* pages of a pool */
+  int32_t max_pages;   /* columns of the table */
+  int32_t page_rows;   /* 16, 32, 64 or 128 */
+  int32_t* table;      /* [B][max_pages] page numbers; -1 behind a sequence's last page, and nowhere else */
+  int32_t* refs;       /* [n_pages] table entries that name the page; 0: free */
+  int32_t* len;        /* [B] rows held */
+} dl_pages;
+
+/* Bytes of scratch for dl_pages_fork and dl_pages_compact.  Negative on bad arguments. */
+int64_t dl_pages_scratch_bytes(const dl_ctx* ctx, const dl_pages* pages);
+
+/* Gives every sequence the pages that len[b] + need[b] rows take (need dev [B]; negative counts as 0): the free pages with
+ * the lowest numbers, handed out in order of b.  All or nothing: if the free pages or a row of the table do not suffice
+ * nothing changes and DL_ERR_CAPACITY is recorded (detail: the sequence whose table row is too short, else -1). */
+int32_t dl_pages_reserve(dl_ctx* ctx, const dl_pages* pages, const int32_t* need, void* stream);
+
+/* Gives back all pages of the sequences with gone[b] != 0 (gone dev [B]) and sets their lengths to 0; a page that another
+ * sequence shares stays in use. */
+int32_t dl_pages_free(dl_ctx* ctx, const dl_pages* pages, const uint8_t* gone, void* stream);
+
+/* Every sequence b becomes what sequence parent[b] was before the call (parent dev [B]; parent[b] == b: stays as it is, with
+ * the pages reserved for it; -1: empty).  What b held is given back.  Full pages are shared; a partly filled last page
+ * stays with one holder (the parent if it stays, else its lowest child) and is copied, in all pools, for each other child,
+ * into the lowest free pages in order of b (pages given back by this call among them).  All or nothing as above (detail -1);
+ * a parent out of range records DL_ERR_INVALID_ARG with b, and b stays as it is.
+ *   pools HOST array of n_pools dev pointers, each [n_pages][page_bytes]; page_bytes a multiple of 16;
+ *   scratch dev, 256-byte aligned, caller-owned. */
+int32_t dl_pages_fork(dl_ctx* ctx, const dl_pages* pages, const int32_t* parent, int32_t n_pools, void* const* pools,
+                      int64_t page_bytes, void* scratch, int64_t scratch_bytes, void* stream);
+
+/* Moves the pages in use to the front: afterwards they are pages 0 .. n - 1, n = the number in use, which goes to
+ * *n_live (dev, may be NULL).  A used page with number >= n moves to a free one below, both taken in ascending order;
+ * the others stay.  Arguments as above. */
+int32_t dl_pages_compact(dl_ctx* ctx, const dl_pages* pages, int32_t n_pools, void* const* pools, int64_t page_bytes,
+                         int32_t* n_live, void* scratch, int64_t scratch_bytes, void* stream);
+
+/* ---- extension, NOT in the paper: K/V cache in 4 bits, in pages, with grouped heads --------- */
+
+/* K and V rows in 4 bits under one scale and one lowest value for every 64 dims:  value = s * code + z,  z = min,
+ * s = bf16((max - min) / 15), code = nearest((x - z) * (1 / s)) (ties to even), clipped to 0..15; each operation in fp32.
+ * Where s < 2^-126 all codes are 0.  64 dims with a NaN or an infinity among them (or a range beyond fp32) hold NaN.
+ * K and V share a pool; how a page is laid out inside is the library's business (dl_kv4_read gives the values).
+ * bf16 models, n_heads / n_kv_heads up to 16 (DL_ERR_UNSUPPORTED otherwise).  These calls need the workspace. */
+
+/* Bytes of one page of a pool: n_kv_heads * page_rows * 9 D / 8.  Negative on bad arguments. */
+int64_t dl_kv4_page_bytes(const dl_ctx* ctx, int32_t n_kv_heads, int32_t page_rows);
+
+/* dl_compact_kv for such a cache: appends to every sequence, from row len[b] on and in order, its packed rows
+ * [starts[b], starts[b + 1]) whose keep flag is not 0; with commit, len[b] += their number.  Layers that share a decision
+ * pass commit = 0 but for the last.
+ *   k, v dev bf16 [total][n_kv_heads][D], kv_stride elements from row to row (0: dense; a multiple of 8); starts dev
+ *   [B + 1], ascending; keep dev [total] or NULL (all); pool dev [n_pages][page bytes].
+ * The pages must be reserved: a sequence that lacks one is left untouched and records DL_ERR_CAPACITY with its index.
+ * Pages that other sequences share must not be written: a fork leaves every partly filled page to one sequence. */
+int32_t dl_kv4_append(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, void* pool, const void* k, const void* v,
+                      int64_t kv_stride, const int32_t* starts, const uint8_t* keep, int32_t total, int32_t commit,
+                      void* stream);
+
+/* The values of rows row0[b], row0[b] + 1, ... of every sequence, rounded to bf16, packed: starts[b + 1] - starts[b] rows of
+ * sequence b from packed row starts[b] on.  row0 dev [B]; k_out, v_out dev [total][n_kv_heads][D].  A row without a page
+ * reads as zero and records DL_ERR_INVALID_ARG with b. */
+int32_t dl_kv4_read(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, const void* pool, const int32_t* row0,
+                    const int32_t* starts, int32_t total, void* k_out, void* v_out, void* stream);
+
+/* dl_sparse_attn_decode (Eq. 6) over such a cache: one new token per sequence attends the values of rows [0, len[b]) and
+ * its own bf16 k_t, v_t; where keep[b] != 0 its row is appended in 4 bits at row len[b] (the page must be reserved, else
+ * DL_ERR_CAPACITY and no write).  Lengths are not advanced: dl_commit_len (cap = max_pages * page_rows) closes the step.
+ *   q_t, out dev bf16 [B][n_heads][D]; k_t, v_t dev bf16 [B][n_kv_heads][D]; keep dev [B] or NULL.
+ * Rows below len[b] without a page are left out and record DL_ERR_INVALID_ARG with b. */
+int32_t dl_kv4_attn_decode(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, void* pool, const void* q_t,
+                           const void* k_t, const void* v_t, const uint8_t* keep, float scale, void* out, void* stream);
+
 /* ---- checked build ---------------------------------------------------------------------- */
 
 /* The library can be built with -DDL_BOUNDS=1 (libdl_sparse_checked.so): every store a kernel makes through an

@@ -35,6 +35,8 @@ EXPORTS = [
     "dl_predictor2_scratch_bytes", "dl_predictor2_values", "dl_prefill_select2", "dl_decode_keep2",
     "dl_decode_step_stack", "dl_quantize_kv_fp8", "dl_sparse_attn_decode_fp8", "dl_build_is_checked",
     "dl_selftest_bounds", "dl_sparse_attn_decode_fp8_layers",
+    "dl_attn_prefill_packed", "dl_pages_scratch_bytes", "dl_pages_reserve", "dl_pages_free", "dl_pages_fork",
+    "dl_pages_compact", "dl_kv4_page_bytes", "dl_kv4_append", "dl_kv4_read", "dl_kv4_attn_decode",
 ]
 
 
@@ -61,6 +63,38 @@ class LayerStackDesc(C.Structure):
 class Predictor2Desc(C.Structure):
     _fields_ = [("inp", LinearDesc), ("n_blocks", C.c_int32), ("blocks", C.POINTER(VitBlockDesc)),
                 ("h1", LinearDesc), ("h2", LinearDesc), ("w3", C.c_void_p), ("b3", C.c_void_p)]
+
+
+class PagesDesc(C.Structure):
+    _fields_ = [("B", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("page_rows", C.c_int32),
+                ("table", C.c_void_p), ("refs", C.c_void_p), ("len", C.c_void_p)]
+
+
+class Pages:
+    """The books of a paged cache (dl_pages in dl.h) as device tensors: `table` [B, max_pages] (-1 where there is no
+    page), `refs` [n_pages], `cache_len` [B], all int32 views of one tensor, `book`."""
+
+    def __init__(self, B: int, n_pages: int, max_pages: int, page_rows: int, device="cuda"):
+        self.B, self.n_pages, self.max_pages, self.page_rows = B, n_pages, max_pages, page_rows
+        up = lambda n: (n + 3) // 4 * 4                              # 16-byte steps
+        a, b = up(B * max_pages), up(n_pages)
+        self.book = torch.zeros(a + b + up(B), dtype=torch.int32, device=device)
+        self.table = self.book[:B * max_pages].view(B, max_pages)
+        self.table.fill_(-1)
+        self.refs = self.book[a:a + n_pages]
+        self.cache_len = self.book[a + b:a + b + B]
+        self.desc = PagesDesc(B, n_pages, max_pages, page_rows, self.table.data_ptr(), self.refs.data_ptr(),
+                              self.cache_len.data_ptr())
+        self._scratch = None
+
+    def scratch(self, ctx: "Context") -> torch.Tensor:
+        """Scratch of dl_pages_fork and dl_pages_compact, allocated at the first use."""
+        if self._scratch is None:
+            n = lib().dl_pages_scratch_bytes(ctx._h, C.byref(self.desc))
+            if n < 0:
+                raise DlError(int(n), "dl_pages_scratch_bytes")
+            self._scratch = torch.empty(max(int(n), 256), dtype=torch.uint8, device=self.book.device)
+        return self._scratch
 
 
 class PredictorDesc(C.Structure):
@@ -140,6 +174,16 @@ def lib() -> C.CDLL:
             "dl_selftest_bounds": (i32, [vp, vp]),
             "dl_quantize_kv_fp8": (i32, [vp, vp, vp, vp, i32, i32, vp, vp]),
             "dl_sparse_attn_decode_fp8": (i32, [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, f32, vp, vp]),
+            "dl_attn_prefill_packed": (i32, [vp, vp, vp, vp, i64, i64, vp, i32, i32, i32, i32, f32, vp, vp]),
+            "dl_pages_scratch_bytes": (i64, [vp, C.POINTER(PagesDesc)]),
+            "dl_pages_reserve": (i32, [vp, C.POINTER(PagesDesc), vp, vp]),
+            "dl_pages_free": (i32, [vp, C.POINTER(PagesDesc), vp, vp]),
+            "dl_pages_fork": (i32, [vp, C.POINTER(PagesDesc), vp, i32, C.POINTER(vp), i64, vp, i64, vp]),
+            "dl_pages_compact": (i32, [vp, C.POINTER(PagesDesc), i32, C.POINTER(vp), i64, vp, vp, i64, vp]),
+            "dl_kv4_page_bytes": (i64, [vp, i32, i32]),
+            "dl_kv4_append": (i32, [vp, C.POINTER(PagesDesc), i32, vp, vp, vp, i64, vp, vp, i32, i32, vp]),
+            "dl_kv4_read": (i32, [vp, C.POINTER(PagesDesc), i32, vp, vp, vp, i32, vp, vp, vp]),
+            "dl_kv4_attn_decode": (i32, [vp, C.POINTER(PagesDesc), i32, vp, vp, vp, vp, vp, f32, vp, vp]),
             "dl_decode_step_host": (i32, [vp, P, vp, i32, f32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                           vp, vp, C.POINTER(vp), C.POINTER(vp), i32, vp, f32, vp]),
             "dl_decode_steps_host": (i32, [vp, P, i32, i32, f32, i32, C.POINTER(vp), C.POINTER(vp), C.POINTER(vp),
@@ -168,6 +212,19 @@ def _ptr(t):
             raise ValueError("tensor must be contiguous")
         return t.data_ptr()
     return int(t)
+
+
+def _rows(t, what: str):
+    """Pointer and row stride (in elements) of packed rows [total, heads, D] whose last two dimensions are dense."""
+    if t.dim() != 3 or (t.shape[0] > 0 and (t.stride(2) != 1 or t.stride(1) != t.shape[2])):
+        raise ValueError(f"{what}: want [rows, heads, D] with dense heads")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2])
+
+
+def _want(t, dtype, shape, what: str):
+    """A tensor the kernels will read or write by this shape and type."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: want {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
 
 
 def _stream(stream=None):
@@ -385,6 +442,108 @@ class Context:
         self._check(lib().dl_decode_keep2(self._h, C.byref(p.desc), _ptr(x_t), x_t.shape[0], _ptr(scratch),
                                           scratch.numel(), _ptr(d_out), _ptr(keep_out), _stream(stream)),
                     "dl_decode_keep2")
+
+    # ---- packed prompts, pages, the 4-bit cache (extensions, not in the paper)
+    def attn_prefill_packed(self, q, k, v, starts, max_rows, scale, out, stream=None):
+        """dl_attn_prefill_packed: q [total, n_heads, D], k / v [total, n_kv_heads, D] (parts of one projection's output
+        will do: rows may be strided), starts int32 [B + 1], max_rows: length of the longest sequence."""
+        total, n_kv = q.shape[0], k.shape[1]
+        _want(q, self.dtype, (total, self.H, self.D), "q")
+        _want(k, self.dtype, (total, n_kv, self.D), "k")
+        _want(v, self.dtype, (total, n_kv, self.D), "v")
+        _want(out, self.dtype, (total, self.H, self.D), "out")
+        _want(starts, torch.int32, (starts.numel(),), "starts")
+        (qp, qs), (kp, ks), (vp, vs) = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
+        if ks != vs:
+            raise ValueError("k and v must have the same row stride")
+        self._check(lib().dl_attn_prefill_packed(self._h, qp, kp, vp, qs, ks, _ptr(starts), starts.numel() - 1, n_kv, total,
+                                                 int(max_rows), float(scale), _ptr(out), _stream(stream)),
+                    "dl_attn_prefill_packed")
+
+    def pages_reserve(self, pages: Pages, need, stream=None):
+        _want(need, torch.int32, (pages.B,), "need")
+        self._check(lib().dl_pages_reserve(self._h, C.byref(pages.desc), _ptr(need), _stream(stream)), "dl_pages_reserve")
+
+    def pages_free(self, pages: Pages, gone, stream=None):
+        _want(gone, torch.uint8, (pages.B,), "gone")
+        self._check(lib().dl_pages_free(self._h, C.byref(pages.desc), _ptr(gone), _stream(stream)), "dl_pages_free")
+
+    def _pools(self, pages: Pages, pools):
+        for p in pools:
+            if p.shape[0] != pages.n_pages or not p.is_contiguous() or p.numel() * p.element_size() != pools[0].numel() * pools[0].element_size():
+                raise ValueError("pools: want contiguous tensors [n_pages, ...] of one size")
+        page_bytes = pools[0].numel() * pools[0].element_size() // pages.n_pages if pools else 0
+        return len(pools), self.pointer_array(pools), page_bytes
+
+    def pages_fork(self, pages: Pages, parent, pools, stream=None):
+        """dl_pages_fork; pools: list of tensors [n_pages, ...], one per layer."""
+        _want(parent, torch.int32, (pages.B,), "parent")
+        n, arr, page_bytes = self._pools(pages, pools)
+        scratch = pages.scratch(self)
+        self._check(lib().dl_pages_fork(self._h, C.byref(pages.desc), _ptr(parent), n, arr, page_bytes, _ptr(scratch),
+                                        scratch.numel(), _stream(stream)), "dl_pages_fork")
+
+    def pages_compact(self, pages: Pages, pools, n_live=None, stream=None):
+        """dl_pages_compact; n_live: int32 tensor [1] for the number of pages in use, or None."""
+        if n_live is not None:
+            _want(n_live, torch.int32, (1,), "n_live")
+        n, arr, page_bytes = self._pools(pages, pools)
+        scratch = pages.scratch(self)
+        self._check(lib().dl_pages_compact(self._h, C.byref(pages.desc), n, arr, page_bytes, _ptr(n_live), _ptr(scratch),
+                                           scratch.numel(), _stream(stream)), "dl_pages_compact")
+
+    def kv4_pool(self, pages: Pages, n_kv_heads: int) -> torch.Tensor:
+        """A pool of 4-bit pages (uint8 [n_pages, page bytes]) for these books."""
+        n = lib().dl_kv4_page_bytes(self._h, n_kv_heads, pages.page_rows)
+        if n < 0:
+            raise DlError(int(n), "dl_kv4_page_bytes")
+        return torch.zeros(pages.n_pages, int(n), dtype=torch.uint8, device=pages.book.device)
+
+    def _want_pool(self, pages: Pages, pool, n_kv: int):
+        n = lib().dl_kv4_page_bytes(self._h, n_kv, pages.page_rows)
+        if n < 0:
+            raise DlError(int(n), "dl_kv4_page_bytes")
+        _want(pool, torch.uint8, (pages.n_pages, int(n)), "pool")
+
+    def kv4_append(self, pages: Pages, pool, k, v, starts, keep=None, commit=True, stream=None):
+        """dl_kv4_append: k, v [total, n_kv_heads, D] bf16 (rows may be strided), starts int32 [B + 1], keep uint8 [total]."""
+        total, n_kv = k.shape[0], k.shape[1]
+        _want(k, self.dtype, (total, n_kv, self.D), "k")
+        _want(v, self.dtype, (total, n_kv, self.D), "v")
+        _want(starts, torch.int32, (pages.B + 1,), "starts")
+        if keep is not None:
+            _want(keep, torch.uint8, (total,), "keep")
+        self._want_pool(pages, pool, n_kv)
+        (kp, ks), (vp, vs) = _rows(k, "k"), _rows(v, "v")
+        if ks != vs:
+            raise ValueError("k and v must have the same row stride")
+        self._check(lib().dl_kv4_append(self._h, C.byref(pages.desc), n_kv, _ptr(pool), kp, vp, ks, _ptr(starts), _ptr(keep),
+                                        total, int(bool(commit)), _stream(stream)), "dl_kv4_append")
+
+    def kv4_read(self, pages: Pages, pool, row0, starts, k_out, v_out, stream=None):
+        """dl_kv4_read: rows from row0[b] on of every sequence into k_out, v_out [total, n_kv_heads, D] bf16."""
+        total, n_kv = k_out.shape[0], k_out.shape[1]
+        _want(k_out, self.dtype, (total, n_kv, self.D), "k_out")
+        _want(v_out, self.dtype, (total, n_kv, self.D), "v_out")
+        _want(row0, torch.int32, (pages.B,), "row0")
+        _want(starts, torch.int32, (pages.B + 1,), "starts")
+        self._want_pool(pages, pool, n_kv)
+        self._check(lib().dl_kv4_read(self._h, C.byref(pages.desc), n_kv, _ptr(pool), _ptr(row0), _ptr(starts), total,
+                                      _ptr(k_out), _ptr(v_out), _stream(stream)), "dl_kv4_read")
+
+    def kv4_attn_decode(self, pages: Pages, pool, q_t, k_t, v_t, keep, scale, out, stream=None):
+        """dl_kv4_attn_decode: q_t, out [B, n_heads, D]; k_t, v_t [B, n_kv_heads, D]; keep uint8 [B] or None."""
+        n_kv = k_t.shape[1]
+        _want(q_t, self.dtype, (pages.B, self.H, self.D), "q_t")
+        _want(out, self.dtype, (pages.B, self.H, self.D), "out")
+        _want(k_t, self.dtype, (pages.B, n_kv, self.D), "k_t")
+        _want(v_t, self.dtype, (pages.B, n_kv, self.D), "v_t")
+        if keep is not None:
+            _want(keep, torch.uint8, (pages.B,), "keep")
+        self._want_pool(pages, pool, n_kv)
+        self._check(lib().dl_kv4_attn_decode(self._h, C.byref(pages.desc), n_kv, _ptr(pool), _ptr(q_t), _ptr(k_t),
+                                             _ptr(v_t), _ptr(keep), float(scale), _ptr(out), _stream(stream)),
+                    "dl_kv4_attn_decode")
 
     def selftest_wait_timeout(self, polls: int = 64, stream=None):
         self._check(lib().dl_selftest_wait_timeout(self._h, int(polls), _stream(stream)), "dl_selftest_wait_timeout")

@@ -9,7 +9,7 @@ namespace dl {
 
 static inline int64_t align256(int64_t v) { return (v + 255) & ~int64_t(255); }
 
-int64_t workspace_layout(const dl_model_desc& d, int32_t max_batch, int32_t max_rows, int32_t cap,
+int64_t workspace_layout(const dl_model_desc& d, int32_t sm_count, int32_t max_batch, int32_t max_rows, int32_t cap,
                          Workspace* ws) {
   int64_t off = 0;
   auto take = [&](int64_t bytes) { int64_t o = off; off = align256(off + bytes); return o; };
@@ -26,6 +26,7 @@ int64_t workspace_layout(const dl_model_desc& d, int32_t max_batch, int32_t max_
   const int64_t o_pstick = take((int64_t)kPredMaxSplit * 4);
   const int64_t o_commit = take(2 * 4);
   const int64_t o_ones = take(max_batch);
+  const int64_t o_kv4 = take(d.dtype == DL_BF16 ? kv4_scratch_floats(sm_count, d) * 4 : 0);
   if (ws) {
     char* b = ws->base;
     ws->status = reinterpret_cast<DeviceStatus*>(b + o_status);
@@ -41,6 +42,7 @@ int64_t workspace_layout(const dl_model_desc& d, int32_t max_batch, int32_t max_
     ws->dec_commit = reinterpret_cast<int32_t*>(b + o_commit);
     ws->ones = reinterpret_cast<uint8_t*>(b + o_ones);
     ws->pred_rows_padded = rows_pad;
+    ws->kv4_partial = reinterpret_cast<float*>(b + o_kv4);
     ws->max_batch = max_batch; ws->max_rows = max_rows; ws->cap = cap;
   }
   return off;
@@ -135,20 +137,20 @@ int32_t dl_destroy(dl_ctx* ctx) {
 
 int64_t dl_workspace_bytes(const dl_ctx* ctx, int32_t max_batch, int32_t max_rows, int32_t cap) {
   if (!ctx || max_batch <= 0 || max_rows < 0 || cap <= 0) return DL_ERR_INVALID_ARG;
-  return workspace_layout(ctx->desc, max_batch, max_rows, cap, nullptr);
+  return workspace_layout(ctx->desc, ctx->sm_count, max_batch, max_rows, cap, nullptr);
 }
 
 int32_t dl_set_workspace(dl_ctx* ctx, void* dev_ptr, int64_t bytes, int32_t max_batch, int32_t max_rows,
                          int32_t cap, void* stream) {
   if (!ctx || !dev_ptr || max_batch <= 0 || max_rows < 0 || cap <= 0) return DL_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(dev_ptr) & 255u) return DL_ERR_ALIGNMENT;
-  const int64_t need = workspace_layout(ctx->desc, max_batch, max_rows, cap, nullptr);
+  const int64_t need = workspace_layout(ctx->desc, ctx->sm_count, max_batch, max_rows, cap, nullptr);
   if (bytes < need) return DL_ERR_WORKSPACE;
   DeviceGuard g(ctx->device);
   ctx->ws = Workspace();
   ctx->ws.base = static_cast<char*>(dev_ptr);
   ctx->ws.bytes = bytes;
-  workspace_layout(ctx->desc, max_batch, max_rows, cap, &ctx->ws);
+  workspace_layout(ctx->desc, ctx->sm_count, max_batch, max_rows, cap, &ctx->ws);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaMemsetAsync(ctx->ws.status, 0, sizeof(DeviceStatus), s);
   if (e == cudaSuccess)
@@ -698,6 +700,154 @@ int32_t dl_decode_steps_host(dl_ctx* ctx, const dl_predictor* p_txt, int32_t n_s
   if (st != DL_OK) return st;
   if (e == cudaSuccess) e = e1 != cudaSuccess ? e1 : (e2 != cudaSuccess ? e2 : e3);
   return cuda_status(ctx, e);
+}
+
+// ---- packed prompts, pages, 4-bit cache
+
+static int32_t check_pages(const dl_ctx* ctx, const dl_pages* p) {
+  if (!ctx || !p || p->B < 0 || p->n_pages <= 0 || p->max_pages <= 0) return DL_ERR_INVALID_ARG;
+  if (p->page_rows != 16 && p->page_rows != 32 && p->page_rows != 64 && p->page_rows != 128) return DL_ERR_UNSUPPORTED;
+  if (p->B > 2048 || (int64_t)p->max_pages * p->page_rows >= (1LL << 31)) return DL_ERR_UNSUPPORTED;
+  if (p->B > 0 && (!p->table || !p->refs || !p->len)) return DL_ERR_INVALID_ARG;
+  if (misaligned(p->table) || misaligned(p->refs) || misaligned(p->len)) return DL_ERR_ALIGNMENT;
+  return DL_OK;
+}
+
+static int32_t check_kv4(const dl_ctx* ctx, const dl_pages* p, int32_t n_kv_heads, const void* pool) {
+  const int32_t st = check_pages(ctx, p);
+  if (st != DL_OK) return st;
+  if (n_kv_heads <= 0 || ctx->desc.n_heads % n_kv_heads != 0 || !pool) return DL_ERR_INVALID_ARG;
+  if (misaligned(pool)) return DL_ERR_ALIGNMENT;
+  if (ctx->desc.dtype != DL_BF16 || ctx->desc.n_heads / n_kv_heads > 16) return DL_ERR_UNSUPPORTED;
+  // tiles of 16 rows are counted in 32 bits, of the pool and of a call
+  const int64_t tiles = (int64_t)n_kv_heads * (p->page_rows / 16);
+  if (tiles * p->n_pages >= (1LL << 31) || tiles * p->max_pages * (p->B > 0 ? p->B : 1) >= (1LL << 31)) return DL_ERR_UNSUPPORTED;
+  if (!ctx->ws.base || p->B > ctx->ws.max_batch) return DL_ERR_WORKSPACE;
+  return DL_OK;
+}
+
+int32_t dl_attn_prefill_packed(dl_ctx* ctx, const void* q, const void* k, const void* v, int64_t q_stride,
+                               int64_t kv_stride, const int32_t* starts, int32_t B, int32_t n_kv_heads, int32_t total,
+                               int32_t max_rows, float scale, void* out, void* stream) {
+  if (!ctx || B < 0 || total < 0 || max_rows < 0 || n_kv_heads <= 0 || ctx->desc.n_heads % n_kv_heads != 0)
+    return DL_ERR_INVALID_ARG;
+  if (!(scale > 0.f)) return DL_ERR_INVALID_ARG;
+  if (!attn_packed_supported(ctx)) return DL_ERR_UNSUPPORTED;
+  if (B == 0 || total == 0 || max_rows == 0) return DL_OK;
+  if (!q || !k || !v || !starts || !out) return DL_ERR_INVALID_ARG;
+  const int64_t D = ctx->desc.head_dim, qw = D * ctx->desc.n_heads, kw = D * n_kv_heads;
+  if (q_stride == 0) q_stride = qw;
+  if (kv_stride == 0) kv_stride = kw;
+  if (q_stride < qw || kv_stride < kw) return DL_ERR_INVALID_ARG;
+  if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out) || q_stride % 8 != 0 || kv_stride % 8 != 0)
+    return DL_ERR_ALIGNMENT;
+  if (q_stride >= (1LL << 32) || kv_stride >= (1LL << 32) || B >= (1 << 24)) return DL_ERR_UNSUPPORTED;
+  DeviceGuard g(ctx->device);
+  return cuda_status(ctx, launch_attn_packed(ctx, q, k, v, q_stride, kv_stride, starts, B, n_kv_heads, total, max_rows,
+                                             scale, out, static_cast<cudaStream_t>(stream)));
+}
+
+int64_t dl_pages_scratch_bytes(const dl_ctx* ctx, const dl_pages* pages) {
+  const int32_t st = check_pages(ctx, pages);
+  return st != DL_OK ? st : align256(pages_scratch_bytes(pages));
+}
+
+int32_t dl_pages_reserve(dl_ctx* ctx, const dl_pages* pages, const int32_t* need, void* stream) {
+  const int32_t st = check_pages(ctx, pages);
+  if (st != DL_OK) return st;
+  if (pages->B == 0) return DL_OK;
+  if (!need) return DL_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  return cuda_status(ctx, launch_pages_reserve(ctx, pages, need, static_cast<cudaStream_t>(stream)));
+}
+
+int32_t dl_pages_free(dl_ctx* ctx, const dl_pages* pages, const uint8_t* gone, void* stream) {
+  const int32_t st = check_pages(ctx, pages);
+  if (st != DL_OK) return st;
+  if (pages->B == 0) return DL_OK;
+  if (!gone) return DL_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  return cuda_status(ctx, launch_pages_free(ctx, pages, gone, static_cast<cudaStream_t>(stream)));
+}
+
+static int32_t check_pools(const dl_pages* p, int32_t n_pools, void* const* pools, int64_t page_bytes, const void* scratch,
+                           int64_t scratch_bytes) {
+  if (n_pools < 0 || page_bytes < 0 || (n_pools > 0 && !pools) || !scratch) return DL_ERR_INVALID_ARG;
+  if (page_bytes % 16 != 0 || (reinterpret_cast<uintptr_t>(scratch) & 255u) != 0) return DL_ERR_ALIGNMENT;
+  for (int32_t i = 0; i < n_pools; ++i) {
+    if (!pools[i]) return DL_ERR_INVALID_ARG;
+    if (misaligned(pools[i])) return DL_ERR_ALIGNMENT;
+  }
+  if (page_bytes >= (1LL << 40)) return DL_ERR_UNSUPPORTED;
+  return scratch_bytes < pages_scratch_bytes(p) ? DL_ERR_WORKSPACE : DL_OK;
+}
+
+int32_t dl_pages_fork(dl_ctx* ctx, const dl_pages* pages, const int32_t* parent, int32_t n_pools, void* const* pools,
+                      int64_t page_bytes, void* scratch, int64_t scratch_bytes, void* stream) {
+  int32_t st = check_pages(ctx, pages);
+  if (st == DL_OK) st = check_pools(pages, n_pools, pools, page_bytes, scratch, scratch_bytes);
+  if (st != DL_OK) return st;
+  if (pages->B == 0) return DL_OK;
+  if (!parent) return DL_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  return cuda_status(ctx, launch_pages_fork(ctx, pages, parent, n_pools, pools, page_bytes, scratch, static_cast<cudaStream_t>(stream)));
+}
+
+int32_t dl_pages_compact(dl_ctx* ctx, const dl_pages* pages, int32_t n_pools, void* const* pools, int64_t page_bytes,
+                         int32_t* n_live, void* scratch, int64_t scratch_bytes, void* stream) {
+  int32_t st = check_pages(ctx, pages);
+  if (st == DL_OK) st = check_pools(pages, n_pools, pools, page_bytes, scratch, scratch_bytes);
+  if (st != DL_OK) return st;
+  if (pages->B == 0) return DL_OK;
+  DeviceGuard g(ctx->device);
+  return cuda_status(ctx, launch_pages_compact(ctx, pages, n_pools, pools, page_bytes, n_live, scratch, static_cast<cudaStream_t>(stream)));
+}
+
+int64_t dl_kv4_page_bytes(const dl_ctx* ctx, int32_t n_kv_heads, int32_t page_rows) {
+  if (!ctx || n_kv_heads <= 0) return DL_ERR_INVALID_ARG;
+  if (page_rows != 16 && page_rows != 32 && page_rows != 64 && page_rows != 128) return DL_ERR_UNSUPPORTED;
+  return (int64_t)n_kv_heads * page_rows * 9 * ctx->desc.head_dim / 8;
+}
+
+int32_t dl_kv4_append(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, void* pool, const void* k, const void* v,
+                      int64_t kv_stride, const int32_t* starts, const uint8_t* keep, int32_t total, int32_t commit,
+                      void* stream) {
+  const int32_t st = check_kv4(ctx, pages, n_kv_heads, pool);
+  if (st != DL_OK) return st;
+  if (total < 0) return DL_ERR_INVALID_ARG;
+  if (pages->B == 0 || total == 0) return DL_OK;
+  if (!k || !v || !starts) return DL_ERR_INVALID_ARG;
+  const int64_t w = (int64_t)n_kv_heads * ctx->desc.head_dim;
+  if (kv_stride == 0) kv_stride = w;
+  if (kv_stride < w) return DL_ERR_INVALID_ARG;
+  if (misaligned(k) || misaligned(v) || kv_stride % 8 != 0) return DL_ERR_ALIGNMENT;
+  if (kv_stride >= (1LL << 32) || w * 32 * 2 >= (1LL << 31)) return DL_ERR_UNSUPPORTED;
+  DeviceGuard g(ctx->device);
+  return cuda_status(ctx, launch_kv4_append(ctx, pages, n_kv_heads, pool, k, v, kv_stride, starts, keep, total, commit, static_cast<cudaStream_t>(stream)));
+}
+
+int32_t dl_kv4_read(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, const void* pool, const int32_t* row0,
+                    const int32_t* starts, int32_t total, void* k_out, void* v_out, void* stream) {
+  const int32_t st = check_kv4(ctx, pages, n_kv_heads, pool);
+  if (st != DL_OK) return st;
+  if (total < 0) return DL_ERR_INVALID_ARG;
+  if (pages->B == 0 || total == 0) return DL_OK;
+  if (!row0 || !starts || !k_out || !v_out) return DL_ERR_INVALID_ARG;
+  if (misaligned(k_out) || misaligned(v_out)) return DL_ERR_ALIGNMENT;
+  DeviceGuard g(ctx->device);
+  return cuda_status(ctx, launch_kv4_read(ctx, pages, n_kv_heads, pool, row0, starts, total, k_out, v_out, static_cast<cudaStream_t>(stream)));
+}
+
+int32_t dl_kv4_attn_decode(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, void* pool, const void* q_t,
+                           const void* k_t, const void* v_t, const uint8_t* keep, float scale, void* out, void* stream) {
+  const int32_t st = check_kv4(ctx, pages, n_kv_heads, pool);
+  if (st != DL_OK) return st;
+  if (!(scale > 0.f)) return DL_ERR_INVALID_ARG;
+  if (pages->B == 0) return DL_OK;
+  if (!q_t || !k_t || !v_t || !out) return DL_ERR_INVALID_ARG;
+  if (misaligned(q_t) || misaligned(k_t) || misaligned(v_t) || misaligned(out)) return DL_ERR_ALIGNMENT;
+  DeviceGuard g(ctx->device);
+  return cuda_status(ctx, launch_attn_decode_kv4(ctx, pages, n_kv_heads, pool, q_t, k_t, v_t, keep, scale, out, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

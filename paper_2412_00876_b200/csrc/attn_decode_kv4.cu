@@ -1,0 +1,641 @@
+// Decode attention over a paged 4-bit K/V cache with grouped heads (an extension of Eq. 6; NOT in the paper).
+//
+// One new token per sequence: its G = H / Hkv query heads of a K/V head attend the rows the sequence's pages hold
+// (kv4.cuh: value = s * code + z per 64 values) and the token's own k_t, v_t in bf16.  bf16 models, D = 64 or 128.
+//
+// Bound by the bytes of the cache: 18 D bytes per 16 rows and K/V head.  The codes are never turned into values:
+//   scores   q . k = sum over groups of  s * (q . codes) + z * (sum of q over the group)
+//   outputs  O     = sum over keys of (p s) codes + p z
+// so the matrix instructions work on the codes themselves, and s and z are applied once per key and group.  A code in
+// bits 0-3 or 4-7 of a half word IS an fp16 number (a subnormal: code * 2^-24 or code * 2^-20), so eight codes become
+// four operand registers with one shift and four ANDs; the powers of two are taken out in q (an exact scaling by 1/16
+// of the dims concerned) and at the end.  The query heads are the N side of mma.sync m16n8k16 and 16 keys (scores) or
+// 16 dims (outputs) its M side, so that up to 8 heads of a group cost one pass over the codes:
+//   S^T[key][head] = K codes [16 keys][16 dims] x q^T          A straight from shared memory, B = q (registers)
+//   O^T[dim][head] += V^T codes [16 dims][16 keys] x P^T       A: a byte permute pairs two keys, B: P through movmatrix
+// The order in which keys meet the k index is key(i) = (i >> 1) + 4 (i & 1) within 8, chosen with the page layout so that
+// both operands' loads are free of bank conflicts.  P s is rounded to fp16 (11 bits) after division by a power of two
+// 2^E that tracks the largest s; the maximum in use of the softmax lags by up to 2^8, so P <= 2^8, P s 2^-E <= 2^12.
+// q is scaled by a power of two into fp16's range (exact down to 2^-28 of a head's largest value).
+//
+// Work: the tiles of all (sequence, K/V head) pairs in one line, cut into equal ranges, one per warp: every warp
+// streams the same number of tiles whatever the lengths are, through its own ring of tiles (one bulk copy each).  A
+// pair that lies within one range is finished there; the parts of the others go to scratch and a second kernel,
+// launched to overlap, joins them in order (no atomics: the same call gives the same bits).  Page numbers are fetched
+// 32 tiles ahead, a lane each.
+#include <algorithm>
+
+#include "kv4.cuh"
+#include "pipeline.cuh"
+
+namespace dl {
+
+struct K4Args {
+  const __nv_bfloat16* q; const __nv_bfloat16* k_t; const __nv_bfloat16* v_t;   // [B][H][D], [B][Hk][D]
+  uint8_t* pool; PagesArg pg; const uint8_t* keep; __nv_bfloat16* out;
+  float* partial; DeviceStatus* status;
+  int32_t H, Hk, G, grid_warps, stages;
+  float scale_log2;
+};
+
+constexpr int kK4Warps = 4;              // warps per CTA
+constexpr int kK4Lag = 8;                // log2 units by which the maximum in use may lag
+constexpr int kK4MinTiles = 2;           // fewest tiles worth a warp of its own
+constexpr int kK4MergeThreads = 128;
+
+// floats of a part: D sums per head, then the head's maximum and its sum of exponentials (16-byte steps)
+template <int D> __host__ __device__ constexpr int k4_slot(int G) { return G * (D + 4); }
+
+__device__ __forceinline__ int k4_rows(const PagesArg& p, int b) {
+  return (int)min((long long)max(__ldg(p.len + b), 0), (long long)p.max_pages * (kKv4Rows << p.tile_shift));
+}
+// tiles of one K/V head of a sequence of n rows; an empty one counts 1, so that somebody writes its output
+__device__ __forceinline__ int k4_units(int n) { return max(1, (n + kKv4Rows - 1) / kKv4Rows); }
+
+// pre[b] = units in front of sequence b, pre[B] = all; called by the whole CTA
+__device__ __forceinline__ void k4_prefix(const PagesArg& p, int Hk, int* pre, int* sums) {
+  const int T = blockDim.x, per = (p.B + T - 1) / T, from = min(p.B, (int)threadIdx.x * per), to = min(p.B, from + per);
+  int c = 0;
+  for (int b = from; b < to; ++b) { c += k4_units(k4_rows(p, b)) * Hk; pre[b + 1] = c; }
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int run = c;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, run, o);
+    if (lane >= o) run += v;
+  }
+  if (lane == 31) sums[warp] = run;
+  __syncthreads();
+  int base = run - c;
+  for (int w = 0; w < warp; ++w) base += sums[w];
+  for (int b = from; b < to; ++b) pre[b + 1] += base;
+  if (threadIdx.x == 0) pre[0] = 0;
+  __syncthreads();
+}
+__device__ __forceinline__ int k4_find(const int* pre, int B, int u) {
+  int lo = 0, hi = B - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (pre[mid] <= u) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+// the line of `total` units as W ranges
+__device__ __forceinline__ int k4_width(int total, int grid_warps) { return max(1, min(grid_warps, total / kK4MinTiles)); }
+__device__ __forceinline__ int k4_range(int w, int total, int W) { return (int)((long long)w * total / W); }
+__device__ __forceinline__ int k4_owner(int u, int total, int W) { return (int)((((long long)u + 1) * W - 1) / total); }
+
+__device__ __forceinline__ void k4_mma(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t k4_transpose(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ uint32_t k4_f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float k4_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float k4_pow2(int e) { return __int_as_float((e + 127) << 23); }     // -126 <= e <= 127
+__device__ __forceinline__ uint32_t k4_lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint2 k4_lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+
+// 16 values of a query or key row from dim `d` on, as floats (zeros where !on)
+__device__ __forceinline__ void k4_load16(const __nv_bfloat16* p, bool on, float* x) {
+  uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
+  if (on) { a = __ldg(reinterpret_cast<const uint4*>(p)); b = __ldg(reinterpret_cast<const uint4*>(p) + 1); }
+  const uint32_t u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) { x[2 * i] = bf16lo(u[i]); x[2 * i + 1] = bf16hi(u[i]); }
+}
+
+template <int D, int NT>                                          // NT: blocks of 8 query heads
+__global__ void __launch_bounds__(kK4Warps * 32, NT == 1 ? 4 : 2)
+attn_decode_kv4_kernel(const K4Args a) {
+  using F = Kv4<D>;
+  constexpr int NG = F::NG;
+  extern __shared__ __align__(128) char smem[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, j = lane & 3;
+  const int NS = a.stages;
+  char* ring = smem + (size_t)warp * NS * F::TILE;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (size_t)kK4Warps * NS * F::TILE) + warp * NS;
+  int* pre = reinterpret_cast<int*>(smem + (size_t)kK4Warps * NS * (F::TILE + 8));
+  __shared__ int sh_sums[kK4Warps];
+  __shared__ int sh_abort;
+  volatile int* abort_flag = &sh_abort;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (tid == 0) sh_abort = 0;
+  if (lane == 0) {
+    for (int s = 0; s < NS; ++s) mbar_init(smem_u32(&bars[s]), 1);
+    fence_mbar_init();
+  }
+  k4_prefix(a.pg, a.Hk, pre, sh_sums);                            // (its barriers also publish the above)
+  const int total = pre[a.pg.B], W = k4_width(total, a.grid_warps);
+  const int gw = warp * gridDim.x + blockIdx.x;                   // few ranges go to as many SMs as there are
+  if (gw >= W) return;
+  const int u0 = k4_range(gw, total, W), u1 = k4_range(gw + 1, total, W);
+
+  // ---- page numbers: lane i holds those of unit base + i, this block of 32 and (requested ahead) the next
+  int nx_page = -1, nx_b = -1, nx_hk = 0, nx_t = 0;               // nx_b < 0: nothing to copy
+  auto request = [&](int base) {
+    const int u = base + lane;
+    nx_b = -1;
+    if (u < u1) {
+      const int b = k4_find(pre, a.pg.B, u), rem = u - pre[b], units = (pre[b + 1] - pre[b]) / a.Hk;
+      nx_hk = rem / units;
+      nx_t = rem - nx_hk * units;
+      if (nx_t * kKv4Rows < k4_rows(a.pg, b)) {
+        nx_b = b;
+        nx_page = __ldg(a.pg.table + (size_t)b * a.pg.max_pages + (nx_t >> a.pg.tile_shift));
+      }
+    }
+  };
+  auto resolve = [&]() {
+    int idx = -1;
+    if (nx_b >= 0) {
+      idx = kv4_tile_index(a.pg, nx_page, a.Hk, nx_hk, nx_t);
+      if (idx < 0) report_status(a.status, DL_ERR_INVALID_ARG, nx_b);
+    }
+    return idx;
+  };
+  request(u0);
+  int cur_idx = resolve(), p_base = u0;
+  request(u0 + 32);
+  uint32_t absent = 0;                                            // slots whose tile was not fetched
+  int p_u = u0, p_slot = 0;
+  auto produce = [&]() {
+    if (p_u == p_base + 32) {
+      cur_idx = resolve();
+      p_base += 32;
+      request(p_base + 32);
+    }
+    const int idx = __shfl_sync(0xffffffffu, cur_idx, p_u - p_base);
+    const uint32_t bar = smem_u32(&bars[p_slot]);
+    if (lane == 0) {
+      if (idx >= 0) {
+        mbar_expect_tx(bar, F::TILE);
+        bulk_g2s(smem_u32(ring + (size_t)p_slot * F::TILE), a.pool + (long long)idx * F::TILE, F::TILE, bar);
+      } else {
+        mbar_arrive(bar);
+      }
+    }
+    absent = idx >= 0 ? absent & ~(1u << p_slot) : absent | (1u << p_slot);
+    ++p_u;
+    if (++p_slot == NS) p_slot = 0;
+  };
+  for (int i = 0; i < NS && p_u < u1; ++i) produce();
+
+  // ---- where the consumer is
+  int b = k4_find(pre, a.pg.B, u0);
+  int units = (pre[b + 1] - pre[b]) / a.Hk, hk = (u0 - pre[b]) / units, t = (u0 - pre[b]) - hk * units;
+  int slot = 0, phase = 0;
+  for (int u = u0; u < u1;) {
+    // ================ one (sequence, K/V head), or the part of it that lies in this range
+    const int n = k4_rows(a.pg, b), seg0 = u - t, seg1 = seg0 + units, part_end = min(seg1, u1);
+    uint32_t qb[NT][NG][4][2];                                    // B operand: head r of block nt, 16 dims per step
+    float qs[NT][NG][2], fq[NT][2], se[NT][2];                    // of heads 2j, 2j + 1: sum of q * scale, score factor, own score
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const bool on = nt * 8 + r < a.G;
+      const __nv_bfloat16* qp = a.q + ((size_t)b * a.H + hk * a.G + nt * 8 + r) * D;
+      float x[NG][16], dot = 0.f, sum[NG], mx = 0.f;
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        float y[16];
+        k4_load16(qp + 64 * g + 16 * j, on, x[g]);
+        k4_load16(a.k_t + ((size_t)b * a.Hk + hk) * D + 64 * g + 16 * j, true, y);
+        sum[g] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          dot = fmaf(x[g][i], y[i], dot);
+          sum[g] += x[g][i];
+          mx = fmaxf(mx, fabsf(x[g][i]));
+        }
+      }
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) {
+        dot += __shfl_xor_sync(0xffffffffu, dot, o);
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+#pragma unroll
+        for (int g = 0; g < NG; ++g) sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], o);
+      }
+      const int e = max(-100, min(110, (int)(__float_as_uint(mx) >> 23) - 127));   // |q| < 2^(e + 1)
+      const float down = k4_pow2(13 - e), down16 = down * 0.0625f;
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          const float* y = x[g] + 8 * w;
+          qb[nt][g][2 * w][0] = k4_f16x2(y[0] * down, y[4] * down);
+          qb[nt][g][2 * w][1] = k4_f16x2(y[1] * down16, y[5] * down16);
+          qb[nt][g][2 * w + 1][0] = k4_f16x2(y[2] * down, y[6] * down);
+          qb[nt][g][2 * w + 1][1] = k4_f16x2(y[3] * down16, y[7] * down16);
+        }
+      const float fr = a.scale_log2 * k4_pow2(e + 11);            // 2^24 of the codes, 2^(e - 13) of q
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int from = (2 * j + c) * 4;
+        fq[nt][c] = __shfl_sync(0xffffffffu, fr, from);
+        se[nt][c] = __shfl_sync(0xffffffffu, dot, from) * a.scale_log2;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) qs[nt][g][c] = __shfl_sync(0xffffffffu, sum[g], from) * a.scale_log2;
+      }
+    }
+    // ---- Eq. 6's append, by the warp that has the pair's first tile: lanes 0 .. D/8-1 hold k_t, the next D/8 v_t
+    if (t == 0 && a.keep != nullptr && a.keep[b] != 0) {
+      constexpr int LR = D / 8;
+      const int l = lane % LR;
+      const bool is_v = lane >= LR, on = lane < 2 * LR;
+      const uint4 raw = __ldg(reinterpret_cast<const uint4*>((is_v ? a.v_t : a.k_t) + ((size_t)b * a.Hk + hk) * D) + l);
+      uint32_t word;
+      const uint32_t code = kv4_quantise8(raw, word);
+      const int pi = n >> (a.pg.tile_shift + 4);
+      const int idx = pi < a.pg.max_pages
+                          ? kv4_tile_index(a.pg, __ldg(a.pg.table + (size_t)b * a.pg.max_pages + pi), a.Hk, hk, n >> 4) : -1;
+      if (idx < 0) {
+        if (lane == 0 && hk == 0) report_status(a.status, DL_ERR_CAPACITY, b);
+      } else if (on && DL_IN_BOUNDS(a.status, KID_DECODE_KV4, idx, ((long long)a.pg.n_pages * a.Hk) << a.pg.tile_shift)) {
+        kv4_store8<D>(a.pool + (long long)idx * F::TILE, n & 15, l, is_v, code, word);
+      }
+    }
+
+    float m[NT][2], l_run[NT][2], zacc[NT][NG][2], acc[NT][NG][4][4];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      m[nt][0] = m[nt][1] = -INFINITY;
+      l_run[nt][0] = l_run[nt][1] = 0.f;
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        zacc[nt][g][0] = zacc[nt][g][1] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[nt][g][i][0] = acc[nt][g][i][1] = acc[nt][g][i][2] = acc[nt][g][i][3] = 0.f;
+      }
+    }
+    int E = -200;                                                 // P s is held as P s 2^-E; none yet
+    float down_e = 0.f, s_limit = 0.f;                            // 2^-E, 2^(E + 4)
+
+    // ================ tiles
+    for (; u < part_end; ++u, ++t) {
+      mbar_wait(smem_u32(&bars[slot]), phase, abort_flag);
+      if (!((absent >> slot) & 1u) && !*abort_flag) {
+        const uint32_t tile = smem_u32(ring + (size_t)slot * F::TILE);
+        const int nr = n - t * kKv4Rows;                          // rows of this tile, 16 or more: all
+        const int key0 = (r >> 1) + 4 * (r & 1);                  // this lane's keys: key0 and key0 + 8
+        float d[NT][NG][4];
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) d[nt][g][0] = d[nt][g][1] = d[nt][g][2] = d[nt][g][3] = 0.f;
+          const uint32_t ka = tile + kv4_group_off<D>(key0, g) + 8 * j;
+          const uint2 w0 = k4_lds64(ka), w1 = k4_lds64(ka + 8 * F::RB);
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            const uint32_t x = w ? w0.y : w0.x, y = w ? w1.y : w1.x, x8 = x >> 8, y8 = y >> 8;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              k4_mma(d[nt][g], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qb[nt][g][2 * w][0], qb[nt][g][2 * w][1]);
+              k4_mma(d[nt][g], x8 & 0x000F000Fu, y8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x00F000F0u, qb[nt][g][2 * w + 1][0], qb[nt][g][2 * w + 1][1]);
+            }
+          }
+        }
+        // ---- words of this lane's two keys; whatever stands in rows past the end counts nothing
+        const bool ok0 = key0 < nr, ok1 = key0 + 8 < nr;
+        float ks[2][NG], kz[2][NG], vs[2][NG], vz[2][NG];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const bool ok = i ? ok1 : ok0;
+          uint32_t kw[NG], vw[NG];
+          const uint32_t at = tile + (key0 + 8 * i) * 4 * NG;
+          if (NG == 2) {
+            const uint2 x = k4_lds64(at + F::KM), y = k4_lds64(at + F::VM);
+            kw[0] = x.x; kw[NG - 1] = x.y; vw[0] = y.x; vw[NG - 1] = y.y;
+          } else {
+            kw[0] = k4_lds32(at + F::KM); vw[0] = k4_lds32(at + F::VM);
+          }
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            ks[i][g] = bf16lo(kw[g]); kz[i][g] = bf16hi(kw[g]);
+            vs[i][g] = ok ? bf16lo(vw[g]) : 0.f; vz[i][g] = ok ? bf16hi(vw[g]) : 0.f;
+          }
+        }
+        float s[NT][4];
+        bool raise = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {                           // i: key (i >> 1), head 2j + (i & 1)
+            const int ki = i >> 1, c = i & 1;
+            float dot = 0.f, off = 0.f;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+              dot = fmaf(ks[ki][g], d[nt][g][i], dot);
+              off = fmaf(kz[ki][g], qs[nt][g][c], off);
+            }
+            s[nt][i] = (ki ? ok1 : ok0) ? fmaf(fq[nt][c], dot, off) : -INFINITY;
+            raise |= s[nt][i] > m[nt][c] + (float)kK4Lag;
+          }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int g = 0; g < NG; ++g) raise |= vs[i][g] > s_limit;
+        if (__any_sync(0xffffffffu, raise)) {
+          // rare: the maxima in use go up to what has been seen, and so does 2^E
+          float top = 0.f;
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int g = 0; g < NG; ++g) top = fmaxf(top, vs[i][g]);
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          float corr_e = 1.f;
+          if (top > s_limit) {
+            const int en = max(-100, min(120, (int)(__float_as_uint(top) >> 23) - 127));
+            if (en > E) {
+              corr_e = E == -200 ? 1.f : k4_pow2(max(-126, E - en));
+              E = en;
+              down_e = k4_pow2(-E);
+              s_limit = k4_pow2(min(127, E + 4));
+            }
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              float mx = fmaxf(s[nt][c], s[nt][2 + c]);
+#pragma unroll
+              for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+              mx = fmaxf(mx, m[nt][c]);
+              const float corr = m[nt][c] == -INFINITY ? (mx == -INFINITY ? 1.f : 0.f) : k4_exp2(m[nt][c] - mx);
+              m[nt][c] = mx;
+              l_run[nt][c] *= corr;
+#pragma unroll
+              for (int g = 0; g < NG; ++g) {
+                zacc[nt][g][c] *= corr;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { acc[nt][g][i][c] *= corr * corr_e; acc[nt][g][i][2 + c] *= corr * corr_e; }
+              }
+            }
+        }
+        float p[NT][4];
+        uint32_t pb[NT][NG][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float mc = m[nt][i & 1];
+            p[nt][i] = k4_exp2(s[nt][i] - (mc == -INFINITY ? 0.f : mc));
+            l_run[nt][i & 1] += p[nt][i];
+          }
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) zacc[nt][g][c] = fmaf(p[nt][c], vz[0][g], fmaf(p[nt][2 + c], vz[1][g], zacc[nt][g][c]));
+            const float f0 = vs[0][g] * down_e, f1 = vs[1][g] * down_e;
+            pb[nt][g][0] = k4_transpose(k4_f16x2(p[nt][0] * f0, p[nt][1] * f0));
+            pb[nt][g][1] = k4_transpose(k4_f16x2(p[nt][2] * f1, p[nt][3] * f1));
+          }
+        }
+        // ---- O^T += V^T P^T: lane's keys j, 4 + j, 8 + j, 12 + j, its dims 64 g + 8 r .. + 7
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          const uint32_t va = tile + F::V + 4 * r;
+          const uint32_t wA = k4_lds32(va + kv4_group_off<D>(j, g)), wB = k4_lds32(va + kv4_group_off<D>(4 + j, g));
+          const uint32_t wC = k4_lds32(va + kv4_group_off<D>(8 + j, g)), wD = k4_lds32(va + kv4_group_off<D>(12 + j, g));
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t x = __byte_perm(wA, wB, h ? 0x7632 : 0x5410), y = __byte_perm(wC, wD, h ? 0x7632 : 0x5410);
+            const uint32_t x8 = x >> 8, y8 = y >> 8;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              k4_mma(acc[nt][g][2 * h], x & 0x000F000Fu, x & 0x00F000F0u, y & 0x000F000Fu, y & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
+              k4_mma(acc[nt][g][2 * h + 1], x8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x000F000Fu, y8 & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
+            }
+          }
+        }
+      }
+      __syncwarp();
+      if (p_u < u1 && !*abort_flag) produce();
+      if (++slot == NS) { slot = 0; phase ^= 1; }
+    }
+
+    // ================ finish the part
+    const float up = E == -200 ? 0.f : k4_pow2(E);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+          l_run[nt][c] += __shfl_xor_sync(0xffffffffu, l_run[nt][c], o);
+#pragma unroll
+          for (int g = 0; g < NG; ++g) zacc[nt][g][c] += __shfl_xor_sync(0xffffffffu, zacc[nt][g][c], o);
+        }
+        const int head = nt * 8 + 2 * j + c;
+        if (head >= a.G) continue;                                // (after the shuffles of this pair)
+        const bool whole = seg0 >= u0 && seg1 <= u1;
+        // this lane's dims 64 g + 8 r + 0 .. 7 of the head
+        float o[NG][8];
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            o[g][2 * i] = fmaf(acc[nt][g][i][c] * 16777216.f, up, zacc[nt][g][c]);
+            o[g][2 * i + 1] = fmaf(acc[nt][g][i][2 + c] * 1048576.f, up, zacc[nt][g][c]);
+          }
+        if (whole) {
+          const float mine = se[nt][c], M = fmaxf(m[nt][c], mine);
+          const float wc = m[nt][c] == -INFINITY ? 0.f : k4_exp2(m[nt][c] - M), we = k4_exp2(mine - M);
+          const float inv = 1.f / fmaf(l_run[nt][c], wc, we);
+          const __nv_bfloat16* vt = a.v_t + ((size_t)b * a.Hk + hk) * D;
+          const size_t at = ((size_t)b * a.H + hk * a.G + head) * D;
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            const uint4 vw = __ldg(reinterpret_cast<const uint4*>(vt + 64 * g + 8 * r));
+            const uint32_t v[4] = {vw.x, vw.y, vw.z, vw.w};
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const __nv_bfloat162 y = __floats2bfloat162_rn(fmaf(o[g][2 * i], wc, we * bf16lo(v[i])) * inv,
+                                                             fmaf(o[g][2 * i + 1], wc, we * bf16hi(v[i])) * inv);
+              w[i] = *reinterpret_cast<const uint32_t*>(&y);
+            }
+            if (DL_IN_BOUNDS(a.status, KID_DECODE_KV4, at + 64 * g + 8 * r + 7, (size_t)a.pg.B * a.H * D))
+              *reinterpret_cast<uint4*>(a.out + at + 64 * g + 8 * r) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        } else {
+          // slot 0 of a range: the pair that began before it; slot 1: the one that goes on behind it
+          float* pp = a.partial + ((size_t)gw * 2 + (seg0 < u0 ? 0 : 1)) * k4_slot<D>(a.G) + (size_t)head * (D + 4);
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            *reinterpret_cast<float4*>(pp + 64 * g + 8 * r) = make_float4(o[g][0], o[g][1], o[g][2], o[g][3]);
+            *reinterpret_cast<float4*>(pp + 64 * g + 8 * r + 4) = make_float4(o[g][4], o[g][5], o[g][6], o[g][7]);
+          }
+          if (r == 0) { pp[D] = m[nt][c]; pp[D + 1] = l_run[nt][c]; }
+        }
+      }
+    if (t == units) {
+      t = 0;
+      if (++hk == a.Hk) {
+        hk = 0;
+        if (++b < a.pg.B) units = (pre[b + 1] - pre[b]) / a.Hk;
+      }
+    }
+  }
+  if (*abort_flag) {
+    if (lane == 0) report_status(a.status, DL_ERR_TIMEOUT, blockIdx.x);
+    // copies still in flight must land before the CTA's shared memory goes: the last NS tiles requested
+    for (int v = max(u0, p_u - NS); v < p_u; ++v)
+      for (int i = 0; i < kSpinLimit && !mbar_try_wait(smem_u32(&bars[(v - u0) % NS]), ((v - u0) / NS) & 1); ++i) __nanosleep(40);
+  }
+}
+
+// Joins the parts of a pair that several ranges share: one CTA per query head, parts dealt to its warps in order, four
+// dims per lane.
+template <int D>
+__global__ void __launch_bounds__(kK4MergeThreads)
+attn_merge_kv4_kernel(const K4Args a) {
+  constexpr int NW = kK4MergeThreads / 32, PL = D / 32;           // dims per lane
+  extern __shared__ __align__(128) char smem[];
+  int* pre = reinterpret_cast<int*>(smem);
+  __shared__ int sh_sums[NW];
+  __shared__ float sh_o[NW][D], sh_l[NW];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int b = blockIdx.x / a.H, head = blockIdx.x - b * a.H, hk = head / a.G, hg = head - hk * a.G;
+  k4_prefix(a.pg, a.Hk, pre, sh_sums);
+  const int total = pre[a.pg.B], W = k4_width(total, a.grid_warps);
+  const int units = (pre[b + 1] - pre[b]) / a.Hk, s0 = pre[b] + hk * units;
+  const int first = k4_owner(s0, total, W), last = k4_owner(s0 + units - 1, total, W);
+  if (first == last) {
+    // this grid must not retire before its predecessor has: what follows in the stream relies on both
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    return;
+  }
+  // the token's own score (every warp for itself)
+  const __nv_bfloat16* qp = a.q + ((size_t)b * a.H + head) * D + lane * PL;
+  const __nv_bfloat16* kp = a.k_t + ((size_t)b * a.Hk + hk) * D + lane * PL;
+  float own = 0.f;
+#pragma unroll
+  for (int i = 0; i < PL; ++i) own = fmaf(__bfloat162float(qp[i]), __bfloat162float(kp[i]), own);
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) own += __shfl_xor_sync(0xffffffffu, own, o);
+  own *= a.scale_log2;
+  asm volatile("griddepcontrol.wait;" ::: "memory");              // the parts are written from here on
+  auto part = [&](int w) {
+    return a.partial + ((size_t)w * 2 + (w == first && k4_range(w, total, W) <= s0 ? 1 : 0)) * k4_slot<D>(a.G) + (size_t)hg * (D + 4);
+  };
+  float M = own;
+  for (int w = first + lane; w <= last; w += 32) M = fmaxf(M, __ldcg(part(w) + D));
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  float o[PL], l = 0.f;
+#pragma unroll
+  for (int i = 0; i < PL; ++i) o[i] = 0.f;
+#pragma unroll 4
+  for (int w = first + warp; w <= last; w += NW) {
+    const float* pp = part(w);
+    const float mw = __ldcg(pp + D), wt = mw == -INFINITY ? 0.f : k4_exp2(mw - M);
+    float x[PL];
+    if (PL == 4) {
+      const float4 y = __ldcg(reinterpret_cast<const float4*>(pp + lane * PL));
+      x[0] = y.x; x[1] = y.y; x[PL - 2] = y.z; x[PL - 1] = y.w;
+    } else {
+      const float2 y = __ldcg(reinterpret_cast<const float2*>(pp + lane * PL));
+      x[0] = y.x; x[1] = y.y;
+    }
+    l = fmaf(__ldcg(pp + D + 1), wt, l);
+#pragma unroll
+    for (int i = 0; i < PL; ++i) o[i] = fmaf(x[i], wt, o[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < PL; ++i) sh_o[warp][lane * PL + i] = o[i];
+  if (lane == 0) sh_l[warp] = l;
+  __syncthreads();
+  const int dim = threadIdx.x;
+  if (dim < D) {
+    const float we = k4_exp2(own - M);
+    float num = we * __bfloat162float(a.v_t[((size_t)b * a.Hk + hk) * D + dim]), den = we;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) { num += sh_o[w][dim]; den += sh_l[w]; }
+    const size_t at = ((size_t)b * a.H + head) * D + dim;
+    if (DL_IN_BOUNDS(a.status, KID_DECODE_KV4, at, (size_t)a.pg.B * a.H * D)) a.out[at] = __float2bfloat16_rn(num / den);
+  }
+}
+
+template <int D, int NT>
+static cudaError_t k4_launch(const dl_ctx* ctx, K4Args& a, cudaStream_t s) {
+  constexpr int kCtas = NT == 1 ? 4 : 2;
+  const size_t pre_bytes = (size_t)(a.pg.B + 1) * sizeof(int);
+  const int per_cta = (ctx->smem_optin + 1024) / kCtas - 1024;
+  int ns = (int)((per_cta - (int)pre_bytes - 256) / (kK4Warps * (Kv4<D>::TILE + 8)));
+  ns = std::min(ns, 12);
+  if (ns < 2) return cudaErrorInvalidConfiguration;
+  a.stages = ns;
+  const size_t smem = (size_t)kK4Warps * ns * (Kv4<D>::TILE + 8) + pre_bytes;
+  auto kernel = attn_decode_kv4_kernel<D, NT>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  const int grid = ctx->sm_count * kCtas;
+  a.grid_warps = grid * kK4Warps;
+  kernel<<<grid, kK4Warps * 32, smem, s>>>(a);
+  e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(a.pg.B * a.H);
+  cfg.blockDim = dim3(kK4MergeThreads);
+  cfg.dynamicSmemBytes = pre_bytes;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, attn_merge_kv4_kernel<D>, (const K4Args)a);
+}
+
+// floats of scratch: two parts for each range
+int64_t kv4_scratch_floats(int32_t sm_count, const dl_model_desc& d) {
+  const int64_t G = std::min(d.n_heads, 16);
+  return std::max((int64_t)sm_count * 4 * kK4Warps * 2 * std::min<int64_t>(G, 8),
+                  (int64_t)sm_count * 2 * kK4Warps * 2 * G) * (d.head_dim + 4);
+}
+
+cudaError_t launch_attn_decode_kv4(const dl_ctx* ctx, const dl_pages* p, int32_t Hk, void* pool, const void* q,
+                                   const void* k_t, const void* v_t, const uint8_t* keep, float scale, void* out,
+                                   cudaStream_t s) {
+  const dl_model_desc& d = ctx->desc;
+  K4Args a;
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.k_t = static_cast<const __nv_bfloat16*>(k_t);
+  a.v_t = static_cast<const __nv_bfloat16*>(v_t);
+  a.pool = static_cast<uint8_t*>(pool);
+  a.pg = pages_arg(p);
+  a.keep = keep;
+  a.out = static_cast<__nv_bfloat16*>(out);
+  a.partial = ctx->ws.kv4_partial;
+  a.status = ctx->ws.status;
+  a.H = d.n_heads; a.Hk = Hk; a.G = d.n_heads / Hk;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  if (d.head_dim == 128) return a.G <= 8 ? k4_launch<128, 1>(ctx, a, s) : k4_launch<128, 2>(ctx, a, s);
+  return a.G <= 8 ? k4_launch<64, 1>(ctx, a, s) : k4_launch<64, 2>(ctx, a, s);
+}
+
+}  // namespace dl

@@ -1,0 +1,426 @@
+// Causal attention over packed prompts with grouped heads, on the tensor cores (Eq. 1 on whole prompts: what the layers in
+// front of the token selection compute).  bf16, head_dim 64 or 128.
+//
+// Rows [starts[b], starts[b+1]) of q [total][H][D] and k, v [total][Hkv][D] are sequence b.  Query head h reads K/V
+// head h / G, G = H / Hkv.  A query tile is 128 rows of (position, head): 128 / P positions of P heads of one group, P the
+// largest power of two that divides G (one TMA box [positions][P heads][64 dims] is just that), so that a group's heads
+// share every K/V tile and short prompts fill a tile sooner.  A work item is (sequence, P heads, PAIR of query tiles),
+// pairs counted from the sequence's end; the two tiles are the CTA's two lanes, the later positions lane A.  One
+// persistent CTA per SM walks the items, longest first.
+//   warp 8        : the producer: Q tiles, then K and V tiles of 128 rows through one ring of four slots, used by both
+//                   lanes (a K/V tile crosses from L2 once per 256 query rows)
+//   warps 9, 10   : the MMA-issuing thread of lane A / B: S = Q K^T (128 x N) into tensor memory, O += P V with P read
+//                   from tensor memory; block u = P_u V_u, then Q K_{u+1}^T over P in order behind it
+//   warps 0-3/4-7 : softmax and epilogue of lane A / B, one row per thread (attn_prefill_softmax.cuh)
+//   warp 11       : allocates tensor memory (512 columns: O_A | S_A | O_B | S_B); the first CTA's checks `starts`
+// A lane alternates between its softmax and its MMAs; the two lanes settle half a period apart and so overlap.
+// The last tile of a lane uses N = its keys rounded up to 16; where that reaches past the sequence's end, the softmax
+// warps zero those V rows in shared memory first (0 * x must stay 0 for any bit pattern of a neighbour's rows).
+// Every wait is bounded (pipeline.cuh); an abort leaves DL_ERR_TIMEOUT in the status word.
+#include <algorithm>
+
+#include "attn_prefill.cuh"
+#include "attn_prefill_softmax.cuh"
+#include "common.cuh"
+#include "tc05.cuh"
+
+namespace dl {
+
+constexpr int kPkThreads = 384;
+constexpr int kPkSlots = 4;                            // K/V ring: two K and two V tiles
+constexpr int kPkBM = 128, kPkBN = 128;
+
+template <int D> struct Pk {
+  static constexpr int HALF = 128 * 128;               // 128 rows of 64 dims
+  static constexpr int TILE = (D / 64) * HALF;         // one operand tile
+  static constexpr int KV = 2 * TILE;                  // offset of the ring (behind the two Q tiles)
+  static constexpr int STAGE = KV + kPkSlots * TILE;   // output staging, 4 KB per softmax warp
+  static constexpr int BAR = STAGE + 8 * 4096;
+  static constexpr int SMEM = BAR + 512;
+};
+
+struct PkMaps { alignas(64) unsigned char q[128]; alignas(64) unsigned char k[128]; alignas(64) unsigned char v[128]; alignas(64) unsigned char o[128]; };
+
+struct PkArgs {
+  const int32_t* starts; __nv_bfloat16* out; DeviceStatus* status;
+  int32_t B, H, G, total, max_rows, said_rows;         // max_rows: the caller's said_rows, or total if that is less
+  int32_t p_shift;                                     // P = 1 << p_shift heads per tile
+  int32_t n_hs;                                        // H / P
+  int32_t pairs;                                       // pairs of tiles of a sequence of max_rows rows
+  float scale_log2;
+};
+
+struct PkItem { int b, h0, row0, n, q_hi, n_kv; };     // n_kv: key tiles of lane A
+struct PkLane { int q0, q_hi, n_tiles; bool exists; };
+
+__device__ __forceinline__ PkLane pk_lane(const PkArgs& a, const PkItem& I, int x) {
+  const int PB = kPkBM >> a.p_shift;                   // positions per tile
+  PkLane L;
+  L.q_hi = I.q_hi - x * PB;
+  L.exists = L.q_hi > 0;
+  L.q0 = max(L.q_hi - PB, 0);
+  L.n_tiles = (L.q_hi + kPkBN - 1) / kPkBN;
+  return L;
+}
+// keys of tile j that a lane's MMAs cover
+__device__ __forceinline__ int pk_cols(const PkLane& L, int j) { return min(kPkBN, (L.q_hi - j * kPkBN + 15) & ~15); }
+
+// Items in the order every role walks them: pair 0 (the last positions) of all sequences and heads first.
+struct PkWalker {
+  const PkArgs& a;
+  int p, b, hs, db, dh, s0, s1;
+  __device__ __forceinline__ explicit PkWalker(const PkArgs& a_) : a(a_) {
+    const int per = a.B * a.n_hs;
+    p = (int)blockIdx.x / per;
+    const int r = (int)blockIdx.x - p * per;
+    b = r / a.n_hs;
+    hs = r - b * a.n_hs;
+    db = (int)gridDim.x / a.n_hs;
+    dh = (int)gridDim.x - db * a.n_hs;
+    s0 = s1 = 0;
+    fetch();
+  }
+  __device__ __forceinline__ void fetch() {
+    if (p < a.pairs) { s0 = ld_early(a.starts + b); s1 = ld_early(a.starts + b + 1); }
+  }
+  __device__ __forceinline__ bool next(PkItem& I) {
+    for (;;) {
+      if (p >= a.pairs) return false;
+      const int cp = p, cb = b, ch = hs, c0 = min(max(s0, 0), a.total), c1 = min(max(s1, c0), a.total);
+      hs += dh;
+      b += db;
+      if (hs >= a.n_hs) { hs -= a.n_hs; ++b; }
+      while (b >= a.B) { b -= a.B; ++p; }
+      fetch();
+      I.b = cb;
+      I.h0 = ch << a.p_shift;
+      I.row0 = c0;
+      I.n = min(c1 - c0, a.max_rows);
+      I.q_hi = I.n - cp * (2 * kPkBM >> a.p_shift);
+      if (I.q_hi <= 0) continue;
+      I.n_kv = (I.q_hi + kPkBN - 1) / kPkBN;
+      return true;
+    }
+  }
+};
+
+template <int D>
+__global__ void __launch_bounds__(kPkThreads, 1)
+attn_packed_kernel(const __grid_constant__ PkMaps maps, const PkArgs a) {
+  using S = Pk<D>;
+  extern __shared__ __align__(1024) char smem[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (smem_u32(smem) & 1023u) {                        // the swizzled tiles need 1024-byte alignment
+    if (tid == 0) report_status(a.status, DL_ERR_ALIGNMENT, -1);
+    return;
+  }
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::BAR);
+  auto kv_full = [&](int i) { return smem_u32(bars + i); };
+  auto kv_empty = [&](int i) { return smem_u32(bars + kPkSlots + i); };
+  enum { Q_FULL = 0, Q_EMPTY, S_FULL, P_FULL, O_FULL, O_FREE, N_BAR };
+  auto bar = [&](int x, int i) { return smem_u32(bars + 2 * kPkSlots + x * N_BAR + i); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 32);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 33);
+
+  if (tid == 0) {
+    *abort_flag = 0;
+    for (int i = 0; i < kPkSlots; ++i) { mbar_init(kv_full(i), 1); mbar_init(kv_empty(i), 2); }
+    for (int x = 0; x < 2; ++x)
+      for (int i = 0; i < N_BAR; ++i) mbar_init(bar(x, i), (i == P_FULL || i == O_FREE) ? 4 : 1);
+    fence_mbar_init();
+  }
+  if (warp == 11) { tmem_alloc(smem_u32(tmem_slot), 512); tmem_relinquish(); }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp == 8) {
+    // ---------------------------------------------------------------- producer
+    reg_dec<kAtRegsSmall>();
+    if (lane == 0) {
+      const CUtensorMap* mq = reinterpret_cast<const CUtensorMap*>(maps.q);
+      const CUtensorMap* mk = reinterpret_cast<const CUtensorMap*>(maps.k);
+      const CUtensorMap* mv = reinterpret_cast<const CUtensorMap*>(maps.v);
+      tma_prefetch_desc(mq);
+      tma_prefetch_desc(mk);
+      tma_prefetch_desc(mv);
+      PkWalker W(a);
+      PkItem I;
+      int n_q[2] = {0, 0}, t = 0;                      // Q tiles per lane, ring tiles so far
+      auto load_q = [&](int x) {
+        const PkLane L = pk_lane(a, I, x);
+        if (!L.exists) return;
+        mbar_wait_spin(bar(x, Q_EMPTY), ((uint32_t)n_q[x] & 1u) ^ 1u, abort_flag);
+        if (*abort_flag) return;
+        ++n_q[x];
+        mbar_expect_tx(bar(x, Q_FULL), S::TILE);
+#pragma unroll
+        for (int hf = 0; hf < D / 64; ++hf)
+          tma_load_3d(smem_u32(smem + x * S::TILE + hf * S::HALF), mq, 64 * hf, I.h0, I.row0 + L.q0, bar(x, Q_FULL));
+      };
+      auto load_kv = [&](const CUtensorMap* m, int j) {
+        const int slot = t % kPkSlots;
+        mbar_wait_spin(kv_empty(slot), ((uint32_t)(t / kPkSlots) & 1u) ^ 1u, abort_flag);
+        if (*abort_flag) return;
+        ++t;
+        mbar_expect_tx(kv_full(slot), S::TILE);
+#pragma unroll
+        for (int hf = 0; hf < D / 64; ++hf)
+          tma_load_3d(smem_u32(smem + S::KV + slot * S::TILE + hf * S::HALF), m, 64 * hf, I.h0 / a.G, I.row0 + j * kPkBN, kv_full(slot));
+      };
+      while (!*abort_flag && W.next(I)) {
+        load_q(0);
+        load_kv(mk, 0);
+        load_q(1);
+        load_kv(mv, 0);
+        for (int u = 1; u < I.n_kv && !*abort_flag; ++u) { load_kv(mk, u); load_kv(mv, u); }
+      }
+      if (*abort_flag) {
+        // what was requested must land before the CTA's shared memory is released
+        for (int i = max(0, t - kPkSlots); i < t; ++i)
+          for (int k = 0; k < kSpinLimit && !mbar_try_wait(kv_full(i % kPkSlots), (uint32_t)(i / kPkSlots) & 1u); ++k) __nanosleep(40);
+        for (int x = 0; x < 2; ++x)
+          if (n_q[x] > 0)
+            for (int k = 0; k < kSpinLimit && !mbar_try_wait(bar(x, Q_FULL), (uint32_t)(n_q[x] - 1) & 1u); ++k) __nanosleep(40);
+      }
+    }
+  } else if (warp == 9 || warp == 10) {
+    // ---------------------------------------------------------------- MMA issuer of one lane
+    reg_dec<kAtRegsSmall>();
+    if (lane == 0) {
+      const int x = warp - 9;
+      const uint32_t t_o = tmem + x * kAtLaneCols + kAtColO, t_s = tmem + x * kAtLaneCols + kAtColS;
+      const uint32_t idesc_pv = idesc_bf16(kPkBM, D, 0, 1);            // B (= V) is MN-major
+      const uint64_t q_desc = smem_desc_sw128(smem_u32(smem + x * S::TILE));
+      PkWalker W(a);
+      PkItem I;
+      int n_item = 0, g0 = 0, ring0 = 0;               // this lane's items and key tiles, the ring's tiles so far
+      while (!*abort_flag && W.next(I)) {
+        const PkLane L = pk_lane(a, I, x);
+        const int n_sub = L.exists ? L.n_tiles : 0;
+        auto full = [&](int u, int is_v) {             // waits for K_u or V_u; returns its slot
+          const int t = ring0 + 2 * u + is_v;
+          mbar_wait_spin(kv_full(t % kPkSlots), (uint32_t)(t / kPkSlots) & 1u, abort_flag);
+          return t % kPkSlots;
+        };
+        for (int u = -1; u < n_sub; ++u) {
+          if (n_sub == 0) break;
+          const bool has_pv = u >= 0, has_qk = u + 1 < n_sub;
+          const int g = g0 + u;
+          int sv = 0, sk = 0;
+          if (!has_pv) mbar_wait_spin(bar(x, Q_FULL), (uint32_t)n_item & 1u, abort_flag);
+          if (has_pv) sv = full(u, 1);
+          if (has_qk) sk = full(u + 1, 0);
+          if (u == 0) mbar_wait_spin(bar(x, O_FREE), ((uint32_t)n_item & 1u) ^ 1u, abort_flag);   // previous item's O has been read
+          if (has_pv) mbar_wait_spin(bar(x, P_FULL), (uint32_t)g & 1u, abort_flag);
+          tc_fence_after();
+          if (*abort_flag) break;
+          if (has_pv) {
+            uint64_t vd = smem_desc_sw128_mn(smem_u32(smem + S::KV + sv * S::TILE), S::HALF);
+            const int ksteps = pk_cols(L, u) >> 4;
+#pragma unroll 1
+            for (int ks = 0; ks < ksteps; ++ks, vd += 2048 >> 4)
+              mma_ts(t_o, t_s + ks * 8, vd, idesc_pv, (u | ks) != 0);
+            mma_commit(kv_empty(sv));
+            if (!has_qk) mma_commit(bar(x, O_FULL));
+          }
+          if (has_qk) {
+            uint64_t qd = q_desc, kd = smem_desc_sw128(smem_u32(smem + S::KV + sk * S::TILE));
+            const uint32_t idesc_qk = idesc_bf16(kPkBM, (uint32_t)pk_cols(L, u + 1));
+#pragma unroll 1
+            for (int ks = 0; ks < D / 16; ++ks) {
+              mma_ss(t_s, qd, kd, idesc_qk, ks != 0);
+              const uint64_t step = (ks == 3) ? (uint64_t)((S::HALF - 96) >> 4) : 2ull;
+              qd += step;
+              kd += step;
+            }
+            mma_commit(bar(x, S_FULL));
+            mma_commit(kv_empty(sk));
+            if (u + 2 == n_sub) mma_commit(bar(x, Q_EMPTY));
+          }
+        }
+        // tiles that only the other lane uses: this lane's share of the release, in the ring's order
+        for (int u = n_sub; u < I.n_kv && !*abort_flag; ++u) {
+          const int sk = full(u, 0);
+          if (*abort_flag) break;
+          mbar_arrive(kv_empty(sk));
+          const int sv = full(u, 1);
+          if (*abort_flag) break;
+          mbar_arrive(kv_empty(sv));
+        }
+        ring0 += 2 * I.n_kv;
+        g0 += n_sub;
+        if (n_sub > 0) ++n_item;
+      }
+    }
+  } else if (warp < 8) {
+    // ---------------------------------------------------------------- softmax / epilogue warps of one lane
+    reg_inc<kAtRegsSoftmax>();
+    const int x = warp >> 2, quad = warp & 3;
+    const int row = quad * 32 + lane;                                  // row within the query tile
+    const uint32_t lane_off = (uint32_t)(quad * 32) << 16;
+    const uint32_t s_addr = tmem + lane_off + x * kAtLaneCols + kAtColS;
+    const uint32_t o_addr = tmem + lane_off + x * kAtLaneCols + kAtColO;
+    const CUtensorMap* mo = reinterpret_cast<const CUtensorMap*>(maps.o);
+    char* so = smem + S::STAGE + warp * 4096;                          // this warp's 4 KB: two 32 x 32 blocks
+    const int P = 1 << a.p_shift, w_pos = (quad * 32) >> a.p_shift;    // this warp's first position in the tile
+    const int w_last = (quad * 32 + 31) >> a.p_shift;
+    PkWalker W(a);
+    PkItem I;
+    int g0 = 0, ring0 = 0, n_item = 0;
+    while (W.next(I)) {
+      const PkLane L = pk_lane(a, I, x);
+      if (!L.exists) { ring0 += 2 * I.n_kv; continue; }
+      const int pos = L.q0 + (row >> a.p_shift);                       // this thread's position
+      const int r0 = L.q0 + w_pos;                                     // the warp's first position
+      float m_used = -INFINITY, l_run = 0.f;
+      const int n_sub = L.n_tiles;
+      for (int u = 0; u < n_sub; ++u) {
+        const int c0 = u * kPkBN;
+        // 32-column chunks of this tile that some row of the warp may see
+        const int n_ch = min(4, (min(L.q_hi, L.q0 + w_last + 1) - c0 + 31) >> 5);
+        mbar_wait_spin(bar(x, S_FULL), (uint32_t)(g0 + u) & 1u, abort_flag);
+        __syncwarp();
+        tc_fence_after();
+        at_softmax_chunks<1>(s_addr, o_addr, n_ch, pos - c0, c0 - r0, pos < L.q_hi, u > 0 ? D / 32 : 0, a.scale_log2, m_used, l_run);
+        const int pad = c0 + pk_cols(L, u) - I.n;                      // rows past the sequence's end that P V covers
+        if (pad > 0) {
+          const int t = ring0 + 2 * u + 1;
+          mbar_wait_spin(kv_full(t % kPkSlots), (uint32_t)(t / kPkSlots) & 1u, abort_flag);
+          char* v_s = smem + S::KV + (t % kPkSlots) * S::TILE;
+          const int valid = I.n - c0;
+          for (int w = row; w < pad * (D / 8); w += 128) {
+            const int rr = valid + w / (D / 8), c = w % (D / 8);
+            *reinterpret_cast<uint4*>(v_s + (c >> 3) * S::HALF + rr * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+          }
+          fence_proxy_async();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(x, P_FULL));
+      }
+      // ---- epilogue: O / l -> bf16 -> out, 64 columns per round through this warp's staging (16-byte units XOR-swizzled
+      // by row pair: the 64-byte swizzle of the tensor map)
+      mbar_wait_spin(bar(x, O_FULL), (uint32_t)n_item & 1u, abort_flag);
+      __syncwarp();
+      tc_fence_after();
+      const float inv = 1.0f / l_run;
+      const bool whole = L.q0 + w_last < L.q_hi;                       // warp-uniform
+#pragma unroll 1
+      for (int rd = 0; rd < D / 64; ++rd) {
+        uint32_t o[64];
+        tmem_ld64(o_addr + rd * 64, o);
+        if (lane == 0) bulk_wait_read<0>();              // earlier stores must have read the staging
+        tmem_ld_wait();
+        if (rd == D / 64 - 1) tc_fence_before();         // all of O is in registers: the next item may overwrite it
+        __syncwarp();
+        if (rd == D / 64 - 1 && lane == 0) mbar_arrive(bar(x, O_FREE));
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const uint32_t* ob = o + 32 * blk + 8 * u;
+            uint4 w;
+            w.x = cvt_bf16x2(__uint_as_float(ob[0]) * inv, __uint_as_float(ob[1]) * inv);
+            w.y = cvt_bf16x2(__uint_as_float(ob[2]) * inv, __uint_as_float(ob[3]) * inv);
+            w.z = cvt_bf16x2(__uint_as_float(ob[4]) * inv, __uint_as_float(ob[5]) * inv);
+            w.w = cvt_bf16x2(__uint_as_float(ob[6]) * inv, __uint_as_float(ob[7]) * inv);
+            *reinterpret_cast<uint4*>(so + blk * 2048 + lane * 64 + ((u ^ ((lane >> 1) & 3)) << 4)) = w;
+          }
+        }
+        if (whole) {
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) {
+            tma_store_4d(mo, smem_u32(so), rd * 64, I.h0, I.row0 + r0, 0);
+            tma_store_4d(mo, smem_u32(so + 2048), rd * 64 + 32, I.h0, I.row0 + r0, 0);
+            bulk_commit();
+          }
+        } else {
+          __syncwarp();
+#pragma unroll
+          for (int blk = 0; blk < 2; ++blk) {
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+              const int r = it * 8 + (lane >> 2), u = lane & 3;
+              const uint4 w = *reinterpret_cast<const uint4*>(so + blk * 2048 + r * 64 + ((u ^ ((r >> 1) & 3)) << 4));
+              const int rp = L.q0 + ((quad * 32 + r) >> a.p_shift);
+              const size_t at = ((size_t)(I.row0 + rp) * a.H + I.h0 + ((quad * 32 + r) & (P - 1))) * D + (2 * rd + blk) * 32 + u * 8;
+              if (rp < L.q_hi && DL_IN_BOUNDS(a.status, KID_PACKED, at + 7, (size_t)a.total * a.H * D))
+                *reinterpret_cast<uint4*>(a.out + at) = w;
+            }
+          }
+          __syncwarp();                                  // the next round overwrites what these loads read
+        }
+      }
+      g0 += n_sub;
+      ring0 += 2 * I.n_kv;
+      ++n_item;
+    }
+    if (lane == 0) bulk_wait_read<0>();                  // staged data must be read before shared memory goes
+    if (*abort_flag && row == 0) report_status(a.status, DL_ERR_TIMEOUT, blockIdx.x);
+  } else {
+    reg_dec<kAtRegsSmall>();                             // same budget as the rest of its warpgroup
+    // starts that lead out of the tensors (they are clamped wherever they are used) and sequences longer than max_rows
+    // (cut off there) are reported
+    if (blockIdx.x == 0)
+      for (int b = lane; b < a.B; b += 32) {
+        const int s0 = __ldg(a.starts + b), s1 = __ldg(a.starts + b + 1);
+        if (s0 < 0 || s1 < s0 || s1 > a.total || s1 - s0 > a.said_rows) report_status(a.status, DL_ERR_INVALID_ARG, b);
+      }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 11) { tc_fence_after(); tmem_dealloc(tmem, 512); }
+}
+
+template <int D>
+static cudaError_t pk_launch(dl_ctx* ctx, const void* q, const void* k, const void* v, int64_t q_stride, int64_t kv_stride,
+                             int32_t Hk, PkArgs& a, cudaStream_t s) {
+  const int P = 1 << a.p_shift;
+  PkMaps maps;
+  const uint64_t dq[3] = {(uint64_t)D, (uint64_t)a.H, (uint64_t)a.total}, sq[2] = {2ull * D, 2ull * q_stride};
+  const uint64_t dk[3] = {(uint64_t)D, (uint64_t)Hk, (uint64_t)a.total}, sk[2] = {2ull * D, 2ull * kv_stride};
+  const uint64_t dout[4] = {(uint64_t)D, (uint64_t)a.H, (uint64_t)a.total, 1}, so[3] = {2ull * D, 2ull * D * a.H, 2ull * D * a.H * a.total};
+  const uint32_t bq[3] = {64u, (uint32_t)P, (uint32_t)(kPkBM / P)}, bk[3] = {64u, 1u, (uint32_t)kPkBN};
+  const uint32_t bo[4] = {32u, (uint32_t)P, (uint32_t)(32 / P), 1u};
+  if (!encode_bf16_map(ctx->tmap_encode, reinterpret_cast<CUtensorMap*>(maps.q), q, 3, dq, sq, bq) ||
+      !encode_bf16_map(ctx->tmap_encode, reinterpret_cast<CUtensorMap*>(maps.k), k, 3, dk, sk, bk) ||
+      !encode_bf16_map(ctx->tmap_encode, reinterpret_cast<CUtensorMap*>(maps.v), v, 3, dk, sk, bk) ||
+      !encode_bf16_map(ctx->tmap_encode, reinterpret_cast<CUtensorMap*>(maps.o), a.out, 4, dout, so, bo, CU_TENSOR_MAP_SWIZZLE_64B))
+    return cudaErrorInvalidValue;
+  const long long items = (long long)a.B * a.n_hs * a.pairs;
+  if (items >= (1LL << 31)) return cudaErrorInvalidValue;
+  cudaError_t e = cudaFuncSetAttribute(attn_packed_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Pk<D>::SMEM);
+  if (e != cudaSuccess) return e;
+  attn_packed_kernel<D><<<(int)std::min<long long>(items, ctx->sm_count), kPkThreads, Pk<D>::SMEM, s>>>(maps, a);
+  return cudaGetLastError();
+}
+
+bool attn_packed_supported(const dl_ctx* ctx) {
+  const dl_model_desc& d = ctx->desc;
+  return d.dtype == DL_BF16 && ctx->tmap_encode != nullptr && (size_t)ctx->smem_optin >= (size_t)Pk<128>::SMEM;
+}
+
+cudaError_t launch_attn_packed(dl_ctx* ctx, const void* q, const void* k, const void* v, int64_t q_stride, int64_t kv_stride,
+                               const int32_t* starts, int32_t B, int32_t Hk, int32_t total, int32_t max_rows, float scale,
+                               void* out, cudaStream_t s) {
+  const dl_model_desc& d = ctx->desc;
+  PkArgs a;
+  a.starts = starts;
+  a.out = static_cast<__nv_bfloat16*>(out);
+  a.status = ctx->ws.base ? ctx->ws.status : nullptr;
+  a.B = B; a.H = d.n_heads; a.G = d.n_heads / Hk; a.total = total; a.max_rows = std::min(max_rows, total);
+  a.said_rows = max_rows;
+  a.p_shift = 0;
+  while (a.p_shift < 4 && a.G % (2 << a.p_shift) == 0) ++a.p_shift;
+  a.n_hs = a.H >> a.p_shift;
+  const int pair_rows = 2 * kPkBM >> a.p_shift;
+  a.pairs = (a.max_rows + pair_rows - 1) / pair_rows;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  return d.head_dim == 128 ? pk_launch<128>(ctx, q, k, v, q_stride, kv_stride, Hk, a, s)
+                           : pk_launch<64>(ctx, q, k, v, q_stride, kv_stride, Hk, a, s);
+}
+
+}  // namespace dl

@@ -44,26 +44,24 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
 }
 
 // The rare path of the softmax below: the row's maximum in use has been raised, so everything the row has
-// accumulated under the old one is multiplied by corr = 2^(old - new): its 128 columns of O in tensor memory
-// (if the item has accumulated anything yet) and the n_stored chunks of P (16 columns of bf16 pairs each) that
+// accumulated under the old one is multiplied by corr = 2^(old - new): its o_blocks blocks of 32 columns of O in tensor
+// memory (none if the item has not accumulated anything yet) and the n_stored chunks of P (16 columns of bf16 pairs each) that
 // this tile has already written.  Kept out of line: it runs once or twice per row, not once per tile.
-static __device__ __noinline__ void at_rescale_row(uint32_t o_addr, uint32_t p_addr, int n_stored, float corr, int o_valid) {
+static __device__ __noinline__ void at_rescale_row(uint32_t o_addr, uint32_t p_addr, int n_stored, float corr, int o_blocks) {
   const uint64_t corr2 = pack2(corr, corr);
-  if (o_valid) {
 #pragma unroll 1
-    for (int cc = 0; cc < 4; ++cc) {
-      uint32_t o[32];
-      tmem_ld32(o_addr + cc * 32, o);
-      tmem_ld_wait();
+  for (int cc = 0; cc < o_blocks; ++cc) {
+    uint32_t o[32];
+    tmem_ld32(o_addr + cc * 32, o);
+    tmem_ld_wait();
 #pragma unroll
-      for (int i = 0; i < 32; i += 2) {
-        float y0, y1;
-        unpack2(fmul2(pack2(__uint_as_float(o[i]), __uint_as_float(o[i + 1])), corr2), y0, y1);
-        o[i] = __float_as_uint(y0);
-        o[i + 1] = __float_as_uint(y1);
-      }
-      tmem_st32(o_addr + cc * 32, o);
+    for (int i = 0; i < 32; i += 2) {
+      float y0, y1;
+      unpack2(fmul2(pack2(__uint_as_float(o[i]), __uint_as_float(o[i + 1])), corr2), y0, y1);
+      o[i] = __float_as_uint(y0);
+      o[i + 1] = __float_as_uint(y1);
     }
+    tmem_st32(o_addr + cc * 32, o);
   }
 #pragma unroll 1
   for (int cc = 0; cc < n_stored; ++cc) {
@@ -98,10 +96,10 @@ __device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t* r) {
 // quadrant.  Fully unrolled (4 chunks) the pass cost 15 % of the kernel's time more than in two rolled halves of 64
 // columns, and those 3 % more than this form on short contexts.
 //   n_ch: 32-column chunks that some row of the warp may see (chunks beyond get P = 0); column c is visible to this
-//   row iff c <= vis; owned: the row belongs to this tile; o_valid: the item has accumulated into O already.
+//   row iff c <= vis; owned: the row belongs to this tile; o_blocks: blocks of 32 columns of O that the item has accumulated into (0: none yet).
 template <int NPOLY>
 __device__ __forceinline__ void at_softmax_chunks(uint32_t s_addr, uint32_t o_addr, int n_ch, int vis, int c0_minus_r0,
-                                                  bool owned, int o_valid, float scale_log2, float& m_used, float& l_run) {
+                                                  bool owned, int o_blocks, float scale_log2, float& m_used, float& l_run) {
   const int n_q = max(min(4, n_ch), 0);
   const uint64_t sc2 = pack2(scale_log2, scale_log2);
   uint32_t buf[32];
@@ -134,7 +132,7 @@ __device__ __forceinline__ void at_softmax_chunks(uint32_t s_addr, uint32_t o_ad
       const uint64_t corr2 = pack2(corr, corr);
 #pragma unroll
       for (int i = 0; i < 4; ++i) l2[i] = fmul2(l2[i], corr2);
-      at_rescale_row(o_addr, s_addr, q, corr, o_valid);
+      at_rescale_row(o_addr, s_addr, q, corr, o_blocks);
     }
     const uint64_t nm2 = pack2(-m_used, -m_used);
     uint64_t t[16];

@@ -249,7 +249,7 @@ attn_prefill_tc_kernel(const __grid_constant__ AtMaps maps, const AtArgs a) {
         }
         __syncwarp();
         tc_fence_after();
-        at_softmax_chunks<1>(s_addr, o_addr, n_ch, grow - c0, c0 - r0, grow < L.q_hi, u > 0, a.scale_log2, m_used, l_run);
+        at_softmax_chunks<1>(s_addr, o_addr, n_ch, grow - c0, c0 - r0, grow < L.q_hi, u > 0 ? 4 : 0, a.scale_log2, m_used, l_run);
         if (take_turns && lane == 0) in_softmax[4 * x + quad] = 0;
         if (u == n_sub - 1 && L.q_hi == I.n) {
           // last tile of the sequence: the P V covers keys up to the next multiple of 16; zero the V rows between

@@ -35,7 +35,8 @@ __device__ __forceinline__ void report_status(DeviceStatus* st, int32_t code, lo
 enum KernelId : int {
   KID_DECODE_MMA = 1, KID_DECODE_SIMT = 2, KID_DECODE_FP8 = 3, KID_COMPACT_PLAN = 4, KID_COMPACT_COPY = 5,
   KID_TOPK = 6, KID_KEEP = 7, KID_PREFILL_TOP = 8, KID_PREFILL_SIMT = 9, KID_PREFILL_TC = 10, KID_QUANTIZE = 11,
-  KID_PREDICTOR = 12, KID_SELFTEST = 0x7e
+  KID_PREDICTOR = 12, KID_PACKED = 13, KID_KV4_APPEND = 14, KID_KV4_READ = 15, KID_DECODE_KV4 = 16, KID_PAGES = 17,
+  KID_SELFTEST = 0x7e
 };
 #ifdef DL_BOUNDS
 __device__ __forceinline__ bool bounds_ok(DeviceStatus* st, int kid, long long idx, long long extent) {
@@ -77,9 +78,10 @@ struct Workspace {
   float* pred_split = nullptr;        // [unit tiles][kPredKSplit][kPredRowTile][tile width] raw sums of the decode-shape predictor
   int32_t* pred_split_ticket = nullptr;   // [kPredMaxSplit]; zero between launches
   int32_t pred_rows_padded = 0;
+  float* kv4_partial = nullptr;       // parts of split pairs of the 4-bit decode attention (attn_decode_kv4.cu)
 };
 
-int64_t workspace_layout(const dl_model_desc& d, int32_t max_batch, int32_t max_rows, int32_t cap,
+int64_t workspace_layout(const dl_model_desc& d, int32_t sm_count, int32_t max_batch, int32_t max_rows, int32_t cap,
                          Workspace* ws /* may be null: size query only */);
 
 struct Options {
@@ -180,6 +182,29 @@ cudaError_t launch_attn_prefill_tc(dl_ctx* ctx, const void* q, const void* k_cac
                                    const int32_t* cache_len, int32_t B, int32_t cap, int32_t n_max,
                                    float scale, void* out, cudaStream_t s);
 bool attn_prefill_tc_supported(const dl_ctx* ctx);
+
+bool attn_packed_supported(const dl_ctx* ctx);
+cudaError_t launch_attn_packed(dl_ctx* ctx, const void* q, const void* k, const void* v, int64_t q_stride, int64_t kv_stride,
+                               const int32_t* starts, int32_t B, int32_t Hk, int32_t total, int32_t max_rows, float scale,
+                               void* out, cudaStream_t s);
+
+int64_t kv4_scratch_floats(int32_t sm_count, const dl_model_desc& d);
+cudaError_t launch_kv4_append(const dl_ctx* ctx, const dl_pages* p, int32_t Hk, void* pool, const void* k, const void* v,
+                              int64_t stride, const int32_t* starts, const uint8_t* keep, int32_t total, int32_t commit,
+                              cudaStream_t s);
+cudaError_t launch_kv4_read(const dl_ctx* ctx, const dl_pages* p, int32_t Hk, const void* pool, const int32_t* row0,
+                            const int32_t* starts, int32_t total, void* k_out, void* v_out, cudaStream_t s);
+cudaError_t launch_attn_decode_kv4(const dl_ctx* ctx, const dl_pages* p, int32_t Hk, void* pool, const void* q,
+                                   const void* k_t, const void* v_t, const uint8_t* keep, float scale, void* out,
+                                   cudaStream_t s);
+
+int64_t pages_scratch_bytes(const dl_pages* p);
+cudaError_t launch_pages_reserve(const dl_ctx* ctx, const dl_pages* p, const int32_t* need, cudaStream_t s);
+cudaError_t launch_pages_free(const dl_ctx* ctx, const dl_pages* p, const uint8_t* gone, cudaStream_t s);
+cudaError_t launch_pages_fork(const dl_ctx* ctx, const dl_pages* p, const int32_t* parent, int32_t n_pools,
+                              void* const* pools, int64_t page_bytes, void* scratch, cudaStream_t s);
+cudaError_t launch_pages_compact(const dl_ctx* ctx, const dl_pages* p, int32_t n_pools, void* const* pools,
+                                 int64_t page_bytes, int32_t* live, void* scratch, cudaStream_t s);
 
 int64_t predictor_paper_scratch_bytes(int64_t rows);
 bool predictor_paper_supported(const dl_ctx* ctx);
