@@ -6,6 +6,7 @@ built the import of this module's `lib()` raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 
@@ -85,12 +86,13 @@ class Pages:
         self.cache_len = self.book[a + b:a + b + B]
         self.desc = PagesDesc(B, n_pages, max_pages, page_rows, self.table.data_ptr(), self.refs.data_ptr(),
                               self.cache_len.data_ptr())
+        self.ref = C.pointer(self.desc)
         self._scratch = None
 
     def scratch(self, ctx: "Context") -> torch.Tensor:
         """Scratch of dl_pages_fork and dl_pages_compact, allocated at the first use."""
         if self._scratch is None:
-            n = lib().dl_pages_scratch_bytes(ctx._h, C.byref(self.desc))
+            n = lib().dl_pages_scratch_bytes(ctx._h, self.ref)
             if n < 0:
                 raise DlError(int(n), "dl_pages_scratch_bytes")
             self._scratch = torch.empty(max(int(n), 256), dtype=torch.uint8, device=self.book.device)
@@ -178,8 +180,8 @@ def lib() -> C.CDLL:
             "dl_pages_scratch_bytes": (i64, [vp, C.POINTER(PagesDesc)]),
             "dl_pages_reserve": (i32, [vp, C.POINTER(PagesDesc), vp, vp]),
             "dl_pages_free": (i32, [vp, C.POINTER(PagesDesc), vp, vp]),
-            "dl_pages_fork": (i32, [vp, C.POINTER(PagesDesc), vp, i32, C.POINTER(vp), i64, vp, i64, vp]),
-            "dl_pages_compact": (i32, [vp, C.POINTER(PagesDesc), i32, C.POINTER(vp), i64, vp, vp, i64, vp]),
+            "dl_pages_fork": (i32, [vp, C.POINTER(PagesDesc), vp, i32, vp, i64, vp, i64, vp]),
+            "dl_pages_compact": (i32, [vp, C.POINTER(PagesDesc), i32, vp, i64, vp, vp, i64, vp]),
             "dl_kv4_page_bytes": (i64, [vp, i32, i32]),
             "dl_kv4_append": (i32, [vp, C.POINTER(PagesDesc), i32, vp, vp, vp, i64, vp, vp, i32, i32, vp]),
             "dl_kv4_read": (i32, [vp, C.POINTER(PagesDesc), i32, vp, vp, vp, i32, vp, vp, vp]),
@@ -214,17 +216,31 @@ def _ptr(t):
     return int(t)
 
 
-def _rows(t, what: str):
-    """Pointer and row stride (in elements) of packed rows [total, heads, D] whose last two dimensions are dense."""
-    if t.dim() != 3 or (t.shape[0] > 0 and (t.stride(2) != 1 or t.stride(1) != t.shape[2])):
-        raise ValueError(f"{what}: want [rows, heads, D] with dense heads")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2])
+# raw handle of a device's current stream; the public call builds a Stream object around it, a few microseconds a call
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _want(t, dtype, shape, what: str):
-    """A tensor the kernels will read or write by this shape and type."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{what}: want {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+def _refuse(t, dtype, shape, what, index):
+    raise ValueError(f"{what}: want a contiguous {dtype} {tuple(shape)} on cuda:{index}, got {t.dtype} {tuple(t.shape)} "
+                     f"with strides {t.stride()} on {t.device}")
+
+
+def _arg(t, dtype, shape, what: str, index: int) -> int:
+    """Pointer of a tensor that the kernels read or write by this type and shape."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        _refuse(t, dtype, shape, what, index)
+    return t.data_ptr()
+
+
+def _rows(t, dtype, shape, what: str, index: int):
+    """Pointer and row stride (in elements) of packed rows [rows, heads, D] whose last two dimensions are dense."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
+        _refuse(t, dtype, shape, what, index)
+    s0, s1, s2 = t.stride()
+    if shape[0] > 0 and (s2 != 1 or (s1 != shape[2] and shape[1] > 1)):
+        raise ValueError(f"{what}: want rows with dense heads, got strides {t.stride()}")
+    return t.data_ptr(), (s0 if shape[0] > 1 else shape[1] * shape[2])
 
 
 def _stream(stream=None):
@@ -444,106 +460,109 @@ class Context:
                     "dl_decode_keep2")
 
     # ---- packed prompts, pages, the 4-bit cache (extensions, not in the paper)
+    # These check type, shape and device of every tensor; without `stream` they use the current one of the context's device.
+    def _on(self, stream):
+        return _raw_stream(self.device.index) if stream is None else stream.cuda_stream
+
     def attn_prefill_packed(self, q, k, v, starts, max_rows, scale, out, stream=None):
         """dl_attn_prefill_packed: q [total, n_heads, D], k / v [total, n_kv_heads, D] (parts of one projection's output
         will do: rows may be strided), starts int32 [B + 1], max_rows: length of the longest sequence."""
-        total, n_kv = q.shape[0], k.shape[1]
-        _want(q, self.dtype, (total, self.H, self.D), "q")
-        _want(k, self.dtype, (total, n_kv, self.D), "k")
-        _want(v, self.dtype, (total, n_kv, self.D), "v")
-        _want(out, self.dtype, (total, self.H, self.D), "out")
-        _want(starts, torch.int32, (starts.numel(),), "starts")
-        (qp, qs), (kp, ks), (vp, vs) = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
+        total, n_kv, D, i = q.shape[0], k.shape[1], self.D, self.device.index
+        qp, qs = _rows(q, self.dtype, (total, self.H, D), "q", i)
+        kp, ks = _rows(k, self.dtype, (total, n_kv, D), "k", i)
+        vp, vs = _rows(v, self.dtype, (total, n_kv, D), "v", i)
         if ks != vs:
             raise ValueError("k and v must have the same row stride")
-        self._check(lib().dl_attn_prefill_packed(self._h, qp, kp, vp, qs, ks, _ptr(starts), starts.numel() - 1, n_kv, total,
-                                                 int(max_rows), float(scale), _ptr(out), _stream(stream)),
-                    "dl_attn_prefill_packed")
+        n = starts.shape[0]
+        self._check(lib().dl_attn_prefill_packed(
+            self._h, qp, kp, vp, qs, ks, _arg(starts, torch.int32, (n,), "starts", i), n - 1, n_kv, total, max_rows, scale,
+            _arg(out, self.dtype, (total, self.H, D), "out", i), self._on(stream)), "dl_attn_prefill_packed")
 
     def pages_reserve(self, pages: Pages, need, stream=None):
-        _want(need, torch.int32, (pages.B,), "need")
-        self._check(lib().dl_pages_reserve(self._h, C.byref(pages.desc), _ptr(need), _stream(stream)), "dl_pages_reserve")
+        """dl_pages_reserve: need int32 [B]."""
+        self._check(lib().dl_pages_reserve(self._h, pages.ref, _arg(need, torch.int32, (pages.B,), "need", self.device.index),
+                                           self._on(stream)), "dl_pages_reserve")
 
     def pages_free(self, pages: Pages, gone, stream=None):
-        _want(gone, torch.uint8, (pages.B,), "gone")
-        self._check(lib().dl_pages_free(self._h, C.byref(pages.desc), _ptr(gone), _stream(stream)), "dl_pages_free")
+        """dl_pages_free: gone uint8 [B]."""
+        self._check(lib().dl_pages_free(self._h, pages.ref, _arg(gone, torch.uint8, (pages.B,), "gone", self.device.index),
+                                        self._on(stream)), "dl_pages_free")
 
     def _pools(self, pages: Pages, pools):
+        """Count, array of pointers and bytes of a page of `pools`, tensors [n_pages, ...] that are alike."""
+        if not pools:
+            return 0, None, 0
+        n_bytes, index = pools[0].nbytes, self.device.index
         for p in pools:
-            if p.shape[0] != pages.n_pages or not p.is_contiguous() or p.numel() * p.element_size() != pools[0].numel() * pools[0].element_size():
-                raise ValueError("pools: want contiguous tensors [n_pages, ...] of one size")
-        page_bytes = pools[0].numel() * pools[0].element_size() // pages.n_pages if pools else 0
-        return len(pools), self.pointer_array(pools), page_bytes
+            if p.nbytes != n_bytes or not p.is_contiguous() or p.get_device() != index:
+                raise ValueError(f"pools: want contiguous tensors of one size on cuda:{index}")
+        if pools[0].shape[0] != pages.n_pages:
+            raise ValueError(f"pools: want {pages.n_pages} pages, got {tuple(pools[0].shape)}")
+        ptrs = array.array("Q", [p.data_ptr() for p in pools])
+        return len(ptrs), ptrs, n_bytes // pages.n_pages
 
     def pages_fork(self, pages: Pages, parent, pools, stream=None):
-        """dl_pages_fork; pools: list of tensors [n_pages, ...], one per layer."""
-        _want(parent, torch.int32, (pages.B,), "parent")
-        n, arr, page_bytes = self._pools(pages, pools)
+        """dl_pages_fork: parent int32 [B]; pools: list of tensors [n_pages, ...], one per layer."""
+        n, ptrs, page_bytes = self._pools(pages, pools)
         scratch = pages.scratch(self)
-        self._check(lib().dl_pages_fork(self._h, C.byref(pages.desc), _ptr(parent), n, arr, page_bytes, _ptr(scratch),
-                                        scratch.numel(), _stream(stream)), "dl_pages_fork")
+        self._check(lib().dl_pages_fork(
+            self._h, pages.ref, _arg(parent, torch.int32, (pages.B,), "parent", self.device.index), n,
+            ptrs.buffer_info()[0] if n else None, page_bytes, scratch.data_ptr(), scratch.shape[0], self._on(stream)),
+            "dl_pages_fork")
 
     def pages_compact(self, pages: Pages, pools, n_live=None, stream=None):
         """dl_pages_compact; n_live: int32 tensor [1] for the number of pages in use, or None."""
-        if n_live is not None:
-            _want(n_live, torch.int32, (1,), "n_live")
-        n, arr, page_bytes = self._pools(pages, pools)
+        n, ptrs, page_bytes = self._pools(pages, pools)
         scratch = pages.scratch(self)
-        self._check(lib().dl_pages_compact(self._h, C.byref(pages.desc), n, arr, page_bytes, _ptr(n_live), _ptr(scratch),
-                                           scratch.numel(), _stream(stream)), "dl_pages_compact")
+        live = None if n_live is None else _arg(n_live, torch.int32, (1,), "n_live", self.device.index)
+        self._check(lib().dl_pages_compact(self._h, pages.ref, n, ptrs.buffer_info()[0] if n else None, page_bytes, live,
+                                           scratch.data_ptr(), scratch.shape[0], self._on(stream)), "dl_pages_compact")
+
+    def kv4_page_bytes(self, n_kv_heads: int, page_rows: int) -> int:
+        n = lib().dl_kv4_page_bytes(self._h, n_kv_heads, page_rows)
+        if n < 0:
+            raise DlError(int(n), "dl_kv4_page_bytes")
+        return int(n)
 
     def kv4_pool(self, pages: Pages, n_kv_heads: int) -> torch.Tensor:
         """A pool of 4-bit pages (uint8 [n_pages, page bytes]) for these books."""
-        n = lib().dl_kv4_page_bytes(self._h, n_kv_heads, pages.page_rows)
-        if n < 0:
-            raise DlError(int(n), "dl_kv4_page_bytes")
-        return torch.zeros(pages.n_pages, int(n), dtype=torch.uint8, device=pages.book.device)
+        return torch.zeros(pages.n_pages, self.kv4_page_bytes(n_kv_heads, pages.page_rows), dtype=torch.uint8,
+                           device=pages.book.device)
 
-    def _want_pool(self, pages: Pages, pool, n_kv: int):
-        n = lib().dl_kv4_page_bytes(self._h, n_kv, pages.page_rows)
-        if n < 0:
-            raise DlError(int(n), "dl_kv4_page_bytes")
-        _want(pool, torch.uint8, (pages.n_pages, int(n)), "pool")
+    def _pool(self, pages: Pages, pool, n_kv: int) -> int:
+        return _arg(pool, torch.uint8, (pages.n_pages, n_kv * pages.page_rows * 9 * self.D // 8), "pool", self.device.index)
 
     def kv4_append(self, pages: Pages, pool, k, v, starts, keep=None, commit=True, stream=None):
         """dl_kv4_append: k, v [total, n_kv_heads, D] bf16 (rows may be strided), starts int32 [B + 1], keep uint8 [total]."""
-        total, n_kv = k.shape[0], k.shape[1]
-        _want(k, self.dtype, (total, n_kv, self.D), "k")
-        _want(v, self.dtype, (total, n_kv, self.D), "v")
-        _want(starts, torch.int32, (pages.B + 1,), "starts")
-        if keep is not None:
-            _want(keep, torch.uint8, (total,), "keep")
-        self._want_pool(pages, pool, n_kv)
-        (kp, ks), (vp, vs) = _rows(k, "k"), _rows(v, "v")
+        total, n_kv, i = k.shape[0], k.shape[1], self.device.index
+        kp, ks = _rows(k, self.dtype, (total, n_kv, self.D), "k", i)
+        vp, vs = _rows(v, self.dtype, (total, n_kv, self.D), "v", i)
         if ks != vs:
             raise ValueError("k and v must have the same row stride")
-        self._check(lib().dl_kv4_append(self._h, C.byref(pages.desc), n_kv, _ptr(pool), kp, vp, ks, _ptr(starts), _ptr(keep),
-                                        total, int(bool(commit)), _stream(stream)), "dl_kv4_append")
+        self._check(lib().dl_kv4_append(
+            self._h, pages.ref, n_kv, self._pool(pages, pool, n_kv), kp, vp, ks,
+            _arg(starts, torch.int32, (pages.B + 1,), "starts", i),
+            None if keep is None else _arg(keep, torch.uint8, (total,), "keep", i), total, 1 if commit else 0,
+            self._on(stream)), "dl_kv4_append")
 
     def kv4_read(self, pages: Pages, pool, row0, starts, k_out, v_out, stream=None):
         """dl_kv4_read: rows from row0[b] on of every sequence into k_out, v_out [total, n_kv_heads, D] bf16."""
-        total, n_kv = k_out.shape[0], k_out.shape[1]
-        _want(k_out, self.dtype, (total, n_kv, self.D), "k_out")
-        _want(v_out, self.dtype, (total, n_kv, self.D), "v_out")
-        _want(row0, torch.int32, (pages.B,), "row0")
-        _want(starts, torch.int32, (pages.B + 1,), "starts")
-        self._want_pool(pages, pool, n_kv)
-        self._check(lib().dl_kv4_read(self._h, C.byref(pages.desc), n_kv, _ptr(pool), _ptr(row0), _ptr(starts), total,
-                                      _ptr(k_out), _ptr(v_out), _stream(stream)), "dl_kv4_read")
+        total, n_kv, i = k_out.shape[0], k_out.shape[1], self.device.index
+        shape = (total, n_kv, self.D)
+        self._check(lib().dl_kv4_read(
+            self._h, pages.ref, n_kv, self._pool(pages, pool, n_kv), _arg(row0, torch.int32, (pages.B,), "row0", i),
+            _arg(starts, torch.int32, (pages.B + 1,), "starts", i), total, _arg(k_out, self.dtype, shape, "k_out", i),
+            _arg(v_out, self.dtype, shape, "v_out", i), self._on(stream)), "dl_kv4_read")
 
     def kv4_attn_decode(self, pages: Pages, pool, q_t, k_t, v_t, keep, scale, out, stream=None):
         """dl_kv4_attn_decode: q_t, out [B, n_heads, D]; k_t, v_t [B, n_kv_heads, D]; keep uint8 [B] or None."""
-        n_kv = k_t.shape[1]
-        _want(q_t, self.dtype, (pages.B, self.H, self.D), "q_t")
-        _want(out, self.dtype, (pages.B, self.H, self.D), "out")
-        _want(k_t, self.dtype, (pages.B, n_kv, self.D), "k_t")
-        _want(v_t, self.dtype, (pages.B, n_kv, self.D), "v_t")
-        if keep is not None:
-            _want(keep, torch.uint8, (pages.B,), "keep")
-        self._want_pool(pages, pool, n_kv)
-        self._check(lib().dl_kv4_attn_decode(self._h, C.byref(pages.desc), n_kv, _ptr(pool), _ptr(q_t), _ptr(k_t),
-                                             _ptr(v_t), _ptr(keep), float(scale), _ptr(out), _stream(stream)),
-                    "dl_kv4_attn_decode")
+        n_kv, B, i = k_t.shape[1], pages.B, self.device.index
+        big, small = (B, self.H, self.D), (B, n_kv, self.D)
+        self._check(lib().dl_kv4_attn_decode(
+            self._h, pages.ref, n_kv, self._pool(pages, pool, n_kv), _arg(q_t, self.dtype, big, "q_t", i),
+            _arg(k_t, self.dtype, small, "k_t", i), _arg(v_t, self.dtype, small, "v_t", i),
+            None if keep is None else _arg(keep, torch.uint8, (B,), "keep", i), scale,
+            _arg(out, self.dtype, big, "out", i), self._on(stream)), "dl_kv4_attn_decode")
 
     def selftest_wait_timeout(self, polls: int = 64, stream=None):
         self._check(lib().dl_selftest_wait_timeout(self._h, int(polls), _stream(stream)), "dl_selftest_wait_timeout")

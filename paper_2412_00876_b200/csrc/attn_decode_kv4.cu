@@ -6,23 +6,24 @@
 // Bound by the bytes of the cache: 18 D bytes per 16 rows and K/V head.  The codes are never turned into values:
 //   scores   q . k = sum over groups of  s * (q . codes) + z * (sum of q over the group)
 //   outputs  O     = sum over keys of (p s) codes + p z
-// so the matrix instructions work on the codes themselves, and s and z are applied once per key and group.  A code in
-// bits 0-3 or 4-7 of a half word IS an fp16 number (a subnormal: code * 2^-24 or code * 2^-20), so eight codes become
-// four operand registers with one shift and four ANDs; the powers of two are taken out in q (an exact scaling by 1/16
-// of the dims concerned) and at the end.  The query heads are the N side of mma.sync m16n8k16 and 16 keys (scores) or
-// 16 dims (outputs) its M side, so that up to 8 heads of a group cost one pass over the codes:
+// so the matrix instructions work on the codes themselves, and s and z are applied once per key and group.
+// A code in bits 0-3 or 4-7 of a half word IS an fp16 number (a subnormal: code * 2^-24 or code * 2^-20), so eight codes
+// become four operand registers of mma.sync m16n8k16 with one shift and four ANDs; the powers of two are taken out in q
+// (an exact scaling by 1/16 of the dims concerned) and at the end.  (As e4m3 bytes, where a code is code * 2^-9, they
+// would take one shift and two ANDs, but the 8-bit m16n8k32 is made of conversions and two 16-bit products on this GPU:
+// 364 instead of 250 instructions a tile.)  q is divided by a power of two into fp16's range (exact down to 2^-28 of a head's
+// largest value).  P s is rounded to fp16 (11 bits) after division by a power of two 2^E that tracks the largest s; the
+// maximum in use of the softmax lags by up to 2^8, so P s 2^-E <= 2^12.
+// The query heads are the N side and 16 keys (scores) or 16 dims (outputs) the M side, so that up to 8 heads of a group
+// cost one pass over the codes:
 //   S^T[key][head] = K codes [16 keys][16 dims] x q^T          A straight from shared memory, B = q (registers)
-//   O^T[dim][head] += V^T codes [16 dims][16 keys] x P^T       A: a byte permute pairs two keys, B: P through movmatrix
-// The order in which keys meet the k index is key(i) = (i >> 1) + 4 (i & 1) within 8, chosen with the page layout so that
-// both operands' loads are free of bank conflicts.  P s is rounded to fp16 (11 bits) after division by a power of two
-// 2^E that tracks the largest s; the maximum in use of the softmax lags by up to 2^8, so P <= 2^8, P s 2^-E <= 2^12.
-// q is scaled by a power of two into fp16's range (exact down to 2^-28 of a head's largest value).
+//   O^T[dim][head] += V^T codes [16 dims][16 keys] x P^T       A straight from shared memory, B: P through movmatrix
 //
-// Work: the tiles of all (sequence, K/V head) pairs in one line, cut into equal ranges, one per warp: every warp
-// streams the same number of tiles whatever the lengths are, through its own ring of tiles (one bulk copy each).  A
-// pair that lies within one range is finished there; the parts of the others go to scratch and a second kernel,
+// Work: the units (32 rows: two tiles) of all (sequence, K/V head) pairs in one line, cut into equal ranges, one per warp:
+// every warp streams the same number of units whatever the lengths are, through its own ring (one bulk copy per
+// tile).  A pair that lies within one range is finished there; the parts of the others go to scratch and a second kernel,
 // launched to overlap, joins them in order (no atomics: the same call gives the same bits).  Page numbers are fetched
-// 32 tiles ahead, a lane each.
+// 16 units ahead, a tile per lane; the lane that holds a tile's number copies it.
 #include <algorithm>
 
 #include "kv4.cuh"
@@ -39,9 +40,12 @@ struct K4Args {
 };
 
 constexpr int kK4Warps = 4;              // warps per CTA
+// CTAs per SM by blocks of 8 query heads: what their registers allow
+__host__ __device__ constexpr int k4_ctas(int nt) { return nt == 1 ? 4 : 2; }
 constexpr int kK4Lag = 8;                // log2 units by which the maximum in use may lag
-constexpr int kK4MinTiles = 2;           // fewest tiles worth a warp of its own
-constexpr int kK4MergeThreads = 128;
+constexpr int kK4Unit = 32;              // rows of a unit: two tiles
+constexpr int kK4MinUnits = 1;           // fewest units worth a warp of its own
+constexpr int kK4MergeWarps = 16;        // most warps of a joining CTA
 
 // floats of a part: D sums per head, then the head's maximum and its sum of exponentials (16-byte steps)
 template <int D> __host__ __device__ constexpr int k4_slot(int G) { return G * (D + 4); }
@@ -49,8 +53,8 @@ template <int D> __host__ __device__ constexpr int k4_slot(int G) { return G * (
 __device__ __forceinline__ int k4_rows(const PagesArg& p, int b) {
   return (int)min((long long)max(__ldg(p.len + b), 0), (long long)p.max_pages * (kKv4Rows << p.tile_shift));
 }
-// tiles of one K/V head of a sequence of n rows; an empty one counts 1, so that somebody writes its output
-__device__ __forceinline__ int k4_units(int n) { return max(1, (n + kKv4Rows - 1) / kKv4Rows); }
+// units of one K/V head of a sequence of n rows; an empty one counts 1, so that somebody writes its output
+__device__ __forceinline__ int k4_units(int n) { return max(1, (n + kK4Unit - 1) / kK4Unit); }
 
 // pre[b] = units in front of sequence b, pre[B] = all; called by the whole CTA
 __device__ __forceinline__ void k4_prefix(const PagesArg& p, int Hk, int* pre, int* sums) {
@@ -81,7 +85,7 @@ __device__ __forceinline__ int k4_find(const int* pre, int B, int u) {
   return lo;
 }
 // the line of `total` units as W ranges
-__device__ __forceinline__ int k4_width(int total, int grid_warps) { return max(1, min(grid_warps, total / kK4MinTiles)); }
+__device__ __forceinline__ int k4_width(int total, int grid_warps) { return max(1, min(grid_warps, total / kK4MinUnits)); }
 __device__ __forceinline__ int k4_range(int w, int total, int W) { return (int)((long long)w * total / W); }
 __device__ __forceinline__ int k4_owner(int u, int total, int W) { return (int)((((long long)u + 1) * W - 1) / total); }
 
@@ -91,6 +95,14 @@ __device__ __forceinline__ void k4_mma(float* c, uint32_t a0, uint32_t a1, uint3
       "{%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// the same into fresh accumulators
+__device__ __forceinline__ void k4_mma_first(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%10, %10, %10, %10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t k4_transpose(uint32_t v) {
   uint32_t r;
@@ -129,20 +141,19 @@ __device__ __forceinline__ void k4_load16(const __nv_bfloat16* p, bool on, float
 }
 
 template <int D, int NT>                                          // NT: blocks of 8 query heads
-__global__ void __launch_bounds__(kK4Warps * 32, NT == 1 ? 4 : 2)
+__global__ void __launch_bounds__(kK4Warps * 32, k4_ctas(NT))
 attn_decode_kv4_kernel(const K4Args a) {
   using F = Kv4<D>;
   constexpr int NG = F::NG;
   extern __shared__ __align__(128) char smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, j = lane & 3;
   const int NS = a.stages;
-  char* ring = smem + (size_t)warp * NS * F::TILE;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (size_t)kK4Warps * NS * F::TILE) + warp * NS;
-  int* pre = reinterpret_cast<int*>(smem + (size_t)kK4Warps * NS * (F::TILE + 8));
+  char* ring = smem + (size_t)warp * NS * (2 * F::TILE);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (size_t)kK4Warps * NS * (2 * F::TILE)) + warp * NS;
+  int* pre = reinterpret_cast<int*>(smem + (size_t)kK4Warps * NS * (2 * F::TILE + 8));
   __shared__ int sh_sums[kK4Warps];
   __shared__ int sh_abort;
   volatile int* abort_flag = &sh_abort;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (tid == 0) sh_abort = 0;
   if (lane == 0) {
     for (int s = 0; s < NS; ++s) mbar_init(smem_u32(&bars[s]), 1);
@@ -154,15 +165,16 @@ attn_decode_kv4_kernel(const K4Args a) {
   if (gw >= W) return;
   const int u0 = k4_range(gw, total, W), u1 = k4_range(gw + 1, total, W);
 
-  // ---- page numbers: lane i holds those of unit base + i, this block of 32 and (requested ahead) the next
+  // ---- page numbers: lane 2 i + h holds that of tile h of unit base + i, for this block of 16 units and (requested
+  //      ahead) the next
   int nx_page = -1, nx_b = -1, nx_hk = 0, nx_t = 0;               // nx_b < 0: nothing to copy
   auto request = [&](int base) {
-    const int u = base + lane;
+    const int u = base + (lane >> 1);
     nx_b = -1;
     if (u < u1) {
       const int b = k4_find(pre, a.pg.B, u), rem = u - pre[b], units = (pre[b + 1] - pre[b]) / a.Hk;
       nx_hk = rem / units;
-      nx_t = rem - nx_hk * units;
+      nx_t = 2 * (rem - nx_hk * units) + (lane & 1);
       if (nx_t * kKv4Rows < k4_rows(a.pg, b)) {
         nx_b = b;
         nx_page = __ldg(a.pg.table + (size_t)b * a.pg.max_pages + (nx_t >> a.pg.tile_shift));
@@ -178,28 +190,29 @@ attn_decode_kv4_kernel(const K4Args a) {
     return idx;
   };
   request(u0);
-  int cur_idx = resolve(), p_base = u0;
-  request(u0 + 32);
-  uint32_t absent = 0;                                            // slots whose tile was not fetched
+  int cur_idx = resolve(), p_at = 0;                              // p_at: place of the next unit in this block
+  request(u0 + 16);
+  uint32_t here = 0;                                              // bits 2 s, 2 s + 1: which tiles of slot s were fetched
   int p_u = u0, p_slot = 0;
   auto produce = [&]() {
-    if (p_u == p_base + 32) {
+    if (p_at == 16) {
       cur_idx = resolve();
-      p_base += 32;
-      request(p_base + 32);
+      p_at = 0;
+      request(p_u + 16);
     }
-    const int idx = __shfl_sync(0xffffffffu, cur_idx, p_u - p_base);
+    const bool mine = (lane >> 1) == p_at && cur_idx >= 0;
+    const uint32_t got = (__ballot_sync(0xffffffffu, mine) >> (2 * p_at)) & 3u;
     const uint32_t bar = smem_u32(&bars[p_slot]);
     if (lane == 0) {
-      if (idx >= 0) {
-        mbar_expect_tx(bar, F::TILE);
-        bulk_g2s(smem_u32(ring + (size_t)p_slot * F::TILE), a.pool + (long long)idx * F::TILE, F::TILE, bar);
-      } else {
-        mbar_arrive(bar);
-      }
+      if (got) mbar_expect_tx(bar, got == 3u ? 2 * F::TILE : F::TILE);
+      else mbar_arrive(bar);
     }
-    absent = idx >= 0 ? absent & ~(1u << p_slot) : absent | (1u << p_slot);
+    __syncwarp();
+    if (mine)
+      bulk_g2s(smem_u32(ring + (size_t)(2 * p_slot + (lane & 1)) * F::TILE), a.pool + (long long)cur_idx * F::TILE, F::TILE, bar);
+    here = (here & ~(3u << (2 * p_slot))) | (got << (2 * p_slot));
     ++p_u;
+    ++p_at;
     if (++p_slot == NS) p_slot = 0;
   };
   for (int i = 0; i < NS && p_u < u1; ++i) produce();
@@ -208,6 +221,7 @@ attn_decode_kv4_kernel(const K4Args a) {
   int b = k4_find(pre, a.pg.B, u0);
   int units = (pre[b + 1] - pre[b]) / a.Hk, hk = (u0 - pre[b]) / units, t = (u0 - pre[b]) - hk * units;
   int slot = 0, phase = 0;
+  bool gave_up = false;                                           // a wait ran out
   for (int u = u0; u < u1;) {
     // ================ one (sequence, K/V head), or the part of it that lies in this range
     const int n = k4_rows(a.pg, b), seg0 = u - t, seg1 = seg0 + units, part_end = min(seg1, u1);
@@ -260,7 +274,7 @@ attn_decode_kv4_kernel(const K4Args a) {
         for (int g = 0; g < NG; ++g) qs[nt][g][c] = __shfl_sync(0xffffffffu, sum[g], from) * a.scale_log2;
       }
     }
-    // ---- Eq. 6's append, by the warp that has the pair's first tile: lanes 0 .. D/8-1 hold k_t, the next D/8 v_t
+    // ---- Eq. 6's append, by the warp that has the pair's first unit: lanes 0 .. D/8-1 hold k_t, the next D/8 v_t
     if (t == 0 && a.keep != nullptr && a.keep[b] != 0) {
       constexpr int LR = D / 8;
       const int l = lane % LR;
@@ -281,7 +295,7 @@ attn_decode_kv4_kernel(const K4Args a) {
     float m[NT][2], l_run[NT][2], zacc[NT][NG][2], acc[NT][NG][4][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      m[nt][0] = m[nt][1] = -INFINITY;
+      m[nt][0] = m[nt][1] = 0.f;                                  // (not a maximum yet: see `seen`)
       l_run[nt][0] = l_run[nt][1] = 0.f;
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
@@ -290,41 +304,41 @@ attn_decode_kv4_kernel(const K4Args a) {
         for (int i = 0; i < 4; ++i) acc[nt][g][i][0] = acc[nt][g][i][1] = acc[nt][g][i][2] = acc[nt][g][i][3] = 0.f;
       }
     }
+    uint32_t seen = 0;                                            // heads (bit 2 nt + c) whose maximum in use has been set
     int E = -200;                                                 // P s is held as P s 2^-E; none yet
     float down_e = 0.f, s_limit = 0.f;                            // 2^-E, 2^(E + 4)
 
-    // ================ tiles
+    // ================ units
     for (; u < part_end; ++u, ++t) {
-      mbar_wait(smem_u32(&bars[slot]), phase, abort_flag);
-      if (!((absent >> slot) & 1u) && !*abort_flag) {
-        const uint32_t tile = smem_u32(ring + (size_t)slot * F::TILE);
-        const int nr = n - t * kKv4Rows;                          // rows of this tile, 16 or more: all
-        const int key0 = (r >> 1) + 4 * (r & 1);                  // this lane's keys: key0 and key0 + 8
-        float d[NT][NG][4];
+      if (!mbar_try_wait(smem_u32(&bars[slot]), phase) && !mbar_wait(smem_u32(&bars[slot]), phase, abort_flag)) { gave_up = true; break; }
+      const uint32_t got = (here >> (2 * slot)) & 3u;
+      if (got != 0) {
+        const uint32_t unit = smem_u32(ring + (size_t)slot * (2 * F::TILE));
+        // ---- scores of the codes: lane's keys r and r + 8 of both tiles, its heads 2j, 2j + 1
+        float d[2][NT][NG][4];
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) d[nt][g][0] = d[nt][g][1] = d[nt][g][2] = d[nt][g][3] = 0.f;
-          const uint32_t ka = tile + kv4_group_off<D>(key0, g) + 8 * j;
-          const uint2 w0 = k4_lds64(ka), w1 = k4_lds64(ka + 8 * F::RB);
+          for (int g = 0; g < NG; ++g) {
+            const uint32_t ka = unit + h * F::TILE + kv4_k_off<D>(r, g) + 8 * j;
+            const uint2 w0 = k4_lds64(ka), w1 = k4_lds64(ka + 8 * F::RB);
 #pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            const uint32_t x = w ? w0.y : w0.x, y = w ? w1.y : w1.x, x8 = x >> 8, y8 = y >> 8;
+            for (int w = 0; w < 2; ++w) {
+              const uint32_t x = w ? w0.y : w0.x, y = w ? w1.y : w1.x, x8 = x >> 8, y8 = y >> 8;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              k4_mma(d[nt][g], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qb[nt][g][2 * w][0], qb[nt][g][2 * w][1]);
-              k4_mma(d[nt][g], x8 & 0x000F000Fu, y8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x00F000F0u, qb[nt][g][2 * w + 1][0], qb[nt][g][2 * w + 1][1]);
+              for (int nt = 0; nt < NT; ++nt) {
+                if (w == 0) k4_mma_first(d[h][nt][g], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qb[nt][g][0][0], qb[nt][g][0][1]);
+                else k4_mma(d[h][nt][g], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qb[nt][g][2][0], qb[nt][g][2][1]);
+                k4_mma(d[h][nt][g], x8 & 0x000F000Fu, y8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x00F000F0u, qb[nt][g][2 * w + 1][0], qb[nt][g][2 * w + 1][1]);
+              }
             }
           }
-        }
-        // ---- words of this lane's two keys; whatever stands in rows past the end counts nothing
-        const bool ok0 = key0 < nr, ok1 = key0 + 8 < nr;
-        float ks[2][NG], kz[2][NG], vs[2][NG], vz[2][NG];
+        // ---- words of the lane's four keys (index 2 h + i: key r + 8 i of tile h)
+        float vs[4][NG], vz[4][NG], s[NT][4][2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const bool ok = i ? ok1 : ok0;
+        for (int k = 0; k < 4; ++k) {
           uint32_t kw[NG], vw[NG];
-          const uint32_t at = tile + (key0 + 8 * i) * 4 * NG;
+          const uint32_t at = unit + (k >> 1) * F::TILE + (r + 8 * (k & 1)) * 4 * NG;
           if (NG == 2) {
             const uint2 x = k4_lds64(at + F::KM), y = k4_lds64(at + F::VM);
             kw[0] = x.x; kw[NG - 1] = x.y; vw[0] = y.x; vw[NG - 1] = y.y;
@@ -332,40 +346,45 @@ attn_decode_kv4_kernel(const K4Args a) {
             kw[0] = k4_lds32(at + F::KM); vw[0] = k4_lds32(at + F::VM);
           }
 #pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            ks[i][g] = bf16lo(kw[g]); kz[i][g] = bf16hi(kw[g]);
-            vs[i][g] = ok ? bf16lo(vw[g]) : 0.f; vz[i][g] = ok ? bf16hi(vw[g]) : 0.f;
-          }
+          for (int g = 0; g < NG; ++g) { vs[k][g] = bf16lo(vw[g]); vz[k][g] = bf16hi(vw[g]); }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              float dot = 0.f, off = -m[nt][c];                   // s: score less the maximum in use
+#pragma unroll
+              for (int g = 0; g < NG; ++g) {
+                dot = fmaf(bf16lo(kw[g]), d[k >> 1][nt][g][2 * (k & 1) + c], dot);
+                off = fmaf(bf16hi(kw[g]), qs[nt][g][c], off);
+              }
+              s[nt][k][c] = fmaf(fq[nt][c], dot, off);
+            }
         }
-        float s[NT][4];
-        bool raise = false;
+        const int nr = n - t * kK4Unit;
+        if (nr < kK4Unit || got != 3u) {
+          // the last unit of a sequence, or one with a page missing: whatever stands in rows that are not there counts nothing
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (16 * (k >> 1) + r + 8 * (k & 1) >= nr || !((got >> (k >> 1)) & 1u)) {
+#pragma unroll
+              for (int g = 0; g < NG; ++g) vs[k][g] = vz[k][g] = 0.f;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) s[nt][k][0] = s[nt][k][1] = -INFINITY;
+            }
+        }
+        bool raise = seen != (1u << (2 * NT)) - 1u;
+        float top = fmaxf(fmaxf(vs[0][0], vs[1][0]), fmaxf(vs[2][0], vs[3][0]));
+        if (NG == 2) top = fmaxf(top, fmaxf(fmaxf(vs[0][NG - 1], vs[1][NG - 1]), fmaxf(vs[2][NG - 1], vs[3][NG - 1])));
+        raise |= top > s_limit;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {                           // i: key (i >> 1), head 2j + (i & 1)
-            const int ki = i >> 1, c = i & 1;
-            float dot = 0.f, off = 0.f;
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-              dot = fmaf(ks[ki][g], d[nt][g][i], dot);
-              off = fmaf(kz[ki][g], qs[nt][g][c], off);
-            }
-            s[nt][i] = (ki ? ok1 : ok0) ? fmaf(fq[nt][c], dot, off) : -INFINITY;
-            raise |= s[nt][i] > m[nt][c] + (float)kK4Lag;
-          }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int g = 0; g < NG; ++g) raise |= vs[i][g] > s_limit;
+          for (int c = 0; c < 2; ++c)
+            raise |= fmaxf(fmaxf(s[nt][0][c], s[nt][1][c]), fmaxf(s[nt][2][c], s[nt][3][c])) > (float)kK4Lag;
         if (__any_sync(0xffffffffu, raise)) {
           // rare: the maxima in use go up to what has been seen, and so does 2^E
-          float top = 0.f;
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int g = 0; g < NG; ++g) top = fmaxf(top, vs[i][g]);
-#pragma unroll
-          for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
           float corr_e = 1.f;
           if (top > s_limit) {
             const int en = max(-100, min(120, (int)(__float_as_uint(top) >> 23) - 127));
@@ -380,12 +399,17 @@ attn_decode_kv4_kernel(const K4Args a) {
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-              float mx = fmaxf(s[nt][c], s[nt][2 + c]);
+              float mx = fmaxf(fmaxf(s[nt][0][c], s[nt][1][c]), fmaxf(s[nt][2][c], s[nt][3][c]));
 #pragma unroll
               for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-              mx = fmaxf(mx, m[nt][c]);
-              const float corr = m[nt][c] == -INFINITY ? (mx == -INFINITY ? 1.f : 0.f) : k4_exp2(m[nt][c] - mx);
-              m[nt][c] = mx;
+              // up by mx (the first time: to it, wherever it is); a head without a finite score yet stays
+              const bool known = (seen >> (2 * nt + c)) & 1u, finite = mx > -INFINITY && mx < INFINITY;
+              const float by = finite && (!known || mx > 0.f) ? mx : 0.f;
+              const float corr = known ? k4_exp2(-by) : 1.f;
+              if (finite) seen |= 1u << (2 * nt + c);
+              m[nt][c] += by;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) s[nt][k][c] -= by;
               l_run[nt][c] *= corr;
 #pragma unroll
               for (int g = 0; g < NG; ++g) {
@@ -395,47 +419,52 @@ attn_decode_kv4_kernel(const K4Args a) {
               }
             }
         }
-        float p[NT][4];
-        uint32_t pb[NT][NG][2];
+        // ---- P, and O^T += V^T (P s)^T tile by tile: lane's row pairs j and j + 4, its dims 64 g + 8 r .. + 7
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int h = 0; h < 2; ++h) {
+          uint32_t pb[NT][NG][2];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float mc = m[nt][i & 1];
-            p[nt][i] = k4_exp2(s[nt][i] - (mc == -INFINITY ? 0.f : mc));
-            l_run[nt][i & 1] += p[nt][i];
+          for (int nt = 0; nt < NT; ++nt) {
+            float p[2][2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                p[i][c] = k4_exp2(s[nt][2 * h + i][c]);
+                l_run[nt][c] += p[i][c];
+              }
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const float f = vs[2 * h + i][g] * down_e;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) zacc[nt][g][c] = fmaf(p[i][c], vz[2 * h + i][g], zacc[nt][g][c]);
+                pb[nt][g][i] = k4_transpose(k4_f16x2(p[i][0] * f, p[i][1] * f));
+              }
           }
 #pragma unroll
           for (int g = 0; g < NG; ++g) {
+            const uint32_t va = unit + h * F::TILE;
+            const uint2 wx = k4_lds64(va + kv4_v_off<D>(j, 64 * g + 8 * r)), wy = k4_lds64(va + kv4_v_off<D>(j + 4, 64 * g + 8 * r));
 #pragma unroll
-            for (int c = 0; c < 2; ++c) zacc[nt][g][c] = fmaf(p[nt][c], vz[0][g], fmaf(p[nt][2 + c], vz[1][g], zacc[nt][g][c]));
-            const float f0 = vs[0][g] * down_e, f1 = vs[1][g] * down_e;
-            pb[nt][g][0] = k4_transpose(k4_f16x2(p[nt][0] * f0, p[nt][1] * f0));
-            pb[nt][g][1] = k4_transpose(k4_f16x2(p[nt][2] * f1, p[nt][3] * f1));
-          }
-        }
-        // ---- O^T += V^T P^T: lane's keys j, 4 + j, 8 + j, 12 + j, its dims 64 g + 8 r .. + 7
+            for (int w = 0; w < 2; ++w) {
+              const uint32_t x = w ? wx.y : wx.x, y = w ? wy.y : wy.x, x8 = x >> 8, y8 = y >> 8;
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          const uint32_t va = tile + F::V + 4 * r;
-          const uint32_t wA = k4_lds32(va + kv4_group_off<D>(j, g)), wB = k4_lds32(va + kv4_group_off<D>(4 + j, g));
-          const uint32_t wC = k4_lds32(va + kv4_group_off<D>(8 + j, g)), wD = k4_lds32(va + kv4_group_off<D>(12 + j, g));
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t x = __byte_perm(wA, wB, h ? 0x7632 : 0x5410), y = __byte_perm(wC, wD, h ? 0x7632 : 0x5410);
-            const uint32_t x8 = x >> 8, y8 = y >> 8;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              k4_mma(acc[nt][g][2 * h], x & 0x000F000Fu, x & 0x00F000F0u, y & 0x000F000Fu, y & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
-              k4_mma(acc[nt][g][2 * h + 1], x8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x000F000Fu, y8 & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
+              for (int nt = 0; nt < NT; ++nt) {
+                k4_mma(acc[nt][g][2 * w], x & 0x000F000Fu, x & 0x00F000F0u, y & 0x000F000Fu, y & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
+                k4_mma(acc[nt][g][2 * w + 1], x8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x000F000Fu, y8 & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
+              }
             }
           }
         }
       }
       __syncwarp();
-      if (p_u < u1 && !*abort_flag) produce();
+      if (p_u < u1) produce();
       if (++slot == NS) { slot = 0; phase ^= 1; }
     }
+    if (__any_sync(0xffffffffu, gave_up)) break;
+    if (u == u1) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the joining kernel may come up
 
     // ================ finish the part
     const float up = E == -200 ? 0.f : k4_pow2(E);
@@ -451,6 +480,7 @@ attn_decode_kv4_kernel(const K4Args a) {
         }
         const int head = nt * 8 + 2 * j + c;
         if (head >= a.G) continue;                                // (after the shuffles of this pair)
+        const float top = l_run[nt][c] == 0.f ? -INFINITY : m[nt][c];   // nothing attended: no maximum
         const bool whole = seg0 >= u0 && seg1 <= u1;
         // this lane's dims 64 g + 8 r + 0 .. 7 of the head
         float o[NG][8];
@@ -462,8 +492,8 @@ attn_decode_kv4_kernel(const K4Args a) {
             o[g][2 * i + 1] = fmaf(acc[nt][g][i][2 + c] * 1048576.f, up, zacc[nt][g][c]);
           }
         if (whole) {
-          const float mine = se[nt][c], M = fmaxf(m[nt][c], mine);
-          const float wc = m[nt][c] == -INFINITY ? 0.f : k4_exp2(m[nt][c] - M), we = k4_exp2(mine - M);
+          const float mine = se[nt][c], M = fmaxf(top, mine);
+          const float wc = top == -INFINITY ? 0.f : k4_exp2(top - M), we = k4_exp2(mine - M);
           const float inv = 1.f / fmaf(l_run[nt][c], wc, we);
           const __nv_bfloat16* vt = a.v_t + ((size_t)b * a.Hk + hk) * D;
           const size_t at = ((size_t)b * a.H + hk * a.G + head) * D;
@@ -489,7 +519,7 @@ attn_decode_kv4_kernel(const K4Args a) {
             *reinterpret_cast<float4*>(pp + 64 * g + 8 * r) = make_float4(o[g][0], o[g][1], o[g][2], o[g][3]);
             *reinterpret_cast<float4*>(pp + 64 * g + 8 * r + 4) = make_float4(o[g][4], o[g][5], o[g][6], o[g][7]);
           }
-          if (r == 0) { pp[D] = m[nt][c]; pp[D + 1] = l_run[nt][c]; }
+          if (r == 0) { pp[D] = top; pp[D + 1] = l_run[nt][c]; }
         }
       }
     if (t == units) {
@@ -500,7 +530,7 @@ attn_decode_kv4_kernel(const K4Args a) {
       }
     }
   }
-  if (*abort_flag) {
+  if (__any_sync(0xffffffffu, gave_up)) {
     if (lane == 0) report_status(a.status, DL_ERR_TIMEOUT, blockIdx.x);
     // copies still in flight must land before the CTA's shared memory goes: the last NS tiles requested
     for (int v = max(u0, p_u - NS); v < p_u; ++v)
@@ -511,13 +541,14 @@ attn_decode_kv4_kernel(const K4Args a) {
 // Joins the parts of a pair that several ranges share: one CTA per query head, parts dealt to its warps in order, four
 // dims per lane.
 template <int D>
-__global__ void __launch_bounds__(kK4MergeThreads)
+__global__ void __launch_bounds__(kK4MergeWarps * 32)
 attn_merge_kv4_kernel(const K4Args a) {
-  constexpr int NW = kK4MergeThreads / 32, PL = D / 32;           // dims per lane
+  constexpr int PL = D / 32;                                      // dims per lane
+  const int NW = blockDim.x >> 5;
   extern __shared__ __align__(128) char smem[];
   int* pre = reinterpret_cast<int*>(smem);
-  __shared__ int sh_sums[NW];
-  __shared__ float sh_o[NW][D], sh_l[NW];
+  __shared__ int sh_sums[kK4MergeWarps];
+  __shared__ float sh_o[kK4MergeWarps][D], sh_l[kK4MergeWarps], sh_m[kK4MergeWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int b = blockIdx.x / a.H, head = blockIdx.x - b * a.H, hk = head / a.G, hg = head - hk * a.G;
   k4_prefix(a.pg, a.Hk, pre, sh_sums);
@@ -539,42 +570,67 @@ attn_merge_kv4_kernel(const K4Args a) {
   for (int o = 1; o < 32; o <<= 1) own += __shfl_xor_sync(0xffffffffu, own, o);
   own *= a.scale_log2;
   asm volatile("griddepcontrol.wait;" ::: "memory");              // the parts are written from here on
+  const int first_slot = k4_range(first, total, W) <= s0 ? 1 : 0; // the pair begins inside that range
   auto part = [&](int w) {
-    return a.partial + ((size_t)w * 2 + (w == first && k4_range(w, total, W) <= s0 ? 1 : 0)) * k4_slot<D>(a.G) + (size_t)hg * (D + 4);
+    return a.partial + ((size_t)w * 2 + (w == first ? first_slot : 0)) * k4_slot<D>(a.G) + (size_t)hg * (D + 4);
   };
-  float M = own;
-  for (int w = first + lane; w <= last; w += 32) M = fmaxf(M, __ldcg(part(w) + D));
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  float o[PL], l = 0.f;
+  float M = -INFINITY, o[PL], l = 0.f;                            // of this warp's parts
 #pragma unroll
   for (int i = 0; i < PL; ++i) o[i] = 0.f;
-#pragma unroll 4
-  for (int w = first + warp; w <= last; w += NW) {
-    const float* pp = part(w);
-    const float mw = __ldcg(pp + D), wt = mw == -INFINITY ? 0.f : k4_exp2(mw - M);
-    float x[PL];
-    if (PL == 4) {
-      const float4 y = __ldcg(reinterpret_cast<const float4*>(pp + lane * PL));
-      x[0] = y.x; x[1] = y.y; x[PL - 2] = y.z; x[PL - 1] = y.w;
-    } else {
-      const float2 y = __ldcg(reinterpret_cast<const float2*>(pp + lane * PL));
-      x[0] = y.x; x[1] = y.y;
-    }
-    l = fmaf(__ldcg(pp + D + 1), wt, l);
+  constexpr int NB = 5;                                           // parts in flight
+  for (int w0 = first + warp; w0 <= last; w0 += NB * NW) {
+    float mw[NB], lw[NB], x[NB][PL], top = M;
 #pragma unroll
-    for (int i = 0; i < PL; ++i) o[i] = fmaf(x[i], wt, o[i]);
+    for (int k = 0; k < NB; ++k) {
+      const int w = w0 + k * NW;
+      mw[k] = -INFINITY;
+      lw[k] = 0.f;
+#pragma unroll
+      for (int i = 0; i < PL; ++i) x[k][i] = 0.f;
+      if (w <= last) {
+        const float* pp = part(w);
+        const float2 ml = __ldcg(reinterpret_cast<const float2*>(pp + D));
+        mw[k] = ml.x;
+        lw[k] = ml.y;
+        if (PL == 4) {
+          const float4 y = __ldcg(reinterpret_cast<const float4*>(pp + lane * PL));
+          x[k][0] = y.x; x[k][1] = y.y; x[k][PL - 2] = y.z; x[k][PL - 1] = y.w;
+        } else {
+          const float2 y = __ldcg(reinterpret_cast<const float2*>(pp + lane * PL));
+          x[k][0] = y.x; x[k][1] = y.y;
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < NB; ++k) top = fmaxf(top, mw[k]);
+    const float corr = M == -INFINITY ? 0.f : k4_exp2(M - top);
+    M = top;
+    l *= corr;
+#pragma unroll
+    for (int i = 0; i < PL; ++i) o[i] *= corr;
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      const float wt = mw[k] == -INFINITY ? 0.f : k4_exp2(mw[k] - M);
+      l = fmaf(lw[k], wt, l);
+#pragma unroll
+      for (int i = 0; i < PL; ++i) o[i] = fmaf(x[k][i], wt, o[i]);
+    }
   }
 #pragma unroll
   for (int i = 0; i < PL; ++i) sh_o[warp][lane * PL + i] = o[i];
-  if (lane == 0) sh_l[warp] = l;
+  if (lane == 0) { sh_l[warp] = l; sh_m[warp] = M; }
   __syncthreads();
   const int dim = threadIdx.x;
   if (dim < D) {
-    const float we = k4_exp2(own - M);
+    float top = own;
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, sh_m[w]);
+    const float we = k4_exp2(own - top);
     float num = we * __bfloat162float(a.v_t[((size_t)b * a.Hk + hk) * D + dim]), den = we;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) { num += sh_o[w][dim]; den += sh_l[w]; }
+    for (int w = 0; w < NW; ++w) {
+      const float wt = sh_m[w] == -INFINITY ? 0.f : k4_exp2(sh_m[w] - top);
+      num = fmaf(sh_o[w][dim], wt, num);
+      den = fmaf(sh_l[w], wt, den);
+    }
     const size_t at = ((size_t)b * a.H + head) * D + dim;
     if (DL_IN_BOUNDS(a.status, KID_DECODE_KV4, at, (size_t)a.pg.B * a.H * D)) a.out[at] = __float2bfloat16_rn(num / den);
   }
@@ -582,17 +638,23 @@ attn_merge_kv4_kernel(const K4Args a) {
 
 template <int D, int NT>
 static cudaError_t k4_launch(const dl_ctx* ctx, K4Args& a, cudaStream_t s) {
-  constexpr int kCtas = NT == 1 ? 4 : 2;
+  constexpr int kCtas = k4_ctas(NT);
   const size_t pre_bytes = (size_t)(a.pg.B + 1) * sizeof(int);
   const int per_cta = (ctx->smem_optin + 1024) / kCtas - 1024;
-  int ns = (int)((per_cta - (int)pre_bytes - 256) / (kK4Warps * (Kv4<D>::TILE + 8)));
-  ns = std::min(ns, 12);
+  int ns = (int)((per_cta - (int)pre_bytes - 256) / (kK4Warps * (2 * Kv4<D>::TILE + 8)));
+  ns = std::min(ns, 8);
   if (ns < 2) return cudaErrorInvalidConfiguration;
   a.stages = ns;
-  const size_t smem = (size_t)kK4Warps * ns * (Kv4<D>::TILE + 8) + pre_bytes;
+  const size_t smem = (size_t)kK4Warps * ns * (2 * Kv4<D>::TILE + 8) + pre_bytes;
   auto kernel = attn_decode_kv4_kernel<D, NT>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e != cudaSuccess) return e;
+  cudaError_t e = cudaSuccess;
+  static int attr_set[64];                                        // the most asked for so far on a device
+  int& most = attr_set[ctx->device & 63];
+  if (most < (int)smem) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    most = (int)smem;
+  }
   const int grid = ctx->sm_count * kCtas;
   a.grid_warps = grid * kK4Warps;
   kernel<<<grid, kK4Warps * 32, smem, s>>>(a);
@@ -600,7 +662,8 @@ static cudaError_t k4_launch(const dl_ctx* ctx, K4Args& a, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(a.pg.B * a.H);
-  cfg.blockDim = dim3(kK4MergeThreads);
+  // a warp per eight parts or so (pairs share the ranges evenly when there are few of them)
+  cfg.blockDim = dim3(a.grid_warps / ((long long)a.pg.B * a.Hk) >= 32 ? kK4MergeWarps * 32 : 128);
   cfg.dynamicSmemBytes = pre_bytes;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
@@ -614,8 +677,8 @@ static cudaError_t k4_launch(const dl_ctx* ctx, K4Args& a, cudaStream_t s) {
 // floats of scratch: two parts for each range
 int64_t kv4_scratch_floats(int32_t sm_count, const dl_model_desc& d) {
   const int64_t G = std::min(d.n_heads, 16);
-  return std::max((int64_t)sm_count * 4 * kK4Warps * 2 * std::min<int64_t>(G, 8),
-                  (int64_t)sm_count * 2 * kK4Warps * 2 * G) * (d.head_dim + 4);
+  return std::max((int64_t)sm_count * k4_ctas(1) * kK4Warps * 2 * std::min<int64_t>(G, 8),
+                  (int64_t)sm_count * k4_ctas(2) * kK4Warps * 2 * G) * (d.head_dim + 4);
 }
 
 cudaError_t launch_attn_decode_kv4(const dl_ctx* ctx, const dl_pages* p, int32_t Hk, void* pool, const void* q,

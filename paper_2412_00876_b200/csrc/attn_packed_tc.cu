@@ -392,8 +392,12 @@ static cudaError_t pk_launch(dl_ctx* ctx, const void* q, const void* k, const vo
     return cudaErrorInvalidValue;
   const long long items = (long long)a.B * a.n_hs * a.pairs;
   if (items >= (1LL << 31)) return cudaErrorInvalidValue;
-  cudaError_t e = cudaFuncSetAttribute(attn_packed_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Pk<D>::SMEM);
-  if (e != cudaSuccess) return e;
+  static int attr_set[64];
+  if (!attr_set[ctx->device & 63]) {
+    const cudaError_t e = cudaFuncSetAttribute(attn_packed_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Pk<D>::SMEM);
+    if (e != cudaSuccess) return e;
+    attr_set[ctx->device & 63] = 1;
+  }
   attn_packed_kernel<D><<<(int)std::min<long long>(items, ctx->sm_count), kPkThreads, Pk<D>::SMEM, s>>>(maps, a);
   return cudaGetLastError();
 }

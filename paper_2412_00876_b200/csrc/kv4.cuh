@@ -7,10 +7,13 @@
 // are 0.  A group with a NaN or an infinity in it, or with a range beyond fp32, holds NaN.
 //
 // A page of page_rows rows holds, per K/V head, page_rows / 16 tiles of 16 rows; a tile is 18 D consecutive bytes:
-//   K codes [16][D/2] | V codes [16][D/2] | K words [16][D/64] | V words [16][D/64]       word = s | z << 16 (bf16 bits)
-// A 32-bit unit of codes holds 8 consecutive dims, lowest dim in the lowest 4 bits.  For D = 128 the two 32-byte
-// halves of a code row (its two groups) are swapped in rows where kv4_flip(row) is 1: the decode kernel's fragment loads
-// then touch every bank once.  One tile is one bulk copy, so a cache is read in pieces of 2304 (1152) bytes.
+//   K codes [16][D/2] | V codes [8][D] | K words [16][D/64] | V words [16][D/64]       word = s | z << 16 (bf16 bits)
+// K: a 32-bit unit holds 8 consecutive dims of a row, lowest dim in the lowest 4 bits; for D = 128 the two 32-byte halves of
+// a row (its two groups) are swapped in rows with bit 1 set.  V: the rows 2i, 2i + 1 share D bytes; a 32-bit unit holds 4
+// consecutive dims, of row 2i in its lower half and of row 2i + 1 in its upper half (what one fp16 operand register of
+// P V wants); the 16-byte steps of a pair are XORed with 2 (i & 3) (D = 64: 2 (i >> 1 & 1)).  With both orders the decode
+// kernel's fragment loads touch every bank once.  One tile is one bulk copy, so a cache is read in pieces of 2304
+// (1152) bytes.
 #pragma once
 
 #include "common.cuh"
@@ -30,11 +33,14 @@ template <int D> struct Kv4 {
   static_assert(TILE == 18 * D, "tile size");
 };
 
-__host__ __device__ __forceinline__ int kv4_flip(int row) { return ((row >> 1) ^ (row >> 2)) & 1; }
-
-// byte offset, inside a tile, of the 32-byte half (D = 128) or row (D = 64) that holds group g of `row`'s K codes
-template <int D> __host__ __device__ __forceinline__ int kv4_group_off(int row, int g) {
-  return row * Kv4<D>::RB + (D == 128 ? 32 * (g ^ kv4_flip(row)) : 0);
+// byte offset, inside a tile, of the 32 bytes that hold group g of `row`'s K codes
+template <int D> __device__ __forceinline__ int kv4_k_off(int row, int g) {
+  return row * Kv4<D>::RB + (D == 128 ? 32 * (g ^ ((row >> 1) & 1)) : 0);
+}
+// byte offset, inside a tile, of the 8 bytes (two units: dims d .. d + 7, d a multiple of 8) of row pair i's V codes
+template <int D> __device__ __forceinline__ int kv4_v_off(int i, int d) {
+  const int step = (d >> 4) ^ (D == 128 ? 2 * (i & 3) : 2 * ((i >> 1) & 1));
+  return Kv4<D>::V + i * D + 16 * step + (d & 8);
 }
 
 // Eight consecutive values per lane (`raw`: bf16), eight lanes per group (lanes 8i .. 8i + 7): this lane's codes, and the
@@ -80,12 +86,24 @@ __device__ __forceinline__ uint32_t kv4_quantise8(uint4 raw, uint32_t& word) {
 }
 
 // Stores what kv4_quantise8 gave for lane `l` (0 .. D/8 - 1: dims 8 l .. 8 l + 7) of row `row` of the tile at `tile`;
-// is_v picks the tensor.
+// is_v picks the tensor.  No byte of another row is written.
 template <int D> __device__ __forceinline__ void kv4_store8(uint8_t* tile, int row, int l, bool is_v, uint32_t code, uint32_t word) {
   const int g = l >> 3;
-  *reinterpret_cast<uint32_t*>(tile + (is_v ? Kv4<D>::V : 0) + kv4_group_off<D>(row, g) + 4 * (l & 7)) = code;
+  if (is_v) {
+    uint16_t* to = reinterpret_cast<uint16_t*>(tile + kv4_v_off<D>(row >> 1, 8 * l)) + (row & 1);
+    to[0] = (uint16_t)code;
+    to[2] = (uint16_t)(code >> 16);
+  } else {
+    *reinterpret_cast<uint32_t*>(tile + kv4_k_off<D>(row, g) + 4 * (l & 7)) = code;
+  }
   if ((l & 7) == 0)
     *reinterpret_cast<uint32_t*>(tile + (is_v ? Kv4<D>::VM : Kv4<D>::KM) + (row * Kv4<D>::NG + g) * 4) = word;
+}
+// The codes that it stored.
+template <int D> __device__ __forceinline__ uint32_t kv4_load8(const uint8_t* tile, int row, int l, bool is_v) {
+  if (!is_v) return __ldg(reinterpret_cast<const uint32_t*>(tile + kv4_k_off<D>(row, l >> 3) + 4 * (l & 7)));
+  const uint2 w = __ldg(reinterpret_cast<const uint2*>(tile + kv4_v_off<D>(row >> 1, 8 * l)));
+  return __byte_perm(w.x, w.y, (row & 1) ? 0x7632 : 0x5410);
 }
 
 // What a paged call knows of the pages, by value.

@@ -3,8 +3,9 @@
 //
 //   plan   : per sequence, count the kept rows, check that the pages for them are there, note the first destination
 //            row and (optionally) advance the length: one CTA per sequence;
-//   append : a CTA takes 32 packed source rows, ranks the kept ones and quantises them, 8 values per lane, 8 lanes per
-//            group; dropped rows are not read;
+//   append : a CTA takes up to 32 packed source rows, ranks the kept ones and quantises them, 8 values per lane, 8
+//            lanes per group; dropped rows are not read.  A thread stays at one place of the row (head, tensor, 8 dims)
+//            and walks the kept rows, four loads in flight; wide rows are shared by several CTAs (grid y);
 //   read   : the same walk the other way, codes to bf16.
 // Both are bound by HBM: a kept row costs 2 D bytes in and 9 D / 16 out per head and tensor.
 #include <algorithm>
@@ -14,7 +15,8 @@
 namespace dl {
 
 constexpr int kK4Threads = 256;
-constexpr int kK4Rows = 32;              // packed rows per CTA
+constexpr int kK4Rows = 32;              // most packed rows per CTA
+constexpr int kK4Unroll = 4;             // rows a thread has in flight
 
 __device__ __forceinline__ int k4_block_sum(int v, int* sh) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -33,14 +35,37 @@ __device__ __forceinline__ int k4_block_sum(int v, int* sh) {
 // leads out of a buffer.
 __device__ __forceinline__ int k4_start(const int32_t* starts, int b, int total) { return min(max(__ldg(starts + b), 0), total); }
 
+// All of them into shared memory (B + 1 ints): a search there costs no round trips to L2.
+__device__ __forceinline__ void k4_load_starts(const int32_t* starts, int B, int total, int* st) {
+  for (int b = threadIdx.x; b <= B; b += kK4Threads) st[b] = k4_start(starts, b, total);
+  __syncthreads();
+}
+
 // The sequence that packed row r belongs to: the last b whose start is <= r (so empty sequences own nothing), or -1.
-__device__ __forceinline__ int k4_sequence(const int32_t* starts, int B, int total, int r) {
+__device__ __forceinline__ int k4_sequence(const int* st, int B, int r) {
   int lo = -1, hi = B - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if (k4_start(starts, mid, total) <= r) lo = mid; else hi = mid - 1;
+    if (st[mid] <= r) lo = mid; else hi = mid - 1;
   }
-  return (lo >= 0 && r < k4_start(starts, lo + 1, total)) ? lo : -1;
+  return (lo >= 0 && r < st[lo + 1]) ? lo : -1;
+}
+
+// A thread's place in a row of U units (8 values of one head and tensor each): unit `rem`, starting at the CTA's row
+// `first` and going on by `step` rows; rem >= U: no place.
+struct K4Place { int rem, first, step; };
+__device__ __forceinline__ K4Place k4_place(int U) {
+  K4Place p;
+  if (U >= kK4Threads) {
+    p.rem = blockIdx.y * kK4Threads + threadIdx.x;
+    p.first = 0;
+    p.step = 1;
+  } else {
+    p.step = kK4Threads / U;
+    p.first = threadIdx.x / U;
+    p.rem = p.first < p.step ? threadIdx.x - p.first * U : U;
+  }
+  return p;
 }
 
 // kept rows among packed rows [from, to), counted by the whole CTA
@@ -54,6 +79,7 @@ __global__ void __launch_bounds__(kK4Threads)
 kv4_plan_kernel(const PagesArg pg, int32_t* len, const int32_t* __restrict__ starts, const uint8_t* __restrict__ keep,
                 int32_t total, int32_t commit, int32_t* plan_base, int32_t* plan_count, DeviceStatus* st) {
   __shared__ int sh[kK4Threads / 32];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the append kernel may start
   const int b = blockIdx.x;
   const int from = k4_start(starts, b, total), to = max(from, k4_start(starts, b + 1, total));
   const int count = keep ? k4_count(keep, from, to, sh) : to - from;
@@ -75,31 +101,32 @@ kv4_plan_kernel(const PagesArg pg, int32_t* len, const int32_t* __restrict__ sta
   }
 }
 
-// k, v: packed rows [total] of Hk * D values, `stride` values apart.
+// k, v: packed rows [total] of Hk * D values, `stride` values apart; `rows` of them per CTA.
 template <int D>
 __global__ void __launch_bounds__(kK4Threads)
 kv4_append_kernel(const PagesArg pg, uint8_t* __restrict__ pool, int32_t Hk, const __nv_bfloat16* __restrict__ k,
                   const __nv_bfloat16* __restrict__ v, long long stride, const int32_t* __restrict__ starts,
-                  const uint8_t* __restrict__ keep, int32_t total, const int32_t* __restrict__ plan_base,
-                  const int32_t* __restrict__ plan_count, DeviceStatus* st) {
+                  const uint8_t* __restrict__ keep, int32_t total, int32_t rows, const int32_t* plan_base,
+                  const int32_t* plan_count, DeviceStatus* st) {
+  extern __shared__ int seq_start[];
   __shared__ int sh[kK4Threads / 32];
-  __shared__ int row_src[kK4Rows], row_dst[kK4Rows], row_page[kK4Rows], n_kept;
-  const int t0 = blockIdx.x * kK4Rows;
-  const int b0 = k4_sequence(starts, pg.B, total, t0);
+  __shared__ long long row_src[kK4Rows], row_tile[kK4Rows];       // offset of a kept row's source, first tile of its page's
+  __shared__ int row_in[kK4Rows], n_kept;                         // K/V head 0 plus its tile in the page; its row in the tile
+  const int t0 = blockIdx.x * rows;
+  k4_load_starts(starts, pg.B, total, seq_start);
+  const int b0 = k4_sequence(seq_start, pg.B, t0);
   int before = 0;                                                  // kept rows of the first row's sequence in front of it
-  if (b0 >= 0) {
-    const int from = k4_start(starts, b0, total);
-    before = keep ? k4_count(keep, from, t0, sh) : t0 - from;
-  }
+  if (b0 >= 0) before = keep ? k4_count(keep, seq_start[b0], t0, sh) : t0 - seq_start[b0];
+  asm volatile("griddepcontrol.wait;" ::: "memory");              // the plan
   if (threadIdx.x < 32) {
     const int r = t0 + threadIdx.x;
-    const int b = r < total ? k4_sequence(starts, pg.B, total, r) : -1;
+    const int b = (int)threadIdx.x < rows && r < total ? k4_sequence(seq_start, pg.B, r) : -1;
     const bool f = b >= 0 && (keep == nullptr || keep[r] != 0);
     const unsigned m = __ballot_sync(0xffffffffu, f);
     int dst = -1, page = -1;
-    if (f && plan_count[b] >= 0) {
-      const int head = max(k4_start(starts, b, total) - t0, 0);   // first lane of this sequence
-      dst = plan_base[b] + (b == b0 ? before : 0) + __popc(m & ((1u << threadIdx.x) - 1u) & ~((1u << head) - 1u));
+    if (f && __ldcg(plan_count + b) >= 0) {
+      const int head = max(seq_start[b] - t0, 0);                 // first lane of this sequence
+      dst = __ldcg(plan_base + b) + (b == b0 ? before : 0) + __popc(m & ((1u << threadIdx.x) - 1u) & ~((1u << head) - 1u));
       if ((dst >> (pg.tile_shift + 4)) < pg.max_pages)
         page = __ldg(pg.table + (size_t)b * pg.max_pages + (dst >> (pg.tile_shift + 4)));
       if ((unsigned)page >= (unsigned)pg.n_pages) dst = -1;       // the plan has checked this; never a wild store
@@ -107,27 +134,40 @@ kv4_append_kernel(const PagesArg pg, uint8_t* __restrict__ pool, int32_t Hk, con
     const unsigned w = __ballot_sync(0xffffffffu, dst >= 0);
     if (dst >= 0) {
       const int i = __popc(w & ((1u << threadIdx.x) - 1u));
-      row_src[i] = r; row_dst[i] = dst; row_page[i] = page;
+      row_src[i] = r * stride;
+      row_tile[i] = kv4_tile_index(pg, page, Hk, 0, dst >> 4);
+      row_in[i] = dst & 15;
     }
     if (threadIdx.x == 0) n_kept = __popc(w);
   }
   __syncthreads();
-  constexpr int LR = D / 8;                                       // lanes per row of one head and tensor
-  const int half = Hk * LR, U = 2 * half, n = n_kept * U;
-  const int n_up = (n + 31) & ~31;                                // whole warps stay together for the shuffles
-  for (int i = blockIdx.y * kK4Threads + threadIdx.x; i < n_up; i += gridDim.y * kK4Threads) {
-    const bool on = i < n;
-    const int j = on ? i : n - 1;
-    const int row = j / U, rem = j - row * U;
-    const bool is_v = rem >= half;
-    const int l = is_v ? rem - half : rem;
-    const uint4 raw = __ldg(reinterpret_cast<const uint4*>((is_v ? v : k) + row_src[row] * stride + (long long)l * 8));
-    uint32_t word;
-    const uint32_t code = kv4_quantise8(raw, word);
-    const int hk = l / LR, R = row_dst[row];
-    const long long tile = kv4_tile_index(pg, row_page[row], Hk, hk, R >> 4);
-    if (on && DL_IN_BOUNDS(st, KID_KV4_APPEND, tile, (long long)pg.n_pages * Hk << pg.tile_shift))
-      kv4_store8<D>(pool + tile * Kv4<D>::TILE, R & 15, l - hk * LR, is_v, code, word);
+  constexpr int LR = D / 8;                                       // units per row of one head and tensor
+  const int half = Hk * LR, U = 2 * half, n = n_kept;
+  const K4Place at = k4_place(U);
+  const bool on = at.rem < U;
+  const bool is_v = at.rem >= half;
+  const int l = on ? (is_v ? at.rem - half : at.rem) : 0, hk = l / LR, lr = l - hk * LR;
+  const __nv_bfloat16* src = (is_v ? v : k) + l * 8;
+  const long long head_tiles = (long long)hk << pg.tile_shift;
+  for (int base = 0; base < n; base += at.step * kK4Unroll) {     // the same trips for all lanes: they shuffle together
+    uint4 raw[kK4Unroll];
+#pragma unroll
+    for (int c = 0; c < kK4Unroll; ++c) {
+      const int row = base + c * at.step + at.first;
+      raw[c] = on && row < n ? __ldg(reinterpret_cast<const uint4*>(src + row_src[row])) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int c = 0; c < kK4Unroll; ++c) {
+      if (base + c * at.step >= n) break;
+      const int row = base + c * at.step + at.first;
+      uint32_t word;
+      const uint32_t code = kv4_quantise8(raw[c], word);
+      if (on && row < n) {
+        const long long tile = row_tile[row] + head_tiles;
+        if (DL_IN_BOUNDS(st, KID_KV4_APPEND, tile, (long long)pg.n_pages * Hk << pg.tile_shift))
+          kv4_store8<D>(pool + tile * Kv4<D>::TILE, row_in[row], lr, is_v, code, word);
+      }
+    }
   }
 }
 
@@ -136,66 +176,77 @@ kv4_append_kernel(const PagesArg pg, uint8_t* __restrict__ pool, int32_t Hk, con
 template <int D>
 __global__ void __launch_bounds__(kK4Threads)
 kv4_read_kernel(const PagesArg pg, const uint8_t* __restrict__ pool, int32_t Hk, const int32_t* __restrict__ row0,
-                const int32_t* __restrict__ starts, int32_t total, __nv_bfloat16* __restrict__ k_out,
+                const int32_t* __restrict__ starts, int32_t total, int32_t rows, __nv_bfloat16* __restrict__ k_out,
                 __nv_bfloat16* __restrict__ v_out, DeviceStatus* st) {
-  __shared__ int row_pos[kK4Rows], row_page[kK4Rows];
-  const int t0 = blockIdx.x * kK4Rows;
+  extern __shared__ int seq_start[];
+  __shared__ long long row_tile[kK4Rows];                         // -1: no page, -2: a packed row of no sequence, left as it is
+  __shared__ int row_in[kK4Rows];
+  const int t0 = blockIdx.x * rows;
+  k4_load_starts(starts, pg.B, total, seq_start);
   if (threadIdx.x < 32) {
     const int r = t0 + threadIdx.x;
-    const int b = r < total ? k4_sequence(starts, pg.B, total, r) : -1;
-    int pos = -1, page = -1;                                      // -1: a packed row of no sequence, left as it is
+    const int b = (int)threadIdx.x < rows && r < total ? k4_sequence(seq_start, pg.B, r) : -1;
+    long long tile = -2;
+    int in = 0;
     if (b >= 0) {
-      const long long at = (long long)__ldg(row0 + b) + (r - k4_start(starts, b, total));
-      pos = 0;
-      if (at >= 0 && (at >> (pg.tile_shift + 4)) < pg.max_pages) {
-        pos = (int)at;
-        page = __ldg(pg.table + (size_t)b * pg.max_pages + (pos >> (pg.tile_shift + 4)));
+      const long long pos = (long long)__ldg(row0 + b) + (r - seq_start[b]);
+      tile = -1;
+      if (pos >= 0 && (pos >> (pg.tile_shift + 4)) < pg.max_pages) {
+        const int page = __ldg(pg.table + (size_t)b * pg.max_pages + (pos >> (pg.tile_shift + 4)));
+        tile = kv4_tile_index(pg, page, Hk, 0, (int)(pos >> 4));
+        in = (int)pos & 15;
       }
-      if ((unsigned)page >= (unsigned)pg.n_pages) {
-        page = -1;
-        report_status(st, DL_ERR_INVALID_ARG, b);
-      }
+      if (tile < 0) report_status(st, DL_ERR_INVALID_ARG, b);
     }
-    row_pos[threadIdx.x] = pos;
-    row_page[threadIdx.x] = page;
+    row_tile[threadIdx.x] = tile;
+    row_in[threadIdx.x] = in;
   }
   __syncthreads();
   constexpr int LR = D / 8;
-  const int half = Hk * LR, U = 2 * half, n = min(kK4Rows, total - t0) * U;
-  for (int i = blockIdx.y * kK4Threads + threadIdx.x; i < n; i += gridDim.y * kK4Threads) {
-    const int row = i / U, rem = i - row * U;
-    const bool is_v = rem >= half;
-    const int l = is_v ? rem - half : rem;
-    const int R = row_pos[row];
-    if (R < 0) continue;
-    const int hk = l / LR, lr = l - hk * LR, g = lr >> 3;
-    uint4 o = make_uint4(0u, 0u, 0u, 0u);
-    if (row_page[row] >= 0) {
-      const uint8_t* tile = pool + (long long)kv4_tile_index(pg, row_page[row], Hk, hk, R >> 4) * Kv4<D>::TILE;
-      const uint32_t c = __ldg(reinterpret_cast<const uint32_t*>(tile + (is_v ? Kv4<D>::V : 0) +
-                                                                 kv4_group_off<D>(R & 15, g) + 4 * (lr & 7)));
-      const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(tile + (is_v ? Kv4<D>::VM : Kv4<D>::KM) +
-                                                                 ((R & 15) * Kv4<D>::NG + g) * 4));
-      const float s = bf16lo(w), z = bf16hi(w);
+  const int half = Hk * LR, U = 2 * half, n = min(rows, total - t0);
+  const K4Place at = k4_place(U);
+  if (at.rem >= U) return;
+  const bool is_v = at.rem >= half;
+  const int l = is_v ? at.rem - half : at.rem, hk = l / LR, lr = l - hk * LR, g = lr >> 3;
+  const long long head_tiles = (long long)hk << pg.tile_shift;
+  uint4* out = reinterpret_cast<uint4*>(is_v ? v_out : k_out);
+  for (int base = at.first; base < n; base += at.step * kK4Unroll) {
+    uint32_t code[kK4Unroll], word[kK4Unroll];
+#pragma unroll
+    for (int c = 0; c < kK4Unroll; ++c) {
+      const int row = base + c * at.step;
+      code[c] = word[c] = 0u;
+      if (row < n && row_tile[row] >= 0) {
+        const uint8_t* tile = pool + (row_tile[row] + head_tiles) * Kv4<D>::TILE;
+        const int R = row_in[row];
+        code[c] = kv4_load8<D>(tile, R, lr, is_v);
+        word[c] = __ldg(reinterpret_cast<const uint32_t*>(tile + (is_v ? Kv4<D>::VM : Kv4<D>::KM) + (R * Kv4<D>::NG + g) * 4));
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < kK4Unroll; ++c) {
+      const int row = base + c * at.step;
+      if (row >= n || row_tile[row] == -2) continue;
+      const float s = bf16lo(word[c]), z = bf16hi(word[c]);
       uint32_t p[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float x0 = fmaf((float)((c >> (8 * e)) & 15u), s, z), x1 = fmaf((float)((c >> (8 * e + 4)) & 15u), s, z);
+        const float x0 = fmaf((float)((code[c] >> (8 * e)) & 15u), s, z), x1 = fmaf((float)((code[c] >> (8 * e + 4)) & 15u), s, z);
         p[e] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(x0)) |
                ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(x1)) << 16);
       }
-      o = make_uint4(p[0], p[1], p[2], p[3]);
+      const long long to = (long long)(t0 + row) * half + l;
+      if (DL_IN_BOUNDS(st, KID_KV4_READ, to, (long long)total * half)) out[to] = make_uint4(p[0], p[1], p[2], p[3]);
     }
-    const long long at = (long long)(t0 + row) * half + l;
-    if (DL_IN_BOUNDS(st, KID_KV4_READ, at, (long long)total * half))
-      reinterpret_cast<uint4*>(is_v ? v_out : k_out)[at] = o;
   }
 }
 
-// CTAs along y: the units of a row tile are shared by several CTAs where the rows alone would not fill the GPU
-static int k4_split(const dl_ctx* ctx, int tiles, int Hk) {
-  const int most = std::max(1, kK4Rows * 2 * Hk * ctx->desc.head_dim / 8 / kK4Threads);
-  return std::max(1, std::min(most, 8 * ctx->sm_count / std::max(tiles, 1)));
+// Rows per CTA and the grid: fewer rows where 32 would not fill the GPU eight times over.
+static dim3 k4_grid(const dl_ctx* ctx, int total, int Hk, int* rows) {
+  const int U = 2 * Hk * ctx->desc.head_dim / 8, slabs = U >= kK4Threads ? (U + kK4Threads - 1) / kK4Threads : 1;
+  *rows = kK4Rows;
+  while (*rows > 4 && (long long)((total + *rows - 1) / *rows) * slabs < 8LL * ctx->sm_count) *rows >>= 1;
+  return dim3((total + *rows - 1) / *rows, slabs);
 }
 
 cudaError_t launch_kv4_append(const dl_ctx* ctx, const dl_pages* p, int32_t Hk, void* pool, const void* k, const void* v,
@@ -206,22 +257,30 @@ cudaError_t launch_kv4_append(const dl_ctx* ctx, const dl_pages* p, int32_t Hk, 
                                                ctx->ws.plan_count, ctx->ws.status);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess || total == 0) return e;
-  const int tiles = (total + kK4Rows - 1) / kK4Rows;
-  const dim3 grid(tiles, k4_split(ctx, tiles, Hk));
-  auto kernel = ctx->desc.head_dim == 128 ? kv4_append_kernel<128> : kv4_append_kernel<64>;
-  kernel<<<grid, kK4Threads, 0, s>>>(pg, static_cast<uint8_t*>(pool), Hk, static_cast<const __nv_bfloat16*>(k),
-                                     static_cast<const __nv_bfloat16*>(v), stride, starts, keep, total,
-                                     ctx->ws.plan_base, ctx->ws.plan_count, ctx->ws.status);
-  return cudaGetLastError();
+  int rows;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = k4_grid(ctx, total, Hk, &rows);
+  cfg.blockDim = dim3(kK4Threads);
+  cfg.dynamicSmemBytes = (size_t)(p->B + 1) * sizeof(int);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];                                    // starts while the plan is made, and waits for it
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, ctx->desc.head_dim == 128 ? kv4_append_kernel<128> : kv4_append_kernel<64>, pg,
+                            static_cast<uint8_t*>(pool), Hk, static_cast<const __nv_bfloat16*>(k),
+                            static_cast<const __nv_bfloat16*>(v), (long long)stride, starts, keep, total, (int32_t)rows,
+                            (const int32_t*)ctx->ws.plan_base, (const int32_t*)ctx->ws.plan_count, ctx->ws.status);
 }
 
 cudaError_t launch_kv4_read(const dl_ctx* ctx, const dl_pages* p, int32_t Hk, const void* pool, const int32_t* row0,
                             const int32_t* starts, int32_t total, void* k_out, void* v_out, cudaStream_t s) {
   if (total == 0) return cudaSuccess;
-  const int tiles = (total + kK4Rows - 1) / kK4Rows;
-  const dim3 grid(tiles, k4_split(ctx, tiles, Hk));
+  int rows;
+  const dim3 grid = k4_grid(ctx, total, Hk, &rows);
   auto kernel = ctx->desc.head_dim == 128 ? kv4_read_kernel<128> : kv4_read_kernel<64>;
-  kernel<<<grid, kK4Threads, 0, s>>>(pages_arg(p), static_cast<const uint8_t*>(pool), Hk, row0, starts, total,
+  kernel<<<grid, kK4Threads, (size_t)(p->B + 1) * sizeof(int), s>>>(pages_arg(p), static_cast<const uint8_t*>(pool), Hk, row0, starts, total, rows,
                                      static_cast<__nv_bfloat16*>(k_out), static_cast<__nv_bfloat16*>(v_out),
                                      ctx->ws.status);
   return cudaGetLastError();
