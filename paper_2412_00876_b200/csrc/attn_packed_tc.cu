@@ -5,15 +5,22 @@
 // head h / G, G = H / Hkv.  A query tile is 128 rows of (position, head): 128 / P positions of P heads of one group, P the
 // largest power of two that divides G (one TMA box [positions][P heads][64 dims] is just that), so that a group's heads
 // share every K/V tile and short prompts fill a tile sooner.  A work item is (sequence, P heads, PAIR of query tiles),
-// pairs counted from the sequence's end; the two tiles are the CTA's two lanes, the later positions lane A.  One
-// persistent CTA per SM walks the items, longest first.
+// pairs counted from the sequence's end (aligned to its start they measured 4 % slower on 700 tokens); the two tiles are
+// the CTA's two lanes, the later positions lane A.  One persistent CTA per SM walks the items, longest first.
 //   warp 8        : the producer: Q tiles, then K and V tiles of 128 rows through one ring of four slots, used by both
 //                   lanes (a K/V tile crosses from L2 once per 256 query rows)
-//   warps 9, 10   : the MMA-issuing thread of lane A / B: S = Q K^T (128 x N) into tensor memory, O += P V with P read
-//                   from tensor memory; block u = P_u V_u, then Q K_{u+1}^T over P in order behind it
-//   warps 0-3/4-7 : softmax and epilogue of lane A / B, one row per thread (attn_prefill_softmax.cuh)
+//   warps 9, 10   : issue the MMAs of lane A / B: S = Q K^T (128 x N) into tensor memory, O += P V with P read from
+//                   tensor memory; block u = P_u V_u (its first half as soon as half of P is there), then Q K_{u+1}^T over
+//                   P in order behind it
+//   warps 0-3/4-7 : softmax and epilogue of lane A / B, one row per thread
 //   warp 11       : allocates tensor memory (512 columns: O_A | S_A | O_B | S_B); the first CTA's checks `starts`
-// A lane alternates between its softmax and its MMAs; the two lanes settle half a period apart and so overlap.
+// A lane is a chain: softmax, P V and Q K^T, softmax; tensor memory has no room for a second score buffer.  So the two
+// lanes have to be half a period apart, and every link counts.  On 8192 tokens (32 heads, 8 of K/V), TFLOP/s: 611 with
+// the MMAs issued by a single lane's code (operands moved to uniform registers one by one, 135 cycles an MMA), 800 with the
+// issuing warp uniform, 930 without cubics for a part of the exponentials (the special-function unit is not what is
+// short), 1055 with the passes taking turns, the maximum only looked for where a sum shows that it is needed, and an
+// elected lane issuing, 1130 with the first half of P handed over early.  Without any softmax the same kernel reaches
+// 1635.  Two threads per row (16 softmax warps): 900.
 // The last tile of a lane uses N = its keys rounded up to 16; where that reaches past the sequence's end, the softmax
 // warps zero those V rows in shared memory first (0 * x must stay 0 for any bit pattern of a neighbour's rows).
 // Every wait is bounded (pipeline.cuh); an abort leaves DL_ERR_TIMEOUT in the status word.
@@ -29,6 +36,15 @@ namespace dl {
 constexpr int kPkThreads = 384;
 constexpr int kPkSlots = 4;                            // K/V ring: two K and two V tiles
 constexpr int kPkBM = 128, kPkBN = 128;
+// Registers per thread (the kernel starts every thread at 168): a softmax warp holds a whole score row.  With 216 it spilled.
+constexpr int kPkRegsSmall = 40, kPkRegsSoftmax = 232;
+static_assert(128 * kPkRegsSmall + 256 * kPkRegsSoftmax <= 384 * 168, "more registers than the launch has");
+constexpr float kPkFar = 1048576.f, kPkFarLog2 = 14.f; // a half row's sum, and a score's lead, above which the maximum is looked for again
+constexpr int kPkPatience = 4000;                      // polls a softmax warp waits for its turn
+constexpr int kPkTurnTiles = 2;                        // items of at least so many key tiles take turns at the softmax
+constexpr int kPkNext = 16;                            // pair of columns (of 64) behind which the other lane's pass may start
+constexpr int kPkAhead = 4, kPkBehind = 6, kPkRing = 12;   // pairs between the stages of the exponentials
+static_assert(kPkRing > kPkAhead + kPkBehind, "a pair's place is taken again before it is done");
 
 template <int D> struct Pk {
   static constexpr int HALF = 128 * 128;               // 128 rows of 64 dims
@@ -50,8 +66,9 @@ struct PkArgs {
   float scale_log2;
 };
 
-struct PkItem { int b, h0, row0, n, q_hi, n_kv; };     // n_kv: key tiles of lane A
-struct PkLane { int q0, q_hi, n_tiles; bool exists; };
+// A pair of tiles: the 256 / P positions in front of q_hi (clipped at 0); n_kv: key tiles of its later tile.
+struct PkItem { int b, h0, row0, n, q_hi, n_kv; };
+struct PkLane { int q0, q_hi, n_tiles; bool exists; };   // rows of positions q0 .. q_hi - 1 are the lane's own
 
 __device__ __forceinline__ PkLane pk_lane(const PkArgs& a, const PkItem& I, int x) {
   const int PB = kPkBM >> a.p_shift;                   // positions per tile
@@ -65,7 +82,7 @@ __device__ __forceinline__ PkLane pk_lane(const PkArgs& a, const PkItem& I, int 
 // keys of tile j that a lane's MMAs cover
 __device__ __forceinline__ int pk_cols(const PkLane& L, int j) { return min(kPkBN, (L.q_hi - j * kPkBN + 15) & ~15); }
 
-// Items in the order every role walks them: pair 0 (the last positions) of all sequences and heads first.
+// Items in the order every role walks them: the last pairs of all sequences and heads first.
 struct PkWalker {
   const PkArgs& a;
   int p, b, hs, db, dh, s0, s1;
@@ -104,6 +121,110 @@ struct PkWalker {
   }
 };
 
+// True in one lane of the (whole) warp, always the same one; code under it counts as warp-uniform for the compiler.
+__device__ __forceinline__ bool pk_elect() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
+}
+
+// Maximum of three that stays where it stands: as plain arithmetic on loop-invariant scores the compiler moves the search
+// for the maximum in front of the loop it is a rare part of, and every tile pays for it.
+__device__ __forceinline__ float pk_max3(float x, float y, float z) {
+  float r;
+  asm volatile("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+  return r;
+}
+
+// Waits for this warp's tensor-memory loads; the 64 registers are operands, so that nothing that reads them can move in
+// front of the wait.
+__device__ __forceinline__ void pk_ld_wait64(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]), "+r"(r[32]), "+r"(r[33]), "+r"(r[34]), "+r"(r[35]), "+r"(r[36]), "+r"(r[37]), "+r"(r[38]), "+r"(r[39]), "+r"(r[40]), "+r"(r[41]), "+r"(r[42]), "+r"(r[43]), "+r"(r[44]), "+r"(r[45]), "+r"(r[46]), "+r"(r[47]), "+r"(r[48]), "+r"(r[49]), "+r"(r[50]), "+r"(r[51]), "+r"(r[52]), "+r"(r[53]), "+r"(r[54]), "+r"(r[55]), "+r"(r[56]), "+r"(r[57]), "+r"(r[58]), "+r"(r[59]), "+r"(r[60]), "+r"(r[61]), "+r"(r[62]), "+r"(r[63]) :: "memory");
+}
+
+// The softmax of a score tile that every row of the warp sees whole: one row per thread, its 128 scores in registers, P (as
+// bf16 pairs) over the first half of the score buffer; `half` is called when the first 64 columns of P are there, so that
+// their products may start, `next` when the other lane's pass may.  A row's maximum takes a warp as long as a third of the
+// exponentials, so it is only looked for in an item's first tile.  After that the exponentials are taken relative to the
+// maximum in use, and the tile is done over with a new one only if a score has passed it by far: the sum of the first half
+// shows that (an overflow is an infinite sum), and the second half's maximum, found beside the first half's exponentials.
+// P keeps its relative accuracy at any size.
+template <typename Turn, typename Half, typename Next>
+__device__ __forceinline__ void pk_softmax_full(uint32_t s_addr, uint32_t o_addr, bool owned, int o_blocks, float scale_log2,
+                                                float& m_used, float& l_run, Turn turn, Half half, Next next) {
+  uint32_t s[128];
+  tmem_ld64(s_addr, s);
+  tmem_ld64(s_addr + 64, s + 64);
+  pk_ld_wait64(s);
+  pk_ld_wait64(s + 64);
+  turn();
+  bool look = o_blocks == 0;
+  float t[2 * kPkRing];
+  const uint64_t sc2 = pack2(scale_log2, scale_log2);
+redo:
+  if (look) {
+    float mx[8];
+#pragma unroll
+    for (int w = 0; w < 8; ++w) mx[w] = pk_max3(-INFINITY, __uint_as_float(s[2 * w]), __uint_as_float(s[2 * w + 1]));
+#pragma unroll
+    for (int c = 16; c < 128; c += 16)
+#pragma unroll
+      for (int w = 0; w < 8; ++w) mx[w] = pk_max3(mx[w], __uint_as_float(s[c + 2 * w]), __uint_as_float(s[c + 2 * w + 1]));
+    const float mc = pk_max3(pk_max3(mx[0], mx[1], mx[2]), pk_max3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * scale_log2;
+    const bool need = owned && mc > m_used;
+    const float corr = need ? fast_exp2(m_used - mc) : 1.0f;
+    if (need) m_used = mc;
+    l_run *= corr;
+    if (o_blocks > 0) at_rescale_row(o_addr, s_addr, 0, corr, o_blocks);
+  }
+  const uint64_t nm2 = pack2(-m_used, -m_used);
+  uint64_t l2[4] = {0ull, 0ull, 0ull, 0ull};
+  float far[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+  uint32_t pk[16];
+  // Three stages, pair by pair and a few pairs apart, so that the special-function unit (8 cycles for a warp's
+  // exponential) does not wait for the arithmetic in front of it or behind it.
+#pragma unroll
+  for (int i = 0; i < 64 + kPkAhead + kPkBehind; ++i) {
+    if (i < 64) {
+      float y0, y1;
+      unpack2(ffma2(pack2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), sc2, nm2), y0, y1);
+      t[(2 * i) % (2 * kPkRing)] = y0;
+      t[(2 * i + 1) % (2 * kPkRing)] = y1;
+    }
+    if (i < 32) far[i & 3] = pk_max3(far[i & 3], __uint_as_float(s[64 + 2 * i]), __uint_as_float(s[64 + 2 * i + 1]));
+    const int e = i - kPkAhead;
+    if (e >= 0 && e < 64) {
+      float& e0 = t[(2 * e) % (2 * kPkRing)];
+      float& e1 = t[(2 * e + 1) % (2 * kPkRing)];
+      e0 = fast_exp2(e0);
+      e1 = fast_exp2(e1);
+    }
+    const int c = e - kPkBehind;
+    if (c >= 0) {
+      const float e0 = t[(2 * c) % (2 * kPkRing)], e1 = t[(2 * c + 1) % (2 * kPkRing)];
+      l2[c & 3] = fadd2(l2[c & 3], pack2(e0, e1));
+      pk[c & 15] = cvt_bf16x2(e0, e1);
+      if ((c & 15) == 15) tmem_st16(s_addr + (c & ~15), pk);
+      if (c == 32) {
+        float la, lb;
+        unpack2(fadd2(fadd2(l2[0], l2[1]), fadd2(l2[2], l2[3])), la, lb);
+        const float ahead = fmaxf(fmaxf(far[0], far[1]), fmaxf(far[2], far[3])) * scale_log2 - m_used;
+        if (__any_sync(0xffffffffu, owned && !look && (la + lb > kPkFar || ahead > kPkFarLog2))) {
+          look = true;
+          goto redo;
+        }
+      }
+      if (c == 38) { tmem_st_wait(); half(); }
+      if (c == kPkNext) next();
+    }
+  }
+  float la, lb;
+  unpack2(fadd2(fadd2(l2[0], l2[1]), fadd2(l2[2], l2[3])), la, lb);
+  l_run += la + lb;
+  tmem_st_wait();
+}
+
 template <int D>
 __global__ void __launch_bounds__(kPkThreads, 1)
 attn_packed_kernel(const __grid_constant__ PkMaps maps, const PkArgs a) {
@@ -117,16 +238,18 @@ attn_packed_kernel(const __grid_constant__ PkMaps maps, const PkArgs a) {
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::BAR);
   auto kv_full = [&](int i) { return smem_u32(bars + i); };
   auto kv_empty = [&](int i) { return smem_u32(bars + kPkSlots + i); };
-  enum { Q_FULL = 0, Q_EMPTY, S_FULL, P_FULL, O_FULL, O_FREE, N_BAR };
+  enum { Q_FULL = 0, Q_EMPTY, S_FULL, P_HALF, P_FULL, O_FULL, O_FREE, N_BAR };
   auto bar = [&](int x, int i) { return smem_u32(bars + 2 * kPkSlots + x * N_BAR + i); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 32);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 33);
+  volatile int* passes = reinterpret_cast<volatile int*>(bars + 34);         // [lane x][warp quad]: softmax passes behind it
 
   if (tid == 0) {
     *abort_flag = 0;
+    for (int i = 0; i < 8; ++i) passes[i] = 0;
     for (int i = 0; i < kPkSlots; ++i) { mbar_init(kv_full(i), 1); mbar_init(kv_empty(i), 2); }
     for (int x = 0; x < 2; ++x)
-      for (int i = 0; i < N_BAR; ++i) mbar_init(bar(x, i), (i == P_FULL || i == O_FREE) ? 4 : 1);
+      for (int i = 0; i < N_BAR; ++i) mbar_init(bar(x, i), (i == P_HALF || i == P_FULL || i == O_FREE) ? 4 : 1);
     fence_mbar_init();
   }
   if (warp == 11) { tmem_alloc(smem_u32(tmem_slot), 512); tmem_relinquish(); }
@@ -137,7 +260,7 @@ attn_packed_kernel(const __grid_constant__ PkMaps maps, const PkArgs a) {
 
   if (warp == 8) {
     // ---------------------------------------------------------------- producer
-    reg_dec<kAtRegsSmall>();
+    reg_dec<kPkRegsSmall>();
     if (lane == 0) {
       const CUtensorMap* mq = reinterpret_cast<const CUtensorMap*>(maps.q);
       const CUtensorMap* mk = reinterpret_cast<const CUtensorMap*>(maps.k);
@@ -187,12 +310,16 @@ attn_packed_kernel(const __grid_constant__ PkMaps maps, const PkArgs a) {
     }
   } else if (warp == 9 || warp == 10) {
     // ---------------------------------------------------------------- MMA issuer of one lane
-    reg_dec<kAtRegsSmall>();
-    if (lane == 0) {
+    // The whole warp walks the loop, so that counters and descriptors stay warp-uniform, and one elected lane issues: an MMA
+    // is then an instruction or two.
+    reg_dec<kPkRegsSmall>();
+    {
       const int x = warp - 9;
-      const uint32_t t_o = tmem + x * kAtLaneCols + kAtColO, t_s = tmem + x * kAtLaneCols + kAtColS;
-      const uint32_t idesc_pv = idesc_bf16(kPkBM, D, 0, 1);            // B (= V) is MN-major
-      const uint64_t q_desc = smem_desc_sw128(smem_u32(smem + x * S::TILE));
+      const uint32_t t_o = uniform32(tmem + x * kAtLaneCols + kAtColO), t_s = uniform32(tmem + x * kAtLaneCols + kAtColS);
+      constexpr uint32_t idesc_pv = idesc_bf16(kPkBM, D, 0, 1);        // B (= V) is MN-major
+      const uint64_t q_desc = uniform64(smem_desc_sw128(smem_u32(smem + x * S::TILE)));
+      const uint64_t kv_desc = uniform64(smem_desc_sw128(smem_u32(smem + S::KV)));
+      const uint64_t v_desc = uniform64(smem_desc_sw128_mn(smem_u32(smem + S::KV), S::HALF));
       PkWalker W(a);
       PkItem I;
       int n_item = 0, g0 = 0, ring0 = 0;               // this lane's items and key tiles, the ring's tiles so far
@@ -213,41 +340,54 @@ attn_packed_kernel(const __grid_constant__ PkMaps maps, const PkArgs a) {
           if (has_pv) sv = full(u, 1);
           if (has_qk) sk = full(u + 1, 0);
           if (u == 0) mbar_wait_spin(bar(x, O_FREE), ((uint32_t)n_item & 1u) ^ 1u, abort_flag);   // previous item's O has been read
-          if (has_pv) mbar_wait_spin(bar(x, P_FULL), (uint32_t)g & 1u, abort_flag);
+          if (has_pv) mbar_wait_spin(bar(x, P_HALF), (uint32_t)g & 1u, abort_flag);
+          __syncwarp();
           tc_fence_after();
           if (*abort_flag) break;
+          const uint64_t vd = v_desc + (uint64_t)uniform32((uint32_t)sv * (S::TILE >> 4));
+          const uint64_t kd = kv_desc + (uint64_t)uniform32((uint32_t)sk * (S::TILE >> 4));
+          const uint32_t ksteps = has_pv ? uniform32((uint32_t)pk_cols(L, u) >> 4) : 0u, acc = uniform32(u != 0);
+          const uint32_t idesc_qk = uniform32(idesc_bf16(kPkBM, (uint32_t)pk_cols(L, min(u + 1, n_sub - 1))));
           if (has_pv) {
-            uint64_t vd = smem_desc_sw128_mn(smem_u32(smem + S::KV + sv * S::TILE), S::HALF);
-            const int ksteps = pk_cols(L, u) >> 4;
-#pragma unroll 1
-            for (int ks = 0; ks < ksteps; ++ks, vd += 2048 >> 4)
-              mma_ts(t_o, t_s + ks * 8, vd, idesc_pv, (u | ks) != 0);
-            mma_commit(kv_empty(sv));
-            if (!has_qk) mma_commit(bar(x, O_FULL));
-          }
-          if (has_qk) {
-            uint64_t qd = q_desc, kd = smem_desc_sw128(smem_u32(smem + S::KV + sk * S::TILE));
-            const uint32_t idesc_qk = idesc_bf16(kPkBM, (uint32_t)pk_cols(L, u + 1));
-#pragma unroll 1
-            for (int ks = 0; ks < D / 16; ++ks) {
-              mma_ss(t_s, qd, kd, idesc_qk, ks != 0);
-              const uint64_t step = (ks == 3) ? (uint64_t)((S::HALF - 96) >> 4) : 2ull;
-              qd += step;
-              kd += step;
+            if (pk_elect()) {
+#pragma unroll
+              for (uint32_t ks = 0; ks < 4; ++ks)
+                if (ks < ksteps) mma_ts(t_o, t_s + ks * 8, vd + ks * (2048 >> 4), idesc_pv, ks == 0 ? acc : 1u);
             }
-            mma_commit(bar(x, S_FULL));
-            mma_commit(kv_empty(sk));
-            if (u + 2 == n_sub) mma_commit(bar(x, Q_EMPTY));
+            __syncwarp();
+            mbar_wait_spin(bar(x, P_FULL), (uint32_t)g & 1u, abort_flag);
+            __syncwarp();
+            tc_fence_after();
           }
+          if (pk_elect()) {
+            if (has_pv) {
+#pragma unroll
+              for (uint32_t ks = 4; ks < 8; ++ks)
+                if (ks < ksteps) mma_ts(t_o, t_s + ks * 8, vd + ks * (2048 >> 4), idesc_pv, 1u);
+              mma_commit(kv_empty(sv));
+              if (!has_qk) mma_commit(bar(x, O_FULL));
+            }
+            if (has_qk) {
+#pragma unroll
+              for (uint32_t ks = 0; ks < D / 16; ++ks) {
+                constexpr uint64_t half = S::HALF >> 4;                // the second 64 dims are a tile of their own
+                mma_ss(t_s, q_desc + (ks >> 2) * half + 2 * (ks & 3), kd + (ks >> 2) * half + 2 * (ks & 3), idesc_qk, ks != 0);
+              }
+              mma_commit(bar(x, S_FULL));
+              mma_commit(kv_empty(sk));
+              if (u + 2 == n_sub) mma_commit(bar(x, Q_EMPTY));
+            }
+          }
+          __syncwarp();
         }
         // tiles that only the other lane uses: this lane's share of the release, in the ring's order
         for (int u = n_sub; u < I.n_kv && !*abort_flag; ++u) {
           const int sk = full(u, 0);
           if (*abort_flag) break;
-          mbar_arrive(kv_empty(sk));
+          if (lane == 0) mbar_arrive(kv_empty(sk));
           const int sv = full(u, 1);
           if (*abort_flag) break;
-          mbar_arrive(kv_empty(sv));
+          if (lane == 0) mbar_arrive(kv_empty(sv));
         }
         ring0 += 2 * I.n_kv;
         g0 += n_sub;
@@ -256,7 +396,7 @@ attn_packed_kernel(const __grid_constant__ PkMaps maps, const PkArgs a) {
     }
   } else if (warp < 8) {
     // ---------------------------------------------------------------- softmax / epilogue warps of one lane
-    reg_inc<kAtRegsSoftmax>();
+    reg_inc<kPkRegsSoftmax>();
     const int x = warp >> 2, quad = warp & 3;
     const int row = quad * 32 + lane;                                  // row within the query tile
     const uint32_t lane_off = (uint32_t)(quad * 32) << 16;
@@ -268,22 +408,50 @@ attn_packed_kernel(const __grid_constant__ PkMaps maps, const PkArgs a) {
     const int w_last = (quad * 32 + 31) >> a.p_shift;
     PkWalker W(a);
     PkItem I;
-    int g0 = 0, ring0 = 0, n_item = 0;
+    int g0 = 0, g_twin = 0, ring0 = 0, n_item = 0;                     // g_twin: the other lane's key tiles so far
     while (W.next(I)) {
-      const PkLane L = pk_lane(a, I, x);
-      if (!L.exists) { ring0 += 2 * I.n_kv; continue; }
+      const PkLane L = pk_lane(a, I, x), Lt = pk_lane(a, I, x ^ 1);
+      const int n_twin = Lt.exists ? Lt.n_tiles : 0;
+      if (!L.exists) { ring0 += 2 * I.n_kv; g_twin += n_twin; continue; }
       const int pos = L.q0 + (row >> a.p_shift);                       // this thread's position
       const int r0 = L.q0 + w_pos;                                     // the warp's first position
       float m_used = -INFINITY, l_run = 0.f;
       const int n_sub = L.n_tiles;
+      const int twin0 = n_sub >= kPkTurnTiles ? g_twin : -(1 << 30);   // short items do not wait
       for (int u = 0; u < n_sub; ++u) {
         const int c0 = u * kPkBN;
-        // 32-column chunks of this tile that some row of the warp may see
-        const int n_ch = min(4, (min(L.q_hi, L.q0 + w_last + 1) - c0 + 31) >> 5);
         mbar_wait_spin(bar(x, S_FULL), (uint32_t)(g0 + u) & 1u, abort_flag);
+        // The lanes' softmax passes take turns, A, B, A, B (warp by warp: the twin is the warp of the same scheduler).  Left
+        // alone they fall into step: both softmax together, tensor pipe idle, then both wait for their MMAs.  Only a
+        // matter of speed: the wait gives up after a while.
+        auto turn = [&] {
+          if (lane == 0) {
+            const int before = twin0 + min(u + x, n_twin);
+            for (int i = 0; i < kPkPatience && passes[4 * (x ^ 1) + quad] < before; ++i) { }
+          }
+          __syncwarp();
+        };
         __syncwarp();
         tc_fence_after();
-        at_softmax_chunks<1>(s_addr, o_addr, n_ch, pos - c0, c0 - r0, pos < L.q_hi, u > 0 ? D / 32 : 0, a.scale_log2, m_used, l_run);
+        auto pass_on = [&] { if (lane == 0) passes[4 * x + quad] = g0 + u + 1; };
+        auto hand_over = [&](int which) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(x, which));
+        };
+        if (c0 + kPkBN - 1 <= r0) {
+          pk_softmax_full(s_addr, o_addr, pos < L.q_hi, u > 0 ? D / 32 : 0, a.scale_log2, m_used, l_run, turn,
+                          [&] { hand_over(P_HALF); }, pass_on);
+          hand_over(P_FULL);
+          continue;
+        }
+        // The causal edge or the sequence's end crosses the tile: 32 columns at a time in a rolled loop, those that some row of
+        // the warp may see.  (A second unrolled pass for such tiles is faster by itself and slower in the kernel, by 12 %
+        // on long prompts and 10 % on 700 tokens: the two no longer fit the instruction cache together.)
+        const int n_ch = min(4, (min(L.q_hi, L.q0 + w_last + 1) - c0 + 31) >> 5);
+        turn();
+        at_softmax_chunks<0>(s_addr, o_addr, n_ch, pos - c0, c0 - r0, pos < L.q_hi, u > 0 ? D / 32 : 0, a.scale_log2, m_used, l_run);
+        pass_on();
         const int pad = c0 + pk_cols(L, u) - I.n;                      // rows past the sequence's end that P V covers
         if (pad > 0) {
           const int t = ring0 + 2 * u + 1;
@@ -296,9 +464,8 @@ attn_packed_kernel(const __grid_constant__ PkMaps maps, const PkArgs a) {
           }
           fence_proxy_async();
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(x, P_FULL));
+        hand_over(P_HALF);
+        hand_over(P_FULL);
       }
       // ---- epilogue: O / l -> bf16 -> out, 64 columns per round through this warp's staging (16-byte units XOR-swizzled
       // by row pair: the 64-byte swizzle of the tensor map)
@@ -355,13 +522,14 @@ attn_packed_kernel(const __grid_constant__ PkMaps maps, const PkArgs a) {
         }
       }
       g0 += n_sub;
+      g_twin += n_twin;
       ring0 += 2 * I.n_kv;
       ++n_item;
     }
     if (lane == 0) bulk_wait_read<0>();                  // staged data must be read before shared memory goes
     if (*abort_flag && row == 0) report_status(a.status, DL_ERR_TIMEOUT, blockIdx.x);
   } else {
-    reg_dec<kAtRegsSmall>();                             // same budget as the rest of its warpgroup
+    reg_dec<kPkRegsSmall>();                             // same budget as the rest of its warpgroup
     // starts that lead out of the tensors (they are clamped wherever they are used) and sequences longer than max_rows
     // (cut off there) are reported
     if (blockIdx.x == 0)
