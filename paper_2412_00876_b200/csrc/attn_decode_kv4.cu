@@ -274,21 +274,23 @@ attn_decode_kv4_kernel(const K4Args a) {
         for (int g = 0; g < NG; ++g) qs[nt][g][c] = __shfl_sync(0xffffffffu, sum[g], from) * a.scale_log2;
       }
     }
-    // ---- Eq. 6's append, by the warp that has the pair's first unit: lanes 0 .. D/8-1 hold k_t, the next D/8 v_t
+    // ---- Eq. 6's append, by the warp that has the pair's first unit: lanes 0 .. D/16-1 hold k_t, the next D/16 v_t
     if (t == 0 && a.keep != nullptr && a.keep[b] != 0) {
-      constexpr int LR = D / 8;
+      constexpr int LR = D / 16;
       const int l = lane % LR;
       const bool is_v = lane >= LR, on = lane < 2 * LR;
-      const uint4 raw = __ldg(reinterpret_cast<const uint4*>((is_v ? a.v_t : a.k_t) + ((size_t)b * a.Hk + hk) * D) + l);
+      const uint4* from = reinterpret_cast<const uint4*>((is_v ? a.v_t : a.k_t) + ((size_t)b * a.Hk + hk) * D) + 2 * l;
+      const uint4 lo = __ldg(from), hi = __ldg(from + 1);
+      const uint32_t raw[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
       uint32_t word;
-      const uint32_t code = kv4_quantise8(raw, word);
+      const uint2 code = kv4_quantise16(raw, word);
       const int pi = n >> (a.pg.tile_shift + 4);
       const int idx = pi < a.pg.max_pages
                           ? kv4_tile_index(a.pg, __ldg(a.pg.table + (size_t)b * a.pg.max_pages + pi), a.Hk, hk, n >> 4) : -1;
       if (idx < 0) {
         if (lane == 0 && hk == 0) report_status(a.status, DL_ERR_CAPACITY, b);
       } else if (on && DL_IN_BOUNDS(a.status, KID_DECODE_KV4, idx, ((long long)a.pg.n_pages * a.Hk) << a.pg.tile_shift)) {
-        kv4_store8<D>(a.pool + (long long)idx * F::TILE, n & 15, l, is_v, code, word);
+        kv4_store16<D>(a.pool + (long long)idx * F::TILE, n & 15, l, is_v, code, word);
       }
     }
 

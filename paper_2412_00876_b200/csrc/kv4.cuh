@@ -43,67 +43,99 @@ template <int D> __device__ __forceinline__ int kv4_v_off(int i, int d) {
   return Kv4<D>::V + i * D + 16 * step + (d & 8);
 }
 
-// Eight consecutive values per lane (`raw`: bf16), eight lanes per group (lanes 8i .. 8i + 7): this lane's codes, and the
-// group's word.  All 32 lanes take part.
-__device__ __forceinline__ uint32_t kv4_quantise8(uint4 raw, uint32_t& word) {
-  const uint32_t u[4] = {raw.x, raw.y, raw.z, raw.w};
-  float x[8];
-  bool odd = false;                                   // a NaN or an infinity
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = bf16lo(u[i]);
-    x[2 * i + 1] = bf16hi(u[i]);
-    odd |= (u[i] & 0x7F80u) == 0x7F80u || (u[i] & 0x7F800000u) == 0x7F800000u;
-  }
-  float lo = x[0], hi = x[0];
-#pragma unroll
-  for (int i = 1; i < 8; ++i) { lo = fminf(lo, x[i]); hi = fmaxf(hi, x[i]); }
-#pragma unroll
-  for (int o = 1; o < 8; o <<= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-  }
-  const float range = __fsub_rn(hi, lo);
-  odd |= !(range <= 3.402823466e38f);
-  const uint32_t lane = threadIdx.x & 31;
-  odd = ((__ballot_sync(0xffffffffu, odd) >> (lane & 24)) & 0xFFu) != 0;
-  const __nv_bfloat16 sb = __float2bfloat16_rn(__fdiv_rn(range, 15.f));
-  const float s = __bfloat162float(sb);
-  const bool flat = odd || !(s >= 1.17549435e-38f);
-  const float inv = flat ? 0.f : __frcp_rn(s);
-  uint32_t code = 0;
-  if (!flat) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      // t = nearest integer in the low bits of (v + 2^23); v >= 0, and above 15 only by the rounding of s
-      const float v = fminf(__fmul_rn(__fsub_rn(x[i], lo), inv), 15.f);
-      code |= (__float_as_uint(__fadd_rn(v, 8388608.f)) & 15u) << (4 * i);
-    }
-  }
-  word = odd ? 0x7FC00000u
-             : (uint32_t)__bfloat16_as_ushort(sb) | ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(lo)) << 16);
-  return code;
+// bf16 pairs: minimum and maximum that keep a NaN
+__device__ __forceinline__ uint32_t kv4_min2(uint32_t x, uint32_t y) {
+  uint32_t r;
+  asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+  return r;
+}
+__device__ __forceinline__ uint32_t kv4_max2(uint32_t x, uint32_t y) {
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+  return r;
+}
+// two fp32 operations, each rounded by itself
+__device__ __forceinline__ uint64_t kv4_pack2(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ uint64_t kv4_add2(uint64_t x, uint64_t y) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+  return r;
+}
+__device__ __forceinline__ uint64_t kv4_fma2(uint64_t x, uint64_t y, uint64_t z) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
+  return r;
 }
 
-// Stores what kv4_quantise8 gave for lane `l` (0 .. D/8 - 1: dims 8 l .. 8 l + 7) of row `row` of the tile at `tile`;
-// is_v picks the tensor.  No byte of another row is written.
-template <int D> __device__ __forceinline__ void kv4_store8(uint8_t* tile, int row, int l, bool is_v, uint32_t code, uint32_t word) {
-  const int g = l >> 3;
-  if (is_v) {
-    uint16_t* to = reinterpret_cast<uint16_t*>(tile + kv4_v_off<D>(row >> 1, 8 * l)) + (row & 1);
-    to[0] = (uint16_t)code;
-    to[2] = (uint16_t)(code >> 16);
-  } else {
-    *reinterpret_cast<uint32_t*>(tile + kv4_k_off<D>(row, g) + 4 * (l & 7)) = code;
+// Sixteen consecutive values per lane (`u`: bf16 pairs), four lanes per group (lanes 4i .. 4i + 3): this lane's codes, and
+// the group's word.  All 32 lanes take part.  The extremes are found on bf16 pairs; from the first reduction on a lane
+// holds (min, -max) in one register.
+__device__ __forceinline__ uint2 kv4_quantise16(const uint32_t (&u)[8], uint32_t& word) {
+  uint32_t mn = u[0], mx = u[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) { mn = kv4_min2(mn, u[i]); mx = kv4_max2(mx, u[i]); }
+  mx ^= 0x80008000u;                                                        // -max
+  uint32_t ext = kv4_min2(__byte_perm(mn, mx, 0x5410), __byte_perm(mn, mx, 0x7632));
+  ext = kv4_min2(ext, __shfl_xor_sync(0xffffffffu, ext, 1));
+  ext = kv4_min2(ext, __shfl_xor_sync(0xffffffffu, ext, 2));
+  const float lo = bf16lo(ext), range = __fsub_rn(-bf16hi(ext), lo);
+  const bool odd = !(range <= 3.402823466e38f);                             // a NaN, an infinity, a range beyond fp32
+  const __nv_bfloat16 sb = __float2bfloat16_rn(__fdiv_rn(range, 15.f));
+  const float s = __bfloat162float(sb);
+  // s >= 2^-126 has eight significant bits, so (x - z) / s is at most 15 (1 + 2^-8): no code above 15
+  const bool flat = odd || !(s >= 1.17549435e-38f);
+  const float inv = flat ? 0.f : __frcp_rn(s);
+  const uint64_t lo2 = kv4_pack2(flat ? 0.f : -lo, flat ? 0.f : -lo);
+  const uint64_t magic = kv4_pack2(8388608.f, 8388608.f);                   // 2^23: the nearest integer ends up in the low bits
+  uint32_t c[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t t[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w = flat ? 0u : u[4 * h + i];
+      const uint64_t d = kv4_add2(kv4_pack2(bf16lo(w), bf16hi(w)), lo2);
+      // the products one by one: a packed product and the packed sum behind it become one fused operation, which rounds once
+      // and turns ties of the definition into other codes
+      const uint64_t v = kv4_add2(kv4_pack2(__fmul_rn(__uint_as_float((uint32_t)d), inv), __fmul_rn(__uint_as_float((uint32_t)(d >> 32)), inv)), magic);
+      t[2 * i] = (uint32_t)v;
+      t[2 * i + 1] = (uint32_t)(v >> 32);
+    }
+    uint32_t acc = t[7];
+#pragma unroll
+    for (int i = 6; i >= 0; --i) acc = acc * 16u + t[i];
+    c[h] = acc - 0x4B000000u * 0x11111111u;                                 // what the bits of 2^23 have added up to
   }
-  if ((l & 7) == 0)
+  word = odd ? 0x7FC00000u : (uint32_t)__bfloat16_as_ushort(sb) | (ext << 16);
+  return make_uint2(c[0], c[1]);
+}
+
+// Stores what kv4_quantise16 gave for lane `l` (0 .. D/16 - 1: dims 16 l .. 16 l + 15) of row `row` of the tile at `tile`;
+// is_v picks the tensor.  No byte of another row is written.
+template <int D> __device__ __forceinline__ void kv4_store16(uint8_t* tile, int row, int l, bool is_v, uint2 code, uint32_t word) {
+  const int g = l >> 2;
+  if (is_v) {
+    uint16_t* to = reinterpret_cast<uint16_t*>(tile + kv4_v_off<D>(row >> 1, 16 * l)) + (row & 1);
+    to[0] = (uint16_t)code.x;
+    to[2] = (uint16_t)(code.x >> 16);
+    to[4] = (uint16_t)code.y;
+    to[6] = (uint16_t)(code.y >> 16);
+  } else {
+    *reinterpret_cast<uint2*>(tile + kv4_k_off<D>(row, g) + 8 * (l & 3)) = code;
+  }
+  if ((l & 3) == 0)
     *reinterpret_cast<uint32_t*>(tile + (is_v ? Kv4<D>::VM : Kv4<D>::KM) + (row * Kv4<D>::NG + g) * 4) = word;
 }
 // The codes that it stored.
-template <int D> __device__ __forceinline__ uint32_t kv4_load8(const uint8_t* tile, int row, int l, bool is_v) {
-  if (!is_v) return __ldg(reinterpret_cast<const uint32_t*>(tile + kv4_k_off<D>(row, l >> 3) + 4 * (l & 7)));
-  const uint2 w = __ldg(reinterpret_cast<const uint2*>(tile + kv4_v_off<D>(row >> 1, 8 * l)));
-  return __byte_perm(w.x, w.y, (row & 1) ? 0x7632 : 0x5410);
+template <int D> __device__ __forceinline__ uint2 kv4_load16(const uint8_t* tile, int row, int l, bool is_v) {
+  if (!is_v) return __ldg(reinterpret_cast<const uint2*>(tile + kv4_k_off<D>(row, l >> 2) + 8 * (l & 3)));
+  const uint4 w = __ldg(reinterpret_cast<const uint4*>(tile + kv4_v_off<D>(row >> 1, 16 * l)));
+  const uint32_t pick = (row & 1) ? 0x7632u : 0x5410u;
+  return make_uint2(__byte_perm(w.x, w.y, pick), __byte_perm(w.z, w.w, pick));
 }
 
 // What a paged call knows of the pages, by value.

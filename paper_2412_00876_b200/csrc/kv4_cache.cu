@@ -3,9 +3,9 @@
 //
 //   plan   : per sequence, count the kept rows, check that the pages for them are there, note the first destination
 //            row and (optionally) advance the length: one CTA per sequence;
-//   append : a CTA takes up to 32 packed source rows, ranks the kept ones and quantises them, 8 values per lane, 8
-//            lanes per group; dropped rows are not read.  A thread stays at one place of the row (head, tensor, 8 dims)
-//            and walks the kept rows, four loads in flight; wide rows are shared by several CTAs (grid y);
+//   append : a CTA takes up to 32 packed source rows, ranks the kept ones and quantises them, 16 values per lane, 4
+//            lanes per group; dropped rows are not read.  A thread stays at one place of the row (head, tensor, 16 dims)
+//            and walks the kept rows, two in flight; wide rows are shared by several CTAs (grid y);
 //   read   : the same walk the other way, codes to bf16.
 // Both are bound by HBM: a kept row costs 2 D bytes in and 9 D / 16 out per head and tensor.
 #include <algorithm>
@@ -16,7 +16,7 @@ namespace dl {
 
 constexpr int kK4Threads = 256;
 constexpr int kK4Rows = 32;              // most packed rows per CTA
-constexpr int kK4Unroll = 4;             // rows a thread has in flight
+constexpr int kK4Unroll = 2;             // rows a thread has in flight
 
 __device__ __forceinline__ int k4_block_sum(int v, int* sh) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -51,7 +51,7 @@ __device__ __forceinline__ int k4_sequence(const int* st, int B, int r) {
   return (lo >= 0 && r < st[lo + 1]) ? lo : -1;
 }
 
-// A thread's place in a row of U units (8 values of one head and tensor each): unit `rem`, starting at the CTA's row
+// A thread's place in a row of U units (16 values of one head and tensor each): unit `rem`, starting at the CTA's row
 // `first` and going on by `step` rows; rem >= U: no place.
 struct K4Place { int rem, first, step; };
 __device__ __forceinline__ K4Place k4_place(int U) {
@@ -141,31 +141,38 @@ kv4_append_kernel(const PagesArg pg, uint8_t* __restrict__ pool, int32_t Hk, con
     if (threadIdx.x == 0) n_kept = __popc(w);
   }
   __syncthreads();
-  constexpr int LR = D / 8;                                       // units per row of one head and tensor
+  constexpr int LR = D / 16;                                      // units per row of one head and tensor
   const int half = Hk * LR, U = 2 * half, n = n_kept;
   const K4Place at = k4_place(U);
   const bool on = at.rem < U;
   const bool is_v = at.rem >= half;
   const int l = on ? (is_v ? at.rem - half : at.rem) : 0, hk = l / LR, lr = l - hk * LR;
-  const __nv_bfloat16* src = (is_v ? v : k) + l * 8;
+  const __nv_bfloat16* src = (is_v ? v : k) + l * 16;
   const long long head_tiles = (long long)hk << pg.tile_shift;
   for (int base = 0; base < n; base += at.step * kK4Unroll) {     // the same trips for all lanes: they shuffle together
-    uint4 raw[kK4Unroll];
+    uint32_t raw[kK4Unroll][8];
 #pragma unroll
     for (int c = 0; c < kK4Unroll; ++c) {
       const int row = base + c * at.step + at.first;
-      raw[c] = on && row < n ? __ldg(reinterpret_cast<const uint4*>(src + row_src[row])) : make_uint4(0u, 0u, 0u, 0u);
+      uint4 x = make_uint4(0u, 0u, 0u, 0u), y = x;
+      if (on && row < n) {
+        const uint4* from = reinterpret_cast<const uint4*>(src + row_src[row]);
+        x = __ldg(from);
+        y = __ldg(from + 1);
+      }
+      raw[c][0] = x.x; raw[c][1] = x.y; raw[c][2] = x.z; raw[c][3] = x.w;
+      raw[c][4] = y.x; raw[c][5] = y.y; raw[c][6] = y.z; raw[c][7] = y.w;
     }
 #pragma unroll
     for (int c = 0; c < kK4Unroll; ++c) {
       if (base + c * at.step >= n) break;
       const int row = base + c * at.step + at.first;
       uint32_t word;
-      const uint32_t code = kv4_quantise8(raw[c], word);
+      const uint2 code = kv4_quantise16(raw[c], word);
       if (on && row < n) {
         const long long tile = row_tile[row] + head_tiles;
         if (DL_IN_BOUNDS(st, KID_KV4_APPEND, tile, (long long)pg.n_pages * Hk << pg.tile_shift))
-          kv4_store8<D>(pool + tile * Kv4<D>::TILE, row_in[row], lr, is_v, code, word);
+          kv4_store16<D>(pool + tile * Kv4<D>::TILE, row_in[row], lr, is_v, code, word);
       }
     }
   }
@@ -202,25 +209,27 @@ kv4_read_kernel(const PagesArg pg, const uint8_t* __restrict__ pool, int32_t Hk,
     row_in[threadIdx.x] = in;
   }
   __syncthreads();
-  constexpr int LR = D / 8;
+  constexpr int LR = D / 16;
   const int half = Hk * LR, U = 2 * half, n = min(rows, total - t0);
   const K4Place at = k4_place(U);
   if (at.rem >= U) return;
   const bool is_v = at.rem >= half;
-  const int l = is_v ? at.rem - half : at.rem, hk = l / LR, lr = l - hk * LR, g = lr >> 3;
+  const int l = is_v ? at.rem - half : at.rem, hk = l / LR, lr = l - hk * LR, g = lr >> 2;
   const long long head_tiles = (long long)hk << pg.tile_shift;
   uint4* out = reinterpret_cast<uint4*>(is_v ? v_out : k_out);
+  const uint64_t magic = kv4_pack2(-8388608.f, -8388608.f);
   for (int base = at.first; base < n; base += at.step * kK4Unroll) {
-    uint32_t code[kK4Unroll], word[kK4Unroll];
+    uint2 code[kK4Unroll];
+    uint32_t word[kK4Unroll];
 #pragma unroll
     for (int c = 0; c < kK4Unroll; ++c) {
       const int row = base + c * at.step;
-      code[c] = word[c] = 0u;
+      code[c] = make_uint2(0u, 0u);
+      word[c] = 0u;
       if (row < n && row_tile[row] >= 0) {
         const uint8_t* tile = pool + (row_tile[row] + head_tiles) * Kv4<D>::TILE;
-        const int R = row_in[row];
-        code[c] = kv4_load8<D>(tile, R, lr, is_v);
-        word[c] = __ldg(reinterpret_cast<const uint32_t*>(tile + (is_v ? Kv4<D>::VM : Kv4<D>::KM) + (R * Kv4<D>::NG + g) * 4));
+        code[c] = kv4_load16<D>(tile, row_in[row], lr, is_v);
+        word[c] = __ldg(reinterpret_cast<const uint32_t*>(tile + (is_v ? Kv4<D>::VM : Kv4<D>::KM) + (row_in[row] * Kv4<D>::NG + g) * 4));
       }
     }
 #pragma unroll
@@ -228,22 +237,29 @@ kv4_read_kernel(const PagesArg pg, const uint8_t* __restrict__ pool, int32_t Hk,
       const int row = base + c * at.step;
       if (row >= n || row_tile[row] == -2) continue;
       const float s = bf16lo(word[c]), z = bf16hi(word[c]);
-      uint32_t p[4];
+      const uint64_t s2 = kv4_pack2(s, s), z2 = kv4_pack2(z, z);
+      uint32_t p[8];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x0 = fmaf((float)((code[c] >> (8 * e)) & 15u), s, z), x1 = fmaf((float)((code[c] >> (8 * e + 4)) & 15u), s, z);
-        p[e] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(x0)) |
-               ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(x1)) << 16);
+      for (int e = 0; e < 8; ++e) {
+        // a code in the low bits of 2^23, less 2^23
+        const uint32_t w = (e < 4 ? code[c].x : code[c].y) >> (8 * (e & 3));
+        const uint64_t v = kv4_add2(kv4_pack2(__uint_as_float((w & 15u) | 0x4B000000u), __uint_as_float(((w >> 4) & 15u) | 0x4B000000u)), magic);
+        const uint64_t y = kv4_fma2(v, s2, z2);
+        const __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float((uint32_t)y), __uint_as_float((uint32_t)(y >> 32)));
+        p[e] = *reinterpret_cast<const uint32_t*>(&b);
       }
-      const long long to = (long long)(t0 + row) * half + l;
-      if (DL_IN_BOUNDS(st, KID_KV4_READ, to, (long long)total * half)) out[to] = make_uint4(p[0], p[1], p[2], p[3]);
+      const long long to = 2 * ((long long)(t0 + row) * half + l);
+      if (DL_IN_BOUNDS(st, KID_KV4_READ, to + 1, 2LL * total * half)) {
+        out[to] = make_uint4(p[0], p[1], p[2], p[3]);
+        out[to + 1] = make_uint4(p[4], p[5], p[6], p[7]);
+      }
     }
   }
 }
 
 // Rows per CTA and the grid: fewer rows where 32 would not fill the GPU eight times over.
 static dim3 k4_grid(const dl_ctx* ctx, int total, int Hk, int* rows) {
-  const int U = 2 * Hk * ctx->desc.head_dim / 8, slabs = U >= kK4Threads ? (U + kK4Threads - 1) / kK4Threads : 1;
+  const int U = 2 * Hk * ctx->desc.head_dim / 16, slabs = U >= kK4Threads ? (U + kK4Threads - 1) / kK4Threads : 1;
   *rows = kK4Rows;
   while (*rows > 4 && (long long)((total + *rows - 1) / *rows) * slabs < 8LL * ctx->sm_count) *rows >>= 1;
   return dim3((total + *rows - 1) / *rows, slabs);
