@@ -707,7 +707,8 @@ int32_t dl_decode_steps_host(dl_ctx* ctx, const dl_predictor* p_txt, int32_t n_s
 static int32_t check_pages(const dl_ctx* ctx, const dl_pages* p) {
   if (!ctx || !p || p->B < 0 || p->n_pages <= 0 || p->max_pages <= 0) return DL_ERR_INVALID_ARG;
   if (p->page_rows != 16 && p->page_rows != 32 && p->page_rows != 64 && p->page_rows != 128) return DL_ERR_UNSUPPORTED;
-  if (p->B > 2048 || (int64_t)p->max_pages * p->page_rows >= (1LL << 31)) return DL_ERR_UNSUPPORTED;
+  if (p->B > 2048 || (int64_t)p->max_pages * p->page_rows >= (1LL << 31) || (int64_t)p->B * p->max_pages >= (1LL << 31))
+    return DL_ERR_UNSUPPORTED;
   if (p->B > 0 && (!p->table || !p->refs || !p->len)) return DL_ERR_INVALID_ARG;
   if (misaligned(p->table) || misaligned(p->refs) || misaligned(p->len)) return DL_ERR_ALIGNMENT;
   return DL_OK;

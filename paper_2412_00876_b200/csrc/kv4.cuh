@@ -89,21 +89,16 @@ __device__ __forceinline__ uint2 kv4_quantise16(const uint32_t (&u)[8], uint32_t
   // s >= 2^-126 has eight significant bits, so (x - z) / s is at most 15 (1 + 2^-8): no code above 15
   const bool flat = odd || !(s >= 1.17549435e-38f);
   const float inv = flat ? 0.f : __frcp_rn(s);
-  const uint64_t lo2 = kv4_pack2(flat ? 0.f : -lo, flat ? 0.f : -lo);
-  const uint64_t magic = kv4_pack2(8388608.f, 8388608.f);                   // 2^23: the nearest integer ends up in the low bits
   uint32_t c[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     uint32_t t[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t w = flat ? 0u : u[4 * h + i];
-      const uint64_t d = kv4_add2(kv4_pack2(bf16lo(w), bf16hi(w)), lo2);
-      // the products one by one: a packed product and the packed sum behind it become one fused operation, which rounds once
-      // and turns ties of the definition into other codes
-      const uint64_t v = kv4_add2(kv4_pack2(__fmul_rn(__uint_as_float((uint32_t)d), inv), __fmul_rn(__uint_as_float((uint32_t)(d >> 32)), inv)), magic);
-      t[2 * i] = (uint32_t)v;
-      t[2 * i + 1] = (uint32_t)(v >> 32);
+      // + 2^23: the nearest integer ends up in the low bits (the product is rounded first, as the definition says)
+      const uint32_t w = u[4 * h + i];
+      t[2 * i] = __float_as_uint(__fadd_rn(__fmul_rn(__fsub_rn(bf16lo(w), lo), inv), 8388608.f));
+      t[2 * i + 1] = __float_as_uint(__fadd_rn(__fmul_rn(__fsub_rn(bf16hi(w), lo), inv), 8388608.f));
     }
     uint32_t acc = t[7];
 #pragma unroll
@@ -111,7 +106,7 @@ __device__ __forceinline__ uint2 kv4_quantise16(const uint32_t (&u)[8], uint32_t
     c[h] = acc - 0x4B000000u * 0x11111111u;                                 // what the bits of 2^23 have added up to
   }
   word = odd ? 0x7FC00000u : (uint32_t)__bfloat16_as_ushort(sb) | (ext << 16);
-  return make_uint2(c[0], c[1]);
+  return flat ? make_uint2(0u, 0u) : make_uint2(c[0], c[1]);
 }
 
 // Stores what kv4_quantise16 gave for lane `l` (0 .. D/16 - 1: dims 16 l .. 16 l + 15) of row `row` of the tile at `tile`;

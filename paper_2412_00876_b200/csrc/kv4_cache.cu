@@ -16,6 +16,7 @@ namespace dl {
 
 constexpr int kK4Threads = 256;
 constexpr int kK4Rows = 32;              // most packed rows per CTA
+constexpr int kK4Ctas = 16;              // CTAs per SM worth having
 constexpr int kK4Unroll = 2;             // rows a thread has in flight
 
 __device__ __forceinline__ int k4_block_sum(int v, int* sh) {
@@ -257,11 +258,12 @@ kv4_read_kernel(const PagesArg pg, const uint8_t* __restrict__ pool, int32_t Hk,
   }
 }
 
-// Rows per CTA and the grid: fewer rows where 32 would not fill the GPU eight times over.
+// Rows per CTA and the grid: fewer rows where 32 would not give every SM kK4Ctas CTAs (kept rows are
+// spread unevenly over a batch).
 static dim3 k4_grid(const dl_ctx* ctx, int total, int Hk, int* rows) {
   const int U = 2 * Hk * ctx->desc.head_dim / 16, slabs = U >= kK4Threads ? (U + kK4Threads - 1) / kK4Threads : 1;
   *rows = kK4Rows;
-  while (*rows > 4 && (long long)((total + *rows - 1) / *rows) * slabs < 8LL * ctx->sm_count) *rows >>= 1;
+  while (*rows > 4 && (long long)((total + *rows - 1) / *rows) * slabs < (long long)kK4Ctas * ctx->sm_count) *rows >>= 1;
   return dim3((total + *rows - 1) / *rows, slabs);
 }
 

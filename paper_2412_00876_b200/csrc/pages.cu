@@ -26,32 +26,26 @@ struct PgArgs {
 
 struct PgPools { char* p[kPgPools]; };
 
-// Exclusive scan over the CTA's threads; *sum gets the total.  sh: 33 ints.
-__device__ __forceinline__ int pg_scan(int v, int* sh, int* sum) {
+// Two exclusive scans at once over the CTA's threads; sums: the totals.  sh: 32 int2, not used again by the caller.
+__device__ __forceinline__ int2 pg_scan2(int2 v, int2* sh, int2* sums) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int run = v;
+  int2 run = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(0xffffffffu, run, o);
-    if (lane >= o) run += x;
+    const int x = __shfl_up_sync(0xffffffffu, run.x, o), y = __shfl_up_sync(0xffffffffu, run.y, o);
+    if (lane >= o) { run.x += x; run.y += y; }
   }
   if (lane == 31) sh[warp] = run;
   __syncthreads();
-  if (warp == 0) {
-    int x = sh[lane], y = x;
+  // every warp adds up the 32 warps' totals for itself
+  int2 t = sh[lane], all = t;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int z = __shfl_up_sync(0xffffffffu, y, o);
-      if (lane >= o) y += z;
-    }
-    sh[lane] = y - x;
-    if (lane == 31) sh[32] = y;
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, t.x, o), y = __shfl_up_sync(0xffffffffu, t.y, o);
+    if (lane >= o) { t.x += x; t.y += y; }
   }
-  __syncthreads();
-  const int before = sh[warp] + run - v;
-  *sum = sh[32];
-  __syncthreads();
-  return before;
+  *sums = make_int2(__shfl_sync(0xffffffffu, t.x, 31), __shfl_sync(0xffffffffu, t.y, 31));
+  return make_int2(__shfl_sync(0xffffffffu, t.x - all.x, warp) + run.x - v.x, __shfl_sync(0xffffffffu, t.y - all.y, warp) + run.y - v.y);
 }
 __device__ __forceinline__ bool pg_valid(const PgArgs& a, int p) { return (unsigned)p < (unsigned)a.n_pages; }
 // this thread's run of pages
@@ -70,33 +64,40 @@ pages_reserve_kernel(const PgArgs a, const int32_t* __restrict__ need) {
   extern __shared__ int sm[];
   int* have = sm;                         // [B] pages a sequence has
   int* first = sm + a.B;                  // [B + 1] pages handed out in front of it
-  __shared__ int sh[33], too_long;
+  __shared__ int2 sh[32];
+  __shared__ int too_long;
   if (threadIdx.x == 0) too_long = a.B;
+  int from, to;
+  pg_run(a, from, to);
+  int2 mine = make_int2(0, 0), sums;      // pages wanted by this thread's sequences, free pages in its run
+  for (int p = from; p < to; ++p) mine.y += a.refs[p] == 0;
   __syncthreads();
   const int per = (a.B + kPgThreads - 1) / kPgThreads, b0 = min(a.B, (int)threadIdx.x * per), b1 = min(a.B, b0 + per);
-  int mine = 0;
   for (int b = b0; b < b1; ++b) {
     const int32_t* row = a.table + (size_t)b * a.W;
-    int lo = 0, hi = a.W;                 // a row's pages come first: the first -1 by bisection
+    const int len = max(a.len[b], 0);
+    // a row's pages come first, as many as its rows take at least: look there, and search if that is not so
+    int lo = pg_pages_of(a, len), hi = lo;
+    const bool here = lo == 0 || row[lo - 1] >= 0, end = lo == a.W || row[lo] < 0;
+    if (!here) lo = 0;
+    else if (!end) hi = a.W;
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
       if (row[mid] >= 0) lo = mid + 1; else hi = mid;
     }
     have[b] = lo;
-    const long long rows = (long long)max(a.len[b], 0) + max(need[b], 0);
+    const long long rows = (long long)len + max(need[b], 0);
     const long long want = (rows + (1 << a.shift) - 1) >> a.shift;
     if (want > a.W) atomicMin(&too_long, b);
-    first[b] = mine;
-    mine += (int)max(0LL, min(want, (long long)a.W) - lo);
+    first[b] = mine.x;
+    mine.x += (int)max(0LL, min(want, (long long)a.W) - lo);
   }
-  int wanted;
-  const int before = pg_scan(mine, sh, &wanted);
-  for (int b = b0; b < b1; ++b) first[b] += before;
+  const int2 before = pg_scan2(mine, sh, &sums);
+  const int wanted = sums.x, free_pages = sums.y;
+  for (int b = b0; b < b1; ++b) first[b] += before.x;
   if (threadIdx.x == 0) first[a.B] = wanted;
-  int from, to, c = 0, free_pages;
-  pg_run(a, from, to);
-  for (int p = from; p < to; ++p) c += a.refs[p] == 0;
-  int rank = pg_scan(c, sh, &free_pages);
+  int rank = before.y;
+  __syncthreads();
   if (too_long < a.B || free_pages < wanted) {
     if (threadIdx.x == 0) report_status(a.status, DL_ERR_CAPACITY, too_long < a.B ? too_long : -1);
     return;
@@ -131,16 +132,23 @@ __global__ void pages_free_kernel(const PgArgs a, const uint8_t* __restrict__ go
 // Sequence b becomes a fork of parent[b] as that was before the call.  Full pages are shared; of the children that need a
 // parent's partly filled last page one keeps it (the parent itself if it stays, else the lowest) and each other one
 // gets the lowest free page for a copy.  All or nothing.
+// The counts and the new table rows are kept in shared memory where they fit (near: 1 | 2), else in global memory: one
+// round trip for each step of the bookkeeping otherwise.
 __global__ void __launch_bounds__(kPgThreads)
-pages_fork_kernel(const PgArgs a, const int32_t* __restrict__ parent) {
+pages_fork_kernel(const PgArgs a, const int32_t* __restrict__ parent, int32_t near) {
   extern __shared__ int sm[];
   int* par = sm;                          // [B]
   int* low = sm + a.B;                    // [B] lowest child
   int* rows = sm + 2 * a.B;               // [B] new length
   int* copy = sm + 3 * a.B;               // [B] the last page is to be copied
-  __shared__ int sh[33];
+  int* mine_dst = sm + 4 * a.B;           // [B] pages handed out, in order
+  volatile int* refs = (near & 1) ? sm + 5 * a.B : a.refs;
+  volatile int* fresh = (near & 2) ? sm + 5 * a.B + ((near & 1) ? a.n_pages : 0) : a.fresh;
+  __shared__ int2 sh[32];
   const int T = kPgThreads, tid = threadIdx.x;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (near & 1)
+    for (int p = tid; p < a.n_pages; p += T) refs[p] = a.refs[p];
   for (int b = tid; b < a.B; b += T) {
     int p = parent[b];
     if (p < -1 || p >= a.B) {
@@ -165,54 +173,60 @@ pages_fork_kernel(const PgArgs a, const int32_t* __restrict__ parent) {
     copy[b] = c;
   }
   __syncthreads();
-  // new rows into scratch, counts of the pages that come and go
-  const long long cells = (long long)a.B * a.W;
-  for (long long i = tid; i < cells; i += T) {
-    const int b = (int)(i / a.W), c = (int)(i - (long long)b * a.W), p = par[b];
+  // new rows, counts of the pages that come and go
+  const unsigned cells = (unsigned)a.B * (unsigned)a.W;                      // below 2^31
+  for (unsigned i = tid; i < cells; i += T) {
+    const int b = (int)(i / (unsigned)a.W), c = (int)(i - (unsigned)b * a.W), p = par[b];
     if (p == b) continue;
     const int used = pg_pages_of(a, rows[b]);
     const int old = a.table[i], now = p >= 0 && c < used ? a.table[(size_t)p * a.W + c] : -1;
-    a.fresh[i] = now;
-    if (pg_valid(a, old)) atomicSub(a.refs + old, 1);
-    if (pg_valid(a, now) && !(copy[b] && c == used - 1)) atomicAdd(a.refs + now, 1);
+    fresh[i] = now;
+    if (pg_valid(a, old)) atomicSub(const_cast<int*>(refs) + old, 1);
+    if (pg_valid(a, now) && !(copy[b] && c == used - 1)) atomicAdd(const_cast<int*>(refs) + now, 1);
   }
-  __threadfence();
+  if (!(near & 1)) __threadfence();
   __syncthreads();
   // copies in order of b, free pages in order of index
   const int per = (a.B + T - 1) / T, b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
-  int mine = 0, copies, free_pages, c = 0, from, to;
-  for (int b = b0; b < b1; ++b) mine += copy[b];
-  int at = pg_scan(mine, sh, &copies);
+  int from, to;
+  int2 mine = make_int2(0, 0), sums;
+  for (int b = b0; b < b1; ++b) mine.x += copy[b];
   pg_run(a, from, to);
-  for (int p = from; p < to; ++p) c += __ldcg(a.refs + p) == 0;
-  int rank = pg_scan(c, sh, &free_pages);
-  if (free_pages < copies) {
-    for (long long i = tid; i < cells; i += T) {
-      const int b = (int)(i / a.W), col = (int)(i - (long long)b * a.W);
-      if (par[b] == b) continue;
-      const int old = a.table[i], now = a.fresh[i];
-      if (pg_valid(a, old)) atomicAdd(a.refs + old, 1);
-      if (pg_valid(a, now) && !(copy[b] && col == pg_pages_of(a, rows[b]) - 1)) atomicSub(a.refs + now, 1);
-    }
+  for (int p = from; p < to; ++p) mine.y += refs[p] == 0;
+  const int2 before = pg_scan2(mine, sh, &sums);
+  const int copies = sums.x;
+  int at = before.x, rank = before.y;
+  if (sums.y < copies) {
+    if (!(near & 1))                      // put the counts back
+      for (unsigned i = tid; i < cells; i += T) {
+        const int b = (int)(i / (unsigned)a.W), col = (int)(i - (unsigned)b * a.W);
+        if (par[b] == b) continue;
+        const int old = a.table[i], now = fresh[i];
+        if (pg_valid(a, old)) atomicAdd(const_cast<int*>(refs) + old, 1);
+        if (pg_valid(a, now) && !(copy[b] && col == pg_pages_of(a, rows[b]) - 1)) atomicSub(const_cast<int*>(refs) + now, 1);
+      }
     if (tid == 0) { a.hdr[0] = 0; report_status(a.status, DL_ERR_CAPACITY, -1); }
     return;
   }
   for (int p = from; p < to && rank < copies; ++p)
-    if (__ldcg(a.refs + p) == 0) a.dst[rank++] = p;
+    if (refs[p] == 0) mine_dst[rank++] = p;
   __syncthreads();
   for (int b = b0; b < b1; ++b)
     if (copy[b]) {
-      const size_t cell = (size_t)b * a.W + pg_pages_of(a, rows[b]) - 1;
-      const int d = a.dst[at];
-      a.src[at++] = a.fresh[cell];
-      a.fresh[cell] = d;
-      a.refs[d] = 1;
+      const unsigned cell = (unsigned)b * a.W + pg_pages_of(a, rows[b]) - 1;
+      const int d = mine_dst[at];
+      a.src[at] = fresh[cell];
+      a.dst[at++] = d;
+      fresh[cell] = d;
+      refs[d] = 1;
     }
   __syncthreads();
-  for (long long i = tid; i < cells; i += T) {
-    const int b = (int)(i / a.W);
-    if (par[b] != b) a.table[i] = a.fresh[i];
+  for (unsigned i = tid; i < cells; i += T) {
+    const int b = (int)(i / (unsigned)a.W);
+    if (par[b] != b) a.table[i] = fresh[i];
   }
+  if (near & 1)
+    for (int p = tid; p < a.n_pages; p += T) a.refs[p] = refs[p];
   for (int b = tid; b < a.B; b += T)
     if (par[b] != b) a.len[b] = rows[b];
   if (tid == 0) a.hdr[0] = copies;
@@ -221,19 +235,23 @@ pages_fork_kernel(const PgArgs a, const int32_t* __restrict__ parent) {
 // Pages in use behind the first `live` ids move into the free ids below, both in index order.
 __global__ void __launch_bounds__(kPgThreads)
 pages_compact_kernel(const PgArgs a, int32_t* live_out) {
-  __shared__ int sh[33];
+  __shared__ int2 sh[32], sh2[32];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  int from, to, c = 0, live, moves, holes;
+  int from, to;
+  int2 c = make_int2(0, 0), sums;
   pg_run(a, from, to);
-  for (int p = from; p < to; ++p) c += a.refs[p] != 0;
-  pg_scan(c, sh, &live);
-  int movers = 0, free_below = 0;
+  for (int p = from; p < to; ++p) c.x += a.refs[p] != 0;
+  pg_scan2(c, sh, &sums);
+  const int live = sums.x;
+  c = make_int2(0, 0);                    // pages to move, free pages below
   for (int p = from; p < to; ++p) {
     const bool used = a.refs[p] != 0;
-    movers += used && p >= live;
-    free_below += !used && p < live;
+    c.x += used && p >= live;
+    c.y += !used && p < live;
   }
-  int m = pg_scan(movers, sh, &moves), h = pg_scan(free_below, sh, &holes);   // moves == holes
+  const int2 at = pg_scan2(c, sh2, &sums);
+  int m = at.x, h = at.y;
+  const int moves = sums.x;               // == sums.y
   for (int p = from; p < to; ++p) {
     const bool used = a.refs[p] != 0;
     if (used && p >= live) a.src[m++] = p;
@@ -349,9 +367,22 @@ cudaError_t launch_pages_free(const dl_ctx* ctx, const dl_pages* p, const uint8_
 cudaError_t launch_pages_fork(const dl_ctx* ctx, const dl_pages* p, const int32_t* parent, int32_t n_pools,
                               void* const* pools, int64_t page_bytes, void* scratch, cudaStream_t s) {
   const PgArgs a = pg_args(ctx, p, scratch);
-  const size_t smem = (size_t)4 * p->B * 4;
-  pages_fork_kernel<<<1, kPgThreads, smem, s>>>(a, parent);
-  const cudaError_t e = cudaGetLastError();
+  // shared memory: five lists of B, and the counts and the new rows where 160 KB hold them
+  constexpr size_t kMost = 160 * 1024;
+  size_t smem = (size_t)5 * p->B * 4;
+  int near = 0;
+  if (smem + (size_t)p->n_pages * 4 <= kMost) { near |= 1; smem += (size_t)p->n_pages * 4; }
+  const size_t rows = (size_t)p->B * p->max_pages * 4;
+  if (smem + rows <= kMost) { near |= 2; smem += rows; }
+  cudaError_t e = cudaSuccess;
+  static int attr_set[64];
+  if (smem > 48 * 1024 && !attr_set[ctx->device & 63]) {
+    e = cudaFuncSetAttribute(pages_fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMost);
+    if (e != cudaSuccess) return e;
+    attr_set[ctx->device & 63] = 1;
+  }
+  pages_fork_kernel<<<1, kPgThreads, smem, s>>>(a, parent, near);
+  e = cudaGetLastError();
   return e != cudaSuccess ? e : pg_copy(ctx, a, n_pools, pools, page_bytes, false, s);
 }
 
