@@ -21,8 +21,9 @@
 //
 // Work: the units (32 rows: two tiles) of all (sequence, K/V head) pairs in one line, cut into equal ranges, one per warp:
 // every warp streams the same number of units whatever the lengths are, through its own ring (one bulk copy per
-// tile).  A pair that lies within one range is finished there; the parts of the others go to scratch and a second kernel,
-// launched to overlap, joins them in order (no atomics: the same call gives the same bits).  Page numbers are fetched
+// tile).  A pair that lies within one range is finished there; the parts of the others go to scratch and are joined by a second
+// kernel, in order and without atomics: the same call gives the same bits.  (Joined by the warp that delivers the last
+// part, few of them took as long, and many, 148 at 100k rows and 16 pairs, four times as long as everything else.)  Page numbers are fetched
 // 16 units ahead, a tile per lane; the lane that holds a tile's number copies it.
 #include <algorithm>
 
@@ -41,7 +42,7 @@ struct K4Args {
 
 constexpr int kK4Warps = 4;              // warps per CTA
 // CTAs per SM by blocks of 8 query heads: what their registers allow
-__host__ __device__ constexpr int k4_ctas(int nt) { return nt == 1 ? 4 : 2; }
+__host__ __device__ constexpr int k4_ctas(int nt) { return nt == 1 ? 3 : 2; }
 constexpr int kK4Lag = 8;                // log2 units by which the maximum in use may lag
 constexpr int kK4Unit = 32;              // rows of a unit: two tiles
 constexpr int kK4MinUnits = 1;           // fewest units worth a warp of its own
@@ -56,11 +57,16 @@ __device__ __forceinline__ int k4_rows(const PagesArg& p, int b) {
 // units of one K/V head of a sequence of n rows; an empty one counts 1, so that somebody writes its output
 __device__ __forceinline__ int k4_units(int n) { return max(1, (n + kK4Unit - 1) / kK4Unit); }
 
-// pre[b] = units in front of sequence b, pre[B] = all; called by the whole CTA
-__device__ __forceinline__ void k4_prefix(const PagesArg& p, int Hk, int* pre, int* sums) {
+// pre[b] = units in front of sequence b, pre[B] = all, rows[b] its rows; called by the whole CTA
+__device__ __forceinline__ void k4_prefix(const PagesArg& p, int Hk, int* pre, int* rows, int* sums) {
   const int T = blockDim.x, per = (p.B + T - 1) / T, from = min(p.B, (int)threadIdx.x * per), to = min(p.B, from + per);
   int c = 0;
-  for (int b = from; b < to; ++b) { c += k4_units(k4_rows(p, b)) * Hk; pre[b + 1] = c; }
+  for (int b = from; b < to; ++b) {
+    const int n = k4_rows(p, b);
+    rows[b] = n;
+    c += k4_units(n) * Hk;
+    pre[b + 1] = c;
+  }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int run = c;
 #pragma unroll
@@ -90,23 +96,21 @@ __device__ __forceinline__ int k4_range(int w, int total, int W) { return (int)(
 __device__ __forceinline__ int k4_owner(int u, int total, int W) { return (int)((((long long)u + 1) * W - 1) / total); }
 
 __device__ __forceinline__ void k4_mma(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
       "{%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 // the same into fresh accumulators
 __device__ __forceinline__ void k4_mma_first(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
       "{%10, %10, %10, %10};"
       : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t k4_transpose(uint32_t v) {
   uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
 __device__ __forceinline__ uint32_t k4_f16x2(float lo, float hi) {
@@ -151,6 +155,7 @@ attn_decode_kv4_kernel(const K4Args a) {
   char* ring = smem + (size_t)warp * NS * (2 * F::TILE);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (size_t)kK4Warps * NS * (2 * F::TILE)) + warp * NS;
   int* pre = reinterpret_cast<int*>(smem + (size_t)kK4Warps * NS * (2 * F::TILE + 8));
+  int* rows = pre + a.pg.B + 1;
   __shared__ int sh_sums[kK4Warps];
   __shared__ int sh_abort;
   volatile int* abort_flag = &sh_abort;
@@ -159,7 +164,7 @@ attn_decode_kv4_kernel(const K4Args a) {
     for (int s = 0; s < NS; ++s) mbar_init(smem_u32(&bars[s]), 1);
     fence_mbar_init();
   }
-  k4_prefix(a.pg, a.Hk, pre, sh_sums);                            // (its barriers also publish the above)
+  k4_prefix(a.pg, a.Hk, pre, rows, sh_sums);                      // (its barriers also publish the above)
   const int total = pre[a.pg.B], W = k4_width(total, a.grid_warps);
   const int gw = warp * gridDim.x + blockIdx.x;                   // few ranges go to as many SMs as there are
   if (gw >= W) return;
@@ -172,10 +177,10 @@ attn_decode_kv4_kernel(const K4Args a) {
     const int u = base + (lane >> 1);
     nx_b = -1;
     if (u < u1) {
-      const int b = k4_find(pre, a.pg.B, u), rem = u - pre[b], units = (pre[b + 1] - pre[b]) / a.Hk;
+      const int b = k4_find(pre, a.pg.B, u), rem = u - pre[b], units = k4_units(rows[b]);
       nx_hk = rem / units;
       nx_t = 2 * (rem - nx_hk * units) + (lane & 1);
-      if (nx_t * kKv4Rows < k4_rows(a.pg, b)) {
+      if (nx_t * kKv4Rows < rows[b]) {
         nx_b = b;
         nx_page = __ldg(a.pg.table + (size_t)b * a.pg.max_pages + (nx_t >> a.pg.tile_shift));
       }
@@ -191,7 +196,6 @@ attn_decode_kv4_kernel(const K4Args a) {
   };
   request(u0);
   int cur_idx = resolve(), p_at = 0;                              // p_at: place of the next unit in this block
-  request(u0 + 16);
   uint32_t here = 0;                                              // bits 2 s, 2 s + 1: which tiles of slot s were fetched
   int p_u = u0, p_slot = 0;
   auto produce = [&]() {
@@ -215,16 +219,19 @@ attn_decode_kv4_kernel(const K4Args a) {
     ++p_at;
     if (++p_slot == NS) p_slot = 0;
   };
-  for (int i = 0; i < NS && p_u < u1; ++i) produce();
+  // One unit each first, the rest of the ring behind the query's preparation: asked for all at once, the rings of the
+  // whole GPU take 5 us to fill and the first units arrive in the middle of that.
+  produce();
+  request(u0 + 16);
 
   // ---- where the consumer is
   int b = k4_find(pre, a.pg.B, u0);
-  int units = (pre[b + 1] - pre[b]) / a.Hk, hk = (u0 - pre[b]) / units, t = (u0 - pre[b]) - hk * units;
+  int units = k4_units(rows[b]), hk = (u0 - pre[b]) / units, t = (u0 - pre[b]) - hk * units;
   int slot = 0, phase = 0;
   bool gave_up = false;                                           // a wait ran out
   for (int u = u0; u < u1;) {
     // ================ one (sequence, K/V head), or the part of it that lies in this range
-    const int n = k4_rows(a.pg, b), seg0 = u - t, seg1 = seg0 + units, part_end = min(seg1, u1);
+    const int n = rows[b], seg0 = u - t, seg1 = seg0 + units, part_end = min(seg1, u1);
     uint32_t qb[NT][NG][4][2];                                    // B operand: head r of block nt, 16 dims per step
     float qs[NT][NG][2], fq[NT][2], se[NT][2];                    // of heads 2j, 2j + 1: sum of q * scale, score factor, own score
 #pragma unroll
@@ -274,6 +281,8 @@ attn_decode_kv4_kernel(const K4Args a) {
         for (int g = 0; g < NG; ++g) qs[nt][g][c] = __shfl_sync(0xffffffffu, sum[g], from) * a.scale_log2;
       }
     }
+    if (u == u0)
+      for (int i = 1; i < NS && p_u < u1; ++i) produce();
     // ---- Eq. 6's append, by the warp that has the pair's first unit: lanes 0 .. D/16-1 hold k_t, the next D/16 v_t
     if (t == 0 && a.keep != nullptr && a.keep[b] != 0) {
       constexpr int LR = D / 16;
@@ -310,160 +319,177 @@ attn_decode_kv4_kernel(const K4Args a) {
     int E = -200;                                                 // P s is held as P s 2^-E; none yet
     float down_e = 0.f, s_limit = 0.f;                            // 2^-E, 2^(E + 4)
 
-    // ================ units
-    for (; u < part_end; ++u, ++t) {
-      if (!mbar_try_wait(smem_u32(&bars[slot]), phase) && !mbar_wait(smem_u32(&bars[slot]), phase, abort_flag)) { gave_up = true; break; }
-      const uint32_t got = (here >> (2 * slot)) & 3u;
-      if (got != 0) {
-        const uint32_t unit = smem_u32(ring + (size_t)slot * (2 * F::TILE));
-        // ---- scores of the codes: lane's keys r and r + 8 of both tiles, its heads 2j, 2j + 1
-        float d[2][NT][NG][4];
+    // ================ units.  The products of the next unit's keys stand beside the current unit's exponentials and values, so
+    // that a warp has two independent chains to work on.
+    float d[2][NT][NG][4], vs[4][NG], vz[4][NG], s[NT][4][2];
+    auto key_products = [&](uint32_t unit) {                      // codes times query: lane's keys r and r + 8 of both tiles
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            const uint32_t ka = unit + h * F::TILE + kv4_k_off<D>(r, g) + 8 * j;
-            const uint2 w0 = k4_lds64(ka), w1 = k4_lds64(ka + 8 * F::RB);
+        for (int g = 0; g < NG; ++g) {
+          const uint32_t ka = unit + h * F::TILE + kv4_k_off<D>(r, g) + 8 * j;
+          const uint2 w0 = k4_lds64(ka), w1 = k4_lds64(ka + 8 * F::RB);
 #pragma unroll
-            for (int w = 0; w < 2; ++w) {
-              const uint32_t x = w ? w0.y : w0.x, y = w ? w1.y : w1.x, x8 = x >> 8, y8 = y >> 8;
+          for (int w = 0; w < 2; ++w) {
+            const uint32_t x = w ? w0.y : w0.x, y = w ? w1.y : w1.x, x8 = x >> 8, y8 = y >> 8;
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                if (w == 0) k4_mma_first(d[h][nt][g], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qb[nt][g][0][0], qb[nt][g][0][1]);
-                else k4_mma(d[h][nt][g], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qb[nt][g][2][0], qb[nt][g][2][1]);
-                k4_mma(d[h][nt][g], x8 & 0x000F000Fu, y8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x00F000F0u, qb[nt][g][2 * w + 1][0], qb[nt][g][2 * w + 1][1]);
-              }
+            for (int nt = 0; nt < NT; ++nt) {
+              if (w == 0) k4_mma_first(d[h][nt][g], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qb[nt][g][0][0], qb[nt][g][0][1]);
+              else k4_mma(d[h][nt][g], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qb[nt][g][2][0], qb[nt][g][2][1]);
+              k4_mma(d[h][nt][g], x8 & 0x000F000Fu, y8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x00F000F0u, qb[nt][g][2 * w + 1][0], qb[nt][g][2 * w + 1][1]);
             }
           }
-        // ---- words of the lane's four keys (index 2 h + i: key r + 8 i of tile h)
-        float vs[4][NG], vz[4][NG], s[NT][4][2];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          uint32_t kw[NG], vw[NG];
-          const uint32_t at = unit + (k >> 1) * F::TILE + (r + 8 * (k & 1)) * 4 * NG;
-          if (NG == 2) {
-            const uint2 x = k4_lds64(at + F::KM), y = k4_lds64(at + F::VM);
-            kw[0] = x.x; kw[NG - 1] = x.y; vw[0] = y.x; vw[NG - 1] = y.y;
-          } else {
-            kw[0] = k4_lds32(at + F::KM); vw[0] = k4_lds32(at + F::VM);
-          }
-#pragma unroll
-          for (int g = 0; g < NG; ++g) { vs[k][g] = bf16lo(vw[g]); vz[k][g] = bf16hi(vw[g]); }
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              float dot = 0.f, off = -m[nt][c];                   // s: score less the maximum in use
-#pragma unroll
-              for (int g = 0; g < NG; ++g) {
-                dot = fmaf(bf16lo(kw[g]), d[k >> 1][nt][g][2 * (k & 1) + c], dot);
-                off = fmaf(bf16hi(kw[g]), qs[nt][g][c], off);
-              }
-              s[nt][k][c] = fmaf(fq[nt][c], dot, off);
-            }
         }
-        const int nr = n - t * kK4Unit;
-        if (nr < kK4Unit || got != 3u) {
-          // the last unit of a sequence, or one with a page missing: whatever stands in rows that are not there counts nothing
+    };
+    // Scores less the maximum in use, from the products and the words of the lane's four keys (index 2 h + i: key r + 8 i of
+    // tile h); nr: rows of the unit that are there, got: tiles that are.
+    auto scores = [&](uint32_t unit, int nr, uint32_t got) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (16 * (k >> 1) + r + 8 * (k & 1) >= nr || !((got >> (k >> 1)) & 1u)) {
-#pragma unroll
-              for (int g = 0; g < NG; ++g) vs[k][g] = vz[k][g] = 0.f;
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt) s[nt][k][0] = s[nt][k][1] = -INFINITY;
-            }
+      for (int k = 0; k < 4; ++k) {
+        uint32_t kw[NG], vw[NG];
+        const uint32_t at = unit + (k >> 1) * F::TILE + (r + 8 * (k & 1)) * 4 * NG;
+        if (NG == 2) {
+          const uint2 x = k4_lds64(at + F::KM), y = k4_lds64(at + F::VM);
+          kw[0] = x.x; kw[NG - 1] = x.y; vw[0] = y.x; vw[NG - 1] = y.y;
+        } else {
+          kw[0] = k4_lds32(at + F::KM); vw[0] = k4_lds32(at + F::VM);
         }
-        bool raise = seen != (1u << (2 * NT)) - 1u;
-        float top = fmaxf(fmaxf(vs[0][0], vs[1][0]), fmaxf(vs[2][0], vs[3][0]));
-        if (NG == 2) top = fmaxf(top, fmaxf(fmaxf(vs[0][NG - 1], vs[1][NG - 1]), fmaxf(vs[2][NG - 1], vs[3][NG - 1])));
-        raise |= top > s_limit;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) { vs[k][g] = bf16lo(vw[g]); vz[k][g] = bf16hi(vw[g]); }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int c = 0; c < 2; ++c)
-            raise |= fmaxf(fmaxf(s[nt][0][c], s[nt][1][c]), fmaxf(s[nt][2][c], s[nt][3][c])) > (float)kK4Lag;
-        if (__any_sync(0xffffffffu, raise)) {
-          // rare: the maxima in use go up to what has been seen, and so does 2^E
+          for (int c = 0; c < 2; ++c) {
+            float dot = 0.f, off = -m[nt][c];
 #pragma unroll
-          for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-          float corr_e = 1.f;
-          if (top > s_limit) {
-            const int en = max(-100, min(120, (int)(__float_as_uint(top) >> 23) - 127));
-            if (en > E) {
-              corr_e = E == -200 ? 1.f : k4_pow2(max(-126, E - en));
-              E = en;
-              down_e = k4_pow2(-E);
-              s_limit = k4_pow2(min(127, E + 4));
+            for (int g = 0; g < NG; ++g) {
+              dot = fmaf(bf16lo(kw[g]), d[k >> 1][nt][g][2 * (k & 1) + c], dot);
+              off = fmaf(bf16hi(kw[g]), qs[nt][g][c], off);
+            }
+            s[nt][k][c] = fmaf(fq[nt][c], dot, off);
+          }
+      }
+      if (nr < kK4Unit || got != 3u) {
+        // the last unit of a sequence, or one with a page missing: whatever stands in rows that are not there counts nothing
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (16 * (k >> 1) + r + 8 * (k & 1) >= nr || !((got >> (k >> 1)) & 1u)) {
+#pragma unroll
+            for (int g = 0; g < NG; ++g) vs[k][g] = vz[k][g] = 0.f;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) s[nt][k][0] = s[nt][k][1] = -INFINITY;
+          }
+      }
+    };
+    auto arrived = [&](int sl, int ph) {                          // false: the wait ran out
+      return mbar_try_wait(smem_u32(&bars[sl]), ph) || mbar_wait(smem_u32(&bars[sl]), ph, abort_flag);
+    };
+    auto slot_addr = [&](int sl) { return smem_u32(ring + (size_t)sl * (2 * F::TILE)); };
+    gave_up = !arrived(slot, phase);
+    if (!gave_up) {
+      key_products(slot_addr(slot));
+      scores(slot_addr(slot), n - t * kK4Unit, (here >> (2 * slot)) & 3u);
+    }
+    for (; !gave_up; ++u, ++t) {
+      int next = slot + 1, next_phase = phase;
+      if (next == NS) { next = 0; next_phase ^= 1; }
+      const bool more = u + 1 < part_end;
+      if (more && !arrived(next, next_phase)) { gave_up = true; break; }
+      const uint32_t unit = slot_addr(slot), next_unit = slot_addr(more ? next : slot);
+      bool raise = seen != (1u << (2 * NT)) - 1u;
+      float top = fmaxf(fmaxf(vs[0][0], vs[1][0]), fmaxf(vs[2][0], vs[3][0]));
+      if (NG == 2) top = fmaxf(top, fmaxf(fmaxf(vs[0][NG - 1], vs[1][NG - 1]), fmaxf(vs[2][NG - 1], vs[3][NG - 1])));
+      raise |= top > s_limit;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+          raise |= fmaxf(fmaxf(s[nt][0][c], s[nt][1][c]), fmaxf(s[nt][2][c], s[nt][3][c])) > (float)kK4Lag;
+      if (__any_sync(0xffffffffu, raise)) {
+        // rare: the maxima in use go up to what has been seen, and so does 2^E
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        float corr_e = 1.f;
+        if (top > s_limit) {
+          const int en = max(-100, min(120, (int)(__float_as_uint(top) >> 23) - 127));
+          if (en > E) {
+            corr_e = E == -200 ? 1.f : k4_pow2(max(-126, E - en));
+            E = en;
+            down_e = k4_pow2(-E);
+            s_limit = k4_pow2(min(127, E + 4));
+          }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float mx = fmaxf(fmaxf(s[nt][0][c], s[nt][1][c]), fmaxf(s[nt][2][c], s[nt][3][c]));
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            // up by mx (the first time: to it, wherever it is); a head without a finite score yet stays
+            const bool known = (seen >> (2 * nt + c)) & 1u, finite = mx > -INFINITY && mx < INFINITY;
+            const float by = finite && (!known || mx > 0.f) ? mx : 0.f;
+            const float corr = known ? k4_exp2(-by) : 1.f;
+            if (finite) seen |= 1u << (2 * nt + c);
+            m[nt][c] += by;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s[nt][k][c] -= by;
+            l_run[nt][c] *= corr;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+              zacc[nt][g][c] *= corr;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) { acc[nt][g][i][c] *= corr * corr_e; acc[nt][g][i][2 + c] *= corr * corr_e; }
             }
           }
+      }
+      // ---- P, and O^T += V^T (P s)^T tile by tile: lane's row pairs j and j + 4, its dims 64 g + 8 r .. + 7
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+      for (int h = 0; h < 2; ++h) {
+        uint32_t pb[NT][NG][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float p[2][2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-              float mx = fmaxf(fmaxf(s[nt][0][c], s[nt][1][c]), fmaxf(s[nt][2][c], s[nt][3][c]));
+              p[i][c] = k4_exp2(s[nt][2 * h + i][c]);
+              l_run[nt][c] += p[i][c];
+            }
 #pragma unroll
-              for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-              // up by mx (the first time: to it, wherever it is); a head without a finite score yet stays
-              const bool known = (seen >> (2 * nt + c)) & 1u, finite = mx > -INFINITY && mx < INFINITY;
-              const float by = finite && (!known || mx > 0.f) ? mx : 0.f;
-              const float corr = known ? k4_exp2(-by) : 1.f;
-              if (finite) seen |= 1u << (2 * nt + c);
-              m[nt][c] += by;
+          for (int g = 0; g < NG; ++g)
 #pragma unroll
-              for (int k = 0; k < 4; ++k) s[nt][k][c] -= by;
-              l_run[nt][c] *= corr;
+            for (int i = 0; i < 2; ++i) {
+              const float f = vs[2 * h + i][g] * down_e;
 #pragma unroll
-              for (int g = 0; g < NG; ++g) {
-                zacc[nt][g][c] *= corr;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) { acc[nt][g][i][c] *= corr * corr_e; acc[nt][g][i][2 + c] *= corr * corr_e; }
-              }
+              for (int c = 0; c < 2; ++c) zacc[nt][g][c] = fmaf(p[i][c], vz[2 * h + i][g], zacc[nt][g][c]);
+              pb[nt][g][i] = k4_transpose(k4_f16x2(p[i][0] * f, p[i][1] * f));
             }
         }
-        // ---- P, and O^T += V^T (P s)^T tile by tile: lane's row pairs j and j + 4, its dims 64 g + 8 r .. + 7
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t pb[NT][NG][2];
+        for (int g = 0; g < NG; ++g) {
+          const uint32_t va = unit + h * F::TILE;
+          const uint2 wx = k4_lds64(va + kv4_v_off<D>(j, 64 * g + 8 * r)), wy = k4_lds64(va + kv4_v_off<D>(j + 4, 64 * g + 8 * r));
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            float p[2][2];
+          for (int w = 0; w < 2; ++w) {
+            const uint32_t x = w ? wx.y : wx.x, y = w ? wy.y : wy.x, x8 = x >> 8, y8 = y >> 8;
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-              for (int c = 0; c < 2; ++c) {
-                p[i][c] = k4_exp2(s[nt][2 * h + i][c]);
-                l_run[nt][c] += p[i][c];
-              }
-#pragma unroll
-            for (int g = 0; g < NG; ++g)
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const float f = vs[2 * h + i][g] * down_e;
-#pragma unroll
-                for (int c = 0; c < 2; ++c) zacc[nt][g][c] = fmaf(p[i][c], vz[2 * h + i][g], zacc[nt][g][c]);
-                pb[nt][g][i] = k4_transpose(k4_f16x2(p[i][0] * f, p[i][1] * f));
-              }
-          }
-#pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            const uint32_t va = unit + h * F::TILE;
-            const uint2 wx = k4_lds64(va + kv4_v_off<D>(j, 64 * g + 8 * r)), wy = k4_lds64(va + kv4_v_off<D>(j + 4, 64 * g + 8 * r));
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-              const uint32_t x = w ? wx.y : wx.x, y = w ? wy.y : wy.x, x8 = x >> 8, y8 = y >> 8;
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                k4_mma(acc[nt][g][2 * w], x & 0x000F000Fu, x & 0x00F000F0u, y & 0x000F000Fu, y & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
-                k4_mma(acc[nt][g][2 * w + 1], x8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x000F000Fu, y8 & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
-              }
+            for (int nt = 0; nt < NT; ++nt) {
+              k4_mma(acc[nt][g][2 * w], x & 0x000F000Fu, x & 0x00F000F0u, y & 0x000F000Fu, y & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
+              k4_mma(acc[nt][g][2 * w + 1], x8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x000F000Fu, y8 & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
             }
           }
         }
       }
+      // (without a next unit these are products nobody reads)
+      key_products(next_unit);
       __syncwarp();
       if (p_u < u1) produce();
-      if (++slot == NS) { slot = 0; phase ^= 1; }
+      slot = next;
+      phase = next_phase;
+      if (!more) { ++u; ++t; break; }
+      scores(next_unit, n - (t + 1) * kK4Unit, (here >> (2 * next)) & 3u);
     }
     if (__any_sync(0xffffffffu, gave_up)) break;
     if (u == u1) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the joining kernel may come up
@@ -528,7 +554,7 @@ attn_decode_kv4_kernel(const K4Args a) {
       t = 0;
       if (++hk == a.Hk) {
         hk = 0;
-        if (++b < a.pg.B) units = (pre[b + 1] - pre[b]) / a.Hk;
+        if (++b < a.pg.B) units = k4_units(rows[b]);
       }
     }
   }
@@ -549,13 +575,14 @@ attn_merge_kv4_kernel(const K4Args a) {
   const int NW = blockDim.x >> 5;
   extern __shared__ __align__(128) char smem[];
   int* pre = reinterpret_cast<int*>(smem);
+  int* rows = pre + a.pg.B + 1;
   __shared__ int sh_sums[kK4MergeWarps];
   __shared__ float sh_o[kK4MergeWarps][D], sh_l[kK4MergeWarps], sh_m[kK4MergeWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int b = blockIdx.x / a.H, head = blockIdx.x - b * a.H, hk = head / a.G, hg = head - hk * a.G;
-  k4_prefix(a.pg, a.Hk, pre, sh_sums);
+  k4_prefix(a.pg, a.Hk, pre, rows, sh_sums);
   const int total = pre[a.pg.B], W = k4_width(total, a.grid_warps);
-  const int units = (pre[b + 1] - pre[b]) / a.Hk, s0 = pre[b] + hk * units;
+  const int units = k4_units(rows[b]), s0 = pre[b] + hk * units;
   const int first = k4_owner(s0, total, W), last = k4_owner(s0 + units - 1, total, W);
   if (first == last) {
     // this grid must not retire before its predecessor has: what follows in the stream relies on both
@@ -641,7 +668,7 @@ attn_merge_kv4_kernel(const K4Args a) {
 template <int D, int NT>
 static cudaError_t k4_launch(const dl_ctx* ctx, K4Args& a, cudaStream_t s) {
   constexpr int kCtas = k4_ctas(NT);
-  const size_t pre_bytes = (size_t)(a.pg.B + 1) * sizeof(int);
+  const size_t pre_bytes = (size_t)(2 * a.pg.B + 1) * sizeof(int);
   const int per_cta = (ctx->smem_optin + 1024) / kCtas - 1024;
   int ns = (int)((per_cta - (int)pre_bytes - 256) / (kK4Warps * (2 * Kv4<D>::TILE + 8)));
   ns = std::min(ns, 8);
