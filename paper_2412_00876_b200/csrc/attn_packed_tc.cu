@@ -41,7 +41,7 @@ constexpr int kPkRegsSmall = 40, kPkRegsSoftmax = 232;
 static_assert(128 * kPkRegsSmall + 256 * kPkRegsSoftmax <= 384 * 168, "more registers than the launch has");
 constexpr float kPkFar = 1048576.f, kPkFarLog2 = 14.f; // a half row's sum, and a score's lead, above which the maximum is looked for again
 constexpr int kPkPatience = 4000;                      // polls a softmax warp waits for its turn
-constexpr int kPkTurnTiles = 2;                        // items of at least so many key tiles take turns at the softmax
+constexpr int kPkTurnTiles = 4;                        // items of at least so many key tiles take turns at the softmax
 constexpr int kPkNext = 16;                            // pair of columns (of 64) behind which the other lane's pass may start
 constexpr int kPkAhead = 4, kPkBehind = 6, kPkRing = 12;   // pairs between the stages of the exponentials
 static_assert(kPkRing > kPkAhead + kPkBehind, "a pair's place is taken again before it is done");
@@ -63,6 +63,7 @@ struct PkArgs {
   int32_t p_shift;                                     // P = 1 << p_shift heads per tile
   int32_t n_hs;                                        // H / P
   int32_t pairs;                                       // pairs of tiles of a sequence of max_rows rows
+  int32_t by_column;                                   // columns that a CTA takes one at a time, see PkWalker
   float scale_log2;
 };
 
@@ -82,41 +83,58 @@ __device__ __forceinline__ PkLane pk_lane(const PkArgs& a, const PkItem& I, int 
 // keys of tile j that a lane's MMAs cover
 __device__ __forceinline__ int pk_cols(const PkLane& L, int j) { return min(kPkBN, (L.q_hi - j * kPkBN + 15) & ~15); }
 
-// Items in the order every role walks them: the last pairs of all sequences and heads first.
+// Items in the order every role walks them.  Where sequences are of much the same length and there are several (sequence,
+// heads) columns for every CTA (`by_column`, a multiple of the grid: how many of them go this way), a CTA takes a column
+// at a time, all its pairs, the last one first: K and V of the column stay in L2.  The rest goes pair by pair over all
+// columns, the last pairs first, which spreads a long sequence over all CTAs.  (All of a batch of 32 prompts of 700 tokens
+// with 32 heads pair by pair: 930 MB read from DRAM instead of 560.)
 struct PkWalker {
   const PkArgs& a;
-  int p, b, hs, db, dh, s0, s1;
+  int p, col, s0, s1, n_col, grid;                     // next: pair, column, its start and end (in flight)
   __device__ __forceinline__ explicit PkWalker(const PkArgs& a_) : a(a_) {
-    const int per = a.B * a.n_hs;
-    p = (int)blockIdx.x / per;
-    const int r = (int)blockIdx.x - p * per;
-    b = r / a.n_hs;
-    hs = r - b * a.n_hs;
-    db = (int)gridDim.x / a.n_hs;
-    dh = (int)gridDim.x - db * a.n_hs;
-    s0 = s1 = 0;
+    n_col = a.B * a.n_hs;
+    grid = (int)gridDim.x;
+    p = 0;
+    col = (int)blockIdx.x;
+    if (a.by_column == 0) wrap();
     fetch();
   }
+  __device__ __forceinline__ void wrap() {
+    while (col >= n_col && p < a.pairs) { col -= n_col - a.by_column; ++p; }
+  }
   __device__ __forceinline__ void fetch() {
-    if (p < a.pairs) { s0 = ld_early(a.starts + b); s1 = ld_early(a.starts + b + 1); }
+    s0 = s1 = 0;
+    if (p < a.pairs && col < n_col) {
+      const int b = col / a.n_hs;
+      s0 = ld_early(a.starts + b);
+      s1 = ld_early(a.starts + b + 1);
+    }
   }
   __device__ __forceinline__ bool next(PkItem& I) {
     for (;;) {
       if (p >= a.pairs) return false;
-      const int cp = p, cb = b, ch = hs, c0 = min(max(s0, 0), a.total), c1 = min(max(s1, c0), a.total);
-      hs += dh;
-      b += db;
-      if (hs >= a.n_hs) { hs -= a.n_hs; ++b; }
-      while (b >= a.B) { b -= a.B; ++p; }
-      fetch();
-      I.b = cb;
-      I.h0 = ch << a.p_shift;
+      const int cp = p, cc = col, c0 = min(max(s0, 0), a.total), c1 = min(max(s1, c0), a.total);
+      I.b = cc / a.n_hs;
+      I.h0 = (cc - I.b * a.n_hs) << a.p_shift;
       I.row0 = c0;
       I.n = min(c1 - c0, a.max_rows);
       I.q_hi = I.n - cp * (2 * kPkBM >> a.p_shift);
-      if (I.q_hi <= 0) continue;
       I.n_kv = (I.q_hi + kPkBN - 1) / kPkBN;
-      return true;
+      if (cc < a.by_column) {
+        if (I.q_hi > (2 * kPkBM >> a.p_shift)) {
+          ++p;                                         // the column's next pair: start and end stay
+        } else {
+          p = 0;
+          col += grid;
+          if (col >= a.by_column) wrap();
+          fetch();
+        }
+      } else {
+        col += grid;
+        wrap();
+        fetch();
+      }
+      if (I.q_hi > 0) return true;
     }
   }
 };
@@ -292,6 +310,7 @@ attn_packed_kernel(const __grid_constant__ PkMaps maps, const PkArgs a) {
         for (int hf = 0; hf < D / 64; ++hf)
           tma_load_3d(smem_u32(smem + S::KV + slot * S::TILE + hf * S::HALF), m, 64 * hf, I.h0 / a.G, I.row0 + j * kPkBN, kv_full(slot));
       };
+      // (Bringing the next item's first tiles into L2 ahead of time measured 1-10 % slower.)
       while (!*abort_flag && W.next(I)) {
         load_q(0);
         load_kv(mk, 0);
@@ -558,8 +577,11 @@ static cudaError_t pk_launch(dl_ctx* ctx, const void* q, const void* k, const vo
       !encode_bf16_map(ctx->tmap_encode, reinterpret_cast<CUtensorMap*>(maps.v), v, 3, dk, sk, bk) ||
       !encode_bf16_map(ctx->tmap_encode, reinterpret_cast<CUtensorMap*>(maps.o), a.out, 4, dout, so, bo, CU_TENSOR_MAP_SWIZZLE_64B))
     return cudaErrorInvalidValue;
-  const long long items = (long long)a.B * a.n_hs * a.pairs;
-  if (items >= (1LL << 31)) return cudaErrorInvalidValue;
+  const long long columns = (long long)a.B * a.n_hs, items = columns * a.pairs;
+  if (items >= (1LL << 31) - ctx->sm_count) return cudaErrorInvalidValue;
+  a.by_column = 0;
+  if (2LL * a.B * a.max_rows <= 3LL * a.total && columns >= 4LL * ctx->sm_count)
+    a.by_column = (int)(columns / ctx->sm_count) * ctx->sm_count;
   static int attr_set[64];
   if (!attr_set[ctx->device & 63]) {
     const cudaError_t e = cudaFuncSetAttribute(attn_packed_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Pk<D>::SMEM);
