@@ -71,6 +71,22 @@ __device__ __forceinline__ uint64_t kv4_fma2(uint64_t x, uint64_t y, uint64_t z)
   return r;
 }
 
+// range / 15, correctly rounded (range normal): the product with the rounded reciprocal, corrected once with the exact
+// remainder (Markstein's scheme).
+__device__ __forceinline__ float kv4_div15(float range) {
+  constexpr float c = 1.f / 15.f;
+  const float q = __fmul_rn(range, c);
+  return __fmaf_rn(__fmaf_rn(-15.f, q, range), c, q);
+}
+// 1 / s, correctly rounded, for a normal s of eight significant bits (bf16) up to 2^125: one Newton step from the
+// approximation leaves an error below 2^-44 of the result, and 1 / s, a power of two over an odd number below 256, is never
+// nearer than 2^-33 to the middle between two floats.
+__device__ __forceinline__ float kv4_recip(float s) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(s));
+  return __fmaf_rn(y, __fmaf_rn(-s, y, 1.f), y);
+}
+
 // Sixteen consecutive values per lane (`u`: bf16 pairs), four lanes per group (lanes 4i .. 4i + 3): this lane's codes, and
 // the group's word.  All 32 lanes take part.  The extremes are found on bf16 pairs; from the first reduction on a lane
 // holds (min, -max) in one register.
@@ -84,11 +100,11 @@ __device__ __forceinline__ uint2 kv4_quantise16(const uint32_t (&u)[8], uint32_t
   ext = kv4_min2(ext, __shfl_xor_sync(0xffffffffu, ext, 2));
   const float lo = bf16lo(ext), range = __fsub_rn(-bf16hi(ext), lo);
   const bool odd = !(range <= 3.402823466e38f);                             // a NaN, an infinity, a range beyond fp32
-  const __nv_bfloat16 sb = __float2bfloat16_rn(__fdiv_rn(range, 15.f));
+  const __nv_bfloat16 sb = __float2bfloat16_rn(kv4_div15(range));
   const float s = __bfloat162float(sb);
   // s >= 2^-126 has eight significant bits, so (x - z) / s is at most 15 (1 + 2^-8): no code above 15
   const bool flat = odd || !(s >= 1.17549435e-38f);
-  const float inv = flat ? 0.f : __frcp_rn(s);
+  const float inv = flat ? 0.f : kv4_recip(s);
   uint32_t c[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {

@@ -5,7 +5,7 @@
 //            row and (optionally) advance the length: one CTA per sequence;
 //   append : a CTA takes up to 32 packed source rows, ranks the kept ones and quantises them, 16 values per lane, 4
 //            lanes per group; dropped rows are not read.  A thread stays at one place of the row (head, tensor, 16 dims)
-//            and walks the kept rows, two in flight; wide rows are shared by several CTAs (grid y);
+//            and walks the kept rows (two or four of them at a time measured 2-8 % slower); wide rows are shared by several CTAs (grid y);
 //   read   : the same walk the other way, codes to bf16.
 // Both are bound by HBM: a kept row costs 2 D bytes in and 9 D / 16 out per head and tensor.
 #include <algorithm>
@@ -17,7 +17,6 @@ namespace dl {
 constexpr int kK4Threads = 256;
 constexpr int kK4Rows = 32;              // most packed rows per CTA
 constexpr int kK4Ctas = 16;              // CTAs per SM worth having
-constexpr int kK4Unroll = 2;             // rows a thread has in flight
 
 __device__ __forceinline__ int k4_block_sum(int v, int* sh) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -150,31 +149,18 @@ kv4_append_kernel(const PagesArg pg, uint8_t* __restrict__ pool, int32_t Hk, con
   const int l = on ? (is_v ? at.rem - half : at.rem) : 0, hk = l / LR, lr = l - hk * LR;
   const __nv_bfloat16* src = (is_v ? v : k) + l * 16;
   const long long head_tiles = (long long)hk << pg.tile_shift;
-  for (int base = 0; base < n; base += at.step * kK4Unroll) {     // the same trips for all lanes: they shuffle together
-    uint32_t raw[kK4Unroll][8];
-#pragma unroll
-    for (int c = 0; c < kK4Unroll; ++c) {
-      const int row = base + c * at.step + at.first;
-      uint4 x = make_uint4(0u, 0u, 0u, 0u), y = x;
-      if (on && row < n) {
-        const uint4* from = reinterpret_cast<const uint4*>(src + row_src[row]);
-        x = __ldg(from);
-        y = __ldg(from + 1);
-      }
-      raw[c][0] = x.x; raw[c][1] = x.y; raw[c][2] = x.z; raw[c][3] = x.w;
-      raw[c][4] = y.x; raw[c][5] = y.y; raw[c][6] = y.z; raw[c][7] = y.w;
-    }
-#pragma unroll
-    for (int c = 0; c < kK4Unroll; ++c) {
-      if (base + c * at.step >= n) break;
-      const int row = base + c * at.step + at.first;
-      uint32_t word;
-      const uint2 code = kv4_quantise16(raw[c], word);
-      if (on && row < n) {
-        const long long tile = row_tile[row] + head_tiles;
-        if (DL_IN_BOUNDS(st, KID_KV4_APPEND, tile, (long long)pg.n_pages * Hk << pg.tile_shift))
-          kv4_store16<D>(pool + tile * Kv4<D>::TILE, row_in[row], lr, is_v, code, word);
-      }
+  for (int base = 0; base < n; base += at.step) {                 // the same trips for all lanes: they shuffle together
+    // (rows behind the last kept one, and places behind the row's last, take another's values and store nothing)
+    const int row = base + at.first;
+    const uint4* from = reinterpret_cast<const uint4*>(src + row_src[min(row, n - 1)]);
+    const uint4 x = __ldg(from), y = __ldg(from + 1);
+    const uint32_t raw[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+    uint32_t word;
+    const uint2 code = kv4_quantise16(raw, word);
+    if (on && row < n) {
+      const long long tile = row_tile[row] + head_tiles;
+      if (DL_IN_BOUNDS(st, KID_KV4_APPEND, tile, (long long)pg.n_pages * Hk << pg.tile_shift))
+        kv4_store16<D>(pool + tile * Kv4<D>::TILE, row_in[row], lr, is_v, code, word);
     }
   }
 }
@@ -219,41 +205,32 @@ kv4_read_kernel(const PagesArg pg, const uint8_t* __restrict__ pool, int32_t Hk,
   const long long head_tiles = (long long)hk << pg.tile_shift;
   uint4* out = reinterpret_cast<uint4*>(is_v ? v_out : k_out);
   const uint64_t magic = kv4_pack2(-8388608.f, -8388608.f);
-  for (int base = at.first; base < n; base += at.step * kK4Unroll) {
-    uint2 code[kK4Unroll];
-    uint32_t word[kK4Unroll];
-#pragma unroll
-    for (int c = 0; c < kK4Unroll; ++c) {
-      const int row = base + c * at.step;
-      code[c] = make_uint2(0u, 0u);
-      word[c] = 0u;
-      if (row < n && row_tile[row] >= 0) {
-        const uint8_t* tile = pool + (row_tile[row] + head_tiles) * Kv4<D>::TILE;
-        code[c] = kv4_load16<D>(tile, row_in[row], lr, is_v);
-        word[c] = __ldg(reinterpret_cast<const uint32_t*>(tile + (is_v ? Kv4<D>::VM : Kv4<D>::KM) + (row_in[row] * Kv4<D>::NG + g) * 4));
-      }
+  for (int row = at.first; row < n; row += at.step) {
+    if (row_tile[row] == -2) continue;
+    uint2 code = make_uint2(0u, 0u);
+    uint32_t word = 0u;
+    if (row_tile[row] >= 0) {
+      const uint8_t* tile = pool + (row_tile[row] + head_tiles) * Kv4<D>::TILE;
+      code = kv4_load16<D>(tile, row_in[row], lr, is_v);
+      word = __ldg(reinterpret_cast<const uint32_t*>(tile + (is_v ? Kv4<D>::VM : Kv4<D>::KM) + (row_in[row] * Kv4<D>::NG + g) * 4));
     }
+    const float s = bf16lo(word), z = bf16hi(word);
+    const uint64_t s2 = kv4_pack2(s, s), z2 = kv4_pack2(z, z);
+    uint32_t p[8];
 #pragma unroll
-    for (int c = 0; c < kK4Unroll; ++c) {
-      const int row = base + c * at.step;
-      if (row >= n || row_tile[row] == -2) continue;
-      const float s = bf16lo(word[c]), z = bf16hi(word[c]);
-      const uint64_t s2 = kv4_pack2(s, s), z2 = kv4_pack2(z, z);
-      uint32_t p[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        // a code in the low bits of 2^23, less 2^23
-        const uint32_t w = (e < 4 ? code[c].x : code[c].y) >> (8 * (e & 3));
-        const uint64_t v = kv4_add2(kv4_pack2(__uint_as_float((w & 15u) | 0x4B000000u), __uint_as_float(((w >> 4) & 15u) | 0x4B000000u)), magic);
-        const uint64_t y = kv4_fma2(v, s2, z2);
-        const __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float((uint32_t)y), __uint_as_float((uint32_t)(y >> 32)));
-        p[e] = *reinterpret_cast<const uint32_t*>(&b);
-      }
-      const long long to = 2 * ((long long)(t0 + row) * half + l);
-      if (DL_IN_BOUNDS(st, KID_KV4_READ, to + 1, 2LL * total * half)) {
-        out[to] = make_uint4(p[0], p[1], p[2], p[3]);
-        out[to + 1] = make_uint4(p[4], p[5], p[6], p[7]);
-      }
+    for (int e = 0; e < 8; ++e) {
+      // a code in the low byte of 2^23, less 2^23
+      const uint32_t even = (e < 4 ? code.x : code.y) & 0x0F0F0F0Fu, odd = ((e < 4 ? code.x : code.y) >> 4) & 0x0F0F0F0Fu;
+      const uint64_t v = kv4_add2(kv4_pack2(__uint_as_float(__byte_perm(even, 0x4B000000u, 0x7540 | (e & 3))),
+                                            __uint_as_float(__byte_perm(odd, 0x4B000000u, 0x7540 | (e & 3)))), magic);
+      const uint64_t y = kv4_fma2(v, s2, z2);
+      const __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float((uint32_t)y), __uint_as_float((uint32_t)(y >> 32)));
+      p[e] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    const long long to = 2 * ((long long)(t0 + row) * half + l);
+    if (DL_IN_BOUNDS(st, KID_KV4_READ, to + 1, 2LL * total * half)) {
+      out[to] = make_uint4(p[0], p[1], p[2], p[3]);
+      out[to + 1] = make_uint4(p[4], p[5], p[6], p[7]);
     }
   }
 }
