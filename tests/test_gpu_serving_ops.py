@@ -553,3 +553,154 @@ def test_a_serving_run_together_also_captured():
     assert [pg.cache_len[b].item() for b in alive] == [len(rows[b][0]) for b in alive]
     assert ctx.device_status()[0] == 0
     ctx.close()
+
+
+# ---- paths that ordinary inputs do not take -------------------------------------------------------------------------
+@pytest.mark.parametrize("D,Hk", [(128, 2), (64, 1)])
+@pytest.mark.parametrize("where", [10, 70, 130, 200, 300, 700])
+@pytest.mark.parametrize("lead", [12.0, 60.0, 3000.0])
+def test_packed_scores_that_pass_the_maximum_by_far(D, Hk, where, lead):
+    """From key `where` on the scores stand `lead` (base e) above all earlier ones, then fall back: whatever an item's first
+    tile took for its maximum is wrong by far in the first half, the second half or an edge tile of a later one."""
+    H, lens = 2, [900]
+    dl, ctx = context(H, D)
+    rng = np.random.default_rng(where + D)
+    q, k, v = bf(rng, 900, H, D, scale=0.1), bf(rng, 900, Hk, D, scale=0.1), bf(rng, 900, Hk, D)
+    q[:, :, 0] = 1.0
+    k[:, :, 0] = 0.0
+    k[where:where + 90:9, :, 0] = wl.round_to_storage(np.float32([lead]), "bf16")[0]
+    k[where + 45, :, 0] = wl.round_to_storage(np.float32([lead * 1.25]), "bf16")[0]
+    out = torch.zeros((900, H, D), dtype=torch.bfloat16, device=DEV)
+    ctx.attn_prefill_packed(up(q), up(k), up(v), i32(starts_of(lens)), 900, 1.0, out)
+    rows = np.unique(np.concatenate([np.arange(max(0, where - 2), min(900, where + 60)), np.arange(0, 900, 61), [899]]))
+    ref, ref_abs = np.zeros((len(rows), H, D)), np.zeros((len(rows), H, D))
+    for n, r in enumerate(rows):
+        args = [np.asarray(t, np.float64) for t in (q[r], k[r], v[r], k[:r], v[:r])]
+        ref[n] = pk.attention_decode(*args, 1.0)
+        args[2], args[4] = np.abs(args[2]), np.abs(args[4])
+        ref_abs[n] = pk.attention_decode(*args, 1.0)
+    close(wl.from_torch(out)[rows], ref, ref_abs, "leading scores")
+    assert ctx.device_status()[0] == 0
+    ctx.close()
+
+
+@pytest.mark.parametrize("B,H,Hk,D,lo,hi", [(40, 16, 16, 64, 20, 30), (74, 8, 8, 128, 250, 300), (40, 32, 8, 64, 60, 70)])
+def test_packed_batches_of_like_lengths(B, H, Hk, D, lo, hi):
+    """Enough (sequence, head) columns of like lengths that CTAs take them one at a time; sampled sequences."""
+    dl, ctx = context(H, D, B=B)
+    rng = np.random.default_rng(B + D)
+    lens = rng.integers(lo, hi + 1, B).tolist()
+    st, total = starts_of(lens), sum(lens)
+    q, k, v = bf(rng, total, H, D), bf(rng, total, Hk, D), bf(rng, total, Hk, D)
+    out = torch.full((total, H, D), 9.0, dtype=torch.bfloat16, device=DEV)
+    ctx.attn_prefill_packed(up(q), up(k), up(v), i32(st), max(lens), D ** -0.5, out)
+    got = wl.from_torch(out)
+    assert not np.any(got == 9.0)
+    for b in sorted({0, 1, B // 2, B - 2, B - 1}):
+        a, e = st[b], st[b + 1]
+        for h in (0, H - 1):
+            sl = lambda t, i: t[a:e, i:i + 1]
+            args = sl(q, h), sl(k, h // (H // Hk)), sl(v, h // (H // Hk))
+            ref = pk.attention_packed(*args, [0, e - a], D ** -0.5)
+            close(got[a:e, h:h + 1], ref, pk.attention_packed(args[0], args[1], np.abs(args[2]), [0, e - a], D ** -0.5), f"sequence {b}, head {h}")
+    assert ctx.device_status()[0] == 0
+    ctx.close()
+
+
+def test_offsets_beyond_32_bits():
+    """A pool of more than 4 GB: its last pages hold, read, attend, fork and compact as its first do."""
+    H = Hk = 8
+    D, page = 128, 128
+    dl, ctx = context(H, D)
+    rng = np.random.default_rng(21)
+    page_bytes = Hk * page * 144
+    n_pages = (1 << 32) // page_bytes + 600
+    lens = [300, 260]
+    pg = dl.Pages(2, n_pages, 4, page, DEV)
+    pool = torch.empty(n_pages, page_bytes, dtype=torch.uint8, device=DEV)
+    pg.table[0, :3] = i32([n_pages - 1, 5, n_pages - 400])
+    pg.table[1, :3] = i32([n_pages - 7, n_pages - 2, 0])
+    for p in pg.table[:, :3].flatten().tolist():
+        pg.refs[p] = 1
+    st = starts_of(lens)
+    kv = bf(rng, sum(lens), 2 * Hk, D)
+    d = up(kv)
+    ctx.kv4_append(pg, pool, d[:, :Hk], d[:, Hk:], i32(st))
+    q, kt, vt = bf(rng, 2, H, D), bf(rng, 2, Hk, D), bf(rng, 2, Hk, D)
+    h, lifted = pk.held(kv), lift(kv)
+
+    def check():
+        gk, gv = read(ctx, pg, pool, Hk, D, [0, 0], lens)
+        same_values(gk, h[:, :Hk], "K")
+        same_values(gv, h[:, Hk:], "V")
+        out = torch.zeros(2, H, D, dtype=torch.bfloat16, device=DEV)
+        ctx.kv4_attn_decode(pg, pool, up(q), up(kt), up(vt), None, D ** -0.5, out)
+        for b in range(2):
+            r = slice(st[b], st[b + 1])
+            args = q[b], kt[b], vt[b], h[r, :Hk], h[r, Hk:]
+            close(wl.from_torch(out)[b], pk.attention_decode(*args, D ** -0.5),
+                  pk.attention_decode(q[b], kt[b], np.abs(vt[b]), h[r, :Hk], np.abs(h[r, Hk:]), D ** -0.5), f"sequence {b}",
+                  pk.attention_decode(q[b], kt[b], 0 * vt[b], h[r, :Hk], lifted[r, Hk:], D ** -0.5))
+
+    check()
+    live = torch.zeros(1, dtype=torch.int32, device=DEV)
+    ctx.pages_compact(pg, [pool], live)
+    assert live.item() == 6 and int(pg.table.max()) == 5
+    check()
+    ctx.pages_fork(pg, i32([0, 0]), [pool])
+    pg.cache_len.copy_(i32([300, 300]))
+    gk, _ = read(ctx, pg, pool, Hk, D, [0, 0], [300, 300])
+    same_values(gk[300:], h[:300, :Hk], "forked K")
+    assert ctx.device_status()[0] == 0
+    ctx.close()
+
+
+def test_another_stream_and_graphs_that_share_a_context():
+    """Calls given a stream run on it; two graphs captured with one context, replayed in turn, give what the calls give."""
+    H, Hk, D, page = 8, 2, 64, 16
+    dl, ctx = context(H, D)
+    rng = np.random.default_rng(31)
+    lens = [700, 90]
+    st = starts_of(lens)
+    kv = bf(rng, sum(lens), 2 * Hk, D)
+    pg = books(dl, 2, 60, 45, page, lens, rng)
+    pool = ctx.kv4_pool(pg, Hk)
+    d, q, kt, vt = up(kv), up(bf(rng, 2, H, D)), up(bf(rng, 2, Hk, D)), up(bf(rng, 2, Hk, D))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    out = torch.zeros(2, H, D, dtype=torch.bfloat16, device=DEV)
+    ctx.kv4_append(pg, pool, d[:, :Hk], d[:, Hk:], i32(st), stream=s)
+    ctx.kv4_attn_decode(pg, pool, q, kt, vt, None, 0.1, out, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    ref = out.clone()
+    q2 = up(bf(rng, 2, H, D))
+    out2 = torch.zeros_like(out)
+    ctx.kv4_attn_decode(pg, pool, q2, kt, vt, None, 0.1, out2)
+    ref2 = out2.clone()
+    graphs = []
+    for a, o in ((q, out), (q2, out2)):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            ctx.kv4_attn_decode(pg, pool, a, kt, vt, None, 0.1, o)
+        graphs.append(g)
+    for _ in range(3):
+        out.zero_()
+        out2.zero_()
+        for g in graphs:
+            g.replay()
+        assert torch.equal(out, ref) and torch.equal(out2, ref2)
+    assert ctx.device_status()[0] == 0
+    ctx.close()
+
+
+def test_clean_under_the_checked_build():
+    """The library with -DDL_BOUNDS=1 compares every computed store with its buffer: none of these may lie outside."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    env = dict(os.environ, DL_SPARSE_CHECKED="1")
+    r = subprocess.run([sys.executable, "-m", "pytest", "-q", "-x", "-m", "gpu", os.path.abspath(__file__), "-k",
+                        "test_packed_prompts or test_append or test_decode or test_pages or together"],
+                       capture_output=True, text=True, env=env, cwd=root, timeout=900)
+    assert r.returncode == 0 and " passed" in r.stdout, r.stdout[-2000:] + r.stderr[-2000:]
