@@ -159,6 +159,7 @@ attn_decode_kv4_kernel(const K4Args a) {
   __shared__ int sh_sums[kK4Warps];
   __shared__ int sh_abort;
   volatile int* abort_flag = &sh_abort;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (tid == 0) sh_abort = 0;
   if (lane == 0) {
     for (int s = 0; s < NS; ++s) mbar_init(smem_u32(&bars[s]), 1);
@@ -492,7 +493,6 @@ attn_decode_kv4_kernel(const K4Args a) {
       scores(next_unit, n - (t + 1) * kK4Unit, (here >> (2 * next)) & 3u);
     }
     if (__any_sync(0xffffffffu, gave_up)) break;
-    if (u == u1) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the joining kernel may come up
 
     // ================ finish the part
     const float up = E == -200 ? 0.f : k4_pow2(E);
