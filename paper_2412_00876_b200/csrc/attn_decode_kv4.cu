@@ -159,7 +159,7 @@ attn_decode_kv4_kernel(const K4Args a) {
   __shared__ int sh_sums[kK4Warps];
   __shared__ int sh_abort;
   volatile int* abort_flag = &sh_abort;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  chained_go();                                                   // the joining kernel may come up
   if (tid == 0) sh_abort = 0;
   if (lane == 0) {
     for (int s = 0; s < NS; ++s) mbar_init(smem_u32(&bars[s]), 1);
@@ -586,7 +586,7 @@ attn_merge_kv4_kernel(const K4Args a) {
   const int first = k4_owner(s0, total, W), last = k4_owner(s0 + units - 1, total, W);
   if (first == last) {
     // this grid must not retire before its predecessor has: what follows in the stream relies on both
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    chained_wait();
     return;
   }
   // the token's own score (every warp for itself)
@@ -598,7 +598,7 @@ attn_merge_kv4_kernel(const K4Args a) {
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) own += __shfl_xor_sync(0xffffffffu, own, o);
   own *= a.scale_log2;
-  asm volatile("griddepcontrol.wait;" ::: "memory");              // the parts are written from here on
+  chained_wait();                                                 // the parts have been written from here on
   const int first_slot = k4_range(first, total, W) <= s0 ? 1 : 0; // the pair begins inside that range
   auto part = [&](int w) {
     return a.partial + ((size_t)w * 2 + (w == first ? first_slot : 0)) * k4_slot<D>(a.G) + (size_t)hg * (D + 4);
@@ -689,18 +689,9 @@ static cudaError_t k4_launch(const dl_ctx* ctx, K4Args& a, cudaStream_t s) {
   kernel<<<grid, kK4Warps * 32, smem, s>>>(a);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(a.pg.B * a.H);
   // a warp per eight parts or so (pairs share the ranges evenly when there are few of them)
-  cfg.blockDim = dim3(a.grid_warps / ((long long)a.pg.B * a.Hk) >= 32 ? kK4MergeWarps * 32 : 128);
-  cfg.dynamicSmemBytes = pre_bytes;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, attn_merge_kv4_kernel<D>, (const K4Args)a);
+  const int threads = a.grid_warps / ((long long)a.pg.B * a.Hk) >= 32 ? kK4MergeWarps * 32 : 128;
+  return launch_chained(attn_merge_kv4_kernel<D>, dim3(a.pg.B * a.H), dim3(threads), pre_bytes, s, a);
 }
 
 // floats of scratch: two parts for each range

@@ -134,6 +134,28 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
 // exact-erf GELU in fp32
 __device__ __forceinline__ float gelu_erf(float h) { return 0.5f * h * (1.0f + erff(h * 0.70710678118654752440f)); }
 
+// A launch that is set up while its predecessor in the stream still runs (programmatic stream serialisation).  The kernel
+// calls chained_wait() in every thread before it touches what the predecessor writes, and reads that with ordinary or
+// .cg loads, never through the read-only path (whose lines may be older than the wait); before it, it may only read what
+// was complete when the predecessor began.  A predecessor that calls chained_go() lets it take its place early.  Nothing of
+// the stream's order changes, as no kernel ends before it has waited.
+__device__ __forceinline__ void chained_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void chained_go() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+template <typename... P, typename... A>
+inline cudaError_t launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, A&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
 // ---------------------------------------------------------------------------------------
 // kernel launchers (one per translation unit); all return the launch's cudaError_t
 // ---------------------------------------------------------------------------------------

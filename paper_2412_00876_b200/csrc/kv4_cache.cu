@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(kK4Threads)
 kv4_plan_kernel(const PagesArg pg, int32_t* len, const int32_t* __restrict__ starts, const uint8_t* __restrict__ keep,
                 int32_t total, int32_t commit, int32_t* plan_base, int32_t* plan_count, DeviceStatus* st) {
   __shared__ int sh[kK4Threads / 32];
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the append kernel may start
+  chained_go();                                                    // the append kernel may start
   const int b = blockIdx.x;
   const int from = k4_start(starts, b, total), to = max(from, k4_start(starts, b + 1, total));
   const int count = keep ? k4_count(keep, from, to, sh) : to - from;
@@ -117,7 +117,7 @@ kv4_append_kernel(const PagesArg pg, uint8_t* __restrict__ pool, int32_t Hk, con
   const int b0 = k4_sequence(seq_start, pg.B, t0);
   int before = 0;                                                  // kept rows of the first row's sequence in front of it
   if (b0 >= 0) before = keep ? k4_count(keep, seq_start[b0], t0, sh) : t0 - seq_start[b0];
-  asm volatile("griddepcontrol.wait;" ::: "memory");              // the plan
+  chained_wait();                                                  // the plan
   if (threadIdx.x < 32) {
     const int r = t0 + threadIdx.x;
     const int b = (int)threadIdx.x < rows && r < total ? k4_sequence(seq_start, pg.B, r) : -1;
@@ -253,20 +253,11 @@ cudaError_t launch_kv4_append(const dl_ctx* ctx, const dl_pages* p, int32_t Hk, 
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess || total == 0) return e;
   int rows;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = k4_grid(ctx, total, Hk, &rows);
-  cfg.blockDim = dim3(kK4Threads);
-  cfg.dynamicSmemBytes = (size_t)(p->B + 1) * sizeof(int);
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];                                    // starts while the plan is made, and waits for it
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, ctx->desc.head_dim == 128 ? kv4_append_kernel<128> : kv4_append_kernel<64>, pg,
-                            static_cast<uint8_t*>(pool), Hk, static_cast<const __nv_bfloat16*>(k),
-                            static_cast<const __nv_bfloat16*>(v), (long long)stride, starts, keep, total, (int32_t)rows,
-                            (const int32_t*)ctx->ws.plan_base, (const int32_t*)ctx->ws.plan_count, ctx->ws.status);
+  const dim3 grid = k4_grid(ctx, total, Hk, &rows);
+  return launch_chained(ctx->desc.head_dim == 128 ? kv4_append_kernel<128> : kv4_append_kernel<64>, grid, dim3(kK4Threads),
+                        (size_t)(p->B + 1) * sizeof(int), s, pg, static_cast<uint8_t*>(pool), Hk,
+                        static_cast<const __nv_bfloat16*>(k), static_cast<const __nv_bfloat16*>(v), stride, starts, keep,
+                        total, rows, ctx->ws.plan_base, ctx->ws.plan_count, ctx->ws.status);
 }
 
 cudaError_t launch_kv4_read(const dl_ctx* ctx, const dl_pages* p, int32_t Hk, const void* pool, const int32_t* row0,

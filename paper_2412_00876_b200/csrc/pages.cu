@@ -60,8 +60,9 @@ __device__ __forceinline__ int pg_pages_of(const PgArgs& a, int n) {
 
 // Every sequence gets the pages for len[b] + need[b] rows, the lowest free ones in order of b; all or nothing.
 __global__ void __launch_bounds__(kPgThreads)
-pages_reserve_kernel(const PgArgs a, const int32_t* __restrict__ need) {
+pages_reserve_kernel(const PgArgs a, const int32_t* need) {
   extern __shared__ int sm[];
+  chained_wait();
   int* have = sm;                         // [B] pages a sequence has
   int* first = sm + a.B;                  // [B + 1] pages handed out in front of it
   __shared__ int2 sh[32];
@@ -86,7 +87,7 @@ pages_reserve_kernel(const PgArgs a, const int32_t* __restrict__ need) {
       if (row[mid] >= 0) lo = mid + 1; else hi = mid;
     }
     have[b] = lo;
-    const long long rows = (long long)len + max(need[b], 0);
+    const long long rows = (long long)len + max(__ldcg(need + b), 0);
     const long long want = (rows + (1 << a.shift) - 1) >> a.shift;
     if (want > a.W) atomicMin(&too_long, b);
     first[b] = mine.x;
@@ -118,9 +119,11 @@ pages_reserve_kernel(const PgArgs a, const int32_t* __restrict__ need) {
   }
 }
 
-__global__ void pages_free_kernel(const PgArgs a, const uint8_t* __restrict__ gone) {
+__global__ void pages_free_kernel(const PgArgs a, const uint8_t* gone) {
+  chained_go();
+  chained_wait();
   const int b = blockIdx.x;
-  if (!gone[b]) return;
+  if (!__ldcg(gone + b)) return;
   for (int i = threadIdx.x; i < a.W; i += blockDim.x) {
     const int p = a.table[(size_t)b * a.W + i];
     if (pg_valid(a, p)) atomicSub(a.refs + p, 1);
@@ -132,54 +135,62 @@ __global__ void pages_free_kernel(const PgArgs a, const uint8_t* __restrict__ go
 // Sequence b becomes a fork of parent[b] as that was before the call.  Full pages are shared; of the children that need a
 // parent's partly filled last page one keeps it (the parent itself if it stays, else the lowest) and each other one
 // gets the lowest free page for a copy.  All or nothing.
-// The counts and the new table rows are kept in shared memory where they fit (near: 1 | 2), else in global memory: one
-// round trip for each step of the bookkeeping otherwise.
+// The counts and the table's rows, old and new, are kept in shared memory where they fit (near: 1 | 2), else in global
+// memory, with a round trip for each step of the bookkeeping.
 __global__ void __launch_bounds__(kPgThreads)
-pages_fork_kernel(const PgArgs a, const int32_t* __restrict__ parent, int32_t near) {
+pages_fork_kernel(const PgArgs a, const int32_t* parent, int32_t near) {
   extern __shared__ int sm[];
   int* par = sm;                          // [B]
   int* low = sm + a.B;                    // [B] lowest child
-  int* rows = sm + 2 * a.B;               // [B] new length
+  int* len = sm + 2 * a.B;                // [B] lengths before the call
   int* copy = sm + 3 * a.B;               // [B] the last page is to be copied
   int* mine_dst = sm + 4 * a.B;           // [B] pages handed out, in order
-  volatile int* refs = (near & 1) ? sm + 5 * a.B : a.refs;
-  volatile int* fresh = (near & 2) ? sm + 5 * a.B + ((near & 1) ? a.n_pages : 0) : a.fresh;
+  int* more = sm + 5 * a.B;
+  const unsigned cells = (unsigned)a.B * (unsigned)a.W;                      // below 2^31
+  volatile int* refs = (near & 1) ? more : a.refs;
+  if (near & 1) more += a.n_pages;
+  volatile int* fresh = (near & 2) ? more : a.fresh;
+  const int* old_rows = (near & 2) ? more + cells : a.table;
   __shared__ int2 sh[32];
   const int T = kPgThreads, tid = threadIdx.x;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  chained_go();
+  chained_wait();
+  // everything that is read, in one round trip where it fits
   if (near & 1)
     for (int p = tid; p < a.n_pages; p += T) refs[p] = a.refs[p];
+  if (near & 2)
+    for (unsigned i = tid; i < cells; i += T) const_cast<int*>(old_rows)[i] = a.table[i];
   for (int b = tid; b < a.B; b += T) {
-    int p = parent[b];
+    int p = __ldcg(parent + b);
     if (p < -1 || p >= a.B) {
       report_status(a.status, DL_ERR_INVALID_ARG, b);
       p = b;                              // left as it is
     }
     par[b] = p;
     low[b] = a.B;
-    rows[b] = p >= 0 ? a.len[p] : 0;
+    len[b] = a.len[b];
   }
   __syncthreads();
   for (int b = tid; b < a.B; b += T)
     if (par[b] >= 0) atomicMin(&low[par[b]], b);
   __syncthreads();
+  auto rows_of = [&](int b) { return par[b] >= 0 ? len[par[b]] : 0; };       // new length
   for (int b = tid; b < a.B; b += T) {
-    const int p = par[b];
+    const int p = par[b], n = rows_of(b);
     bool c = false;
-    if (p >= 0 && (rows[b] & ((1 << a.shift) - 1)) != 0 && (par[p] == p ? p : low[p]) != b) {
-      const int used = pg_pages_of(a, rows[b]);
-      c = used > 0 && pg_valid(a, a.table[(size_t)p * a.W + used - 1]);
+    if (p >= 0 && (n & ((1 << a.shift) - 1)) != 0 && (par[p] == p ? p : low[p]) != b) {
+      const int used = pg_pages_of(a, n);
+      c = used > 0 && pg_valid(a, old_rows[(size_t)p * a.W + used - 1]);
     }
     copy[b] = c;
   }
   __syncthreads();
   // new rows, counts of the pages that come and go
-  const unsigned cells = (unsigned)a.B * (unsigned)a.W;                      // below 2^31
   for (unsigned i = tid; i < cells; i += T) {
     const int b = (int)(i / (unsigned)a.W), c = (int)(i - (unsigned)b * a.W), p = par[b];
     if (p == b) continue;
-    const int used = pg_pages_of(a, rows[b]);
-    const int old = a.table[i], now = p >= 0 && c < used ? a.table[(size_t)p * a.W + c] : -1;
+    const int used = pg_pages_of(a, rows_of(b));
+    const int old = old_rows[i], now = p >= 0 && c < used ? old_rows[(size_t)p * a.W + c] : -1;
     fresh[i] = now;
     if (pg_valid(a, old)) atomicSub(const_cast<int*>(refs) + old, 1);
     if (pg_valid(a, now) && !(copy[b] && c == used - 1)) atomicAdd(const_cast<int*>(refs) + now, 1);
@@ -201,9 +212,9 @@ pages_fork_kernel(const PgArgs a, const int32_t* __restrict__ parent, int32_t ne
       for (unsigned i = tid; i < cells; i += T) {
         const int b = (int)(i / (unsigned)a.W), col = (int)(i - (unsigned)b * a.W);
         if (par[b] == b) continue;
-        const int old = a.table[i], now = fresh[i];
+        const int old = old_rows[i], now = fresh[i];
         if (pg_valid(a, old)) atomicAdd(const_cast<int*>(refs) + old, 1);
-        if (pg_valid(a, now) && !(copy[b] && col == pg_pages_of(a, rows[b]) - 1)) atomicSub(const_cast<int*>(refs) + now, 1);
+        if (pg_valid(a, now) && !(copy[b] && col == pg_pages_of(a, rows_of(b)) - 1)) atomicSub(const_cast<int*>(refs) + now, 1);
       }
     if (tid == 0) { a.hdr[0] = 0; report_status(a.status, DL_ERR_CAPACITY, -1); }
     return;
@@ -213,7 +224,7 @@ pages_fork_kernel(const PgArgs a, const int32_t* __restrict__ parent, int32_t ne
   __syncthreads();
   for (int b = b0; b < b1; ++b)
     if (copy[b]) {
-      const unsigned cell = (unsigned)b * a.W + pg_pages_of(a, rows[b]) - 1;
+      const unsigned cell = (unsigned)b * a.W + pg_pages_of(a, rows_of(b)) - 1;
       const int d = mine_dst[at];
       a.src[at] = fresh[cell];
       a.dst[at++] = d;
@@ -228,7 +239,7 @@ pages_fork_kernel(const PgArgs a, const int32_t* __restrict__ parent, int32_t ne
   if (near & 1)
     for (int p = tid; p < a.n_pages; p += T) a.refs[p] = refs[p];
   for (int b = tid; b < a.B; b += T)
-    if (par[b] != b) a.len[b] = rows[b];
+    if (par[b] != b) a.len[b] = rows_of(b);
   if (tid == 0) a.hdr[0] = copies;
 }
 
@@ -236,7 +247,8 @@ pages_fork_kernel(const PgArgs a, const int32_t* __restrict__ parent, int32_t ne
 __global__ void __launch_bounds__(kPgThreads)
 pages_compact_kernel(const PgArgs a, int32_t* live_out) {
   __shared__ int2 sh[32], sh2[32];
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  chained_go();
+  chained_wait();
   int from, to;
   int2 c = make_int2(0, 0), sums;
   pg_run(a, from, to);
@@ -274,7 +286,8 @@ pages_compact_kernel(const PgArgs a, int32_t* live_out) {
 // Copies hdr[0] pages of every pool; with remap, also gives the table's entries of moved pages their new numbers.
 __global__ void __launch_bounds__(kPgCopyThreads)
 pages_copy_kernel(const PgArgs a, const __grid_constant__ PgPools pools, int32_t n_pools, long long page_bytes, int32_t remap) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  chained_go();
+  chained_wait();
   const int n = __ldcg(a.hdr);
   if (remap) {
     const int live = __ldcg(a.hdr + 1);
@@ -337,17 +350,8 @@ static cudaError_t pg_copy(const dl_ctx* ctx, const PgArgs& a, int32_t n_pools, 
     PgPools pp = {};
     const int n = std::min(kPgPools, n_pools - at);
     for (int i = 0; i < n; ++i) pp.p[i] = static_cast<char*>(pools[at + i]);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(ctx->sm_count * 8);
-    cfg.blockDim = dim3(kPgCopyThreads);
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = at == 0 ? 1 : 0;    // the first copy follows the bookkeeping kernel
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, pages_copy_kernel, a, (const PgPools)pp, n, (long long)page_bytes,
-                                             (int32_t)(remap && at == 0));
+    const cudaError_t e = launch_chained(pages_copy_kernel, dim3(ctx->sm_count * 8), dim3(kPgCopyThreads), 0, s, a, pp, n,
+                                         (long long)page_bytes, (int32_t)(remap && at == 0));
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
@@ -355,24 +359,22 @@ static cudaError_t pg_copy(const dl_ctx* ctx, const PgArgs& a, int32_t n_pools, 
 
 cudaError_t launch_pages_reserve(const dl_ctx* ctx, const dl_pages* p, const int32_t* need, cudaStream_t s) {
   const size_t smem = (size_t)(2 * p->B + 1) * 4;
-  pages_reserve_kernel<<<1, kPgThreads, smem, s>>>(pg_args(ctx, p, nullptr), need);
-  return cudaGetLastError();
+  return launch_chained(pages_reserve_kernel, dim3(1), dim3(kPgThreads), smem, s, pg_args(ctx, p, nullptr), need);
 }
 
 cudaError_t launch_pages_free(const dl_ctx* ctx, const dl_pages* p, const uint8_t* gone, cudaStream_t s) {
-  pages_free_kernel<<<p->B, 128, 0, s>>>(pg_args(ctx, p, nullptr), gone);
-  return cudaGetLastError();
+  return launch_chained(pages_free_kernel, dim3(p->B), dim3(128), 0, s, pg_args(ctx, p, nullptr), gone);
 }
 
 cudaError_t launch_pages_fork(const dl_ctx* ctx, const dl_pages* p, const int32_t* parent, int32_t n_pools,
                               void* const* pools, int64_t page_bytes, void* scratch, cudaStream_t s) {
   const PgArgs a = pg_args(ctx, p, scratch);
-  // shared memory: five lists of B, and the counts and the new rows where 160 KB hold them
+  // shared memory: five lists of B, and the counts and the rows where 160 KB hold them
   constexpr size_t kMost = 160 * 1024;
   size_t smem = (size_t)5 * p->B * 4;
   int near = 0;
   if (smem + (size_t)p->n_pages * 4 <= kMost) { near |= 1; smem += (size_t)p->n_pages * 4; }
-  const size_t rows = (size_t)p->B * p->max_pages * 4;
+  const size_t rows = 2 * (size_t)p->B * p->max_pages * 4;
   if (smem + rows <= kMost) { near |= 2; smem += rows; }
   cudaError_t e = cudaSuccess;
   static int attr_set[64];
@@ -381,16 +383,14 @@ cudaError_t launch_pages_fork(const dl_ctx* ctx, const dl_pages* p, const int32_
     if (e != cudaSuccess) return e;
     attr_set[ctx->device & 63] = 1;
   }
-  pages_fork_kernel<<<1, kPgThreads, smem, s>>>(a, parent, near);
-  e = cudaGetLastError();
+  e = launch_chained(pages_fork_kernel, dim3(1), dim3(kPgThreads), smem, s, a, parent, near);
   return e != cudaSuccess ? e : pg_copy(ctx, a, n_pools, pools, page_bytes, false, s);
 }
 
 cudaError_t launch_pages_compact(const dl_ctx* ctx, const dl_pages* p, int32_t n_pools, void* const* pools,
                                  int64_t page_bytes, int32_t* live, void* scratch, cudaStream_t s) {
   const PgArgs a = pg_args(ctx, p, scratch);
-  pages_compact_kernel<<<1, kPgThreads, 0, s>>>(a, live);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch_chained(pages_compact_kernel, dim3(1), dim3(kPgThreads), 0, s, a, live);
   return e != cudaSuccess ? e : pg_copy(ctx, a, n_pools, pools, page_bytes, true, s);
 }
 
