@@ -10,8 +10,8 @@
 // A code in bits 0-3 or 4-7 of a half word IS an fp16 number (a subnormal: code * 2^-24 or code * 2^-20), so eight codes
 // become four operand registers of mma.sync m16n8k16 with one shift and four ANDs; the powers of two are taken out in q
 // (an exact scaling by 1/16 of the dims concerned) and at the end.  (As e4m3 bytes, where a code is code * 2^-9, they
-// would take one shift and two ANDs, but the 8-bit m16n8k32 is made of conversions and two 16-bit products on this GPU:
-// 364 instead of 250 instructions a tile.)  q is divided by a power of two into fp16's range (exact down to 2^-28 of a head's
+// would take one shift and two ANDs, but the 8-bit m16n8k32 is made of conversions and two 16-bit products on this GPU: an
+// earlier form of the kernel took 364 instead of 250 instructions a tile with it.)  q is divided by a power of two into fp16's range (exact down to 2^-28 of a head's
 // largest value).  P s is rounded to fp16 (11 bits) after division by a power of two 2^E that tracks the largest s; the
 // maximum in use of the softmax lags by up to 2^8, so P s 2^-E <= 2^12.
 // The query heads are the N side and 16 keys (scores) or 16 dims (outputs) the M side, so that up to 8 heads of a group
@@ -23,7 +23,7 @@
 // every warp streams the same number of units whatever the lengths are, through its own ring (one bulk copy per
 // tile).  A pair that lies within one range is finished there; the parts of the others go to scratch and are joined by a second
 // kernel, in order and without atomics: the same call gives the same bits.  (Joined by the warp that delivers the last
-// part, few of them took as long, and many, 148 at 100k rows and 16 pairs, four times as long as everything else.)  Page numbers are fetched
+// part, few parts took as long, and many, 100 and more a pair, four times as long as all the rest.)  Page numbers are fetched
 // 16 units ahead, a tile per lane; the lane that holds a tile's number copies it.
 #include <algorithm>
 
@@ -300,7 +300,7 @@ attn_decode_kv4_kernel(const K4Args a) {
       if (idx < 0) {
         if (lane == 0 && hk == 0) report_status(a.status, DL_ERR_CAPACITY, b);
       } else if (on && DL_IN_BOUNDS(a.status, KID_DECODE_KV4, idx, ((long long)a.pg.n_pages * a.Hk) << a.pg.tile_shift)) {
-        kv4_store16<D>(a.pool + (long long)idx * F::TILE, n & 15, l, is_v, code, word);
+        kv4_store16(a.pool + (long long)idx * F::TILE, kv4_row<D>(n & 15, is_v), l, is_v, code, word);
       }
     }
 
@@ -689,7 +689,7 @@ static cudaError_t k4_launch(const dl_ctx* ctx, K4Args& a, cudaStream_t s) {
   kernel<<<grid, kK4Warps * 32, smem, s>>>(a);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  // a warp per eight parts or so (pairs share the ranges evenly when there are few of them)
+  // 16 warps where a pair has 32 parts or more, else four (pairs share the ranges evenly when there are few of them)
   const int threads = a.grid_warps / ((long long)a.pg.B * a.Hk) >= 32 ? kK4MergeWarps * 32 : 128;
   return launch_chained(attn_merge_kv4_kernel<D>, dim3(a.pg.B * a.H), dim3(threads), pre_bytes, s, a);
 }

@@ -125,27 +125,37 @@ __device__ __forceinline__ uint2 kv4_quantise16(const uint32_t (&u)[8], uint32_t
   return flat ? make_uint2(0u, 0u) : make_uint2(c[0], c[1]);
 }
 
-// Stores what kv4_quantise16 gave for lane `l` (0 .. D/16 - 1: dims 16 l .. 16 l + 15) of row `row` of the tile at `tile`;
-// is_v picks the tensor.  No byte of another row is written.
-template <int D> __device__ __forceinline__ void kv4_store16(uint8_t* tile, int row, int l, bool is_v, uint2 code, uint32_t word) {
-  const int g = l >> 2;
+// Where row `row` of a tile has its codes and words, in a form that is cheap per lane: the codes of lane l (0 .. D/16 - 1:
+// dims 16 l .. 16 l + 15) begin at code + (place ^ turn) with place = 8 l in K, 16 l in V, its group's word at word + 4 (l / 4).
+struct Kv4Row { int code, turn, word, upper; };          // upper (V): the row has the upper halves of its pair's units
+template <int D> __device__ __forceinline__ Kv4Row kv4_row(int row, bool is_v) {
+  Kv4Row r;
+  const int i = row >> 1;
+  r.code = is_v ? kv4_v_off<D>(0, 0) + i * D : row * Kv4<D>::RB;
+  r.turn = is_v ? kv4_v_off<D>(i, 0) - r.code : kv4_k_off<D>(row, 0) - r.code;
+  r.word = (is_v ? Kv4<D>::VM : Kv4<D>::KM) + row * Kv4<D>::NG * 4;
+  r.upper = row & 1;
+  return r;
+}
+// Stores what kv4_quantise16 gave for lane `l` of a row of the tile at `tile`; is_v picks the tensor.  No byte of another row
+// is written.
+__device__ __forceinline__ void kv4_store16(uint8_t* tile, const Kv4Row& r, int l, bool is_v, uint2 code, uint32_t word) {
   if (is_v) {
-    uint16_t* to = reinterpret_cast<uint16_t*>(tile + kv4_v_off<D>(row >> 1, 16 * l)) + (row & 1);
+    uint16_t* to = reinterpret_cast<uint16_t*>(tile + (r.code + 2 * r.upper + ((16 * l) ^ r.turn)));
     to[0] = (uint16_t)code.x;
     to[2] = (uint16_t)(code.x >> 16);
     to[4] = (uint16_t)code.y;
     to[6] = (uint16_t)(code.y >> 16);
   } else {
-    *reinterpret_cast<uint2*>(tile + kv4_k_off<D>(row, g) + 8 * (l & 3)) = code;
+    *reinterpret_cast<uint2*>(tile + (r.code + ((8 * l) ^ r.turn))) = code;
   }
-  if ((l & 3) == 0)
-    *reinterpret_cast<uint32_t*>(tile + (is_v ? Kv4<D>::VM : Kv4<D>::KM) + (row * Kv4<D>::NG + g) * 4) = word;
+  if ((l & 3) == 0) *reinterpret_cast<uint32_t*>(tile + r.word + l) = word;
 }
 // The codes that it stored.
-template <int D> __device__ __forceinline__ uint2 kv4_load16(const uint8_t* tile, int row, int l, bool is_v) {
-  if (!is_v) return __ldg(reinterpret_cast<const uint2*>(tile + kv4_k_off<D>(row, l >> 2) + 8 * (l & 3)));
-  const uint4 w = __ldg(reinterpret_cast<const uint4*>(tile + kv4_v_off<D>(row >> 1, 16 * l)));
-  const uint32_t pick = (row & 1) ? 0x7632u : 0x5410u;
+__device__ __forceinline__ uint2 kv4_load16(const uint8_t* tile, const Kv4Row& r, int l, bool is_v) {
+  if (!is_v) return __ldg(reinterpret_cast<const uint2*>(tile + (r.code + ((8 * l) ^ r.turn))));
+  const uint4 w = __ldg(reinterpret_cast<const uint4*>(tile + (r.code + ((16 * l) ^ r.turn))));
+  const uint32_t pick = r.upper ? 0x7632u : 0x5410u;
   return make_uint2(__byte_perm(w.x, w.y, pick), __byte_perm(w.z, w.w, pick));
 }
 

@@ -5,9 +5,13 @@
 //            row and (optionally) advance the length: one CTA per sequence;
 //   append : a CTA takes up to 32 packed source rows, ranks the kept ones and quantises them, 16 values per lane, 4
 //            lanes per group; dropped rows are not read.  A thread stays at one place of the row (head, tensor, 16 dims)
-//            and walks the kept rows (two or four of them at a time measured 2-8 % slower); wide rows are shared by several CTAs (grid y);
+//            and walks the kept rows; wide rows are shared by several CTAs (grid y);
 //   read   : the same walk the other way, codes to bf16.
-// Both are bound by HBM: a kept row costs 2 D bytes in and 9 D / 16 out per head and tensor.
+// Floor: HBM, a kept row costs 2 D bytes in and 9 D / 16 out per head and tensor.  What the kernels run into is issue: 200
+// (append) and 140 (read) instructions per 16 values a lane, 69 and 57 % of the issue slots, so a row's place in its tile is
+// worked out once per CTA, not per lane.  97 MB to 27 (23.7k rows of 8 heads) and back: 29.5 and 27.4 us, 4.2 and 4.5 TB/s.
+// Measured and not better: two or four rows at a time, the next row's loads ahead, a product and a sum on fp32 pairs, the
+// two rows that share V bytes in the halves of a warp or joined by one thread (0-8 % slower).
 #include <algorithm>
 
 #include "kv4.cuh"
@@ -16,7 +20,7 @@ namespace dl {
 
 constexpr int kK4Threads = 256;
 constexpr int kK4Rows = 32;              // most packed rows per CTA
-constexpr int kK4Ctas = 16;              // CTAs per SM worth having
+constexpr int kK4CtasSm = 8;             // CTAs an SM holds, by threads
 
 __device__ __forceinline__ int k4_block_sum(int v, int* sh) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -68,6 +72,27 @@ __device__ __forceinline__ K4Place k4_place(int U) {
   return p;
 }
 
+// 32 bytes: in one access where the addresses are multiples of 32 (kWide), else in two (a selected batch appended and read:
+// 94.7 against 100.6 us; half a sector at a time, a warp's access takes twice the passes)
+template <bool kWide> __device__ __forceinline__ void k4_load32(const void* p, uint32_t (&r)[8]) {
+  if (kWide) {
+    asm("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(p));
+  } else {
+    const uint4 x = __ldg(static_cast<const uint4*>(p)), y = __ldg(static_cast<const uint4*>(p) + 1);
+    r[0] = x.x; r[1] = x.y; r[2] = x.z; r[3] = x.w; r[4] = y.x; r[5] = y.y; r[6] = y.z; r[7] = y.w;
+  }
+}
+template <bool kWide> __device__ __forceinline__ void k4_store32(void* p, const uint32_t (&r)[8]) {
+  if (kWide) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 :: "l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+  } else {
+    static_cast<uint4*>(p)[0] = make_uint4(r[0], r[1], r[2], r[3]);
+    static_cast<uint4*>(p)[1] = make_uint4(r[4], r[5], r[6], r[7]);
+  }
+}
+
 // kept rows among packed rows [from, to), counted by the whole CTA
 __device__ __forceinline__ int k4_count(const uint8_t* keep, int from, int to, int* sh) {
   int c = 0;
@@ -80,10 +105,9 @@ kv4_plan_kernel(const PagesArg pg, int32_t* len, const int32_t* __restrict__ sta
                 int32_t total, int32_t commit, int32_t* plan_base, int32_t* plan_count, DeviceStatus* st) {
   __shared__ int sh[kK4Threads / 32];
   chained_go();                                                    // the append kernel may start
-  const int b = blockIdx.x;
+  const int b = blockIdx.x, base = len[b];
   const int from = k4_start(starts, b, total), to = max(from, k4_start(starts, b + 1, total));
   const int count = keep ? k4_count(keep, from, to, sh) : to - from;
-  const int base = len[b];
   const long long rows = (long long)pg.max_pages * (kKv4Rows << pg.tile_shift);
   bool ok = base >= 0 && (long long)base + count <= rows;
   if (ok && count > 0) {
@@ -102,16 +126,17 @@ kv4_plan_kernel(const PagesArg pg, int32_t* len, const int32_t* __restrict__ sta
 }
 
 // k, v: packed rows [total] of Hk * D values, `stride` values apart; `rows` of them per CTA.
-template <int D>
-__global__ void __launch_bounds__(kK4Threads)
+template <int D, bool kWide>
+__global__ void __launch_bounds__(kK4Threads, kK4CtasSm)
 kv4_append_kernel(const PagesArg pg, uint8_t* __restrict__ pool, int32_t Hk, const __nv_bfloat16* __restrict__ k,
                   const __nv_bfloat16* __restrict__ v, long long stride, const int32_t* __restrict__ starts,
                   const uint8_t* __restrict__ keep, int32_t total, int32_t rows, const int32_t* plan_base,
                   const int32_t* plan_count, DeviceStatus* st) {
   extern __shared__ int seq_start[];
   __shared__ int sh[kK4Threads / 32];
-  __shared__ long long row_src[kK4Rows], row_tile[kK4Rows];       // offset of a kept row's source, first tile of its page's
-  __shared__ int row_in[kK4Rows], n_kept;                         // K/V head 0 plus its tile in the page; its row in the tile
+  __shared__ long long row_src[kK4Rows], row_tile[kK4Rows];       // offset of a kept row's source, of its tile in head 0
+  __shared__ Kv4Row row_at[2][kK4Rows];                           // its place in the tile, in K and in V
+  __shared__ int n_kept;
   const int t0 = blockIdx.x * rows;
   k4_load_starts(starts, pg.B, total, seq_start);
   const int b0 = k4_sequence(seq_start, pg.B, t0);
@@ -135,8 +160,9 @@ kv4_append_kernel(const PagesArg pg, uint8_t* __restrict__ pool, int32_t Hk, con
     if (dst >= 0) {
       const int i = __popc(w & ((1u << threadIdx.x) - 1u));
       row_src[i] = r * stride;
-      row_tile[i] = kv4_tile_index(pg, page, Hk, 0, dst >> 4);
-      row_in[i] = dst & 15;
+      row_tile[i] = (long long)kv4_tile_index(pg, page, Hk, 0, dst >> 4) * Kv4<D>::TILE;
+      row_at[0][i] = kv4_row<D>(dst & 15, false);
+      row_at[1][i] = kv4_row<D>(dst & 15, true);
     }
     if (threadIdx.x == 0) n_kept = __popc(w);
   }
@@ -148,33 +174,33 @@ kv4_append_kernel(const PagesArg pg, uint8_t* __restrict__ pool, int32_t Hk, con
   const bool is_v = at.rem >= half;
   const int l = on ? (is_v ? at.rem - half : at.rem) : 0, hk = l / LR, lr = l - hk * LR;
   const __nv_bfloat16* src = (is_v ? v : k) + l * 16;
-  const long long head_tiles = (long long)hk << pg.tile_shift;
+  uint8_t* head = pool + ((long long)hk << pg.tile_shift) * Kv4<D>::TILE;
+  const Kv4Row* places = row_at[is_v];
   for (int base = 0; base < n; base += at.step) {                 // the same trips for all lanes: they shuffle together
     // (rows behind the last kept one, and places behind the row's last, take another's values and store nothing)
     const int row = base + at.first;
-    const uint4* from = reinterpret_cast<const uint4*>(src + row_src[min(row, n - 1)]);
-    const uint4 x = __ldg(from), y = __ldg(from + 1);
-    const uint32_t raw[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+    uint32_t raw[8];
+    k4_load32<kWide>(src + row_src[min(row, n - 1)], raw);
     uint32_t word;
     const uint2 code = kv4_quantise16(raw, word);
     if (on && row < n) {
-      const long long tile = row_tile[row] + head_tiles;
-      if (DL_IN_BOUNDS(st, KID_KV4_APPEND, tile, (long long)pg.n_pages * Hk << pg.tile_shift))
-        kv4_store16<D>(pool + tile * Kv4<D>::TILE, row_in[row], lr, is_v, code, word);
+      uint8_t* tile = head + row_tile[row];
+      if (DL_IN_BOUNDS(st, KID_KV4_APPEND, (tile - pool) / Kv4<D>::TILE, (long long)pg.n_pages * Hk << pg.tile_shift))
+        kv4_store16(tile, places[row], lr, is_v, code, word);
     }
   }
 }
 
 // Rows row0[b], row0[b] + 1, ... of every sequence as bf16, packed by `starts`.  A row without a page reads as zero and is
 // reported.
-template <int D>
-__global__ void __launch_bounds__(kK4Threads)
+template <int D, bool kWide>
+__global__ void __launch_bounds__(kK4Threads, kK4CtasSm)
 kv4_read_kernel(const PagesArg pg, const uint8_t* __restrict__ pool, int32_t Hk, const int32_t* __restrict__ row0,
                 const int32_t* __restrict__ starts, int32_t total, int32_t rows, __nv_bfloat16* __restrict__ k_out,
                 __nv_bfloat16* __restrict__ v_out, DeviceStatus* st) {
   extern __shared__ int seq_start[];
   __shared__ long long row_tile[kK4Rows];                         // -1: no page, -2: a packed row of no sequence, left as it is
-  __shared__ int row_in[kK4Rows];
+  __shared__ Kv4Row row_at[2][kK4Rows];
   const int t0 = blockIdx.x * rows;
   k4_load_starts(starts, pg.B, total, seq_start);
   if (threadIdx.x < 32) {
@@ -192,8 +218,9 @@ kv4_read_kernel(const PagesArg pg, const uint8_t* __restrict__ pool, int32_t Hk,
       }
       if (tile < 0) report_status(st, DL_ERR_INVALID_ARG, b);
     }
-    row_tile[threadIdx.x] = tile;
-    row_in[threadIdx.x] = in;
+    row_tile[threadIdx.x] = tile < 0 ? tile : tile * Kv4<D>::TILE;
+    row_at[0][threadIdx.x] = kv4_row<D>(in, false);
+    row_at[1][threadIdx.x] = kv4_row<D>(in, true);
   }
   __syncthreads();
   constexpr int LR = D / 16;
@@ -201,18 +228,20 @@ kv4_read_kernel(const PagesArg pg, const uint8_t* __restrict__ pool, int32_t Hk,
   const K4Place at = k4_place(U);
   if (at.rem >= U) return;
   const bool is_v = at.rem >= half;
-  const int l = is_v ? at.rem - half : at.rem, hk = l / LR, lr = l - hk * LR, g = lr >> 2;
-  const long long head_tiles = (long long)hk << pg.tile_shift;
-  uint4* out = reinterpret_cast<uint4*>(is_v ? v_out : k_out);
+  const int l = is_v ? at.rem - half : at.rem, hk = l / LR, lr = l - hk * LR;
+  const uint8_t* head = pool + ((long long)hk << pg.tile_shift) * Kv4<D>::TILE;
+  const Kv4Row* places = row_at[is_v];
+  __nv_bfloat16* out = (is_v ? v_out : k_out) + l * 16;
   const uint64_t magic = kv4_pack2(-8388608.f, -8388608.f);
   for (int row = at.first; row < n; row += at.step) {
-    if (row_tile[row] == -2) continue;
+    const long long at_tile = row_tile[row];
+    if (at_tile == -2) continue;
     uint2 code = make_uint2(0u, 0u);
     uint32_t word = 0u;
-    if (row_tile[row] >= 0) {
-      const uint8_t* tile = pool + (row_tile[row] + head_tiles) * Kv4<D>::TILE;
-      code = kv4_load16<D>(tile, row_in[row], lr, is_v);
-      word = __ldg(reinterpret_cast<const uint32_t*>(tile + (is_v ? Kv4<D>::VM : Kv4<D>::KM) + (row_in[row] * Kv4<D>::NG + g) * 4));
+    if (at_tile >= 0) {
+      const Kv4Row place = places[row];
+      code = kv4_load16(head + at_tile, place, lr, is_v);
+      word = __ldg(reinterpret_cast<const uint32_t*>(head + at_tile + place.word + (lr & ~3)));
     }
     const float s = bf16lo(word), z = bf16hi(word);
     const uint64_t s2 = kv4_pack2(s, s), z2 = kv4_pack2(z, z);
@@ -227,20 +256,22 @@ kv4_read_kernel(const PagesArg pg, const uint8_t* __restrict__ pool, int32_t Hk,
       const __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float((uint32_t)y), __uint_as_float((uint32_t)(y >> 32)));
       p[e] = *reinterpret_cast<const uint32_t*>(&b);
     }
-    const long long to = 2 * ((long long)(t0 + row) * half + l);
-    if (DL_IN_BOUNDS(st, KID_KV4_READ, to + 1, 2LL * total * half)) {
-      out[to] = make_uint4(p[0], p[1], p[2], p[3]);
-      out[to + 1] = make_uint4(p[4], p[5], p[6], p[7]);
-    }
+    const long long to = (long long)(t0 + row) * (half * 16);
+    if (DL_IN_BOUNDS(st, KID_KV4_READ, to + l * 16 + 15, 16LL * total * half))
+      k4_store32<kWide>(out + to, p);
   }
 }
 
-// Rows per CTA and the grid: fewer rows where 32 would not give every SM kK4Ctas CTAs (kept rows are
-// spread unevenly over a batch).
-static dim3 k4_grid(const dl_ctx* ctx, int total, int Hk, int* rows) {
-  const int U = 2 * Hk * ctx->desc.head_dim / 16, slabs = U >= kK4Threads ? (U + kK4Threads - 1) / kK4Threads : 1;
-  *rows = kK4Rows;
-  while (*rows > 4 && (long long)((total + *rows - 1) / *rows) * slabs < (long long)kK4Ctas * ctx->sm_count) *rows >>= 1;
+// Packed rows per CTA (at most kK4Rows) and the grid: as many CTAs as the GPU holds `waves` times, or a whole multiple.
+// Rows that all count make even CTAs, so that one full wave is best (23.7k rows of 8 heads, append or read: 1, 2, 3, 4
+// waves 33, 33.7, 35.5, 37 us); with a mask the kept rows are spread unevenly and four are (a third kept of 21.9k rows of 32
+// heads, appended and read: 3, 4, 5, 6 waves 92.7, 91.6, 91.5, 91.9 us; 2 waves about 95).
+static dim3 k4_grid(const dl_ctx* ctx, int total, int Hk, int waves, int* rows) {
+  const int U = 2 * Hk * ctx->desc.head_dim / 16, slabs = (U + kK4Threads - 1) / kK4Threads;
+  do {
+    const long long ctas = std::max(1LL, (long long)waves++ * kK4CtasSm * ctx->sm_count / slabs);
+    *rows = (int)((total + ctas - 1) / ctas);
+  } while (*rows > kK4Rows);
   return dim3((total + *rows - 1) / *rows, slabs);
 }
 
@@ -253,8 +284,11 @@ cudaError_t launch_kv4_append(const dl_ctx* ctx, const dl_pages* p, int32_t Hk, 
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess || total == 0) return e;
   int rows;
-  const dim3 grid = k4_grid(ctx, total, Hk, &rows);
-  return launch_chained(ctx->desc.head_dim == 128 ? kv4_append_kernel<128> : kv4_append_kernel<64>, grid, dim3(kK4Threads),
+  const dim3 grid = k4_grid(ctx, total, Hk, keep ? 4 : 1, &rows);
+  const bool wide = ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | (uintptr_t)stride * 2) & 31u) == 0;
+  auto kernel = ctx->desc.head_dim == 128 ? (wide ? kv4_append_kernel<128, true> : kv4_append_kernel<128, false>)
+                                          : (wide ? kv4_append_kernel<64, true> : kv4_append_kernel<64, false>);
+  return launch_chained(kernel, grid, dim3(kK4Threads),
                         (size_t)(p->B + 1) * sizeof(int), s, pg, static_cast<uint8_t*>(pool), Hk,
                         static_cast<const __nv_bfloat16*>(k), static_cast<const __nv_bfloat16*>(v), stride, starts, keep,
                         total, rows, ctx->ws.plan_base, ctx->ws.plan_count, ctx->ws.status);
@@ -264,8 +298,10 @@ cudaError_t launch_kv4_read(const dl_ctx* ctx, const dl_pages* p, int32_t Hk, co
                             const int32_t* starts, int32_t total, void* k_out, void* v_out, cudaStream_t s) {
   if (total == 0) return cudaSuccess;
   int rows;
-  const dim3 grid = k4_grid(ctx, total, Hk, &rows);
-  auto kernel = ctx->desc.head_dim == 128 ? kv4_read_kernel<128> : kv4_read_kernel<64>;
+  const dim3 grid = k4_grid(ctx, total, Hk, 1, &rows);
+  const bool wide = ((reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out)) & 31u) == 0;
+  auto kernel = ctx->desc.head_dim == 128 ? (wide ? kv4_read_kernel<128, true> : kv4_read_kernel<128, false>)
+                                          : (wide ? kv4_read_kernel<64, true> : kv4_read_kernel<64, false>);
   kernel<<<grid, kK4Threads, (size_t)(p->B + 1) * sizeof(int), s>>>(pages_arg(p), static_cast<const uint8_t*>(pool), Hk, row0, starts, total, rows,
                                      static_cast<__nv_bfloat16*>(k_out), static_cast<__nv_bfloat16*>(v_out),
                                      ctx->ws.status);

@@ -215,6 +215,39 @@ def test_append_and_read(Hk, D, page, lens, keep, before):
     ctx.close()
 
 
+@pytest.mark.parametrize("Hk,D", [(1, 64), (2, 64), (3, 128)])
+def test_append_and_read_at_every_allowed_alignment(Hk, D):
+    """Sources and outputs at multiples of 16 bytes that are not multiples of 32, and rows an odd number of 16 bytes apart:
+    the same bits as at multiples of 32."""
+    dl, ctx = context(Hk, D)
+    rng = np.random.default_rng(Hk + D)
+    lens, page = [37, 0, 1, 64], 32
+    st, total, w = starts_of(lens), sum(lens), 2 * Hk * D
+    kv = up(bf(rng, total, 2 * Hk, D))
+    flags = torch.from_numpy((rng.random(total) < 0.7).astype(np.uint8)).to(DEV)
+    kept = [int(flags[a:e].sum()) for a, e in zip(st, st[1:])]
+    pg = books(dl, 4, 12, 3, page, lens, rng)
+    seen = []
+    for shift, gap in [(0, 0), (8, 0), (0, 8), (8, 8), (16, 24)]:
+        rows = torch.zeros(shift + total * (w + gap), dtype=torch.bfloat16, device=DEV)[shift:].view(total, w + gap)[:, :w].view(total, 2 * Hk, D)
+        rows.copy_(kv)
+        pool = ctx.kv4_pool(pg, Hk)
+        pg.cache_len.zero_()
+        ctx.kv4_append(pg, pool, rows[:, :Hk], rows[:, Hk:], i32(st), keep=flags)
+        got = [torch.full((shift + sum(kept) * Hk * D + 8,), 7.0, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+        k, v = (t[shift:shift + sum(kept) * Hk * D].view(sum(kept), Hk, D) for t in got)
+        ctx.kv4_read(pg, pool, i32([0] * 4), i32(starts_of(kept)), k, v)
+        assert all(bool((t[:shift] == 7).all()) and bool((t[-8:] == 7).all()) for t in got)
+        seen.append((pool.clone(), k.clone(), v.clone()))
+    ref = pk.held(kv.float().cpu().numpy()[flags.cpu().numpy() != 0])
+    same_values(seen[0][1].float().cpu().numpy(), ref[:, :Hk], "K")
+    same_values(seen[0][2].float().cpu().numpy(), ref[:, Hk:], "V")
+    for other in seen[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(seen[0], other))
+    assert ctx.device_status()[0] == 0
+    ctx.close()
+
+
 def test_rows_with_nan_and_infinity_hold_nan_in_their_group_only():
     Hk, D = 1, 128
     dl, ctx = context(Hk, D)
