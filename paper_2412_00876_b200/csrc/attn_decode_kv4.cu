@@ -18,6 +18,11 @@
 // cost one pass over the codes:
 //   S^T[key][head] = K codes [16 keys][16 dims] x q^T          A straight from shared memory, B = q (registers)
 //   O^T[dim][head] += V^T codes [16 dims][16 keys] x P^T       A straight from shared memory, B: P through movmatrix
+// (In V the low dims' operand keeps the high dims' bits above its own and their sum is taken off at the end: one operation
+// less per word, 55.3 -> 54.6 us on 4 x 100k rows.)
+// With one query head per K/V head the eight columns hold the same q, so that the four lanes of a row of the products can
+// take one key each of a unit's four instead of all the same four: 218 instructions a tile where the general form takes 272
+// (32 x 784 rows of 32 heads of 128: 34.3 -> 30.7 us).
 //
 // Work: the units (32 rows: two tiles) of all (sequence, K/V head) pairs in one line, cut into equal ranges, one per warp:
 // every warp streams the same number of units whatever the lengths are, through its own ring (one bulk copy per
@@ -144,11 +149,12 @@ __device__ __forceinline__ void k4_load16(const __nv_bfloat16* p, bool on, float
   for (int i = 0; i < 8; ++i) { x[2 * i] = bf16lo(u[i]); x[2 * i + 1] = bf16hi(u[i]); }
 }
 
-template <int D, int NT>                                          // NT: blocks of 8 query heads
+template <int D, int NT, bool kOne>                               // NT: blocks of 8 query heads; kOne: one head per K/V head
 __global__ void __launch_bounds__(kK4Warps * 32, k4_ctas(NT))
 attn_decode_kv4_kernel(const K4Args a) {
   using F = Kv4<D>;
   constexpr int NG = F::NG;
+  constexpr int NC = kOne ? 1 : 2, KL = kOne ? 1 : 4;             // heads a lane keeps of a block; keys of a unit
   extern __shared__ __align__(128) char smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, j = lane & 3;
   const int NS = a.stages;
@@ -234,11 +240,11 @@ attn_decode_kv4_kernel(const K4Args a) {
     // ================ one (sequence, K/V head), or the part of it that lies in this range
     const int n = rows[b], seg0 = u - t, seg1 = seg0 + units, part_end = min(seg1, u1);
     uint32_t qb[NT][NG][4][2];                                    // B operand: head r of block nt, 16 dims per step
-    float qs[NT][NG][2], fq[NT][2], se[NT][2];                    // of heads 2j, 2j + 1: sum of q * scale, score factor, own score
+    float qs[NT][NG][NC], fq[NT][NC], se[NT][NC];                   // of heads 2j, 2j + 1: sum of q * scale, score factor, own score
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const bool on = nt * 8 + r < a.G;
-      const __nv_bfloat16* qp = a.q + ((size_t)b * a.H + hk * a.G + nt * 8 + r) * D;
+      const bool on = kOne || nt * 8 + r < a.G;
+      const __nv_bfloat16* qp = a.q + ((size_t)b * a.H + hk * a.G + (kOne ? 0 : nt * 8 + r)) * D;
       float x[NG][16], dot = 0.f, sum[NG], mx = 0.f;
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
@@ -274,7 +280,7 @@ attn_decode_kv4_kernel(const K4Args a) {
         }
       const float fr = a.scale_log2 * k4_pow2(e + 11);            // 2^24 of the codes, 2^(e - 13) of q
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
+      for (int c = 0; c < NC; ++c) {
         const int from = (2 * j + c) * 4;
         fq[nt][c] = __shfl_sync(0xffffffffu, fr, from);
         se[nt][c] = __shfl_sync(0xffffffffu, dot, from) * a.scale_log2;
@@ -304,14 +310,17 @@ attn_decode_kv4_kernel(const K4Args a) {
       }
     }
 
-    float m[NT][2], l_run[NT][2], zacc[NT][NG][2], acc[NT][NG][4][4];
+    float m[NT][NC], l_run[NT][NC], zacc[NT][NG][NC], acc[NT][NG][4][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      m[nt][0] = m[nt][1] = 0.f;                                  // (not a maximum yet: see `seen`)
-      l_run[nt][0] = l_run[nt][1] = 0.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        m[nt][c] = l_run[nt][c] = 0.f;                            // (not a maximum yet: see `seen`)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) zacc[nt][g][c] = 0.f;
+      }
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        zacc[nt][g][0] = zacc[nt][g][1] = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[nt][g][i][0] = acc[nt][g][i][1] = acc[nt][g][i][2] = acc[nt][g][i][3] = 0.f;
       }
@@ -322,7 +331,7 @@ attn_decode_kv4_kernel(const K4Args a) {
 
     // ================ units.  The products of the next unit's keys stand beside the current unit's exponentials and values, so
     // that a warp has two independent chains to work on.
-    float d[2][NT][NG][4], vs[4][NG], vz[4][NG], s[NT][4][2];
+    float d[2][NT][NG][4], vs[KL][NG], vz[KL][NG], s[NT][KL][NC];
     auto key_products = [&](uint32_t unit) {                      // codes times query: lane's keys r and r + 8 of both tiles
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -342,13 +351,14 @@ attn_decode_kv4_kernel(const K4Args a) {
           }
         }
     };
-    // Scores less the maximum in use, from the products and the words of the lane's four keys (index 2 h + i: key r + 8 i of
-    // tile h); nr: rows of the unit that are there, got: tiles that are.
+    // Scores less the maximum in use, from the products and the words of the lane's keys (index 2 h + i: key r + 8 i of
+    // tile h; with one head every column of the products is the same, and a lane keeps the key whose index is j); nr: rows of the unit that are there, got: tiles that are.
     auto scores = [&](uint32_t unit, int nr, uint32_t got) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < KL; ++k) {
         uint32_t kw[NG], vw[NG];
-        const uint32_t at = unit + (k >> 1) * F::TILE + (r + 8 * (k & 1)) * 4 * NG;
+        const int kk = kOne ? j : k;
+        const uint32_t at = unit + (kk >> 1) * F::TILE + (r + 8 * (kk & 1)) * 4 * NG;
         if (NG == 2) {
           const uint2 x = k4_lds64(at + F::KM), y = k4_lds64(at + F::VM);
           kw[0] = x.x; kw[NG - 1] = x.y; vw[0] = y.x; vw[NG - 1] = y.y;
@@ -360,11 +370,13 @@ attn_decode_kv4_kernel(const K4Args a) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
+          for (int c = 0; c < NC; ++c) {
             float dot = 0.f, off = -m[nt][c];
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-              dot = fmaf(bf16lo(kw[g]), d[k >> 1][nt][g][2 * (k & 1) + c], dot);
+              const float x = kOne ? ((j & 1) ? (j >> 1 ? d[1][nt][g][2] : d[0][nt][g][2]) : (j >> 1 ? d[1][nt][g][0] : d[0][nt][g][0]))
+                                   : d[k >> 1][nt][g][2 * (k & 1) + c];
+              dot = fmaf(bf16lo(kw[g]), x, dot);
               off = fmaf(bf16hi(kw[g]), qs[nt][g][c], off);
             }
             s[nt][k][c] = fmaf(fq[nt][c], dot, off);
@@ -373,13 +385,17 @@ attn_decode_kv4_kernel(const K4Args a) {
       if (nr < kK4Unit || got != 3u) {
         // the last unit of a sequence, or one with a page missing: whatever stands in rows that are not there counts nothing
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (16 * (k >> 1) + r + 8 * (k & 1) >= nr || !((got >> (k >> 1)) & 1u)) {
+        for (int k = 0; k < KL; ++k) {
+          const int kk = kOne ? j : k;
+          if (16 * (kk >> 1) + r + 8 * (kk & 1) >= nr || !((got >> (kk >> 1)) & 1u)) {
 #pragma unroll
             for (int g = 0; g < NG; ++g) vs[k][g] = vz[k][g] = 0.f;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) s[nt][k][0] = s[nt][k][1] = -INFINITY;
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int c = 0; c < NC; ++c) s[nt][k][c] = -INFINITY;
           }
+        }
       }
     };
     auto arrived = [&](int sl, int ph) {                          // false: the wait ran out
@@ -397,15 +413,18 @@ attn_decode_kv4_kernel(const K4Args a) {
       const bool more = u + 1 < part_end;
       if (more && !arrived(next, next_phase)) { gave_up = true; break; }
       const uint32_t unit = slot_addr(slot), next_unit = slot_addr(more ? next : slot);
-      bool raise = seen != (1u << (2 * NT)) - 1u;
-      float top = fmaxf(fmaxf(vs[0][0], vs[1][0]), fmaxf(vs[2][0], vs[3][0]));
-      if (NG == 2) top = fmaxf(top, fmaxf(fmaxf(vs[0][NG - 1], vs[1][NG - 1]), fmaxf(vs[2][NG - 1], vs[3][NG - 1])));
+      bool raise = seen != (kOne ? 1u : (1u << (2 * NT)) - 1u);
+      auto most = [](const float* x, int step) {                  // over the lane's keys
+        return kOne ? x[0] : fmaxf(fmaxf(x[0], x[(KL > 1) * step]), fmaxf(x[(KL > 1) * 2 * step], x[(KL > 1) * 3 * step]));
+      };
+      float top = most(&vs[0][0], NG);
+      if (NG == 2) top = fmaxf(top, most(&vs[0][NG - 1], NG));
       raise |= top > s_limit;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
-          raise |= fmaxf(fmaxf(s[nt][0][c], s[nt][1][c]), fmaxf(s[nt][2][c], s[nt][3][c])) > (float)kK4Lag;
+        for (int c = 0; c < NC; ++c)
+          raise |= most(&s[nt][0][c], NC) > (float)kK4Lag;
       if (__any_sync(0xffffffffu, raise)) {
         // rare: the maxima in use go up to what has been seen, and so does 2^E
 #pragma unroll
@@ -423,10 +442,10 @@ attn_decode_kv4_kernel(const K4Args a) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            float mx = fmaxf(fmaxf(s[nt][0][c], s[nt][1][c]), fmaxf(s[nt][2][c], s[nt][3][c]));
+          for (int c = 0; c < NC; ++c) {
+            float mx = most(&s[nt][0][c], NC);
 #pragma unroll
-            for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            for (int o = kOne ? 1 : 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
             // up by mx (the first time: to it, wherever it is); a head without a finite score yet stays
             const bool known = (seen >> (2 * nt + c)) & 1u, finite = mx > -INFINITY && mx < INFINITY;
             const float by = finite && (!known || mx > 0.f) ? mx : 0.f;
@@ -434,37 +453,61 @@ attn_decode_kv4_kernel(const K4Args a) {
             if (finite) seen |= 1u << (2 * nt + c);
             m[nt][c] += by;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) s[nt][k][c] -= by;
+            for (int k = 0; k < KL; ++k) s[nt][k][c] -= by;
             l_run[nt][c] *= corr;
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
               zacc[nt][g][c] *= corr;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) { acc[nt][g][i][c] *= corr * corr_e; acc[nt][g][i][2 + c] *= corr * corr_e; }
+              for (int i = 0; i < 4; ++i) {
+                acc[nt][g][i][c] *= corr * corr_e;
+                acc[nt][g][i][2 + c] *= corr * corr_e;
+                if (kOne) { acc[nt][g][i][1] *= corr * corr_e; acc[nt][g][i][3] *= corr * corr_e; }
+              }
             }
           }
       }
       // ---- P, and O^T += V^T (P s)^T tile by tile: lane's row pairs j and j + 4, its dims 64 g + 8 r .. + 7
+      // With one head, the lanes of row r hold P s of keys 0 r, r + 8, 16 + r and 24 + r, one pair (the two groups) each, in
+      // columns 4 h + 2 i + g.  For tile h the columns of the other tile are made zero; what the rest of them add up to
+      // nobody reads: the sums of group g are in columns g (tile 0) and 4 + g (tile 1).
+      uint32_t one[2] = {0u, 0u};
+      if (kOne) {
+        const float p = k4_exp2(s[0][0][0]);
+        l_run[0][0] += p;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) zacc[0][g][0] = fmaf(p, vz[0][g], zacc[0][g][0]);
+        const uint32_t y = k4_f16x2(p * (vs[0][0] * down_e), NG == 2 ? p * (vs[0][NG - 1] * down_e) : 0.f);
+        one[0] = k4_transpose(y);
+        one[1] = k4_transpose(__shfl_xor_sync(0xffffffffu, y, 1));
+      }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         uint32_t pb[NT][NG][2];
+        if (kOne) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+          for (int g = 0; g < NG; ++g) {
+            pb[0][g][0] = (r >> 2) == h ? one[0] : 0u;
+            pb[0][g][1] = (r >> 2) == h ? one[1] : 0u;
+          }
+        }
+#pragma unroll
+        for (int nt = 0; nt < (kOne ? 0 : NT); ++nt) {
           float p[2][2];
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              p[i][c] = k4_exp2(s[nt][2 * h + i][c]);
+            for (int c = 0; c < NC; ++c) {
+              p[i][c] = k4_exp2(s[nt][(2 * h + i) % KL][c]);
               l_run[nt][c] += p[i][c];
             }
 #pragma unroll
           for (int g = 0; g < NG; ++g)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              const float f = vs[2 * h + i][g] * down_e;
+              const float f = vs[(2 * h + i) % KL][g] * down_e;
 #pragma unroll
-              for (int c = 0; c < 2; ++c) zacc[nt][g][c] = fmaf(p[i][c], vz[2 * h + i][g], zacc[nt][g][c]);
+              for (int c = 0; c < NC; ++c) zacc[nt][g][c] = fmaf(p[i][c], vz[(2 * h + i) % KL][g], zacc[nt][g][c]);
               pb[nt][g][i] = k4_transpose(k4_f16x2(p[i][0] * f, p[i][1] * f));
             }
         }
@@ -474,11 +517,12 @@ attn_decode_kv4_kernel(const K4Args a) {
           const uint2 wx = k4_lds64(va + kv4_v_off<D>(j, 64 * g + 8 * r)), wy = k4_lds64(va + kv4_v_off<D>(j + 4, 64 * g + 8 * r));
 #pragma unroll
           for (int w = 0; w < 2; ++w) {
-            const uint32_t x = w ? wx.y : wx.x, y = w ? wy.y : wy.x, x8 = x >> 8, y8 = y >> 8;
+            const uint32_t x = w ? wx.y : wx.x, y = w ? wy.y : wy.x;
+            const uint32_t x0 = x & 0x00FF00FFu, y0 = y & 0x00FF00FFu, x1 = __byte_perm(x, 0u, 0x4341), y1 = __byte_perm(y, 0u, 0x4341);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              k4_mma(acc[nt][g][2 * w], x & 0x000F000Fu, x & 0x00F000F0u, y & 0x000F000Fu, y & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
-              k4_mma(acc[nt][g][2 * w + 1], x8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x000F000Fu, y8 & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
+              k4_mma(acc[nt][g][2 * w], x0, x0 & 0x00F000F0u, y0, y0 & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
+              k4_mma(acc[nt][g][2 * w + 1], x1, x1 & 0x00F000F0u, y1, y1 & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
             }
           }
         }
@@ -499,12 +543,22 @@ attn_decode_kv4_kernel(const K4Args a) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
+      for (int c = 0; c < NC; ++c) {
 #pragma unroll
-        for (int o = 4; o < 32; o <<= 1) {
+        for (int o = kOne ? 1 : 4; o < 32; o <<= 1) {
           l_run[nt][c] += __shfl_xor_sync(0xffffffffu, l_run[nt][c], o);
 #pragma unroll
           for (int g = 0; g < NG; ++g) zacc[nt][g][c] += __shfl_xor_sync(0xffffffffu, zacc[nt][g][c], o);
+        }
+        if (kOne) {
+          // both tiles' columns, in one
+#pragma unroll
+          for (int g = 0; g < NG; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              acc[nt][g][i][0] = acc[nt][g][i][g] + __shfl_xor_sync(0xffffffffu, acc[nt][g][i][g], 2);
+              acc[nt][g][i][2] = acc[nt][g][i][2 + g] + __shfl_xor_sync(0xffffffffu, acc[nt][g][i][2 + g], 2);
+            }
         }
         const int head = nt * 8 + 2 * j + c;
         if (head >= a.G) continue;                                // (after the shuffles of this pair)
@@ -516,7 +570,7 @@ attn_decode_kv4_kernel(const K4Args a) {
         for (int g = 0; g < NG; ++g)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            o[g][2 * i] = fmaf(acc[nt][g][i][c] * 16777216.f, up, zacc[nt][g][c]);
+            o[g][2 * i] = fmaf((acc[nt][g][i][c] - acc[nt][g][i][2 + c]) * 16777216.f, up, zacc[nt][g][c]);
             o[g][2 * i + 1] = fmaf(acc[nt][g][i][2 + c] * 1048576.f, up, zacc[nt][g][c]);
           }
         if (whole) {
@@ -665,7 +719,7 @@ attn_merge_kv4_kernel(const K4Args a) {
   }
 }
 
-template <int D, int NT>
+template <int D, int NT, bool kOne>
 static cudaError_t k4_launch(const dl_ctx* ctx, K4Args& a, cudaStream_t s) {
   constexpr int kCtas = k4_ctas(NT);
   const size_t pre_bytes = (size_t)(2 * a.pg.B + 1) * sizeof(int);
@@ -675,7 +729,7 @@ static cudaError_t k4_launch(const dl_ctx* ctx, K4Args& a, cudaStream_t s) {
   if (ns < 2) return cudaErrorInvalidConfiguration;
   a.stages = ns;
   const size_t smem = (size_t)kK4Warps * ns * (2 * Kv4<D>::TILE + 8) + pre_bytes;
-  auto kernel = attn_decode_kv4_kernel<D, NT>;
+  auto kernel = attn_decode_kv4_kernel<D, NT, kOne>;
   cudaError_t e = cudaSuccess;
   static int attr_set[64];                                        // the most asked for so far on a device
   int& most = attr_set[ctx->device & 63];
@@ -717,8 +771,10 @@ cudaError_t launch_attn_decode_kv4(const dl_ctx* ctx, const dl_pages* p, int32_t
   a.status = ctx->ws.status;
   a.H = d.n_heads; a.Hk = Hk; a.G = d.n_heads / Hk;
   a.scale_log2 = scale * 1.4426950408889634f;
-  if (d.head_dim == 128) return a.G <= 8 ? k4_launch<128, 1>(ctx, a, s) : k4_launch<128, 2>(ctx, a, s);
-  return a.G <= 8 ? k4_launch<64, 1>(ctx, a, s) : k4_launch<64, 2>(ctx, a, s);
+  // one head per K/V head: see the top
+  if (a.G == 1) return d.head_dim == 128 ? k4_launch<128, 1, true>(ctx, a, s) : k4_launch<64, 1, true>(ctx, a, s);
+  if (d.head_dim == 128) return a.G <= 8 ? k4_launch<128, 1, false>(ctx, a, s) : k4_launch<128, 2, false>(ctx, a, s);
+  return a.G <= 8 ? k4_launch<64, 1, false>(ctx, a, s) : k4_launch<64, 2, false>(ctx, a, s);
 }
 
 }  // namespace dl

@@ -338,6 +338,56 @@ def test_decode_attention(H, Hk, D, page, lens, spread):
     ctx.close()
 
 
+@pytest.mark.parametrize("H,D,page,lens", [
+    (1, 64, 16, [1]), (2, 64, 32, [31, 32, 33, 63]), (5, 128, 32, [300, 31, 33, 0, 1200]), (32, 128, 64, [90, 700]),
+    (8, 64, 128, [2000, 5]), (1, 128, 16, [15, 17, 47, 48, 49])])
+def test_decode_one_query_head_per_kv_head(H, D, page, lens):
+    """The form whose lanes share a unit's keys out: at the edges of tiles and units, split and whole pairs."""
+    test_decode_attention(H, H, D, page, lens, 1.0)
+    test_decode_attention(H, H, D, page, lens, 30.0)
+
+
+@pytest.mark.parametrize("H,Hk", [(2, 2), (4, 2), (12, 1)])
+def test_decode_a_spoilt_row_or_page_stays_where_it_is(H, Hk):
+    """A NaN in a group of V spoils that group's outputs alone, one in K its head's; rows of a page that is not there count
+    nothing, in every form of the kernel."""
+    D, page, n = 128, 16, 75
+    dl, ctx = context(H, D)
+    rng = np.random.default_rng(H)
+    kv = np.stack([bf(rng, n, 2 * Hk, D)] * 4)
+    kv[1, 37, Hk, 3] = np.nan                                      # V, head 0, group 0
+    kv[2, 20, Hk, 127] = np.inf                                    # V, head 0, group 1
+    kv[3, 9, 0, 64] = np.nan                                       # K, head 0
+    q, kt, vt = (np.repeat(bf(rng, 1, h, D), 4, 0) for h in (H, Hk, Hk))
+    pg = books(dl, 4, 24, 6, page, [n] * 4, rng)
+    pool = ctx.kv4_pool(pg, Hk)
+    d = up(kv.reshape(4 * n, 2 * Hk, D))
+    ctx.kv4_append(pg, pool, d[:, :Hk], d[:, Hk:], i32(starts_of([n] * 4)))
+    out = torch.zeros(4, H, D, dtype=torch.bfloat16, device=DEV)
+    ctx.kv4_attn_decode(pg, pool, up(q), up(kt), up(vt), None, 0.1, out)
+    assert ctx.device_status()[0] == 0
+    o, G = wl.from_torch(out), H // Hk
+    bad = np.zeros(o.shape, bool)
+    bad[1, :G, :64] = bad[2, :G, 64:] = bad[3, :G] = True
+    assert np.array_equal(np.isnan(o), bad)
+    h, lifted = pk.held(kv[0]), lift(kv[0])
+    ref = pk.attention_decode(q[0], kt[0], vt[0], h[:, :Hk], h[:, Hk:], 0.1)
+    ref_abs = pk.attention_decode(q[0], kt[0], np.abs(vt[0]), h[:, :Hk], np.abs(h[:, Hk:]), 0.1)
+    ref_lift = pk.attention_decode(q[0], kt[0], 0 * vt[0], h[:, :Hk], lifted[:, Hk:], 0.1)
+    for b in range(4):
+        close(np.where(bad[b], ref, o[b]), ref, ref_abs, f"sequence {b}", ref_lift)
+    hole = int(pg.table[0, 2])
+    pg.table[0, 2] = 24                                            # no such page
+    ctx.kv4_attn_decode(pg, pool, up(q), up(kt), up(vt), None, 0.1, out)
+    left = np.concatenate([kv[0, :32], kv[0, 48:]])
+    h, lifted = pk.held(left), lift(left)
+    ref = pk.attention_decode(q[0], kt[0], vt[0], h[:, :Hk], h[:, Hk:], 0.1)
+    close(wl.from_torch(out)[0], ref, pk.attention_decode(q[0], kt[0], np.abs(vt[0]), h[:, :Hk], np.abs(h[:, Hk:]), 0.1), "hole",
+          pk.attention_decode(q[0], kt[0], 0 * vt[0], h[:, :Hk], lifted[:, Hk:], 0.1))
+    assert ctx.device_status() == (dl.DL_ERR_INVALID_ARG, 0) and 0 <= hole < 24
+    ctx.close()
+
+
 def test_decode_leaves_out_rows_without_pages_and_reports_full_caches():
     H, Hk, D, page = 4, 2, 128, 16
     dl, ctx = context(H, D)
