@@ -18,10 +18,10 @@
 // cost one pass over the codes:
 //   S^T[key][head] = K codes [16 keys][16 dims] x q^T          A straight from shared memory, B = q (registers)
 //   O^T[dim][head] += V^T codes [16 dims][16 keys] x P^T       A straight from shared memory, B: P through movmatrix
-// (In V the low dims' operand keeps the high dims' bits above its own and their sum is taken off at the end: one operation
-// less per word, 55.3 -> 54.6 us on 4 x 100k rows.)
+// (An operand of V that keeps the high dims' bits above its own, their sum taken off at the end, is one operation less per
+// word and 1 % faster, but sums 17 times as large lose too many bits on long rows: 0.0088 instead of 0.0018 of the outputs.)
 // With one query head per K/V head the eight columns hold the same q, so that the four lanes of a row of the products can
-// take one key each of a unit's four instead of all the same four: 218 instructions a tile where the general form takes 272
+// take one key each of a unit's four instead of all the same four: 225 instructions a tile where the general form takes 280
 // (32 x 784 rows of 32 heads of 128: 34.3 -> 30.7 us).
 //
 // Work: the units (32 rows: two tiles) of all (sequence, K/V head) pairs in one line, cut into equal ranges, one per warp:
@@ -517,12 +517,11 @@ attn_decode_kv4_kernel(const K4Args a) {
           const uint2 wx = k4_lds64(va + kv4_v_off<D>(j, 64 * g + 8 * r)), wy = k4_lds64(va + kv4_v_off<D>(j + 4, 64 * g + 8 * r));
 #pragma unroll
           for (int w = 0; w < 2; ++w) {
-            const uint32_t x = w ? wx.y : wx.x, y = w ? wy.y : wy.x;
-            const uint32_t x0 = x & 0x00FF00FFu, y0 = y & 0x00FF00FFu, x1 = __byte_perm(x, 0u, 0x4341), y1 = __byte_perm(y, 0u, 0x4341);
+            const uint32_t x = w ? wx.y : wx.x, y = w ? wy.y : wy.x, x8 = x >> 8, y8 = y >> 8;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              k4_mma(acc[nt][g][2 * w], x0, x0 & 0x00F000F0u, y0, y0 & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
-              k4_mma(acc[nt][g][2 * w + 1], x1, x1 & 0x00F000F0u, y1, y1 & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
+              k4_mma(acc[nt][g][2 * w], x & 0x000F000Fu, x & 0x00F000F0u, y & 0x000F000Fu, y & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
+              k4_mma(acc[nt][g][2 * w + 1], x8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x000F000Fu, y8 & 0x00F000F0u, pb[nt][g][0], pb[nt][g][1]);
             }
           }
         }
@@ -570,7 +569,7 @@ attn_decode_kv4_kernel(const K4Args a) {
         for (int g = 0; g < NG; ++g)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            o[g][2 * i] = fmaf((acc[nt][g][i][c] - acc[nt][g][i][2 + c]) * 16777216.f, up, zacc[nt][g][c]);
+            o[g][2 * i] = fmaf(acc[nt][g][i][c] * 16777216.f, up, zacc[nt][g][c]);
             o[g][2 * i + 1] = fmaf(acc[nt][g][i][2 + c] * 1048576.f, up, zacc[nt][g][c]);
           }
         if (whole) {
@@ -771,7 +770,6 @@ cudaError_t launch_attn_decode_kv4(const dl_ctx* ctx, const dl_pages* p, int32_t
   a.status = ctx->ws.status;
   a.H = d.n_heads; a.Hk = Hk; a.G = d.n_heads / Hk;
   a.scale_log2 = scale * 1.4426950408889634f;
-  // one head per K/V head: see the top
   if (a.G == 1) return d.head_dim == 128 ? k4_launch<128, 1, true>(ctx, a, s) : k4_launch<64, 1, true>(ctx, a, s);
   if (d.head_dim == 128) return a.G <= 8 ? k4_launch<128, 1, false>(ctx, a, s) : k4_launch<128, 2, false>(ctx, a, s);
   return a.G <= 8 ? k4_launch<64, 1, false>(ctx, a, s) : k4_launch<64, 2, false>(ctx, a, s);

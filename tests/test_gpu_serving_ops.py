@@ -388,6 +388,38 @@ def test_decode_a_spoilt_row_or_page_stays_where_it_is(H, Hk):
     ctx.close()
 
 
+@pytest.mark.parametrize("H,Hk", [(16, 16), (64, 16)])
+def test_decode_sums_over_long_rows_keep_their_bits(H, Hk):
+    """100k rows of 16 heads, so that a warp adds up about 900 rows, with even weights, so that the output is a small mean of
+    large codes.  The output's rounding is at most 2^-8 of it.  The roundings of P s are independent: 2^-11 of
+    sqrt(sum p^2) rms(v - z).  About 56 additions into an accumulator, each cut off at 2^-23 of a sum that grows evenly:
+    28 * 2^-23, below 2^-18, of sum p (v - z)."""
+    D, page, n, head = 128, 128, 100_000, 5
+    dl, ctx = context(H, D)
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    rows = lambda *s: torch.randn(*s, generator=gen, device=DEV).bfloat16()
+    k, v, q, kt, vt = rows(n, Hk, D), rows(n, Hk, D), rows(1, H, D) * 0.25, rows(1, Hk, D), rows(1, Hk, D)
+    pg = dl.Pages(1, 800, 800, page, DEV)
+    ctx.pages_reserve(pg, i32([n]))
+    pool = ctx.kv4_pool(pg, Hk)
+    ctx.kv4_append(pg, pool, k, v, i32([0, n]))
+    out = torch.zeros(1, H, D, dtype=torch.bfloat16, device=DEV)
+    ctx.kv4_attn_decode(pg, pool, q, kt, vt, None, D ** -0.5, out)
+    G = H // Hk
+    mine = slice(head * G, head * G + G)
+    kh, vh = wl.from_torch(k[:, head]), wl.from_torch(v[:, head])
+    kt, vt, q = wl.from_torch(kt[0, head]), wl.from_torch(vt[0, head]), wl.from_torch(q[0, mine])
+    z = np.concatenate([pk.held(kh) @ q.T, (q @ kt)[None]]) * D ** -0.5
+    p = np.exp(z - z.max(0))
+    p /= p.sum(0)
+    ref, spread = p.T @ np.concatenate([pk.held(vh), vt[None]]), p[:-1].T @ lift(vh)
+    rms = lambda x: np.sqrt((x ** 2).mean())
+    bound = EPS * rms(ref) + (2.0 ** -11 * np.sqrt((p ** 2).sum(0).max()) + 2.0 ** -18) * rms(spread)
+    assert rms(wl.from_torch(out[0, mine]) - ref) <= bound
+    assert ctx.device_status()[0] == 0
+    ctx.close()
+
+
 def test_decode_leaves_out_rows_without_pages_and_reports_full_caches():
     H, Hk, D, page = 4, 2, 128, 16
     dl, ctx = context(H, D)
