@@ -420,6 +420,40 @@ def test_decode_sums_over_long_rows_keep_their_bits(H, Hk):
     ctx.close()
 
 
+@pytest.mark.parametrize("H,Hk", [(16, 16), (64, 16)])
+def test_decode_sums_do_not_shrink_with_the_number_of_rows(H, Hk):
+    """4M rows of 16 heads, 40 times the same pages, so that a warp adds up about 36k rows.  The bounds are those above: a
+    sum that is cut off is kept and begun anew after 32 units, 64 additions, 32 * 2^-23 = 2^-18 in all.  (The roundings of P s
+    repeat with the rows: p as of one time.)"""
+    D, page, n, head, times = 128, 128, 782 * 128, 5, 40
+    dl, ctx = context(H, D)
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    rows = lambda *s: torch.randn(*s, generator=gen, device=DEV).bfloat16()
+    k, v, q, kt, vt = rows(n, Hk, D), rows(n, Hk, D), rows(1, H, D) * 0.25, rows(1, Hk, D), rows(1, Hk, D)
+    pg = dl.Pages(1, 782, 782 * times, page, DEV)
+    ctx.pages_reserve(pg, i32([n]))
+    pool = ctx.kv4_pool(pg, Hk)
+    ctx.kv4_append(pg, pool, k, v, i32([0, n]))
+    pg.table.copy_(pg.table[:, :782].repeat(1, times))
+    pg.cache_len.fill_(n * times)
+    out = torch.zeros(1, H, D, dtype=torch.bfloat16, device=DEV)
+    ctx.kv4_attn_decode(pg, pool, q, kt, vt, None, D ** -0.5, out)
+    G = H // Hk
+    mine = slice(head * G, head * G + G)
+    kh, vh = pk.held(wl.from_torch(k[:, head])), wl.from_torch(v[:, head])
+    kt, vt, q = wl.from_torch(kt[0, head]), wl.from_torch(vt[0, head]), wl.from_torch(q[0, mine])
+    z = np.concatenate([kh @ q.T, (q @ kt)[None]]) * D ** -0.5
+    p = np.exp(z - z.max(0))
+    p[:-1] *= times
+    p /= p.sum(0)
+    ref, spread = p.T @ np.concatenate([pk.held(vh), vt[None]]), p[:-1].T @ lift(vh)
+    rms = lambda x: np.sqrt((x ** 2).mean())
+    bound = EPS * rms(ref) + (2.0 ** -11 * np.sqrt((p ** 2).sum(0).max()) + 2.0 ** -18) * rms(spread)
+    assert rms(wl.from_torch(out[0, mine]) - ref) <= bound
+    assert ctx.device_status()[0] == 0
+    ctx.close()
+
+
 def test_decode_leaves_out_rows_without_pages_and_reports_full_caches():
     H, Hk, D, page = 4, 2, 128, 16
     dl, ctx = context(H, D)
