@@ -12,8 +12,12 @@
 // (an exact scaling by 1/16 of the dims concerned) and at the end.  (As e4m3 bytes, where a code is code * 2^-9, they
 // would take one shift and two ANDs, but the 8-bit m16n8k32 is made of conversions and two 16-bit products on this GPU: an
 // earlier form of the kernel took 364 instead of 250 instructions a tile with it.)  q is divided by a power of two into fp16's range (exact down to 2^-28 of a head's
-// largest value).  P s is rounded to fp16 (11 bits) after division by a power of two 2^E that tracks the largest s; the
-// maximum in use of the softmax lags by up to 2^8, so P s 2^-E <= 2^12.
+// largest value).  P s is rounded to fp16 after multiplication by a power of two `fd` of its head and group of dims, which puts
+// the largest P s that they have met so far at 2^9 .. 2^15 (2^-7 .. for values below 2^-110): 2^-11 of every P s down to 2^-23
+// of that one, and no more than 2^-34 of it for any below, however the scores and the sizes of V's rows are spread.  (P alone is held relative to a maximum
+// that lags by up to 2^8.  One power of two for all, following the largest s, takes 57.1 instead of 57.9 us for
+// 4 x 100k rows and 43.4 instead of 45.2 us for 16 heads a K/V head on 16 x 20k; but a row of large values that nobody attends,
+// or a leading score with a value of zero, then pushed the others out of fp16.)
 // The query heads are the N side and 16 keys (scores) or 16 dims (outputs) the M side, so that up to 8 heads of a group
 // cost one pass over the codes:
 //   S^T[key][head] = K codes [16 keys][16 dims] x q^T          A straight from shared memory, B = q (registers)
@@ -57,8 +61,12 @@ constexpr int kK4MergeWarps = 16;        // most warps of a joining CTA
 // sum of many positive terms comes out too small, in proportion to their number.  (600k rows, 8 heads: an error of 0.0040 of
 // the outputs without, 0.0018 with this; 4 x 100k rows 55.4 -> 56 us, every 16 units 57.3.)
 constexpr int kK4Flush = 32;
-// floats a lane keeps of them: the accumulators, the maxima in use, E
-template <int D> __host__ __device__ constexpr int k4_keep(int nt) { return nt * (D / 4 + 4); }
+// floats a lane keeps of them: the accumulators, the maxima in use, the powers of two in use
+template <int D> __host__ __device__ constexpr int k4_keep(int nt) { return nt * (D / 4 + 8); }
+// P s times its power of two: where the largest goes when it passes the limit, the limit (half of fp16's), and the power of two
+// to begin with, the most there is (times P, at most 2^kK4Lag, it is finite)
+constexpr int kK4Put = 9, kK4Most = 15, kK4Begin = 119;
+static_assert(kK4Begin + kK4Lag < 128, "0 * infinity");
 
 // floats of a part: D sums per head, then the head's maximum and its sum of exponentials (16-byte steps)
 template <int D> __host__ __device__ constexpr int k4_slot(int G) { return G * (D + 4); }
@@ -136,6 +144,18 @@ __device__ __forceinline__ float k4_exp2(float x) {
   return y;
 }
 __device__ __forceinline__ float k4_pow2(int e) { return __int_as_float((e + 127) << 23); }     // -126 <= e <= 127
+__device__ __forceinline__ int k4_exponent(float x) { return (int)((uint32_t)__float_as_int(x) >> 23) - 127; }   // x > 0
+// the larger ones of two pairs of fp16 values; a NaN loses
+__device__ __forceinline__ uint32_t k4_max2(uint32_t x, uint32_t y) {
+  uint32_t r;
+  asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+  return r;
+}
+// one of two fp16 values, neither below zero, is 2^kK4Most or more
+__device__ __forceinline__ bool k4_beyond(uint32_t x) {
+  constexpr uint32_t kAdd = 0x8000u - ((kK4Most + 15u) << 10);      // carries into the sign from there on
+  return ((x + (kAdd | kAdd << 16)) & 0x80008000u) != 0u;
+}
 __device__ __forceinline__ uint32_t k4_lds32(uint32_t a) {
   uint32_t v;
   asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
@@ -333,8 +353,13 @@ attn_decode_kv4_kernel(const K4Args a) {
       }
     }
     uint32_t seen = 0;                                            // heads (bit 2 nt + c) whose maximum in use has been set
-    int E = -200;                                                 // P s is held as P s 2^-E; none yet
-    float down_e = 0.f, s_limit = 0.f;                            // 2^-E, 2^(E + 4)
+    float fd[NT][NG][NC];                                         // P s is held as P s fd, a power of two
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) fd[nt][g][c] = k4_pow2(kK4Begin);
 
     // ================ units.  The products of the next unit's keys stand beside the current unit's exponentials and values, so
     // that a warp has two independent chains to work on.
@@ -405,22 +430,29 @@ attn_decode_kv4_kernel(const K4Args a) {
         }
       }
     };
-    // Adds to the accumulators what has been kept of them (rounded sums), with the maxima and 2^E it was kept at brought up
-    // to those in use; `out`: keeps the result and clears the accumulators.
+    // Adds to the accumulators what has been kept of them (rounded sums), with the maxima and powers of two it was kept at
+    // brought to those in use; `out`: keeps the result and clears the accumulators.
     auto flush = [&](bool in, bool out) {
       float4* keep = reinterpret_cast<float4*>(a.sums + (size_t)gw * (32 * k4_keep<D>(NT))) + lane;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float4* mine = keep + nt * 8 * k4_keep<D>(1);
-        float f[2] = {0.f, 0.f};
+        float4 was_m = make_float4(0.f, 0.f, 0.f, 0.f), was_fd = was_m;
         if (in) {
-          const float4 was = __ldcg(mine + 32 * 4 * NG);          // (a head without a score had sums of zero, whatever its maximum)
-          const float e = k4_pow2(max(-126, min(0, __float_as_int(was.z) - E)));
-          f[0] = fminf(1.f, k4_exp2(was.x - m[nt][0])) * e;
-          f[1] = kOne ? f[0] : fminf(1.f, k4_exp2(was.y - m[nt][NC - 1])) * e;
+          was_m = __ldcg(mine + 32 * 4 * NG);
+          was_fd = __ldcg(mine + 32 * (4 * NG + 1));
         }
 #pragma unroll
-        for (int g = 0; g < NG; ++g)
+        for (int g = 0; g < NG; ++g) {
+          float f[2] = {0.f, 0.f};
+          if (in) {
+            // (a power of two goes up by less than its maximum does; a head without a score had sums of zero, whatever its
+            // maximum)
+            const int e0 = k4_exponent(fd[nt][g][0]) - k4_exponent(g == 0 ? was_fd.x : was_fd.y);
+            const int e1 = k4_exponent(fd[nt][g][NC - 1]) - k4_exponent(g == 0 ? was_fd.z : was_fd.w);
+            f[0] = fminf(1.f, k4_exp2(was_m.x - m[nt][0] + (float)e0));
+            f[1] = kOne ? f[0] : fminf(1.f, k4_exp2(was_m.y - m[nt][NC - 1] + (float)e1));
+          }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             float* x = acc[nt][g][i];
@@ -434,7 +466,11 @@ attn_decode_kv4_kernel(const K4Args a) {
               x[0] = x[1] = x[2] = x[3] = 0.f;
             }
           }
-        if (out) __stcg(mine + 32 * 4 * NG, make_float4(m[nt][0], m[nt][NC - 1], __int_as_float(E), 0.f));
+        }
+        if (out) {
+          __stcg(mine + 32 * 4 * NG, make_float4(m[nt][0], m[nt][NC - 1], 0.f, 0.f));
+          __stcg(mine + 32 * (4 * NG + 1), make_float4(fd[nt][0][0], fd[nt][NG - 1][0], fd[nt][0][NC - 1], fd[nt][NG - 1][NC - 1]));
+        }
       }
     };
     auto arrived = [&](int sl, int ph) {                          // false: the wait ran out
@@ -452,32 +488,44 @@ attn_decode_kv4_kernel(const K4Args a) {
       const bool more = u + 1 < part_end;
       if (more && !arrived(next, next_phase)) { gave_up = true; break; }
       const uint32_t unit = slot_addr(slot), next_unit = slot_addr(more ? next : slot);
-      bool raise = seen != (kOne ? 1u : (1u << (2 * NT)) - 1u);
       auto most = [](const float* x, int step) {                  // over the lane's keys
         return kOne ? x[0] : fmaxf(fmaxf(x[0], x[(KL > 1) * step]), fmaxf(x[(KL > 1) * 2 * step], x[(KL > 1) * 3 * step]));
       };
-      float top = most(&vs[0][0], NG);
-      if (NG == 2) top = fmaxf(top, most(&vs[0][NG - 1], NG));
-      raise |= top > s_limit;
+      // P, and P s in fp16: of heads 2j and 2j + 1 for each key and group, with one head of both groups
+      float p[NT][KL][NC];
+      uint32_t y[NT][kOne ? 1 : NG][KL];
+      auto weigh = [&] {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int k = 0; k < KL; ++k)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) p[nt][k][c] = k4_exp2(s[nt][k][c]);
+      };
+      auto products = [&] {                                       // returns the largest two
+        uint32_t top = 0u;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int g = 0; g < (kOne ? 1 : NG); ++g)
+#pragma unroll
+            for (int k = 0; k < KL; ++k) {
+              y[nt][g][k] = kOne ? k4_f16x2(p[nt][k][0] * fd[nt][0][0] * vs[k][0], NG == 2 ? p[nt][k][0] * fd[nt][NG - 1][0] * vs[k][NG - 1] : 0.f)
+                                 : k4_f16x2(p[nt][k][0] * fd[nt][g][0] * vs[k][g], p[nt][k][NC - 1] * fd[nt][g][NC - 1] * vs[k][g]);
+              top = k4_max2(top, y[nt][g][k]);
+            }
+        return top;
+      };
+      weigh();
+      bool raise = seen != (kOne ? 1u : (1u << (2 * NT)) - 1u) || k4_beyond(products());
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int c = 0; c < NC; ++c)
           raise |= most(&s[nt][0][c], NC) > (float)kK4Lag;
       if (__any_sync(0xffffffffu, raise)) {
-        // rare: the maxima in use go up to what has been seen, and so does 2^E
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        float corr_e = 1.f;
-        if (top > s_limit) {
-          const int en = max(-100, min(120, (int)(__float_as_uint(top) >> 23) - 127));
-          if (en > E) {
-            corr_e = E == -200 ? 1.f : k4_pow2(max(-126, E - en));
-            E = en;
-            down_e = k4_pow2(-E);
-            s_limit = k4_pow2(min(127, E + 4));
-          }
-        }
+        // rare: the maxima in use go up to what has been seen, and powers of two come down from what they make too large
+        float fix[NT][NG][NC];                                    // what that makes of the accumulators
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -487,69 +535,79 @@ attn_decode_kv4_kernel(const K4Args a) {
             for (int o = kOne ? 1 : 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
             // up by mx (the first time: to it, wherever it is); a head without a finite score yet stays
             const bool known = (seen >> (2 * nt + c)) & 1u, finite = mx > -INFINITY && mx < INFINITY;
-            const float by = finite && (!known || mx > 0.f) ? mx : 0.f;
-            const float corr = known ? k4_exp2(-by) : 1.f;
+            const float by = finite && (!known || mx > 0.f) ? mx : 0.f, up = known ? by : 0.f;
+            const float corr = k4_exp2(-up);
             if (finite) seen |= 1u << (2 * nt + c);
             m[nt][c] += by;
 #pragma unroll
             for (int k = 0; k < KL; ++k) s[nt][k][c] -= by;
             l_run[nt][c] *= corr;
+            // the weights met so far are that much smaller from now on: their power of two makes up for it as far as it may, so
+            // that their likes keep their bits, and the sums take the rest
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
               zacc[nt][g][c] *= corr;
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                acc[nt][g][i][c] *= corr * corr_e;
-                acc[nt][g][i][2 + c] *= corr * corr_e;
-                if (kOne) { acc[nt][g][i][1] *= corr * corr_e; acc[nt][g][i][3] *= corr * corr_e; }
-              }
+              const int e = k4_exponent(fd[nt][g][c]), go = min((int)fminf(up, 250.f), kK4Begin - e);
+              fix[nt][g][c] = k4_exp2((float)go - up);
+              fd[nt][g][c] = k4_pow2(e + go);
             }
           }
+        weigh();
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+              float w = 0.f;                                      // the largest P s (a NaN is none)
+#pragma unroll
+              for (int k = 0; k < KL; ++k) w = fmaxf(w, p[nt][k][c] * vs[k][g]);
+#pragma unroll
+              for (int o = kOne ? 1 : 4; o < 32; o <<= 1) w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, o));
+              // (an infinite one that is not p's fault is 2^128 and a little more, which fits, too)
+              const int e = k4_exponent(fd[nt][g][c]), to = w * fd[nt][g][c] >= k4_pow2(kK4Most) ? kK4Put - k4_exponent(w) : e;
+              fix[nt][g][c] *= k4_pow2(max(-126, to - e));
+              fd[nt][g][c] = k4_pow2(to);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              acc[nt][g][i][0] *= fix[nt][g][0];
+              acc[nt][g][i][1] *= fix[nt][g][NC - 1];             // (with one head all columns are its own)
+              acc[nt][g][i][2] *= fix[nt][g][0];
+              acc[nt][g][i][3] *= fix[nt][g][NC - 1];
+            }
+          }
+        products();
       }
-      // ---- P, and O^T += V^T (P s)^T tile by tile: lane's row pairs j and j + 4, its dims 64 g + 8 r .. + 7
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int k = 0; k < KL; ++k)
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            l_run[nt][c] += p[nt][k][c];
+#pragma unroll
+            for (int g = 0; g < NG; ++g) zacc[nt][g][c] = fmaf(p[nt][k][c], vz[k][g], zacc[nt][g][c]);
+          }
+      // ---- O^T += V^T (P s)^T tile by tile: lane's row pairs j and j + 4, its dims 64 g + 8 r .. + 7
       // With one head, the lanes of row r hold P s of keys 0 r, r + 8, 16 + r and 24 + r, one pair (the two groups) each, in
       // columns 4 h + 2 i + g.  For tile h the columns of the other tile are made zero; what the rest of them add up to
       // nobody reads: the sums of group g are in columns g (tile 0) and 4 + g (tile 1).
       uint32_t one[2] = {0u, 0u};
       if (kOne) {
-        const float p = k4_exp2(s[0][0][0]);
-        l_run[0][0] += p;
-#pragma unroll
-        for (int g = 0; g < NG; ++g) zacc[0][g][0] = fmaf(p, vz[0][g], zacc[0][g][0]);
-        const uint32_t y = k4_f16x2(p * (vs[0][0] * down_e), NG == 2 ? p * (vs[0][NG - 1] * down_e) : 0.f);
-        one[0] = k4_transpose(y);
-        one[1] = k4_transpose(__shfl_xor_sync(0xffffffffu, y, 1));
+        one[0] = k4_transpose(y[0][0][0]);
+        one[1] = k4_transpose(__shfl_xor_sync(0xffffffffu, y[0][0][0], 1));
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         uint32_t pb[NT][NG][2];
-        if (kOne) {
 #pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            pb[0][g][0] = (r >> 2) == h ? one[0] : 0u;
-            pb[0][g][1] = (r >> 2) == h ? one[1] : 0u;
-          }
-        }
-#pragma unroll
-        for (int nt = 0; nt < (kOne ? 0 : NT); ++nt) {
-          float p[2][2];
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-              p[i][c] = k4_exp2(s[nt][(2 * h + i) % KL][c]);
-              l_run[nt][c] += p[i][c];
-            }
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int g = 0; g < NG; ++g)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const float f = vs[(2 * h + i) % KL][g] * down_e;
-#pragma unroll
-              for (int c = 0; c < NC; ++c) zacc[nt][g][c] = fmaf(p[i][c], vz[(2 * h + i) % KL][g], zacc[nt][g][c]);
-              pb[nt][g][i] = k4_transpose(k4_f16x2(p[i][0] * f, p[i][1] * f));
-            }
-        }
+            for (int i = 0; i < 2; ++i)
+              pb[nt][g][i] = kOne ? ((r >> 2) == h ? one[i] : 0u) : k4_transpose(y[nt][g % (kOne ? 1 : NG)][(2 * h + i) % KL]);
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
           const uint32_t va = unit + h * F::TILE;
@@ -580,7 +638,6 @@ attn_decode_kv4_kernel(const K4Args a) {
 
     // ================ finish the part
     if (u - max(seg0, u0) > kK4Flush) flush(true, false);
-    const float up = E == -200 ? 0.f : k4_pow2(E);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -611,6 +668,7 @@ attn_decode_kv4_kernel(const K4Args a) {
         for (int g = 0; g < NG; ++g)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
+            const float up = k4_pow2(-k4_exponent(fd[nt][g][c]));
             o[g][2 * i] = fmaf(acc[nt][g][i][c] * 16777216.f, up, zacc[nt][g][c]);
             o[g][2 * i + 1] = fmaf(acc[nt][g][i][2 + c] * 1048576.f, up, zacc[nt][g][c]);
           }
