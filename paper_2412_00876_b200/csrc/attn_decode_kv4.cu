@@ -262,7 +262,7 @@ attn_decode_kv4_kernel(const K4Args a) {
   int b = k4_find(pre, a.pg.B, u0);
   int units = k4_units(rows[b]), hk = (u0 - pre[b]) / units, t = (u0 - pre[b]) - hk * units;
   int slot = 0, phase = 0;
-  bool gave_up = false;                                           // a wait ran out
+  bool gave_up = false;                                           // a wait ran out (the lane's own, until the warp has agreed)
   for (int u = u0; u < u1;) {
     // ================ one (sequence, K/V head), or the part of it that lies in this range
     const int n = rows[b], seg0 = u - t, seg1 = seg0 + units, part_end = min(seg1, u1);
@@ -477,16 +477,15 @@ attn_decode_kv4_kernel(const K4Args a) {
       return mbar_try_wait(smem_u32(&bars[sl]), ph) || mbar_wait(smem_u32(&bars[sl]), ph, abort_flag);
     };
     auto slot_addr = [&](int sl) { return smem_u32(ring + (size_t)sl * (2 * F::TILE)); };
+    // (After a wait that ran out the products are of whatever the slot holds, up to the vote.)
     gave_up = !arrived(slot, phase);
-    if (!gave_up) {
-      key_products(slot_addr(slot));
-      scores(slot_addr(slot), n - t * kK4Unit, (here >> (2 * slot)) & 3u);
-    }
-    for (; !gave_up; ++u, ++t) {
+    key_products(slot_addr(slot));
+    scores(slot_addr(slot), n - t * kK4Unit, (here >> (2 * slot)) & 3u);
+    for (;; ++u, ++t) {
       int next = slot + 1, next_phase = phase;
       if (next == NS) { next = 0; next_phase ^= 1; }
       const bool more = u + 1 < part_end;
-      if (more && !arrived(next, next_phase)) { gave_up = true; break; }
+      if (more && !arrived(next, next_phase)) gave_up = true;
       const uint32_t unit = slot_addr(slot), next_unit = slot_addr(more ? next : slot);
       auto most = [](const float* x, int step) {                  // over the lane's keys
         return kOne ? x[0] : fmaxf(fmaxf(x[0], x[(KL > 1) * step]), fmaxf(x[(KL > 1) * 2 * step], x[(KL > 1) * 3 * step]));
@@ -517,13 +516,14 @@ attn_decode_kv4_kernel(const K4Args a) {
         return top;
       };
       weigh();
-      bool raise = seen != (kOne ? 1u : (1u << (2 * NT)) - 1u) || k4_beyond(products());
+      bool raise = gave_up || seen != (kOne ? 1u : (1u << (2 * NT)) - 1u) || k4_beyond(products());
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int c = 0; c < NC; ++c)
           raise |= most(&s[nt][0][c], NC) > (float)kK4Lag;
       if (__any_sync(0xffffffffu, raise)) {
+        if (!warp_agreed(!gave_up)) { gave_up = true; break; }
         // rare: the maxima in use go up to what has been seen, and powers of two come down from what they make too large
         float fix[NT][NG][NC];                                    // what that makes of the accumulators
 #pragma unroll
@@ -634,7 +634,7 @@ attn_decode_kv4_kernel(const K4Args a) {
       if (!more) { ++u; ++t; break; }
       scores(next_unit, n - (t + 1) * kK4Unit, (here >> (2 * next)) & 3u);
     }
-    if (__any_sync(0xffffffffu, gave_up)) break;
+    if (gave_up) break;                                           // (the whole warp)
 
     // ================ finish the part
     if (u - max(seg0, u0) > kK4Flush) flush(true, false);
@@ -711,7 +711,7 @@ attn_decode_kv4_kernel(const K4Args a) {
       }
     }
   }
-  if (__any_sync(0xffffffffu, gave_up)) {
+  if (gave_up) {
     if (lane == 0) report_status(a.status, DL_ERR_TIMEOUT, blockIdx.x);
     // copies still in flight must land before the CTA's shared memory goes: the last NS tiles requested
     for (int v = max(u0, p_u - NS); v < p_u; ++v)

@@ -65,6 +65,9 @@ __device__ __forceinline__ bool mbar_wait_spin(uint32_t bar, uint32_t parity, vo
   *abort = 1;
   return false;
 }
+// One answer for a whole warp whose lanes have waited each for itself: true if none of them gave up.  Lanes may leave a loop
+// of votes, shuffles or matrix instructions on nothing else: a wait that runs out may do so for some of them only.
+__device__ __forceinline__ bool warp_agreed(bool ok) { return __all_sync(0xffffffffu, ok); }
 // 1-D bulk copy global -> shared; both addresses 16-byte aligned, bytes a multiple of 16.
 __device__ __forceinline__ void bulk_g2s(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"

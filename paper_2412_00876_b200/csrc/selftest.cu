@@ -22,7 +22,12 @@ __global__ void wait_timeout_kernel(int polls, DeviceStatus* st) {
   const bool ok = mbar_wait(smem_u32(&bar), 0, abort_flag, polls);
   // a second waiter sees the raised flag and leaves at once, as the roles of a pipelined kernel do
   const bool ok2 = mbar_wait(smem_u32(&bar), 0, abort_flag, polls);
-  if (threadIdx.x == 0 && !ok && !ok2 && *abort_flag) report_status(st, DL_ERR_TIMEOUT, 0x5e1f);
+  // lanes that got different answers leave a loop of votes together
+  const bool mine = (threadIdx.x & 1) == 0 || ok;
+  int turns = 0;
+  while (turns < 4 && __any_sync(0xffffffffu, threadIdx.x == turns) && warp_agreed(mine)) ++turns;
+  const bool together = __all_sync(0xffffffffu, turns == 0);
+  if (threadIdx.x == 0 && !ok && !ok2 && *abort_flag && together) report_status(st, DL_ERR_TIMEOUT, 0x5e1f);
 }
 
 // One checked store one element past the end of a 64-word buffer: the checked build must skip it and record it.
