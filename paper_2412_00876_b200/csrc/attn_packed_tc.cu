@@ -330,7 +330,7 @@ attn_packed_kernel(const __grid_constant__ PkMaps maps, const PkArgs a) {
   } else if (warp == 9 || warp == 10) {
     // ---------------------------------------------------------------- MMA issuer of one lane
     // The whole warp walks the loop, so that counters and descriptors stay warp-uniform, and one elected lane issues: an MMA
-    // is then an instruction or two.
+    // is then an instruction or two.  Its lanes wait each for itself, so the warp agrees before it goes on or stops.
     reg_dec<kPkRegsSmall>();
     {
       const int x = warp - 9;
@@ -342,12 +342,14 @@ attn_packed_kernel(const __grid_constant__ PkMaps maps, const PkArgs a) {
       PkWalker W(a);
       PkItem I;
       int n_item = 0, g0 = 0, ring0 = 0;               // this lane's items and key tiles, the ring's tiles so far
-      while (!*abort_flag && W.next(I)) {
+      bool ok = true, stop = false;                    // this lane's waits so far; the warp has agreed to stop
+      auto wait = [&](uint32_t b, uint32_t parity) { ok = mbar_wait_spin(b, parity & 1u, abort_flag) && ok; };
+      while (!stop && W.next(I)) {
         const PkLane L = pk_lane(a, I, x);
         const int n_sub = L.exists ? L.n_tiles : 0;
         auto full = [&](int u, int is_v) {             // waits for K_u or V_u; returns its slot
           const int t = ring0 + 2 * u + is_v;
-          mbar_wait_spin(kv_full(t % kPkSlots), (uint32_t)(t / kPkSlots) & 1u, abort_flag);
+          wait(kv_full(t % kPkSlots), (uint32_t)(t / kPkSlots));
           return t % kPkSlots;
         };
         for (int u = -1; u < n_sub; ++u) {
@@ -355,14 +357,13 @@ attn_packed_kernel(const __grid_constant__ PkMaps maps, const PkArgs a) {
           const bool has_pv = u >= 0, has_qk = u + 1 < n_sub;
           const int g = g0 + u;
           int sv = 0, sk = 0;
-          if (!has_pv) mbar_wait_spin(bar(x, Q_FULL), (uint32_t)n_item & 1u, abort_flag);
+          if (!has_pv) wait(bar(x, Q_FULL), (uint32_t)n_item);
           if (has_pv) sv = full(u, 1);
           if (has_qk) sk = full(u + 1, 0);
-          if (u == 0) mbar_wait_spin(bar(x, O_FREE), ((uint32_t)n_item & 1u) ^ 1u, abort_flag);   // previous item's O has been read
-          if (has_pv) mbar_wait_spin(bar(x, P_HALF), (uint32_t)g & 1u, abort_flag);
-          __syncwarp();
+          if (u == 0) wait(bar(x, O_FREE), (uint32_t)n_item ^ 1u);            // previous item's O has been read
+          if (has_pv) wait(bar(x, P_HALF), (uint32_t)g);
+          if (!warp_agreed(ok)) { stop = true; break; }
           tc_fence_after();
-          if (*abort_flag) break;
           const uint64_t vd = v_desc + (uint64_t)uniform32((uint32_t)sv * (S::TILE >> 4));
           const uint64_t kd = kv_desc + (uint64_t)uniform32((uint32_t)sk * (S::TILE >> 4));
           const uint32_t ksteps = has_pv ? uniform32((uint32_t)pk_cols(L, u) >> 4) : 0u, acc = uniform32(u != 0);
@@ -374,7 +375,7 @@ attn_packed_kernel(const __grid_constant__ PkMaps maps, const PkArgs a) {
                 if (ks < ksteps) mma_ts(t_o, t_s + ks * 8, vd + ks * (2048 >> 4), idesc_pv, ks == 0 ? acc : 1u);
             }
             __syncwarp();
-            mbar_wait_spin(bar(x, P_FULL), (uint32_t)g & 1u, abort_flag);
+            wait(bar(x, P_FULL), (uint32_t)g);         // (agreed on at the next turn: a vote here costs 0.5 % of long prompts)
             __syncwarp();
             tc_fence_after();
           }
@@ -400,13 +401,12 @@ attn_packed_kernel(const __grid_constant__ PkMaps maps, const PkArgs a) {
           __syncwarp();
         }
         // tiles that only the other lane uses: this lane's share of the release, in the ring's order
-        for (int u = n_sub; u < I.n_kv && !*abort_flag; ++u) {
+        for (int u = n_sub; u < I.n_kv && !stop; ++u) {
           const int sk = full(u, 0);
-          if (*abort_flag) break;
-          if (lane == 0) mbar_arrive(kv_empty(sk));
+          if (lane == 0 && ok) mbar_arrive(kv_empty(sk));
           const int sv = full(u, 1);
-          if (*abort_flag) break;
-          if (lane == 0) mbar_arrive(kv_empty(sv));
+          if (lane == 0 && ok) mbar_arrive(kv_empty(sv));
+          stop = !warp_agreed(ok);
         }
         ring0 += 2 * I.n_kv;
         g0 += n_sub;

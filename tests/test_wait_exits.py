@@ -4,8 +4,6 @@ off the sources, since a GPU that meets the fault may hang."""
 import os
 import re
 
-import pytest
-
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2412_00876_b200", "csrc")
 
 
@@ -30,3 +28,11 @@ def test_decode_over_4_bits_leaves_its_loops_together():
     for part in body.split("arrived(")[2:]:
         until = part[:part.index("warp_agreed(!gave_up)")] if "warp_agreed(!gave_up)" in part else part
         assert not re.search(r"if \(!?gave_up\)|\(; *!gave_up", until), "a branch on a lane's own wait"
+
+
+def test_packed_prompts_issue_matrix_instructions_together():
+    text = code("attn_packed_tc.cu")
+    issuers = text[text.index("} else if (warp == 9 || warp == 10) {"):text.index("} else if (warp < 8) {")]
+    assert issuers.count("warp_agreed(ok)") >= 2 and "pk_elect()" in issuers
+    assert not exits_on(issuers, r"\*abort_flag"), "a lane leaves on what it has read for itself"
+    assert not re.search(r"mbar_wait_spin\((?!b, parity)", issuers), "a wait whose answer is lost"
