@@ -240,6 +240,8 @@ def _rows(t, dtype, shape, what: str, index: int):
     s0, s1, s2 = t.stride()
     if shape[0] > 0 and (s2 != 1 or (s1 != shape[2] and shape[1] > 1)):
         raise ValueError(f"{what}: want rows with dense heads, got strides {t.stride()}")
+    if shape[0] > 1 and s0 < shape[1] * shape[2]:                    # (0 would mean dense rows to the library)
+        raise ValueError(f"{what}: rows must not overlap, got strides {t.stride()}")
     return t.data_ptr(), (s0 if shape[0] > 1 else shape[1] * shape[2])
 
 
