@@ -462,9 +462,16 @@ class Context:
                     "dl_decode_keep2")
 
     # ---- packed prompts, pages, the 4-bit cache (extensions, not in the paper)
-    # These check type, shape and device of every tensor; without `stream` they use the current one of the context's device.
+    # These check type, shape and device of every tensor, and the books' device; without `stream` they use the current one
+    # of the context's device.
     def _on(self, stream):
         return _raw_stream(self.device.index) if stream is None else stream.cuda_stream
+
+    def _books(self, pages: Pages):
+        """The books for the library, which follows their pointers on the context's device."""
+        if pages.book.get_device() != self.device.index:
+            raise ValueError(f"pages: want books on cuda:{self.device.index}, got {pages.book.device}")
+        return pages.ref
 
     def attn_prefill_packed(self, q, k, v, starts, max_rows, scale, out, stream=None):
         """dl_attn_prefill_packed: q [total, n_heads, D], k / v [total, n_kv_heads, D] (parts of one projection's output
@@ -482,13 +489,15 @@ class Context:
 
     def pages_reserve(self, pages: Pages, need, stream=None):
         """dl_pages_reserve: need int32 [B]."""
-        self._check(lib().dl_pages_reserve(self._h, pages.ref, _arg(need, torch.int32, (pages.B,), "need", self.device.index),
-                                           self._on(stream)), "dl_pages_reserve")
+        self._check(lib().dl_pages_reserve(
+            self._h, self._books(pages), _arg(need, torch.int32, (pages.B,), "need", self.device.index), self._on(stream)),
+            "dl_pages_reserve")
 
     def pages_free(self, pages: Pages, gone, stream=None):
         """dl_pages_free: gone uint8 [B]."""
-        self._check(lib().dl_pages_free(self._h, pages.ref, _arg(gone, torch.uint8, (pages.B,), "gone", self.device.index),
-                                        self._on(stream)), "dl_pages_free")
+        self._check(lib().dl_pages_free(
+            self._h, self._books(pages), _arg(gone, torch.uint8, (pages.B,), "gone", self.device.index), self._on(stream)),
+            "dl_pages_free")
 
     def _pools(self, pages: Pages, pools):
         """Count, array of pointers and bytes of a page of `pools`, tensors [n_pages, ...] that are alike."""
@@ -505,19 +514,21 @@ class Context:
 
     def pages_fork(self, pages: Pages, parent, pools, stream=None):
         """dl_pages_fork: parent int32 [B]; pools: list of tensors [n_pages, ...], one per layer."""
+        books = self._books(pages)
         n, ptrs, page_bytes = self._pools(pages, pools)
         scratch = pages.scratch(self)
         self._check(lib().dl_pages_fork(
-            self._h, pages.ref, _arg(parent, torch.int32, (pages.B,), "parent", self.device.index), n,
+            self._h, books, _arg(parent, torch.int32, (pages.B,), "parent", self.device.index), n,
             ptrs.buffer_info()[0] if n else None, page_bytes, scratch.data_ptr(), scratch.shape[0], self._on(stream)),
             "dl_pages_fork")
 
     def pages_compact(self, pages: Pages, pools, n_live=None, stream=None):
         """dl_pages_compact; n_live: int32 tensor [1] for the number of pages in use, or None."""
+        books = self._books(pages)
         n, ptrs, page_bytes = self._pools(pages, pools)
         scratch = pages.scratch(self)
         live = None if n_live is None else _arg(n_live, torch.int32, (1,), "n_live", self.device.index)
-        self._check(lib().dl_pages_compact(self._h, pages.ref, n, ptrs.buffer_info()[0] if n else None, page_bytes, live,
+        self._check(lib().dl_pages_compact(self._h, books, n, ptrs.buffer_info()[0] if n else None, page_bytes, live,
                                            scratch.data_ptr(), scratch.shape[0], self._on(stream)), "dl_pages_compact")
 
     def kv4_page_bytes(self, n_kv_heads: int, page_rows: int) -> int:
@@ -542,7 +553,7 @@ class Context:
         if ks != vs:
             raise ValueError("k and v must have the same row stride")
         self._check(lib().dl_kv4_append(
-            self._h, pages.ref, n_kv, self._pool(pages, pool, n_kv), kp, vp, ks,
+            self._h, self._books(pages), n_kv, self._pool(pages, pool, n_kv), kp, vp, ks,
             _arg(starts, torch.int32, (pages.B + 1,), "starts", i),
             None if keep is None else _arg(keep, torch.uint8, (total,), "keep", i), total, 1 if commit else 0,
             self._on(stream)), "dl_kv4_append")
@@ -552,8 +563,8 @@ class Context:
         total, n_kv, i = k_out.shape[0], k_out.shape[1], self.device.index
         shape = (total, n_kv, self.D)
         self._check(lib().dl_kv4_read(
-            self._h, pages.ref, n_kv, self._pool(pages, pool, n_kv), _arg(row0, torch.int32, (pages.B,), "row0", i),
-            _arg(starts, torch.int32, (pages.B + 1,), "starts", i), total, _arg(k_out, self.dtype, shape, "k_out", i),
+            self._h, self._books(pages), n_kv, self._pool(pages, pool, n_kv),
+            _arg(row0, torch.int32, (pages.B,), "row0", i), _arg(starts, torch.int32, (pages.B + 1,), "starts", i), total, _arg(k_out, self.dtype, shape, "k_out", i),
             _arg(v_out, self.dtype, shape, "v_out", i), self._on(stream)), "dl_kv4_read")
 
     def kv4_attn_decode(self, pages: Pages, pool, q_t, k_t, v_t, keep, scale, out, stream=None):
@@ -561,7 +572,7 @@ class Context:
         n_kv, B, i = k_t.shape[1], pages.B, self.device.index
         big, small = (B, self.H, self.D), (B, n_kv, self.D)
         self._check(lib().dl_kv4_attn_decode(
-            self._h, pages.ref, n_kv, self._pool(pages, pool, n_kv), _arg(q_t, self.dtype, big, "q_t", i),
+            self._h, self._books(pages), n_kv, self._pool(pages, pool, n_kv), _arg(q_t, self.dtype, big, "q_t", i),
             _arg(k_t, self.dtype, small, "k_t", i), _arg(v_t, self.dtype, small, "v_t", i),
             None if keep is None else _arg(keep, torch.uint8, (B,), "keep", i), scale,
             _arg(out, self.dtype, big, "out", i), self._on(stream)), "dl_kv4_attn_decode")

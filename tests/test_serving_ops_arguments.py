@@ -29,3 +29,32 @@ def test_rows_that_do_not_are_taken_with_their_stride():
     assert rows(flat[:0].view(0, 2, 64))[1] in (0, 128)
     with pytest.raises(ValueError, match="dense heads"):
         rows(flat.as_strided((10, 2, 64), (256, 128, 1)))
+
+
+class NoLibrary:
+    """Stands in for the library: a call that gets this far was not refused."""
+
+    def __getattr__(self, name):
+        def call(*a):
+            raise AssertionError(f"{name} was called")
+        return call
+
+
+@pytest.mark.parametrize("call", ["reserve", "free", "fork", "compact", "append", "read", "attend"])
+def test_books_on_another_device_are_refused(monkeypatch, call):
+    """The books' pointers go to the kernels: books of the CPU (or of another GPU) must not get there."""
+    monkeypatch.setattr(dl, "lib", lambda: NoLibrary())
+    monkeypatch.setattr(dl, "_arg", lambda t, dtype, shape, what, index: t.data_ptr())      # every other tensor is in order
+    monkeypatch.setattr(dl, "_rows", lambda t, dtype, shape, what, index: (t.data_ptr(), 0))
+    ctx = dl.Context.__new__(dl.Context)
+    ctx._h, ctx.device, ctx.dtype, ctx.H, ctx.D = None, torch.device("cuda", 0), torch.bfloat16, 2, 64
+    monkeypatch.setattr(ctx, "_on", lambda stream: 0)
+    monkeypatch.setattr(ctx, "_pools", lambda pages, pools: (0, None, 0))
+    pages, x = dl.Pages(2, 4, 2, 16, device="cpu"), torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    n = torch.zeros(3, dtype=torch.int32)
+    calls = {"reserve": lambda: ctx.pages_reserve(pages, n), "free": lambda: ctx.pages_free(pages, n),
+             "fork": lambda: ctx.pages_fork(pages, n, []), "compact": lambda: ctx.pages_compact(pages, []),
+             "append": lambda: ctx.kv4_append(pages, x, x, x, n), "read": lambda: ctx.kv4_read(pages, x, n, n, x, x),
+             "attend": lambda: ctx.kv4_attn_decode(pages, x, x, x, x, None, 1.0, x)}
+    with pytest.raises(ValueError, match="books on cuda:0, got cpu"):
+        calls[call]()
