@@ -799,8 +799,9 @@ int32_t dl_pages_compact(dl_ctx* ctx, const dl_pages* pages, int32_t n_pools, vo
   int32_t st = check_pages(ctx, pages);
   if (st == DL_OK) st = check_pools(pages, n_pools, pools, page_bytes, scratch, scratch_bytes);
   if (st != DL_OK) return st;
-  if (pages->B == 0) return DL_OK;
   DeviceGuard g(ctx->device);
+  if (pages->B == 0)                      // no sequence: no page in use
+    return n_live ? cuda_status(ctx, cudaMemsetAsync(n_live, 0, sizeof(int32_t), static_cast<cudaStream_t>(stream))) : DL_OK;
   return cuda_status(ctx, launch_pages_compact(ctx, pages, n_pools, pools, page_bytes, n_live, scratch, static_cast<cudaStream_t>(stream)));
 }
 
