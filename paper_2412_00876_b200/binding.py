@@ -564,16 +564,18 @@ class Context:
         shape = (total, n_kv, self.D)
         self._check(lib().dl_kv4_read(
             self._h, self._books(pages), n_kv, self._pool(pages, pool, n_kv),
-            _arg(row0, torch.int32, (pages.B,), "row0", i), _arg(starts, torch.int32, (pages.B + 1,), "starts", i), total, _arg(k_out, self.dtype, shape, "k_out", i),
-            _arg(v_out, self.dtype, shape, "v_out", i), self._on(stream)), "dl_kv4_read")
+            _arg(row0, torch.int32, (pages.B,), "row0", i), _arg(starts, torch.int32, (pages.B + 1,), "starts", i), total,
+            _arg(k_out, self.dtype, shape, "k_out", i), _arg(v_out, self.dtype, shape, "v_out", i), self._on(stream)),
+            "dl_kv4_read")
 
     def kv4_attn_decode(self, pages: Pages, pool, q_t, k_t, v_t, keep, scale, out, stream=None):
         """dl_kv4_attn_decode: q_t, out [B, n_heads, D]; k_t, v_t [B, n_kv_heads, D]; keep uint8 [B] or None."""
         n_kv, B, i = k_t.shape[1], pages.B, self.device.index
         big, small = (B, self.H, self.D), (B, n_kv, self.D)
         self._check(lib().dl_kv4_attn_decode(
-            self._h, self._books(pages), n_kv, self._pool(pages, pool, n_kv), _arg(q_t, self.dtype, big, "q_t", i),
-            _arg(k_t, self.dtype, small, "k_t", i), _arg(v_t, self.dtype, small, "v_t", i),
+            self._h, self._books(pages), n_kv, self._pool(pages, pool, n_kv),
+            _arg(q_t, self.dtype, big, "q_t", i), _arg(k_t, self.dtype, small, "k_t", i),
+            _arg(v_t, self.dtype, small, "v_t", i),
             None if keep is None else _arg(keep, torch.uint8, (B,), "keep", i), scale,
             _arg(out, self.dtype, big, "out", i), self._on(stream)), "dl_kv4_attn_decode")
 
