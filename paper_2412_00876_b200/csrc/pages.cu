@@ -377,8 +377,9 @@ cudaError_t launch_pages_fork(const dl_ctx* ctx, const dl_pages* p, const int32_
   const size_t rows = 2 * (size_t)p->B * p->max_pages * 4;
   if (smem + rows <= kMost) { near |= 2; smem += rows; }
   cudaError_t e = cudaSuccess;
+  // (asked for whatever this call takes: the 48 KB that a kernel has without asking also hold its static arrays)
   static int attr_set[64];
-  if (smem > 48 * 1024 && !attr_set[ctx->device & 63]) {
+  if (!attr_set[ctx->device & 63]) {
     e = cudaFuncSetAttribute(pages_fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMost);
     if (e != cudaSuccess) return e;
     attr_set[ctx->device & 63] = 1;

@@ -1,8 +1,10 @@
 """Edges of the serving calls that ordinary batches do not reach."""
+import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_serving_ops import DEV, context
+from oracle import paged_kv4 as pk
+from tests.test_gpu_serving_ops import DEV, context, i32
 
 pytestmark = pytest.mark.gpu
 
@@ -14,5 +16,85 @@ def test_compacting_the_pages_of_no_sequence_says_that_none_is_in_use():
     ctx.pages_compact(pg, [], live)
     assert live.item() == 0
     ctx.pages_compact(pg, [])
+    assert ctx.device_status()[0] == 0
+    ctx.close()
+
+
+@pytest.mark.parametrize("n_pages", [12100, 12120, 12168, 12184, 12185, 12300])
+def test_fork_with_books_of_about_48_kb(n_pages):
+    """The shared memory of the bookkeeping on either side of what a kernel may have without asking for more."""
+    dl, ctx = context(4, 64)
+    pg = dl.Pages(8, n_pages, 4, 16, DEV)
+    pg.table[0, :2] = i32([3, n_pages - 1])
+    pg.refs[[3, n_pages - 1]] = 1
+    pg.cache_len[0] = 20
+    pool = torch.arange(n_pages, device=DEV).to(torch.int32).repeat_interleave(4).view(n_pages, 4).contiguous()
+    ctx.pages_fork(pg, i32([0, 0, 2, 3, 4, 5, 6, 7]), [pool])
+    assert pg.table[:2].tolist() == [[3, n_pages - 1, -1, -1], [3, 0, -1, -1]]
+    assert pg.cache_len.tolist() == [20, 20] + [0] * 6 and pool[0].tolist() == [n_pages - 1] * 4
+    assert ctx.device_status()[0] == 0
+    ctx.close()
+
+
+@pytest.mark.parametrize("B,n_pages,width", [(2048, 30000, 16), (300, 50000, 20), (300, 20000, 100), (2048, 9000, 4), (2048, 50000, 16)])
+def test_books_that_shared_memory_does_not_hold(B, n_pages, width):
+    """Fork, reserve, free and compact with counts, rows or both in global memory; and a fork that finds too few pages."""
+    dl, ctx = context(4, 64, B=B)
+    rng = np.random.default_rng(B)
+    page = 16
+    rows = rng.integers(0, (width - 1) * page, B)
+    order, at, pages = rng.permutation(n_pages).tolist(), 0, []
+    room = n_pages * 3 // 4
+    for b in range(B):
+        c = min(-(-int(rows[b]) // page), max(0, room - at))
+        rows[b] = min(rows[b], c * page)
+        pages.append(order[at:at + c])
+        at += c
+    o = pk.Books(n_pages, page, width, pages, rows.tolist(), list(range(n_pages)))
+    pg = dl.Pages(B, n_pages, width, page, DEV)
+    pg.table.copy_(i32(o.table()))
+    pg.refs.copy_(i32(o.refs()))
+    pg.cache_len.copy_(i32(o.length))
+    pool = torch.arange(n_pages, device=DEV).to(torch.int32).repeat_interleave(4).view(n_pages, 4).contiguous()
+
+    def agree():
+        assert np.array_equal(pg.table.cpu().numpy(), o.table())
+        assert pg.refs.tolist() == o.refs() and pg.cache_len.tolist() == o.length
+        assert torch.equal(pool[:, 0].cpu(), torch.tensor(o.data, dtype=torch.int32))
+
+    parent = np.where(rng.random(B) < 0.6, np.arange(B), rng.integers(-1, B, B))
+    assert o.fork(parent.tolist())
+    ctx.pages_fork(pg, i32(parent), [pool])
+    agree()
+    need = rng.integers(0, page, B)
+    ok = o.reserve(need.tolist())
+    ctx.pages_reserve(pg, i32(need))
+    assert ctx.device_status()[0] == (0 if ok else dl.DL_ERR_CAPACITY)
+    agree()
+    # no free page is left: a fork that has to copy changes nothing
+    free = (pg.refs == 0)
+    was, bytes_was = pg.book.clone(), pool.clone()
+    pg.refs[free] = 1
+    full = pg.book.clone()
+    src = int(np.argmax([n % page != 0 for n in o.length]))
+    parent = np.where(np.arange(B) % 2 == 0, src, np.arange(B))
+    ctx.pages_fork(pg, i32(parent), [pool])
+    lost = sum(len(o.pages[b]) for b in range(0, B, 2))
+    if ctx.device_status() == (dl.DL_ERR_CAPACITY, -1):
+        assert torch.equal(pg.book, full) and torch.equal(pool, bytes_was)
+        pg.book.copy_(was)
+    else:
+        assert lost > 0                                           # what the others gave back was enough
+        pg.book.copy_(was)
+        pool.copy_(bytes_was)
+    gone = rng.random(B) < 0.5
+    o.release(gone)
+    ctx.pages_free(pg, torch.tensor(gone, dtype=torch.uint8, device=DEV))
+    live = torch.zeros(1, dtype=torch.int32, device=DEV)
+    n = o.compact()
+    ctx.pages_compact(pg, [pool], live)
+    assert live.item() == n
+    assert np.array_equal(pg.table.cpu().numpy(), o.table()) and pg.refs.tolist() == o.refs()
+    assert torch.equal(pool[:n, 0].cpu(), torch.tensor(o.data[:n], dtype=torch.int32))
     assert ctx.device_status()[0] == 0
     ctx.close()
