@@ -830,12 +830,11 @@ static cudaError_t k4_launch(const dl_ctx* ctx, K4Args& a, cudaStream_t s) {
   const size_t smem = (size_t)kK4Warps * ns * (2 * Kv4<D>::TILE + 8) + pre_bytes;
   auto kernel = attn_decode_kv4_kernel<D, NT, kOne>;
   cudaError_t e = cudaSuccess;
-  static int attr_set[64];                                        // the most asked for so far on a device
-  int& most = attr_set[ctx->device & 63];
-  if (most < (int)smem) {
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  static int attr_set[64];                                        // (all calls ask for the same: two threads may)
+  if (!attr_set[ctx->device & 63]) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, per_cta - 256);
     if (e != cudaSuccess) return e;
-    most = (int)smem;
+    attr_set[ctx->device & 63] = 1;
   }
   const int grid = ctx->sm_count * kCtas;
   a.grid_warps = grid * kK4Warps;

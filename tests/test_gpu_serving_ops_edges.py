@@ -98,3 +98,47 @@ def test_books_that_shared_memory_does_not_hold(B, n_pages, width):
     assert torch.equal(pool[:n, 0].cpu(), torch.tensor(o.data[:n], dtype=torch.int32))
     assert ctx.device_status()[0] == 0
     ctx.close()
+
+
+FIRST_CALLS = """
+import threading, torch
+from paper_2412_00876_b200 import binding as dl
+
+def one(H, Hk, D, B, ready, out, errors):
+    try:
+        torch.cuda.set_device(0)
+        ctx = dl.Context(64, H, D, 64, torch.bfloat16, 0, max_batch=B, cap=64)
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            pg = dl.Pages(B, B, 1, 16)
+            pool = ctx.kv4_pool(pg, Hk)
+            q, k = torch.ones(B, H, D, device="cuda").bfloat16(), torch.ones(B, Hk, D, device="cuda").bfloat16()
+            o = torch.zeros_like(q)
+            s.synchronize()
+            ready.wait()
+            ctx.kv4_attn_decode(pg, pool, q, k, k, None, 0.1, o)
+            s.synchronize()
+        out.append(bool((o == 1).all()) and ctx.device_status()[0] == 0)
+    except Exception as e:
+        errors.append(repr(e))
+
+for H, Hk, D in ((2, 2, 64), (2, 1, 64), (16, 1, 64), (2, 2, 128), (2, 1, 128), (16, 1, 128)):
+    sizes = (1, 2000, 1, 2000, 300, 1, 2000, 600)
+    ready, out, errors = threading.Barrier(len(sizes)), [], []
+    threads = [threading.Thread(target=one, args=(H, Hk, D, B, ready, out, errors)) for B in sizes]
+    for t in threads: t.start()
+    for t in threads: t.join()
+    assert not errors and out == [True] * len(sizes), (H, Hk, D, out, errors)
+print("first calls agree")
+"""
+
+
+def test_first_calls_from_several_threads():
+    """Batches of different sizes ask for different amounts of shared memory: the first calls of a form, from threads with a
+    context and a stream each, must not leave a smaller limit behind one another's launches."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], capture_output=True, text=True, cwd=root, timeout=300)
+    assert r.returncode == 0 and "first calls agree" in r.stdout, r.stdout[-2000:] + r.stderr[-2000:]
