@@ -434,7 +434,8 @@ attn_packed_kernel(const __grid_constant__ PkMaps maps, const PkArgs a) {
       if (!L.exists) { ring0 += 2 * I.n_kv; g_twin += n_twin; continue; }
       const int pos = L.q0 + (row >> a.p_shift);                       // this thread's position
       const int r0 = L.q0 + w_pos;                                     // the warp's first position
-      float m_used = -INFINITY, l_run = 0.f;
+      // (below every score but -inf, and finite: keys that score -inf weigh 0 against it, were they all that came so far)
+      float m_used = -3.402823466e38f, l_run = 0.f;
       const int n_sub = L.n_tiles;
       const int twin0 = n_sub >= kPkTurnTiles ? g_twin : -(1 << 30);   // short items do not wait
       for (int u = 0; u < n_sub; ++u) {

@@ -4,7 +4,8 @@ import pytest
 import torch
 
 from oracle import paged_kv4 as pk
-from tests.test_gpu_serving_ops import DEV, context, i32
+from paper_2412_00876_b200 import workloads as wl
+from tests.test_gpu_serving_ops import DEV, bf, close, context, i32, up
 
 pytestmark = pytest.mark.gpu
 
@@ -142,3 +143,23 @@ def test_first_calls_from_several_threads():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", FIRST_CALLS], capture_output=True, text=True, cwd=root, timeout=300)
     assert r.returncode == 0 and "first calls agree" in r.stdout, r.stdout[-2000:] + r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("D,first", [(64, 128), (128, 128), (128, 300), (128, 40)])
+def test_packed_rows_whose_first_keys_score_minus_infinity(D, first):
+    """Keys of infinite size that score -inf for every query weigh nothing, however many come first; a row that sees no other
+    is NaN."""
+    H, Hk, n = 4, 2, 600
+    dl, ctx = context(H, D)
+    rng = np.random.default_rng(first)
+    q, k, v = bf(rng, n, H, D), bf(rng, n, Hk, D), bf(rng, n, Hk, D)
+    q[:, :, 0] = -1.0
+    k[:first, :, 0] = np.inf
+    out = torch.zeros((n, H, D), dtype=torch.bfloat16, device=DEV)
+    ctx.attn_prefill_packed(up(q), up(k), up(v), i32([0, n]), n, D ** -0.5, out)
+    got = wl.from_torch(out)
+    assert np.isnan(got[:first]).all()
+    args = q[first:], k[first:], v[first:], [0, n - first], D ** -0.5
+    close(got[first:], pk.attention_packed(*args), pk.attention_packed(args[0], args[1], np.abs(args[2]), *args[3:]), "rows behind")
+    assert ctx.device_status()[0] == 0
+    ctx.close()
