@@ -86,7 +86,9 @@ int32_t dl_create(dl_ctx** out, int32_t device, const dl_model_desc* desc);
 int32_t dl_destroy(dl_ctx* ctx);
 
 /* Bytes of scratch the calls below need for up to `max_batch` sequences, `max_rows` predictor
- * rows per call (B * n_vis_max in prefill) and caches of `cap` rows.  Negative on bad args. */
+ * rows per call (B * n_vis_max in prefill) and caches of `cap` rows.  Negative on bad args.
+ * For bf16 models this includes the parts of dl_kv4_attn_decode, whatever the sizes: 32 MB with 16
+ * heads of 128 or more on 148 multiprocessors, less with fewer or smaller heads. */
 int64_t dl_workspace_bytes(const dl_ctx* ctx, int32_t max_batch, int32_t max_rows, int32_t cap);
 
 /* Hands the context its scratch (dev, 256-byte aligned, caller keeps ownership) and clears the

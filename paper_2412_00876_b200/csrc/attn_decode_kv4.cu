@@ -25,8 +25,8 @@
 // (An operand of V that keeps the high dims' bits above its own, their sum taken off at the end, is one operation less per
 // word and 1 % faster, but sums 17 times as large lose too many bits on long rows: 0.0088 instead of 0.0018 of the outputs.)
 // With one query head per K/V head the eight columns hold the same q, so that the four lanes of a row of the products can
-// take one key each of a unit's four instead of all the same four: 225 instructions a tile where the general form takes 280
-// (32 x 784 rows of 32 heads of 128: 34.3 -> 30.7 us).
+// take one key each of a unit's four instead of all the same four: 230 instructions a tile where the general form takes 294
+// (32 x 784 rows of 32 heads of 128: 36.9 -> 32.8 us).
 //
 // Work: the units (32 rows: two tiles) of all (sequence, K/V head) pairs in one line, cut into equal ranges, one per warp:
 // every warp streams the same number of units whatever the lengths are, through its own ring (one bulk copy per
@@ -50,16 +50,16 @@ struct K4Args {
 };
 
 constexpr int kK4Warps = 4;              // warps per CTA
-// CTAs per SM by blocks of 8 query heads: what their registers allow
+// CTAs per SM by blocks of 8 query heads: what their registers allow.  (16 heads take 70 ps a row and K/V head where 8 take 36: as
+// much as two passes of 8 would, at half of their bytes.)
 __host__ __device__ constexpr int k4_ctas(int nt) { return nt == 1 ? 3 : 2; }
 constexpr int kK4Lag = 8;                // log2 units by which the maximum in use may lag
 constexpr int kK4Unit = 32;              // rows of a unit: two tiles
-constexpr int kK4MinUnits = 1;           // fewest units worth a warp of its own
 constexpr int kK4MergeWarps = 16;        // most warps of a joining CTA
 
 // Units after which a part's sums leave the matrix accumulators: those cut every addition off (at 2^-23 of the sum), so a
 // sum of many positive terms comes out too small, in proportion to their number.  (600k rows, 8 heads: an error of 0.0040 of
-// the outputs without, 0.0018 with this; 4 x 100k rows 55.4 -> 56 us, every 16 units 57.3.)
+// the outputs without, 0.0018 with this; 4 x 60-131k rows 57.6 -> 57.8 us, every 16 units 59.2.)
 constexpr int kK4Flush = 32;
 // floats a lane keeps of them: the accumulators, the maxima in use, the powers of two in use
 template <int D> __host__ __device__ constexpr int k4_keep(int nt) { return nt * (D / 4 + 8); }
@@ -111,7 +111,7 @@ __device__ __forceinline__ int k4_find(const int* pre, int B, int u) {
   return lo;
 }
 // the line of `total` units as W ranges
-__device__ __forceinline__ int k4_width(int total, int grid_warps) { return max(1, min(grid_warps, total / kK4MinUnits)); }
+__device__ __forceinline__ int k4_width(int total, int grid_warps) { return max(1, min(grid_warps, total)); }
 __device__ __forceinline__ int k4_range(int w, int total, int W) { return (int)((long long)w * total / W); }
 __device__ __forceinline__ int k4_owner(int u, int total, int W) { return (int)((((long long)u + 1) * W - 1) / total); }
 

@@ -14,13 +14,14 @@
 //                   P in order behind it
 //   warps 0-3/4-7 : softmax and epilogue of lane A / B, one row per thread
 //   warp 11       : allocates tensor memory (512 columns: O_A | S_A | O_B | S_B); the first CTA's checks `starts`
-// A lane is a chain: softmax, P V and Q K^T, softmax; tensor memory has no room for a second score buffer.  So the two
+// A lane is a chain: softmax, P V and Q K^T, softmax; with head_dim 128 tensor memory has no room for a second score buffer
+// (with 64, whose O takes half of its columns, a quarter of it is unused).  So the two
 // lanes have to be half a period apart, and every link counts.  On 8192 tokens (32 heads, 8 of K/V), TFLOP/s: 611 with
 // the MMAs issued by a single lane's code (operands moved to uniform registers one by one, 135 cycles an MMA), 800 with the
 // issuing warp uniform, 930 without cubics for a part of the exponentials (the special-function unit is not what is
 // short), 1055 with the passes taking turns, the maximum only looked for where a sum shows that it is needed, and an
-// elected lane issuing, 1130 with the first half of P handed over early.  Without any softmax the same kernel reaches
-// 1635.  Two threads per row (16 softmax warps): 900.
+// elected lane issuing, 1112 with the first half of P handed over early (two such sequences 1170, eight, over 4 ms, 1025;
+// four with head_dim 64: 669).  Without any softmax the same kernel reaches 1635.  Two threads per row (16 softmax warps): 900.
 // The last tile of a lane uses N = its keys rounded up to 16; where that reaches past the sequence's end, the softmax
 // warps zero those V rows in shared memory first (0 * x must stay 0 for any bit pattern of a neighbour's rows).
 // Every wait is bounded (pipeline.cuh); an abort leaves DL_ERR_TIMEOUT in the status word.
@@ -40,8 +41,12 @@ constexpr int kPkBM = 128, kPkBN = 128;
 constexpr int kPkRegsSmall = 40, kPkRegsSoftmax = 232;
 static_assert(128 * kPkRegsSmall + 256 * kPkRegsSoftmax <= 384 * 168, "more registers than the launch has");
 constexpr float kPkFar = 1048576.f, kPkFarLog2 = 14.f; // a half row's sum, and a score's lead, above which the maximum is looked for again
-constexpr int kPkPatience = 4000;                      // polls a softmax warp waits for its turn
-constexpr int kPkTurnTiles = 4;                        // items of at least so many key tiles take turns at the softmax
+// Polls a softmax warp waits for its turn (300 and 60000 take the same time within 2 %), and the key tiles from which on an
+// item takes turns: 24k rows of 32 / 8 heads in sequences of 700, 1024 and 2048 take 196, 240 and 398 us from 1, 2 or 4 on,
+// 206, 252 and 410 from 8 on, 206, 260 and 450 without; two of 8192 1050 - 1120 and 1225 without; of 256 and 384, 1 % more with 4
+// than with 1.
+constexpr int kPkPatience = 4000;
+constexpr int kPkTurnTiles = 4;
 constexpr int kPkNext = 16;                            // pair of columns (of 64) behind which the other lane's pass may start
 constexpr int kPkAhead = 4, kPkBehind = 6, kPkRing = 12;   // pairs between the stages of the exponentials
 static_assert(kPkRing > kPkAhead + kPkBehind, "a pair's place is taken again before it is done");
@@ -88,6 +93,10 @@ __device__ __forceinline__ int pk_cols(const PkLane& L, int j) { return min(kPkB
 // at a time, all its pairs, the last one first: K and V of the column stay in L2.  The rest goes pair by pair over all
 // columns, the last pairs first, which spreads a long sequence over all CTAs.  (All of a batch of 32 prompts of 700 tokens
 // with 32 heads pair by pair: 930 MB read from DRAM instead of 560.)
+// The rule (the longest at most 1.5 times the mean, four columns a CTA), 32 heads of 128, by columns and pair by pair: 640, 1024
+// and 2048 columns of 624-743 rows 149 / 145, 230 / 242, 444 / 472 us, 512 the same; 32 sequences of up to 1100 rows whose
+// longest is 1.07, 1.3, 1.45 and 1.6 times the mean 407 / 441, 355 / 365, 330 / 337 and 318 / 307; 24 of up to 4000,
+// 1.2 times 2700 / 2650.
 struct PkWalker {
   const PkArgs& a;
   int p, col, s0, s1, n_col, grid;                     // next: pair, column, its start and end (in flight)

@@ -8,10 +8,13 @@
 //            and walks the kept rows; wide rows are shared by several CTAs (grid y);
 //   read   : the same walk the other way, codes to bf16.
 // Floor: HBM, a kept row costs 2 D bytes in and 9 D / 16 out per head and tensor.  What the kernels run into is issue: 200
-// (append) and 140 (read) instructions per 16 values a lane, 69 and 57 % of the issue slots, so a row's place in its tile is
+// (append) and 150 (read) instructions per 16 values a lane, 69 and 57 % of the issue slots, so a row's place in its tile is
 // worked out once per CTA, not per lane.  97 MB to 27 (23.7k rows of 8 heads) and back: 29.5 and 27.4 us, 4.2 and 4.5 TB/s.
 // Measured and not better: two or four rows at a time, the next row's loads ahead, a product and a sum on fp32 pairs, the
 // two rows that share V bytes in the halves of a warp or joined by one thread (0-8 % slower).
+// With a mask every CTA of the append counts the flags in front of its rows, from its sequence's start: nothing at 700 rows, but
+// it grows with the square of the length (one sequence of 8 heads, all rows kept, with a mask and without: 8k rows 24 and 21 us,
+// 32k 58 and 38, 131k 189 and 123).
 #include <algorithm>
 
 #include "kv4.cuh"
