@@ -487,6 +487,116 @@ int32_t dl_kv4_read(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, cons
 int32_t dl_kv4_attn_decode(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, void* pool, const void* q_t,
                            const void* k_t, const void* v_t, const uint8_t* keep, float scale, void* out, void* stream);
 
+/* ---- extension, NOT in the paper: drafted tokens over a paged cache in 16 bits --------------- */
+
+/* A cache in pages (dl_pages above) that holds K and V rows as they are:  page = [K, V][n_kv_heads][page_rows][D] bf16, so
+ * a pool is [n_pages][2][n_kv_heads][page_rows][D].  A step with drafts is: dl_pages_reserve for the nodes, dl_tree_plan,
+ * then in every layer dl_kv16_append (commit = 0: the nodes' rows lie behind the rows held) and dl_kv16_attn_tree, then
+ * dl_tree_verify, and one dl_kv16_commit for all layers.  A prompt (or a chunk of one) is appended with commit = 1 in
+ * its last layer; without drafts a sequence has one node.  dl_pages_fork, dl_pages_free and dl_pages_compact take these pools, too.
+ * bf16 models, n_heads / n_kv_heads up to 128 (DL_ERR_UNSUPPORTED otherwise); these calls need the workspace unless noted. */
+
+/* Rotary positions: the first rot_dim dims of a head are rot_dim / 2 pairs, (i, i + rot_dim / 2), or (2 i, 2 i + 1) if
+ * interleaved; pair i of a row at position p turns by p * freqs[i] radians and is multiplied by `amplitude`.  Angles are taken
+ * in 64 bits (as fractions of a turn), so that far positions lose nothing; the rotation itself is in fp32, rounded once. */
+typedef struct {
+  int32_t rot_dim;       /* a multiple of 16, 0 <= rot_dim <= D */
+  int32_t interleaved;   /* 0: half layout */
+  const double* freqs;   /* dev [rot_dim / 2] */
+  float amplitude;
+} dl_rope;
+
+enum { DL_ROPE_PLAIN = 0, DL_ROPE_LINEAR = 1, DL_ROPE_NTK = 2, DL_ROPE_PARTS = 3 };
+
+/* Host helper: freqs[i] = base^(-2 i / rot_dim), scaled for contexts `factor` times as long as the `orig_len` positions a model
+ * was trained on:  LINEAR: divided by factor;  NTK: base * factor^(rot_dim / (rot_dim - 2)) instead of base;  PARTS: pairs
+ * that turn more than 32 times in orig_len positions stay, those that turn less than once are divided by factor, linear in the
+ * number of turns between, and amplitude = 0.1 ln(factor) + 1 (1 in the other forms).
+ * freqs_out HOST [rot_dim / 2], amplitude_out HOST [1].  rot_dim even, base > 1, factor >= 1, orig_len >= 1 (PARTS). */
+int32_t dl_rope_freqs(int32_t rot_dim, double base, int32_t scaling, double factor, int32_t orig_len, double* freqs_out,
+                      double* amplitude_out);
+
+/* What a step needs to know of its trees.  Sequence b's nodes are the packed rows [starts[b], starts[b + 1]); parent[row] is
+ * the node's parent, counted within the sequence, -1 for a root (node 0 always is one: the last token that is certain), and lower
+ * than the node's own number.  mask_out[row] gets the bits of the node itself and its ancestors (bit j % 32 of word j / 32),
+ * pos_out[row] = pos0[b] + the node's depth.
+ *   parent dev [total]; starts dev [B + 1]; pos0 dev [B] or NULL (0); mask_out dev [total][words], words 1..64, up to 32 * words
+ *   nodes a sequence; pos_out dev [total] or NULL.  Rows of no sequence are left as they were.
+ * A parent that breaks the rule records DL_ERR_INVALID_ARG with the sequence and counts as -1; a sequence with more nodes, too, and
+ * its nodes behind 32 * words are left out.  No workspace needed. */
+int32_t dl_tree_plan(dl_ctx* ctx, const int32_t* parent, const int32_t* starts, const int32_t* pos0, int32_t B, int32_t total,
+                     int32_t words, int32_t* mask_out, int32_t* pos_out, void* stream);
+
+/* Bytes of one page of a pool: 4 * n_kv_heads * page_rows * D.  Negative on bad arguments. */
+int64_t dl_kv16_page_bytes(const dl_ctx* ctx, int32_t n_kv_heads, int32_t page_rows);
+
+/* Rotates q and k to their positions and appends k (rotated) and v to a cache of 16-bit pages, in one pass.
+ * Cache: from row len[b] on and in order, sequence b's packed rows [starts[b], starts[b + 1]) whose keep flag is not 0; with
+ * commit, len[b] += their number.  q_out and k_out get the rotated rows of all sequences, dropped ones among them.
+ *   pages, pool, v: NULL for the rotation alone (of all `total` rows; starts, keep and commit are not looked at then);
+ *   q [total][n_heads][D] with q_out, or both NULL; k, v [total][n_kv_heads][D]; k_out [total][n_kv_heads][D] or NULL; all dev bf16;
+ *   *_stride: elements from one token's row to the next (0: dense), multiples of 8; q_out and k_out may be q and k themselves
+ *   (with the same strides), but not lie over anything else; pos dev [total] (may be NULL without rotation); rope HOST
+ *   struct or NULL (no rotation); starts dev [B + 1], ascending; keep dev [total] or NULL (all).
+ * The pages must be reserved: a sequence that lacks one is left as it was and records DL_ERR_CAPACITY with its index (q_out and
+ * k_out are written).  Pages that other sequences share must not be written: a fork leaves every partly filled page to one.
+ * Rows of no sequence are left as they were, in q_out and k_out, too. */
+int32_t dl_kv16_append(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, void* pool, const void* q, int64_t q_stride,
+                       const void* k, const void* v, int64_t kv_stride, const int32_t* pos, const dl_rope* rope,
+                       const int32_t* starts, const uint8_t* keep, int32_t total, void* q_out, int64_t q_out_stride, void* k_out,
+                       int64_t k_out_stride, int32_t commit, void* stream);
+
+/* Attention of new rows over such a cache: node i of sequence b (packed row starts[b] + i) attends the cache's rows [0, len[b])
+ * and, of the n = starts[b + 1] - starts[b] rows behind them, which hold the nodes' K and V, those that its mask names: row
+ * len[b] + j where bit j % 32 of word j / 32 is set (bits from n on are not looked at).  Query head h reads K/V head
+ * h / (n_heads / n_kv_heads).  A row that sees nothing gives 0.
+ *   q dev bf16 [total][n_heads][D], rotated; q_stride as above; starts dev [B + 1]; mask dev [total][words] or NULL: node i sees
+ *   nodes 0..i (a chain, the next chunk of a prompt, or the single token of a step without drafts);
+ *   max_rows HOST: no sequence has more nodes (nodes behind it are not computed, and DL_ERR_INVALID_ARG is recorded), nor more
+ *   than 32 * words with a mask; out dev bf16 [total][n_heads][D] dense, rows of no sequence are left as they were.
+ * Rows without a page are left out and record DL_ERR_INVALID_ARG with b.  NaN and infinities in rows that nobody may see do not
+ * matter; in v of a node, they may reach every row of its tree (0 * NaN in a matrix product). */
+int32_t dl_kv16_attn_tree(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, const void* pool, const void* q,
+                          int64_t q_stride, const int32_t* starts, int32_t total, int32_t max_rows, const int32_t* mask,
+                          int32_t words, float scale, void* out, void* stream);
+
+enum {
+  DL_VERIFY_GREEDY = 0,      /* a node is accepted iff its token is the first largest of `target`'s row; draft, u not read */
+  DL_VERIFY_SAMPLE = 1,      /* a node's children were drawn from its row of `draft` one after the other, without replacement */
+  DL_VERIFY_REPLACED = 2,    /* ... with replacement */
+  DL_VERIFY_POINT = 3        /* children were chosen without randomness; draft not read */
+};
+
+/* Verifies drafted trees against the target's distributions so that what is kept is distributed as the target's own samples.
+ * Nodes as in dl_tree_plan; target[row] (and draft[row]) is the distribution behind that node.  In the order of their
+ * numbers, nodes whose parent is the node reached so far (at first the root, node 0) are tested; an accepted one is the node
+ * reached.  With p, q the rows of the node reached, and s = 0, R = 1, a = 1 when it is reached, token c of a child with number u
+ *   is accepted iff  a > 0 and (u q(c)) R < r(c) a,  r(v) = p(v) - s q(v) held to [0, 1];   if not, and a > 0:  s += R / a,
+ *   R = sum of r under the new s, a -= q(c) (REPLACED: a stays 1).
+ *   POINT: accepted iff u R < p(c); if not, R -= p(c), and p(c) counts as 0 from then on.
+ * At the end a token is drawn from r as it is there, or from p (held to [0, 1]) if all of r is 0, with the root's number u: the first
+ * v at which the running sum exceeds u times the whole.  These steps are defined bit for bit: fp64 operations in the order
+ * written, sums over r of trunc(r * 2^44), the drawn token's bound (trunc(u * 2^31) * sum) >> 31; no result depends on timing.
+ * GREEDY compares values (NaN counts as -infinity; -0 equals +0) and draws the first largest.
+ *   target dev [total][vocab] fp32 probabilities, or with GREEDY fp32 or bf16 (`dtype`), probabilities or logits alike;
+ *   draft dev [total][vocab] fp32 or NULL; row strides in elements (0: vocab); u dev [total] in [0, 1) (outside: held to it);
+ *   tokens, parent dev [total] (the root's are not read);
+ *   keep_out dev [total]: 1 for the root and the accepted nodes, else 0; count_out dev [B]: their number; next_out dev [B]: the
+ *   token drawn; a sequence without nodes gets 0 and -1.  vocab up to 262144, up to 2048 nodes a sequence.
+ * A token outside the vocabulary is rejected without further effect, a parent as in dl_tree_plan is never reached; both record
+ * DL_ERR_INVALID_ARG with the sequence, as a row without any positive entry does (next -1). */
+int32_t dl_tree_verify(dl_ctx* ctx, const void* target, int32_t dtype, int64_t target_stride, const float* draft,
+                       int64_t draft_stride, const float* u, const int32_t* tokens, const int32_t* parent,
+                       const int32_t* starts, int32_t B, int32_t total, int32_t vocab, int32_t mode, uint8_t* keep_out,
+                       int32_t* count_out, int32_t* next_out, void* stream);
+
+/* Keeps, of every sequence's rows behind len[b] (the nodes [starts[b], starts[b + 1]) appended there), those whose keep flag is not
+ * 0: they move up to row len[b] and on, in order, in all pools, and len[b] += their number.  Rows behind them stay as they are.
+ *   pools HOST array of n_pools dev pointers; starts dev [B + 1]; keep dev [total].
+ * A sequence that lacks a page of these rows is left as it was and records DL_ERR_CAPACITY with its index. */
+int32_t dl_kv16_commit(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, int32_t n_pools, void* const* pools,
+                       const int32_t* starts, const uint8_t* keep, int32_t total, void* stream);
+
 /* ---- checked build ---------------------------------------------------------------------- */
 
 /* The library can be built with -DDL_BOUNDS=1 (libdl_sparse_checked.so): every store a kernel makes through an

@@ -38,7 +38,11 @@ EXPORTS = [
     "dl_selftest_bounds", "dl_sparse_attn_decode_fp8_layers",
     "dl_attn_prefill_packed", "dl_pages_scratch_bytes", "dl_pages_reserve", "dl_pages_free", "dl_pages_fork",
     "dl_pages_compact", "dl_kv4_page_bytes", "dl_kv4_append", "dl_kv4_read", "dl_kv4_attn_decode",
+    "dl_rope_freqs", "dl_tree_plan", "dl_kv16_page_bytes", "dl_kv16_append", "dl_kv16_attn_tree", "dl_tree_verify",
+    "dl_kv16_commit",
 ]
+ROPE_SCALING = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}                        # DL_ROPE_*
+VERIFY_MODES = {"greedy": 0, "sample": 1, "replaced": 2, "point": 3}                # DL_VERIFY_*
 
 
 class ModelDesc(C.Structure):
@@ -97,6 +101,37 @@ class Pages:
                 raise DlError(int(n), "dl_pages_scratch_bytes")
             self._scratch = torch.empty(max(int(n), 256), dtype=torch.uint8, device=self.book.device)
         return self._scratch
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("freqs", C.c_void_p), ("amplitude", C.c_float)]
+
+
+def rope_freqs(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, orig_len: int = 4096):
+    """dl_rope_freqs: turning of the pairs per position (a float64 tensor of the host) and what rotated values are multiplied by."""
+    freqs = torch.zeros(max(rot_dim // 2, 1), dtype=torch.float64)
+    amplitude = C.c_double()
+    st = lib().dl_rope_freqs(rot_dim, float(base), ROPE_SCALING[scaling], float(factor), int(orig_len), freqs.data_ptr(),
+                             C.byref(amplitude))
+    if st != DL_OK:
+        raise DlError(st, "dl_rope_freqs")
+    return freqs[:rot_dim // 2], amplitude.value
+
+
+class Rope:
+    """Rotary positions (dl_rope in dl.h): the first rot_dim dims of a head in half or interleaved layout, with frequencies by
+    dl_rope_freqs or given (`freqs`, radians per position, and `amplitude`)."""
+
+    def __init__(self, rot_dim: int, base: float = 10000.0, interleaved: bool = False, scaling: str = "none",
+                 factor: float = 1.0, orig_len: int = 4096, freqs=None, amplitude: float = 1.0, device="cuda"):
+        if freqs is None:
+            freqs, amplitude = rope_freqs(rot_dim, base, scaling, factor, orig_len)
+        freqs = torch.as_tensor(freqs, dtype=torch.float64)
+        if freqs.shape != (rot_dim // 2,):
+            raise ValueError(f"freqs: want {rot_dim // 2} of them, got {tuple(freqs.shape)}")
+        self.freqs = freqs.to(device).contiguous()
+        self.desc = RopeDesc(rot_dim, 1 if interleaved else 0, self.freqs.data_ptr(), amplitude)
+        self.ref = C.pointer(self.desc)
 
 
 class PredictorDesc(C.Structure):
@@ -186,6 +221,14 @@ def lib() -> C.CDLL:
             "dl_kv4_append": (i32, [vp, C.POINTER(PagesDesc), i32, vp, vp, vp, i64, vp, vp, i32, i32, vp]),
             "dl_kv4_read": (i32, [vp, C.POINTER(PagesDesc), i32, vp, vp, vp, i32, vp, vp, vp]),
             "dl_kv4_attn_decode": (i32, [vp, C.POINTER(PagesDesc), i32, vp, vp, vp, vp, vp, f32, vp, vp]),
+            "dl_rope_freqs": (i32, [i32, C.c_double, i32, C.c_double, i32, vp, C.POINTER(C.c_double)]),
+            "dl_tree_plan": (i32, [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp]),
+            "dl_kv16_page_bytes": (i64, [vp, i32, i32]),
+            "dl_kv16_append": (i32, [vp, C.POINTER(PagesDesc), i32, vp, vp, i64, vp, vp, i64, vp, C.POINTER(RopeDesc), vp, vp,
+                                     i32, vp, i64, vp, i64, i32, vp]),
+            "dl_kv16_attn_tree": (i32, [vp, C.POINTER(PagesDesc), i32, vp, vp, i64, vp, i32, i32, vp, i32, f32, vp, vp]),
+            "dl_tree_verify": (i32, [vp, vp, i32, i64, vp, i64, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp]),
+            "dl_kv16_commit": (i32, [vp, C.POINTER(PagesDesc), i32, i32, vp, vp, vp, i32, vp]),
             "dl_decode_step_host": (i32, [vp, P, vp, i32, f32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                           vp, vp, C.POINTER(vp), C.POINTER(vp), i32, vp, f32, vp]),
             "dl_decode_steps_host": (i32, [vp, P, i32, i32, f32, i32, C.POINTER(vp), C.POINTER(vp), C.POINTER(vp),
@@ -578,6 +621,116 @@ class Context:
             _arg(v_t, self.dtype, small, "v_t", i),
             None if keep is None else _arg(keep, torch.uint8, (B,), "keep", i), scale,
             _arg(out, self.dtype, big, "out", i), self._on(stream)), "dl_kv4_attn_decode")
+
+    # ---- drafted tokens over a paged 16-bit cache (extension, not in the paper)
+    def kv16_page_bytes(self, n_kv_heads: int, page_rows: int) -> int:
+        n = lib().dl_kv16_page_bytes(self._h, n_kv_heads, page_rows)
+        if n < 0:
+            raise DlError(int(n), "dl_kv16_page_bytes")
+        return int(n)
+
+    def kv16_pool(self, pages: Pages, n_kv_heads: int) -> torch.Tensor:
+        """A pool of 16-bit pages (bf16 [n_pages, K and V, n_kv_heads, page_rows, D]) for these books."""
+        self.kv16_page_bytes(n_kv_heads, pages.page_rows)
+        return torch.zeros(pages.n_pages, 2, n_kv_heads, pages.page_rows, self.D, dtype=self.dtype, device=pages.book.device)
+
+    def _pool16(self, pages: Pages, pool, n_kv: int) -> int:
+        return _arg(pool, self.dtype, (pages.n_pages, 2, n_kv, pages.page_rows, self.D), "pool", self.device.index)
+
+    def tree_plan(self, parent, starts, pos0, mask_out, pos_out=None, stream=None):
+        """dl_tree_plan: parent int32 [total], starts int32 [B + 1], pos0 int32 [B] or None; mask_out int32 [total, words],
+        pos_out int32 [total] or None."""
+        i, total, B = self.device.index, parent.shape[0], starts.shape[0] - 1
+        words = mask_out.shape[1]
+        self._check(lib().dl_tree_plan(
+            self._h, _arg(parent, torch.int32, (total,), "parent", i), _arg(starts, torch.int32, (B + 1,), "starts", i),
+            None if pos0 is None else _arg(pos0, torch.int32, (B,), "pos0", i), B, total, words,
+            _arg(mask_out, torch.int32, (total, words), "mask_out", i),
+            None if pos_out is None else _arg(pos_out, torch.int32, (total,), "pos_out", i), self._on(stream)), "dl_tree_plan")
+
+    def _rope(self, rope):
+        """The rotation for the library, which follows the pointer of its frequencies on the context's device."""
+        if rope is None:
+            return None
+        if rope.freqs.get_device() != self.device.index:
+            raise ValueError(f"rope: want frequencies on cuda:{self.device.index}, got {rope.freqs.device}")
+        return rope.ref
+
+    def kv16_append(self, pages, pool, q, k, v, starts, pos, rope, keep=None, q_out=None, k_out=None, commit=True, stream=None):
+        """dl_kv16_append: q [total, n_heads, D] with q_out (or both None), k, v [total, n_kv_heads, D], k_out like k or None, all
+        bf16 (rows may be strided); pos int32 [total]; rope: a Rope or None; starts int32 [B + 1]; keep uint8 [total] or None.
+        pages, pool and v None: the rotation alone."""
+        total, n_kv, i = k.shape[0], k.shape[1], self.device.index
+        big, small, none = (total, self.H, self.D), (total, n_kv, self.D), (None, 0)
+        kp, ks = _rows(k, self.dtype, small, "k", i)
+        vp, vs = _rows(v, self.dtype, small, "v", i) if v is not None else (None, ks)
+        if ks != vs:
+            raise ValueError("k and v must have the same row stride")
+        qp, qs = _rows(q, self.dtype, big, "q", i) if q is not None else none
+        qop, qos = _rows(q_out, self.dtype, big, "q_out", i) if q_out is not None else none
+        kop, kos = _rows(k_out, self.dtype, small, "k_out", i) if k_out is not None else none
+        if (pages is None) != (pool is None) or (pages is not None and v is None):
+            raise ValueError("pages, pool and v go together")
+        self._check(lib().dl_kv16_append(
+            self._h, None if pages is None else self._books(pages), n_kv, None if pool is None else self._pool16(pages, pool, n_kv),
+            qp, qs, kp, vp, ks, None if pos is None else _arg(pos, torch.int32, (total,), "pos", i), self._rope(rope),
+            None if pages is None else _arg(starts, torch.int32, (pages.B + 1,), "starts", i),
+            None if keep is None else _arg(keep, torch.uint8, (total,), "keep", i), total, qop, qos, kop, kos,
+            1 if commit else 0, self._on(stream)), "dl_kv16_append")
+
+    def kv16_attn_tree(self, pages: Pages, pool, q, starts, max_rows, mask, scale, out, stream=None):
+        """dl_kv16_attn_tree: q [total, n_heads, D] (rows may be strided), starts int32 [B + 1], max_rows: most nodes of a
+        sequence; mask int32 [total, words] or None (each node sees those in front of it and itself); out [total, n_heads, D]."""
+        total, n_kv, i = q.shape[0], pool.shape[2], self.device.index
+        qp, qs = _rows(q, self.dtype, (total, self.H, self.D), "q", i)
+        words = 0 if mask is None else mask.shape[1]
+        self._check(lib().dl_kv16_attn_tree(
+            self._h, self._books(pages), n_kv, self._pool16(pages, pool, n_kv), qp, qs,
+            _arg(starts, torch.int32, (pages.B + 1,), "starts", i), total, max_rows,
+            None if mask is None else _arg(mask, torch.int32, (total, words), "mask", i), words, scale,
+            _arg(out, self.dtype, (total, self.H, self.D), "out", i), self._on(stream)), "dl_kv16_attn_tree")
+
+    def _dist(self, t, dtype, total, what):
+        """Pointer and row stride of rows [total, vocab] whose entries lie side by side."""
+        if t.dtype is not dtype or t.dim() != 2 or t.shape[0] != total or t.get_device() != self.device.index:
+            raise ValueError(f"{what}: want {dtype} [{total}, vocab] on cuda:{self.device.index}, got {t.dtype} {tuple(t.shape)} "
+                             f"on {t.device}")
+        if total > 0 and (t.stride(1) != 1 or (total > 1 and t.stride(0) < t.shape[1])):
+            raise ValueError(f"{what}: want dense rows that do not overlap, got strides {t.stride()}")
+        return t.data_ptr(), (t.stride(0) if total > 1 else t.shape[1])
+
+    def tree_verify(self, target, draft, u, tokens, parent, starts, mode, keep_out, count_out, next_out, stream=None):
+        """dl_tree_verify: target [total, vocab] float32 (mode "greedy": or bf16), draft like it (modes "sample" and "replaced")
+        or None, u float32 [total] (None for "greedy"), tokens and parent int32 [total], starts int32 [B + 1]; keep_out uint8
+        [total], count_out and next_out int32 [B]."""
+        i, total, B = self.device.index, tokens.shape[0], starts.shape[0] - 1
+        code = VERIFY_MODES[mode]
+        drafted = mode in ("sample", "replaced")
+        dtype = torch.bfloat16 if mode == "greedy" and target.dtype is torch.bfloat16 else torch.float32
+        tp, ts = self._dist(target, dtype, total, "target")
+        vocab = target.shape[1]
+        dp, ds = None, 0
+        if drafted:
+            dp, ds = self._dist(draft, torch.float32, total, "draft")
+            if draft.shape[1] != vocab:
+                raise ValueError(f"draft: want a vocabulary of {vocab}, got {draft.shape[1]}")
+        self._check(lib().dl_tree_verify(
+            self._h, tp, DL_BF16 if dtype is torch.bfloat16 else DL_F32, ts, dp, ds,
+            None if mode == "greedy" else _arg(u, torch.float32, (total,), "u", i), _arg(tokens, torch.int32, (total,), "tokens", i),
+            _arg(parent, torch.int32, (total,), "parent", i), _arg(starts, torch.int32, (B + 1,), "starts", i), B, total, vocab, code,
+            _arg(keep_out, torch.uint8, (total,), "keep_out", i), _arg(count_out, torch.int32, (B,), "count_out", i),
+            _arg(next_out, torch.int32, (B,), "next_out", i), self._on(stream)), "dl_tree_verify")
+
+    def kv16_commit(self, pages: Pages, pools, starts, keep, stream=None):
+        """dl_kv16_commit: pools: the list of all layers' pools; starts int32 [B + 1]; keep uint8 [total]."""
+        i, total = self.device.index, keep.shape[0]
+        books = self._books(pages)
+        n_kv = pools[0].shape[2] if pools else 1
+        ptrs = array.array("Q", [self._pool16(pages, p, n_kv) for p in pools])
+        self._check(lib().dl_kv16_commit(
+            self._h, books, n_kv, len(ptrs), ptrs.buffer_info()[0] if pools else None,
+            _arg(starts, torch.int32, (pages.B + 1,), "starts", i), _arg(keep, torch.uint8, (total,), "keep", i), total,
+            self._on(stream)), "dl_kv16_commit")
 
     def selftest_wait_timeout(self, polls: int = 64, stream=None):
         self._check(lib().dl_selftest_wait_timeout(self._h, int(polls), _stream(stream)), "dl_selftest_wait_timeout")

@@ -1,5 +1,6 @@
 // Host side of the C ABI: argument checks, workspace layout, dispatch to the kernel launchers.
 // No call here allocates device memory or synchronises, except where dl.h says so.
+#include <math.h>
 #include <new>
 #include <string.h>
 
@@ -850,6 +851,157 @@ int32_t dl_kv4_attn_decode(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_head
   if (misaligned(q_t) || misaligned(k_t) || misaligned(v_t) || misaligned(out)) return DL_ERR_ALIGNMENT;
   DeviceGuard g(ctx->device);
   return cuda_status(ctx, launch_attn_decode_kv4(ctx, pages, n_kv_heads, pool, q_t, k_t, v_t, keep, scale, out, static_cast<cudaStream_t>(stream)));
+}
+
+// ---- drafted tokens over a paged 16-bit cache
+
+static int32_t check_kv16(const dl_ctx* ctx, const dl_pages* p, int32_t n_kv_heads) {
+  const int32_t st = check_pages(ctx, p);
+  if (st != DL_OK) return st;
+  if (n_kv_heads <= 0 || ctx->desc.n_heads % n_kv_heads != 0) return DL_ERR_INVALID_ARG;
+  if (ctx->desc.dtype != DL_BF16 || ctx->desc.n_heads / n_kv_heads > 128) return DL_ERR_UNSUPPORTED;
+  // rows of one head are counted in 32 bits over a pool
+  if (2LL * n_kv_heads * p->page_rows * p->n_pages >= (1LL << 31)) return DL_ERR_UNSUPPORTED;
+  if (!ctx->ws.base || p->B > ctx->ws.max_batch) return DL_ERR_WORKSPACE;
+  return DL_OK;
+}
+
+// row stride of packed rows of `w` values: 0 means dense; a multiple of 8, rows not over one another
+static int32_t check_stride(int64_t* stride, int64_t w) {
+  if (*stride == 0) *stride = w;
+  if (*stride < w) return DL_ERR_INVALID_ARG;
+  if (*stride % 8 != 0) return DL_ERR_ALIGNMENT;
+  return *stride >= (1LL << 32) ? DL_ERR_UNSUPPORTED : DL_OK;
+}
+
+int32_t dl_rope_freqs(int32_t rot_dim, double base, int32_t scaling, double factor, int32_t orig_len, double* freqs_out,
+                      double* amplitude_out) {
+  if (rot_dim < 0 || rot_dim % 2 != 0 || !(base > 1.0) || !(factor >= 1.0) || !freqs_out || !amplitude_out) return DL_ERR_INVALID_ARG;
+  if (scaling < DL_ROPE_PLAIN || scaling > DL_ROPE_PARTS || (scaling == DL_ROPE_PARTS && orig_len < 1)) return DL_ERR_INVALID_ARG;
+  if (scaling == DL_ROPE_NTK && rot_dim > 2) base *= pow(factor, rot_dim / (rot_dim - 2.0));
+  *amplitude_out = scaling == DL_ROPE_PARTS ? 0.1 * log(factor) + 1.0 : 1.0;
+  constexpr double kSlow = 1.0, kFast = 32.0;          // turns in orig_len positions: divided by factor below, left alone above
+  for (int32_t i = 0; i < rot_dim / 2; ++i) {
+    double f = pow(base, -2.0 * i / rot_dim);
+    if (scaling == DL_ROPE_LINEAR) f /= factor;
+    if (scaling == DL_ROPE_PARTS) {
+      const double turns = orig_len * f / 6.283185307179586477;
+      const double part = fmin(fmax((turns - kSlow) / (kFast - kSlow), 0.0), 1.0);
+      f *= part + (1.0 - part) / factor;
+    }
+    freqs_out[i] = f;
+  }
+  return DL_OK;
+}
+
+int32_t dl_tree_plan(dl_ctx* ctx, const int32_t* parent, const int32_t* starts, const int32_t* pos0, int32_t B, int32_t total,
+                     int32_t words, int32_t* mask_out, int32_t* pos_out, void* stream) {
+  if (!ctx || B < 0 || total < 0) return DL_ERR_INVALID_ARG;
+  if (words < 1 || words > 64 || B >= (1 << 24)) return DL_ERR_UNSUPPORTED;
+  if (B == 0 || total == 0) return DL_OK;
+  if (!parent || !starts || !mask_out) return DL_ERR_INVALID_ARG;
+  if (misaligned(parent) || misaligned(starts) || misaligned(pos0) || misaligned(mask_out) || misaligned(pos_out)) return DL_ERR_ALIGNMENT;
+  DeviceGuard g(ctx->device);
+  return cuda_status(ctx, launch_tree_plan(ctx, parent, starts, pos0, B, total, words, mask_out, pos_out, static_cast<cudaStream_t>(stream)));
+}
+
+int64_t dl_kv16_page_bytes(const dl_ctx* ctx, int32_t n_kv_heads, int32_t page_rows) {
+  if (!ctx || n_kv_heads <= 0) return DL_ERR_INVALID_ARG;
+  if (page_rows != 16 && page_rows != 32 && page_rows != 64 && page_rows != 128) return DL_ERR_UNSUPPORTED;
+  return 4LL * n_kv_heads * page_rows * ctx->desc.head_dim;
+}
+
+int32_t dl_kv16_append(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, void* pool, const void* q, int64_t q_stride,
+                       const void* k, const void* v, int64_t kv_stride, const int32_t* pos, const dl_rope* rope,
+                       const int32_t* starts, const uint8_t* keep, int32_t total, void* q_out, int64_t q_out_stride, void* k_out,
+                       int64_t k_out_stride, int32_t commit, void* stream) {
+  if (!ctx || (pages != nullptr) != (pool != nullptr) || (q != nullptr) != (q_out != nullptr)) return DL_ERR_INVALID_ARG;
+  if (pages) {
+    const int32_t st = check_kv16(ctx, pages, n_kv_heads);
+    if (st != DL_OK) return st;
+    if (misaligned(pool)) return DL_ERR_ALIGNMENT;
+  } else {
+    if (n_kv_heads <= 0 || ctx->desc.n_heads % n_kv_heads != 0) return DL_ERR_INVALID_ARG;
+    if (ctx->desc.dtype != DL_BF16) return DL_ERR_UNSUPPORTED;
+  }
+  if (total < 0) return DL_ERR_INVALID_ARG;
+  const int64_t D = ctx->desc.head_dim, qw = D * ctx->desc.n_heads, kw = D * n_kv_heads;
+  if (rope) {
+    if (rope->rot_dim < 0 || rope->rot_dim > D) return DL_ERR_INVALID_ARG;
+    if (rope->rot_dim % 16 != 0) return DL_ERR_UNSUPPORTED;
+    if (rope->rot_dim > 0 && (!rope->freqs || (total > 0 && !pos))) return DL_ERR_INVALID_ARG;
+    if (misaligned(rope->freqs)) return DL_ERR_ALIGNMENT;
+  }
+  if (total == 0 || (pages && pages->B == 0)) return DL_OK;
+  if (!k || (pages && (!v || !starts))) return DL_ERR_INVALID_ARG;
+  if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(q_out) || misaligned(k_out) || misaligned(pos)) return DL_ERR_ALIGNMENT;
+  int64_t* strides[4] = {&q_stride, &kv_stride, &q_out_stride, &k_out_stride};
+  const int64_t widths[4] = {qw, kw, qw, kw};
+  const bool used[4] = {q != nullptr, true, q_out != nullptr, k_out != nullptr};
+  for (int i = 0; i < 4; ++i) {
+    const int32_t st = used[i] ? check_stride(strides[i], widths[i]) : DL_OK;
+    if (st != DL_OK) return st;
+  }
+  if ((q && q_out == q && q_out_stride != q_stride) || (k_out == k && k_out_stride != kv_stride)) return DL_ERR_INVALID_ARG;
+  if (!pages && !q_out && !k_out) return DL_OK;
+  DeviceGuard g(ctx->device);
+  return cuda_status(ctx, launch_kv16_append(ctx, pages, n_kv_heads, pool, q, q_stride, k, v, kv_stride, pos, rope, starts, keep,
+                                             total, q_out, q_out_stride, k_out, k_out_stride, commit,
+                                             static_cast<cudaStream_t>(stream)));
+}
+
+int32_t dl_kv16_attn_tree(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, const void* pool, const void* q,
+                          int64_t q_stride, const int32_t* starts, int32_t total, int32_t max_rows, const int32_t* mask,
+                          int32_t words, float scale, void* out, void* stream) {
+  int32_t st = check_kv16(ctx, pages, n_kv_heads);
+  if (st != DL_OK) return st;
+  if (total < 0 || max_rows < 0 || !(scale > 0.f) || (mask && words < 1)) return DL_ERR_INVALID_ARG;
+  if (mask && words >= (1 << 24)) return DL_ERR_UNSUPPORTED;
+  if (pages->B == 0 || total == 0 || max_rows == 0) return DL_OK;
+  if (!pool || !q || !starts || !out) return DL_ERR_INVALID_ARG;
+  if (misaligned(pool) || misaligned(q) || misaligned(out) || misaligned(mask)) return DL_ERR_ALIGNMENT;
+  st = check_stride(&q_stride, (int64_t)ctx->desc.head_dim * ctx->desc.n_heads);
+  if (st != DL_OK) return st;
+  DeviceGuard g(ctx->device);
+  return cuda_status(ctx, launch_attn_tree(ctx, pages, n_kv_heads, pool, q, q_stride, starts, total, max_rows, mask, words, scale,
+                                           out, static_cast<cudaStream_t>(stream)));
+}
+
+int32_t dl_tree_verify(dl_ctx* ctx, const void* target, int32_t dtype, int64_t target_stride, const float* draft,
+                       int64_t draft_stride, const float* u, const int32_t* tokens, const int32_t* parent,
+                       const int32_t* starts, int32_t B, int32_t total, int32_t vocab, int32_t mode, uint8_t* keep_out,
+                       int32_t* count_out, int32_t* next_out, void* stream) {
+  if (!ctx || B < 0 || total < 0 || vocab <= 0 || mode < DL_VERIFY_GREEDY || mode > DL_VERIFY_POINT) return DL_ERR_INVALID_ARG;
+  if (dtype != DL_F32 && !(dtype == DL_BF16 && mode == DL_VERIFY_GREEDY)) return DL_ERR_UNSUPPORTED;
+  if (vocab > (1 << 18) || B >= (1 << 24)) return DL_ERR_UNSUPPORTED;
+  if (B == 0) return DL_OK;
+  const bool drafted = mode == DL_VERIFY_SAMPLE || mode == DL_VERIFY_REPLACED;
+  if (!starts || !count_out || !next_out) return DL_ERR_INVALID_ARG;
+  if (total > 0 && (!target || !tokens || !parent || !keep_out || (drafted && !draft) || (mode != DL_VERIFY_GREEDY && !u)))
+    return DL_ERR_INVALID_ARG;
+  if (target_stride == 0) target_stride = vocab;
+  if (draft_stride == 0) draft_stride = vocab;
+  if (target_stride < vocab || (drafted && draft_stride < vocab)) return DL_ERR_INVALID_ARG;
+  if (misaligned(target) || (drafted && misaligned(draft)) || misaligned(u) || misaligned(tokens) || misaligned(parent)) return DL_ERR_ALIGNMENT;
+  if (target_stride >= (1LL << 32) || draft_stride >= (1LL << 32)) return DL_ERR_UNSUPPORTED;
+  DeviceGuard g(ctx->device);
+  return cuda_status(ctx, launch_tree_verify(ctx, target, dtype, target_stride, draft, draft_stride, u, tokens, parent, starts, B,
+                                             total, vocab, mode, keep_out, count_out, next_out, static_cast<cudaStream_t>(stream)));
+}
+
+int32_t dl_kv16_commit(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, int32_t n_pools, void* const* pools,
+                       const int32_t* starts, const uint8_t* keep, int32_t total, void* stream) {
+  const int32_t st = check_kv16(ctx, pages, n_kv_heads);
+  if (st != DL_OK) return st;
+  if (total < 0 || n_pools < 0 || (n_pools > 0 && !pools)) return DL_ERR_INVALID_ARG;
+  for (int32_t i = 0; i < n_pools; ++i) {
+    if (!pools[i]) return DL_ERR_INVALID_ARG;
+    if (misaligned(pools[i])) return DL_ERR_ALIGNMENT;
+  }
+  if (pages->B == 0 || total == 0) return DL_OK;
+  if (!starts || !keep) return DL_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  return cuda_status(ctx, launch_kv16_commit(ctx, pages, n_kv_heads, n_pools, pools, starts, keep, total, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -35,7 +35,7 @@ __device__ __forceinline__ void report_status(DeviceStatus* st, int32_t code, lo
 enum KernelId : int {
   KID_DECODE_MMA = 1, KID_DECODE_SIMT = 2, KID_DECODE_FP8 = 3, KID_COMPACT_PLAN = 4, KID_COMPACT_COPY = 5,
   KID_TOPK = 6, KID_KEEP = 7, KID_PREFILL_TOP = 8, KID_PREFILL_SIMT = 9, KID_PREFILL_TC = 10, KID_QUANTIZE = 11,
-  KID_PREDICTOR = 12, KID_PACKED = 13, KID_KV4_APPEND = 14, KID_KV4_READ = 15, KID_DECODE_KV4 = 16, KID_PAGES = 17,
+  KID_PREDICTOR = 12, KID_PACKED = 13, KID_KV4_APPEND = 14, KID_KV4_READ = 15, KID_DECODE_KV4 = 16, KID_PAGES = 17, KID_KV16 = 18, KID_TREE = 19,
   KID_SELFTEST = 0x7e
 };
 #ifdef DL_BOUNDS
@@ -227,6 +227,22 @@ cudaError_t launch_pages_fork(const dl_ctx* ctx, const dl_pages* p, const int32_
                               void* const* pools, int64_t page_bytes, void* scratch, cudaStream_t s);
 cudaError_t launch_pages_compact(const dl_ctx* ctx, const dl_pages* p, int32_t n_pools, void* const* pools,
                                  int64_t page_bytes, int32_t* live, void* scratch, cudaStream_t s);
+
+cudaError_t launch_tree_plan(const dl_ctx* ctx, const int32_t* parent, const int32_t* starts, const int32_t* pos0, int32_t B,
+                             int32_t total, int32_t words, int32_t* mask, int32_t* pos, cudaStream_t s);
+cudaError_t launch_kv16_append(const dl_ctx* ctx, const dl_pages* p, int32_t Hk, void* pool, const void* q, int64_t q_stride,
+                               const void* k, const void* v, int64_t kv_stride, const int32_t* pos, const dl_rope* rope,
+                               const int32_t* starts, const uint8_t* keep, int32_t total, void* q_out, int64_t q_out_stride,
+                               void* k_out, int64_t k_out_stride, int32_t commit, cudaStream_t s);
+cudaError_t launch_kv16_commit(const dl_ctx* ctx, const dl_pages* p, int32_t Hk, int32_t n_pools, void* const* pools,
+                               const int32_t* starts, const uint8_t* keep, int32_t total, cudaStream_t s);
+cudaError_t launch_attn_tree(dl_ctx* ctx, const dl_pages* p, int32_t Hk, const void* pool, const void* q, int64_t q_stride,
+                             const int32_t* starts, int32_t total, int32_t max_rows, const int32_t* mask, int32_t words,
+                             float scale, void* out, cudaStream_t s);
+cudaError_t launch_tree_verify(const dl_ctx* ctx, const void* target, int32_t dtype, int64_t target_stride, const float* draft,
+                               int64_t draft_stride, const float* u, const int32_t* tokens, const int32_t* parent,
+                               const int32_t* starts, int32_t B, int32_t total, int32_t vocab, int32_t mode, uint8_t* keep,
+                               int32_t* count, int32_t* next, cudaStream_t s);
 
 int64_t predictor_paper_scratch_bytes(int64_t rows);
 bool predictor_paper_supported(const dl_ctx* ctx);

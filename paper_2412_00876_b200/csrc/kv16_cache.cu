@@ -1,0 +1,395 @@
+// Rows into the paged 16-bit K/V cache: appended with the position rotation on the way, and kept or dropped once drafts are
+// verified.  An extension, not in the paper: the append of Eq. 6 for rows that are not position-encoded yet.
+//
+//   plan   : (with a keep mask or a commit) per sequence, count the kept rows, check that their pages are there, note the first
+//            destination row, advance the length: one CTA per sequence;
+//   append : a CTA takes a few packed rows; their cos and sin go to shared memory once and serve all heads; then every thread
+//            moves 32 bytes at a time (both halves of 8 pairs), q to q_out, k to k_out and the cache, v to the cache;
+//   commit : accepted rows move up; a thread stays at one 16-byte column of one pool, tensor and head and walks the rows in
+//            order, so that no row is overwritten before it has been read;
+//   tree   : ancestors' bits and depths of tree nodes.
+#include <algorithm>
+
+#include "kv16.cuh"
+
+namespace dl {
+
+constexpr int kK16Threads = 256;
+constexpr int kK16Rows = 8;              // most packed rows per CTA of the append
+
+__device__ __forceinline__ int k16_block_sum(int v, int* sh) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (lane == 0) sh[warp] = v;
+  __syncthreads();
+  int t = 0;
+#pragma unroll
+  for (int w = 0; w < kK16Threads / 32; ++w) t += sh[w];
+  __syncthreads();
+  return t;
+}
+
+// flags that are not 0 among keep[from, to), counted by the whole CTA, 16 at a time
+__device__ __forceinline__ int k16_count(const uint8_t* keep, int from, int to, int* sh) {
+  int c = 0;
+  const int head = min(to, from + (int)((16 - (reinterpret_cast<uintptr_t>(keep + from) & 15)) & 15));
+  const int units = max(0, to - head) / 16;
+  for (int i = from + threadIdx.x; i < head; i += kK16Threads) c += __ldcg(keep + i) != 0;
+  for (int i = threadIdx.x; i < units; i += kK16Threads) {
+    const uint4 w = __ldcg(reinterpret_cast<const uint4*>(keep + head) + i);
+    c += (__popc(__vcmpne4(w.x, 0)) + __popc(__vcmpne4(w.y, 0)) + __popc(__vcmpne4(w.z, 0)) + __popc(__vcmpne4(w.w, 0))) >> 3;
+  }
+  for (int i = head + 16 * units + threadIdx.x; i < to; i += kK16Threads) c += __ldcg(keep + i) != 0;
+  return k16_block_sum(c, sh);
+}
+
+// Whether rows [base, base + count) of sequence b have pages: a sequence's pages come first in its table row, so the last one
+// tells.  (Every row's own page is looked at again where it is written.)
+__device__ __forceinline__ bool k16_fits(const K16Pages& pg, int b, int base, int count) {
+  return base >= 0 && (count == 0 || k16_page(pg, b, (long long)base + count - 1) >= 0);
+}
+
+__global__ void __launch_bounds__(kK16Threads)
+kv16_plan_kernel(const K16Pages pg, const int32_t* starts, const uint8_t* keep, int32_t total, int32_t commit,
+                 int32_t* plan_base, int32_t* plan_count) {
+  __shared__ int sh[kK16Threads / 32];
+  chained_go();
+  chained_wait();
+  const int b = blockIdx.x, base = __ldcg(pg.len + b);
+  const int from = k16_start(starts, b, total), to = max(from, k16_start(starts, b + 1, total));
+  const int count = keep ? k16_count(keep, from, to, sh) : to - from;
+  if (threadIdx.x == 0) {
+    const bool ok = k16_fits(pg, b, base, count);
+    plan_base[b] = base;
+    plan_count[b] = ok ? count : -1;
+    if (ok && commit) pg.len[b] = base + count;
+  }
+}
+
+struct K16Append {
+  const __nv_bfloat16* q; const __nv_bfloat16* k; const __nv_bfloat16* v;
+  __nv_bfloat16* q_out; __nv_bfloat16* k_out; __nv_bfloat16* pool;
+  long long q_stride, kv_stride, q_out_stride, k_out_stride;
+  const int32_t* pos; const double* freqs; const int32_t* starts; const uint8_t* keep;
+  const int32_t* plan_base; const int32_t* plan_count;             // NULL: lengths as they are, nothing dropped
+  int32_t H, Hk, total, rows, rot, interleaved;
+  float amplitude;
+  DeviceStatus* status;
+};
+
+// Eight pairs: x = their first values, y = their second; cs = cos and sin of each, in order.
+__device__ __forceinline__ void k16_turn(float (&x)[8], float (&y)[8], const float2* cs) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float2 w = cs[i];
+    const float a = x[i] * w.x - y[i] * w.y;
+    y[i] = y[i] * w.x + x[i] * w.y;
+    x[i] = a;
+  }
+}
+__device__ __forceinline__ uint32_t k16_pack(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ void k16_rotate(uint4& a, uint4& b, bool interleaved, const float2* cs) {
+  float x[8], y[8];
+  const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
+  uint32_t ra[4], rb[4];
+  if (interleaved) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = bf16lo(wa[i]); y[i] = bf16hi(wa[i]);
+      x[4 + i] = bf16lo(wb[i]); y[4 + i] = bf16hi(wb[i]);
+    }
+    k16_turn(x, y, cs);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { ra[i] = k16_pack(x[i], y[i]); rb[i] = k16_pack(x[4 + i], y[4 + i]); }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = bf16lo(wa[i]); x[2 * i + 1] = bf16hi(wa[i]);
+      y[2 * i] = bf16lo(wb[i]); y[2 * i + 1] = bf16hi(wb[i]);
+    }
+    k16_turn(x, y, cs);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { ra[i] = k16_pack(x[2 * i], x[2 * i + 1]); rb[i] = k16_pack(y[2 * i], y[2 * i + 1]); }
+  }
+  a = make_uint4(ra[0], ra[1], ra[2], ra[3]);
+  b = make_uint4(rb[0], rb[1], rb[2], rb[3]);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kK16Threads)
+kv16_append_kernel(const K16Pages pg, const K16Append a) {
+  extern __shared__ int seq_start[];
+  __shared__ int sh[kK16Threads / 32];
+  __shared__ float2 cs[kK16Rows][D / 2];
+  __shared__ int row_page[kK16Rows], row_in[kK16Rows];            // page (-1: not cached) and row in it
+  __shared__ int row_there[kK16Rows];                              // the row belongs to a sequence
+  chained_go();
+  chained_wait();
+  const int t0 = blockIdx.x * a.rows, n = min(a.rows, a.total - t0);
+  int b0 = -1, before = 0;                                         // the first row's sequence, its kept rows in front
+  if (a.pool) {
+    for (int b = threadIdx.x; b <= pg.B; b += kK16Threads) seq_start[b] = k16_start(a.starts, b, a.total);
+    __syncthreads();
+    b0 = k16_sequence(seq_start, pg.B, t0);
+    if (b0 >= 0) before = a.keep ? k16_count(a.keep, seq_start[b0], t0, sh) : t0 - seq_start[b0];
+  }
+  if (threadIdx.x < 32) {
+    const int t = threadIdx.x, r = t0 + t;
+    const bool in = t < n;
+    const int b = in && a.pool ? k16_sequence(seq_start, pg.B, r) : -1;
+    const bool f = b >= 0 && (a.keep == nullptr || __ldcg(a.keep + r) != 0);
+    const unsigned m = __ballot_sync(0xffffffffu, f);
+    int page = -1, at = 0;
+    if (b >= 0) {
+      const int base = a.plan_base ? __ldcg(a.plan_base + b) : __ldcg(pg.len + b);
+      const bool fits = a.plan_count ? __ldcg(a.plan_count + b) >= 0 : k16_fits(pg, b, base, seq_start[b + 1] - seq_start[b]);
+      if (!fits && r == seq_start[b] && blockIdx.y == 0) report_status(a.status, DL_ERR_CAPACITY, b);
+      if (fits && f) {
+        const int head = max(seq_start[b] - t0, 0);                // first lane of this sequence
+        const long long dst = (long long)base + (b == b0 ? before : 0) + __popc(m & ((1u << t) - 1u) & ~((1u << head) - 1u));
+        page = k16_page(pg, b, dst);
+        at = (int)(dst & ((1 << pg.shift) - 1));
+      }
+    }
+    if (in) {
+      row_page[t] = page;
+      row_in[t] = at;
+      row_there[t] = b >= 0 || a.pool == nullptr;
+    }
+  }
+  const int half = a.rot >> 1;
+  for (int i = threadIdx.x; i < n * half; i += kK16Threads) {
+    const int t = i / half, f = i - t * half;
+    // the angle as a fraction of a turn, 64 bits of it: products with positions wrap around by themselves
+    double turns = __ldcg(a.freqs + f) * 0.15915494309189533577;
+    turns -= floor(turns);
+    const uint64_t step = (uint64_t)__double2ull_rn(turns * 18446744073709551616.0);
+    const int64_t angle = (int64_t)((uint64_t)(int64_t)__ldcg(a.pos + t0 + t) * step);
+    float s, c;
+    sincospif((float)angle * 1.0842021724855044e-19f, &s, &c);     // half turns: 2^-63
+    cs[t][f] = make_float2(c * a.amplitude, s * a.amplitude);
+  }
+  __syncthreads();
+  constexpr int C = D / 16;                                        // units of 32 bytes per head
+  const int uq = a.q_out ? a.H * C : 0, uk = a.Hk * C, U = uq + uk + (a.pool ? uk : 0);
+  const int rot_units = a.rot >> 4;
+  for (int t = 0; t < n; ++t) {
+    if (!row_there[t]) continue;
+    const int page = row_page[t];
+    const long long r = t0 + t;
+    for (int u = blockIdx.y * kK16Threads + threadIdx.x; u < U; u += gridDim.y * kK16Threads) {
+      const int part = u < uq ? 0 : u < uq + uk ? 1 : 2;
+      const int x = u - (part == 0 ? 0 : part == 1 ? uq : uq + uk), h = x / C, c = x % C;
+      if (part > 0 && page < 0 && !(part == 1 && a.k_out)) continue;
+      const __nv_bfloat16* src = (part == 0 ? a.q + r * a.q_stride : (part == 1 ? a.k : a.v) + r * a.kv_stride) + h * D;
+      const bool turn = part < 2 && c < rot_units;
+      const int d0 = turn && !a.interleaved ? 8 * c : 16 * c, d1 = turn && !a.interleaved ? 8 * c + half : 16 * c + 8;
+      uint4 w0 = *reinterpret_cast<const uint4*>(src + d0), w1 = *reinterpret_cast<const uint4*>(src + d1);
+      if (turn) k16_rotate(w0, w1, a.interleaved != 0, &cs[t][8 * c]);
+      if (part == 0 || (part == 1 && a.k_out)) {
+        __nv_bfloat16* o = (part == 0 ? a.q_out + r * a.q_out_stride : a.k_out + r * a.k_out_stride) + h * D;
+        *reinterpret_cast<uint4*>(o + d0) = w0;
+        *reinterpret_cast<uint4*>(o + d1) = w1;
+      }
+      if (part > 0 && page >= 0) {
+        const long long at = k16_row(pg, a.Hk, page, part - 1, h, row_in[t]) * D;
+        if (DL_IN_BOUNDS(a.status, KID_KV16, at + D - 1, (((long long)pg.n_pages * 2 * a.Hk) << pg.shift) * D)) {
+          *reinterpret_cast<uint4*>(a.pool + at + d0) = w0;
+          *reinterpret_cast<uint4*>(a.pool + at + d1) = w1;
+        }
+      }
+    }
+  }
+}
+
+// ---- accepted rows ----------------------------------------------------------------------------------------------------
+constexpr int kK16Pools = 64;            // pools per launch
+struct K16Pools { char* p[kK16Pools]; };
+
+// grid: (sequence, slices of the pools' 16-byte columns).  Moves only; lengths follow in a launch of their own.
+template <int D>
+__global__ void __launch_bounds__(kK16Threads)
+kv16_move_kernel(const K16Pages pg, const __grid_constant__ K16Pools pools, int32_t n_pools, int32_t Hk, const int32_t* starts,
+                 const uint8_t* keep, int32_t total, DeviceStatus* st) {
+  __shared__ int sh[kK16Threads / 32], warp_sum[kK16Threads / 32];
+  __shared__ long long src_row[kK16Threads], dst_row[kK16Threads];  // K row of head 0 in the pool; -1: no page
+  chained_go();
+  chained_wait();
+  const int b = blockIdx.x, base = __ldcg(pg.len + b);
+  const int from = k16_start(starts, b, total), to = max(from, k16_start(starts, b + 1, total));
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  // the last kept row must have a page
+  int last = -1;
+  for (int i = from + threadIdx.x; i < to; i += kK16Threads)
+    if (__ldcg(keep + i) != 0) last = i - from;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) last = max(last, __shfl_xor_sync(0xffffffffu, last, o));
+  if (lane == 0) sh[warp] = last;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kK16Threads / 32; ++w) last = max(last, sh[w]);
+  if (last < 0) return;
+  if (!k16_fits(pg, b, base, last + 1)) {
+    if (blockIdx.y == 0 && threadIdx.x == 0) report_status(st, DL_ERR_CAPACITY, b);
+    return;
+  }
+  constexpr int C = D / 8;
+  const int columns = n_pools * 2 * Hk * C;
+  const long long v_off = (long long)Hk << pg.shift;               // rows from K to V of a page
+  int rank0 = 0;                                                   // kept rows of earlier rounds
+  for (int i0 = 0; i0 <= last; i0 += kK16Threads) {
+    const int i = i0 + threadIdx.x;
+    const bool f = i <= last && __ldcg(keep + from + i) != 0;
+    const unsigned m = __ballot_sync(0xffffffffu, f);
+    if (lane == 0) warp_sum[warp] = __popc(m);
+    __syncthreads();
+    int rank = __popc(m & ((1u << lane) - 1u)), count = 0;
+#pragma unroll
+    for (int w = 0; w < kK16Threads / 32; ++w) {
+      if (w < warp) rank += warp_sum[w];
+      count += warp_sum[w];
+    }
+    if (f) {
+      const long long s = (long long)base + i, d = (long long)base + rank0 + rank;
+      const int ps = k16_page(pg, b, s), pd = k16_page(pg, b, d);
+      const bool there = ps >= 0 && pd >= 0 && s != d;
+      src_row[rank] = there ? k16_row(pg, Hk, ps, 0, 0, s) : -1;
+      dst_row[rank] = there ? k16_row(pg, Hk, pd, 0, 0, d) : -1;
+    }
+    __syncthreads();
+    for (int u = blockIdx.y * kK16Threads + threadIdx.x; u < columns; u += gridDim.y * kK16Threads) {
+      const int c = u % C, h = (u / C) % Hk, kv = (u / (C * Hk)) & 1, l = u / (2 * C * Hk);
+      __nv_bfloat16* pool = reinterpret_cast<__nv_bfloat16*>(pools.p[l]) + (kv * v_off + ((long long)h << pg.shift)) * D + 8 * c;
+      for (int j = 0; j < count; j += 4) {
+        uint4 w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (j + k < count && src_row[j + k] >= 0) w[k] = *reinterpret_cast<const uint4*>(pool + src_row[j + k] * D);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (j + k < count && dst_row[j + k] >= 0 &&
+              DL_IN_BOUNDS(st, KID_KV16, dst_row[j + k], ((long long)pg.n_pages * 2 * Hk) << pg.shift))
+            *reinterpret_cast<uint4*>(pool + dst_row[j + k] * D) = w[k];
+      }
+    }
+    rank0 += count;
+    __syncthreads();
+  }
+}
+
+__global__ void __launch_bounds__(kK16Threads)
+kv16_advance_kernel(const K16Pages pg, const int32_t* starts, const uint8_t* keep, int32_t total) {
+  chained_go();
+  chained_wait();
+  const int b = blockIdx.x * (kK16Threads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (b >= pg.B) return;
+  const int base = __ldcg(pg.len + b);
+  const int from = k16_start(starts, b, total), to = max(from, k16_start(starts, b + 1, total));
+  int count = 0, last = -1;
+  for (int i = from + lane; i < to; i += 32)
+    if (__ldcg(keep + i) != 0) { ++count; last = i - from; }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    count += __shfl_xor_sync(0xffffffffu, count, o);
+    last = max(last, __shfl_xor_sync(0xffffffffu, last, o));
+  }
+  if (lane == 0 && count > 0 && k16_fits(pg, b, base, last + 1)) pg.len[b] = base + count;
+}
+
+// ---- trees ------------------------------------------------------------------------------------------------------------
+// One CTA per sequence: parents in shared memory, a thread per (node, word) walks up.
+__global__ void __launch_bounds__(kK16Threads)
+tree_plan_kernel(const int32_t* parent, const int32_t* starts, const int32_t* pos0, int32_t total, int32_t words,
+                 int32_t* mask, int32_t* pos, DeviceStatus* st) {
+  extern __shared__ int up[];
+  chained_go();
+  chained_wait();
+  const int b = blockIdx.x;
+  const int from = k16_start(starts, b, total), to = max(from, k16_start(starts, b + 1, total));
+  const int n = min(to - from, 32 * words);
+  bool bad = to - from > n;
+  for (int i = threadIdx.x; i < n; i += kK16Threads) {
+    int p = i == 0 ? -1 : __ldcg(parent + from + i);
+    if (p < -1 || p >= i) { bad = true; p = -1; }
+    up[i] = p;
+  }
+  if (bad) report_status(st, DL_ERR_INVALID_ARG, b);
+  __syncthreads();
+  const int first = pos0 ? __ldcg(pos0 + b) : 0;
+  for (int x = threadIdx.x; x < n * words; x += kK16Threads) {
+    const int i = x / words, w = x - i * words;
+    uint32_t bits = 0;
+    int depth = -1;
+    for (int j = i; j >= 0; j = up[j]) {
+      ++depth;
+      if ((j >> 5) == w) bits |= 1u << (j & 31);
+    }
+    mask[(size_t)(from + i) * words + w] = (int32_t)bits;
+    if (w == 0 && pos) pos[from + i] = (int32_t)((uint32_t)first + (uint32_t)depth);
+  }
+}
+
+// ---- launchers --------------------------------------------------------------------------------------------------------
+cudaError_t launch_kv16_append(const dl_ctx* ctx, const dl_pages* p, int32_t Hk, void* pool, const void* q, int64_t q_stride,
+                               const void* k, const void* v, int64_t kv_stride, const int32_t* pos, const dl_rope* rope,
+                               const int32_t* starts, const uint8_t* keep, int32_t total, void* q_out, int64_t q_out_stride,
+                               void* k_out, int64_t k_out_stride, int32_t commit, cudaStream_t s) {
+  const int D = ctx->desc.head_dim, H = ctx->desc.n_heads;
+  const K16Pages pg = k16_pages(p);
+  K16Append a = {};
+  a.q = static_cast<const __nv_bfloat16*>(q); a.k = static_cast<const __nv_bfloat16*>(k); a.v = static_cast<const __nv_bfloat16*>(v);
+  a.q_out = static_cast<__nv_bfloat16*>(q_out); a.k_out = static_cast<__nv_bfloat16*>(k_out); a.pool = static_cast<__nv_bfloat16*>(pool);
+  a.q_stride = q_stride; a.kv_stride = kv_stride; a.q_out_stride = q_out_stride; a.k_out_stride = k_out_stride;
+  a.pos = pos; a.starts = starts; a.keep = pool ? keep : nullptr;
+  a.H = H; a.Hk = Hk; a.total = total;
+  a.amplitude = 1.f;
+  if (rope) { a.freqs = rope->freqs; a.rot = rope->rot_dim; a.interleaved = rope->interleaved; a.amplitude = rope->amplitude; }
+  a.status = ctx->ws.base ? ctx->ws.status : nullptr;
+  if (pool && (keep || commit)) {
+    a.plan_base = ctx->ws.plan_base;
+    a.plan_count = ctx->ws.plan_count;
+    const cudaError_t e = launch_chained(kv16_plan_kernel, dim3(pg.B), dim3(kK16Threads), 0, s, pg, starts, keep, total, commit,
+                                         ctx->ws.plan_base, ctx->ws.plan_count);
+    if (e != cudaSuccess) return e;
+  }
+  const int units = ((q_out ? H : 0) + (pool ? 2 : 1) * Hk) * (D / 16);
+  a.rows = std::min(kK16Rows, std::max(1, total / (8 * ctx->sm_count)));
+  const int slices = a.rows > 1 ? 1 : std::min((units + kK16Threads - 1) / kK16Threads, std::max(1, 8 * ctx->sm_count / total));
+  const dim3 grid((total + a.rows - 1) / a.rows, slices);
+  const size_t smem = pool ? (size_t)(pg.B + 1) * 4 : 0;
+  return D == 128 ? launch_chained(kv16_append_kernel<128>, grid, dim3(kK16Threads), smem, s, pg, a)
+                  : launch_chained(kv16_append_kernel<64>, grid, dim3(kK16Threads), smem, s, pg, a);
+}
+
+cudaError_t launch_kv16_commit(const dl_ctx* ctx, const dl_pages* p, int32_t Hk, int32_t n_pools, void* const* pools,
+                               const int32_t* starts, const uint8_t* keep, int32_t total, cudaStream_t s) {
+  const K16Pages pg = k16_pages(p);
+  DeviceStatus* st = ctx->ws.base ? ctx->ws.status : nullptr;
+  const int D = ctx->desc.head_dim;
+  for (int at = 0; at < n_pools; at += kK16Pools) {
+    K16Pools pp = {};
+    const int n = std::min(kK16Pools, n_pools - at);
+    for (int i = 0; i < n; ++i) pp.p[i] = static_cast<char*>(pools[at + i]);
+    const int slices = (int)std::min<long long>(((long long)n * 2 * Hk * (D / 8) + kK16Threads - 1) / kK16Threads, 4096);
+    const dim3 grid(pg.B, slices);
+    const cudaError_t e = D == 128 ? launch_chained(kv16_move_kernel<128>, grid, dim3(kK16Threads), 0, s, pg, pp, n, Hk, starts, keep, total, st)
+                                   : launch_chained(kv16_move_kernel<64>, grid, dim3(kK16Threads), 0, s, pg, pp, n, Hk, starts, keep, total, st);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_chained(kv16_advance_kernel, dim3((pg.B + kK16Threads / 32 - 1) / (kK16Threads / 32)), dim3(kK16Threads), 0, s,
+                        pg, starts, keep, total);
+}
+
+cudaError_t launch_tree_plan(const dl_ctx* ctx, const int32_t* parent, const int32_t* starts, const int32_t* pos0, int32_t B,
+                             int32_t total, int32_t words, int32_t* mask, int32_t* pos, cudaStream_t s) {
+  const size_t smem = (size_t)std::min(32 * words, total) * 4;
+  return launch_chained(tree_plan_kernel, dim3(B), dim3(kK16Threads), smem, s, parent, starts, pos0, total, words, mask, pos,
+                        ctx->ws.base ? ctx->ws.status : nullptr);
+}
+
+}  // namespace dl
