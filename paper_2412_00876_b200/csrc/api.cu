@@ -1,6 +1,7 @@
 // Host side of the C ABI: argument checks, workspace layout, dispatch to the kernel launchers.
 // No call here allocates device memory or synchronises, except where dl.h says so.
 #include <math.h>
+#include <algorithm>
 #include <new>
 #include <string.h>
 
@@ -27,7 +28,7 @@ int64_t workspace_layout(const dl_model_desc& d, int32_t sm_count, int32_t max_b
   const int64_t o_pstick = take((int64_t)kPredMaxSplit * 4);
   const int64_t o_commit = take(2 * 4);
   const int64_t o_ones = take(max_batch);
-  const int64_t o_kv4 = take(d.dtype == DL_BF16 ? kv4_scratch_floats(sm_count, d) * 4 : 0);
+  const int64_t o_kv4 = take(d.dtype == DL_BF16 ? std::max(kv4_scratch_floats(sm_count, d), attn_tree_scratch_floats(sm_count, d)) * 4 : 0);
   if (ws) {
     char* b = ws->base;
     ws->status = reinterpret_cast<DeviceStatus*>(b + o_status);
@@ -957,6 +958,8 @@ int32_t dl_kv16_attn_tree(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads
   if (st != DL_OK) return st;
   if (total < 0 || max_rows < 0 || !(scale > 0.f) || (mask && words < 1)) return DL_ERR_INVALID_ARG;
   if (mask && words >= (1 << 24)) return DL_ERR_UNSUPPORTED;
+  if ((int64_t)pages->max_pages * pages->page_rows + total >= (1LL << 31) - 256) return DL_ERR_UNSUPPORTED;
+  if (!attn_tree_supported(ctx)) return DL_ERR_UNSUPPORTED;
   if (pages->B == 0 || total == 0 || max_rows == 0) return DL_OK;
   if (!pool || !q || !starts || !out) return DL_ERR_INVALID_ARG;
   if (misaligned(pool) || misaligned(q) || misaligned(out) || misaligned(mask)) return DL_ERR_ALIGNMENT;

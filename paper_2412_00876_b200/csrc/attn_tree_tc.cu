@@ -1,0 +1,836 @@
+// Attention of new rows (trees of drafted tokens, chunks of a prompt, single tokens) over a paged cache in 16 bits, on the tensor
+// cores.  An extension, not in the paper.  bf16, head_dim 64 or 128.
+//
+// Sequence b's n new rows (nodes) attend the cache's rows [0, held) and, by a mask or causally, the n rows behind them, which hold
+// the nodes' own K and V.  The G query heads of a K/V head and the nodes make one matrix: row = (node, head), 128 / G nodes a
+// tile of 128 rows (one TMA box [nodes][G heads][64 dims] is just that).  Keys come in tiles of 128 rows, a TMA box per page.
+// Few rows and many keys is the usual shape, so the work is (sequence, tile of rows, K/V head) items of T key tiles each, and ALL
+// key tiles of a call are cut into as many even ranges as there are CTAs, whatever the lengths are: a CTA's range covers the end
+// of one item, some whole ones, the start of another.  Items cut by a border leave their parts (sums, row maxima) in
+// scratch, and a second kernel joins them in order: no result depends on timing.
+//   warp 8        : the producer: Q tiles, then K and V tiles through a ring
+//   warps 9, 10   : issue the MMAs of lane A / B: S = Q K^T into tensor memory, O += P V with P read from tensor memory
+//   warps 0-3/4-7 : softmax and epilogue of lane A / B, one row per thread
+//   warp 11       : allocates tensor memory (512 columns: O_A | S_A | O_B | S_B)
+// A lane is a chain (softmax, P V and Q K^T, softmax); two of them keep the pipes busy.  What the lanes share is the template's
+// choice.  Up to 128 rows (kPair false): both work on the same rows, lane A the even key tiles, B the odd ones, each through a ring
+// of its own, and an item's end adds the two up.  More rows (kPair true): each lane has a tile of rows, and a K/V tile serves both.
+// Every wait is bounded (pipeline.cuh); an abort leaves DL_ERR_TIMEOUT in the status word.
+#include <algorithm>
+
+#include "attn_packed_softmax.cuh"
+#include "attn_prefill.cuh"
+#include "kv16.cuh"
+#include "tc05.cuh"
+
+namespace dl {
+
+constexpr int kTrThreads = 384;
+constexpr int kTrBM = 128, kTrBN = 128;
+constexpr int kTrRegsSmall = 40, kTrRegsSoftmax = 232;             // as in attn_packed_tc.cu
+constexpr int kTrPatience = 4000, kTrTurnTiles = 4;                // as there: polls for a turn, tiles from which lanes take turns
+constexpr int kTrSeen = 16;                                        // key tiles whose page flags are kept
+
+template <int D, bool kPair> struct Tr {
+  static constexpr int HALF = 128 * 128;               // 128 rows of 64 dims
+  static constexpr int TILE = (D / 64) * HALF;         // one operand tile
+  static constexpr int Q_TILES = kPair ? 2 : 1;
+  static constexpr int SLOTS = D == 128 ? 7 - Q_TILES : 12;
+  // Slots of a ring.  A wait by parity only tells one use of a slot from the next: whoever waits for a slot's uses has to wait for
+  // every one of them.  So lanes that take different tiles have a ring each.
+  static constexpr int RING = kPair ? SLOTS : SLOTS / 2;
+  static constexpr int KV = Q_TILES * TILE;            // offset of the rings (behind the Q tiles)
+  static constexpr int EXCH = KV + SLOTS * TILE;       // [2][128] row maximum and sum of the lanes
+  static constexpr int BAR = EXCH + 2 * 128 * 8;
+  static constexpr int SMEM = BAR + 512;
+};
+
+struct TrMaps { alignas(64) unsigned char q[128]; alignas(64) unsigned char kv[128]; };
+
+// What a CTA's range begins with, for the joining kernel.
+struct TrHead { int b, q0, h, t; int T, n, row0, pad; long long units, first; };
+
+struct TrArgs {
+  const int32_t* starts; const int32_t* mask; __nv_bfloat16* out; DeviceStatus* status;
+  TrHead* heads; float* parts;                         // [grid], [grid][2 slots][rows of an item][D + 2]
+  int32_t H, Hk, G, PB, total, max_rows, said_rows, words;   // PB: nodes per tile of rows
+  int32_t box_rows;                                    // nodes per Q box
+  uint32_t pool_rows;                                  // rows of the pool's tensor map
+  int32_t wide;                                        // out is 32-byte aligned
+  float scale_log2;
+};
+
+// Key tiles of an item: nodes [q0, ...) of a sequence.
+template <bool kPair>
+__device__ __forceinline__ int tr_reach(const TrArgs& a, int q0) { return q0 + (kPair ? 2 : 1) * a.PB; }
+template <bool kPair>
+__device__ __forceinline__ int tr_tiles(const TrArgs& a, int held, int n, int q0) {
+  return (held + (a.mask ? n : min(n, tr_reach<kPair>(a, q0))) + kTrBN - 1) / kTrBN;
+}
+
+struct TrSeq { int row0, n, held; };
+__device__ __forceinline__ TrSeq tr_seq(const K16Pages& pg, const TrArgs& a, int b) {
+  TrSeq s;
+  s.row0 = k16_start(a.starts, b, a.total);
+  s.n = min(max(k16_start(a.starts, b + 1, a.total) - s.row0, 0), a.max_rows);
+  s.held = (int)min((long long)max(__ldcg(pg.len + b), 0), (long long)pg.W << pg.shift);
+  return s;
+}
+
+// A CTA's share of an item: key tiles [t, t + nt) of T.
+struct TrItem { int b, h, row0, n, held, q0, T, t, nt; bool first; };
+// One lane's share of that: rows of nodes [q0, q_hi), `keys` of which it may see, tiles j = lane's first, + step, ...
+struct TrLane { int q0, q_hi, keys, n_tiles; };
+
+template <bool kPair>
+__device__ __forceinline__ TrLane tr_lane(const TrArgs& a, const TrItem& I, int x) {
+  TrLane L;
+  L.q0 = I.q0 + (kPair ? x * a.PB : 0);
+  L.q_hi = min(I.n, L.q0 + a.PB);
+  L.keys = I.held + (a.mask ? I.n : L.q_hi);
+  if (kPair) L.n_tiles = L.q0 < I.n ? min(max((L.keys + kTrBN - 1) / kTrBN - I.t, 0), I.nt) : 0;
+  else L.n_tiles = (I.nt + 1 - x) >> 1;
+  return L;
+}
+// the lane's i-th tile, counted from the share's first
+template <bool kPair> __device__ __forceinline__ int tr_tile(int i, int x) { return kPair ? i : 2 * i + x; }
+// keys of the share's tile j that a lane's MMAs cover
+__device__ __forceinline__ int tr_cols(const TrItem& I, const TrLane& L, int j) {
+  return min(kTrBN, (L.keys - (I.t + j) * kTrBN + 15) & ~15);
+}
+// Walks a CTA's items; every role does so for itself.
+template <bool kPair>
+struct TrWalker {
+  const K16Pages& pg; const TrArgs& a;
+  TrSeq s, ahead;                                      // the sequence, the one behind it (requested early)
+  int b, h, q0, t; long long left; bool first;
+  __device__ __forceinline__ TrWalker(const K16Pages& pg_, const TrArgs& a_, const TrHead& hd) : pg(pg_), a(a_) {
+    b = hd.b; h = hd.h; q0 = hd.q0; t = hd.t; left = hd.units; first = true;
+    if (left > 0) { s = tr_seq(pg, a, b); fetch(); }
+  }
+  __device__ __forceinline__ void fetch() {
+    ahead.row0 = ahead.n = ahead.held = 0;
+    if (b + 1 < pg.B) ahead = tr_seq(pg, a, b + 1);
+  }
+  __device__ __forceinline__ bool next(TrItem& I) {
+    if (left <= 0) return false;
+    I.b = b; I.h = h; I.row0 = s.row0; I.n = s.n; I.held = s.held; I.q0 = q0; I.t = t; I.first = first;
+    I.T = tr_tiles<kPair>(a, s.held, s.n, q0);
+    I.nt = (int)min((long long)(I.T - t), left);
+    left -= I.nt;
+    first = false;
+    t = 0;
+    if (left > 0 && ++h == a.Hk) {
+      h = 0;
+      q0 = tr_reach<kPair>(a, q0);
+      if (q0 >= s.n) {
+        q0 = 0;
+        do { ++b; s = ahead; fetch(); } while (s.n == 0 && b + 1 < pg.B);
+        if (s.n == 0) left = 0;                        // (the ranges end with the last sequence that has nodes)
+      }
+    }
+    return true;
+  }
+};
+
+// 32 bits of a row's mask from bit j0 on (j0 > -32 or lower: zeros come in front and behind).
+__device__ __forceinline__ uint32_t tr_mask_bits(const int32_t* row, int words, int j0) {
+  const int w = j0 >> 5;
+  const uint32_t lo = w >= 0 && w < words ? (uint32_t)__ldcg(row + w) : 0u;
+  const uint32_t hi = w + 1 >= 0 && w + 1 < words ? (uint32_t)__ldcg(row + w + 1) : 0u;
+  return __funnelshift_r(lo, hi, j0 & 31);
+}
+__device__ __forceinline__ uint32_t tr_low(int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u; }
+
+// The softmax of a tile of which a row sees the columns whose bits are set in vis (bit c of word q: column 32 q + c): 32 columns at a
+// time in a rolled loop; otherwise as in attn_prefill_softmax.cuh.
+__device__ __forceinline__ void tr_softmax_words(uint32_t s_addr, uint32_t o_addr, int n_ch, const uint32_t (&vis)[4], bool owned,
+                                                 int o_blocks, float scale_log2, float& m_used, float& l_run) {
+  const uint64_t sc2 = pack2(scale_log2, scale_log2);
+  uint32_t v0 = vis[0], v1 = vis[1], v2 = vis[2], v3 = vis[3];
+#pragma unroll 1
+  for (int q = 0; q < 4; ++q) {
+    uint32_t pk[16];
+    if (q < n_ch) {
+      uint32_t buf[32];
+      tmem_ld32(s_addr + 32 * q, buf);
+      tmem_ld_wait();
+#pragma unroll
+      for (int c = 0; c < 32; ++c)
+        if (!((v0 >> c) & 1)) buf[c] = 0xFF800000u;                // -inf
+      float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int c = 0; c < 32; c += 8) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          mx4[w] = fmax3(mx4[w], __uint_as_float(buf[c + 2 * w]), __uint_as_float(buf[c + 2 * w + 1]));
+      }
+      const float mc = fmax3(mx4[0], mx4[1], fmaxf(mx4[2], mx4[3])) * scale_log2;
+      const bool need = owned && mc > m_used + kRescaleStep;
+      if (__any_sync(0xffffffffu, need)) {
+        const float corr = need ? fast_exp2(m_used - mc) : 1.0f;
+        if (need) m_used = mc;
+        l_run *= corr;
+        at_rescale_row(o_addr, s_addr, q, corr, o_blocks);
+      }
+      const uint64_t nm2 = pack2(-m_used, -m_used);
+      float la = 0.f, lb = 0.f;
+#pragma unroll
+      for (int c = 0; c < 16; ++c) {
+        float e0, e1;
+        unpack2(ffma2(pack2(__uint_as_float(buf[2 * c]), __uint_as_float(buf[2 * c + 1])), sc2, nm2), e0, e1);
+        e0 = fast_exp2(e0);
+        e1 = fast_exp2(e1);
+        la += e0;
+        lb += e1;
+        pk[c] = cvt_bf16x2(e0, e1);
+      }
+      l_run += la + lb;
+    } else {
+#pragma unroll
+      for (int c = 0; c < 16; ++c) pk[c] = 0u;
+    }
+    tmem_st16(s_addr + 16 * q, pk);
+    v0 = v1; v1 = v2; v2 = v3;
+  }
+  tmem_st_wait();
+}
+
+// 32 bytes from registers; where the address is a multiple of 32, in one access
+__device__ __forceinline__ void tr_store32(void* p, const uint32_t* r) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               :: "l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+
+__device__ __forceinline__ void tr_store32_any(void* p, const uint32_t* r, int wide) {
+  if (wide) { tr_store32(p, r); return; }
+  static_cast<uint4*>(p)[0] = make_uint4(r[0], r[1], r[2], r[3]);
+  static_cast<uint4*>(p)[1] = make_uint4(r[4], r[5], r[6], r[7]);
+}
+
+// Where the CTA's even range of all key tiles begins: found by the whole CTA, left in *hd (shared); scratch: shared.
+template <bool kPair>
+__device__ __forceinline__ void tr_find(const K16Pages& pg, const TrArgs& a, TrHead* hd, long long* scratch) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per = (pg.B + kTrThreads - 1) / kTrThreads, b0 = min(pg.B, tid * per), b1 = min(pg.B, b0 + per);
+  auto units = [&](const TrSeq& s) {
+    long long u = 0;
+    for (int q0 = 0; q0 < s.n; q0 = tr_reach<kPair>(a, q0)) u += tr_tiles<kPair>(a, s.held, s.n, q0);
+    return u * a.Hk;
+  };
+  long long mine = 0;
+  for (int b = b0; b < b1; ++b) mine += units(tr_seq(pg, a, b));
+  long long run = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long v = __shfl_up_sync(0xffffffffu, run, o);
+    if (lane >= o) run += v;
+  }
+  if (lane == 31) scratch[warp] = run;
+  if (tid == 0) hd->units = 0;
+  __syncthreads();
+  long long front = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kTrThreads / 32; ++w) {
+    if (w < warp) front += scratch[w];
+    all += scratch[w];
+  }
+  const long long u0 = all * blockIdx.x / gridDim.x, u1 = all * (blockIdx.x + 1) / gridDim.x;
+  long long at = front + run - mine;                   // units in front of this thread's sequences
+  if (u0 < u1 && at <= u0 && u0 < at + mine) {
+    for (int b = b0; b < b1; ++b) {
+      const TrSeq s = tr_seq(pg, a, b);
+      const long long u = units(s);
+      if (u0 >= at + u) { at += u; continue; }
+      int rest_q0 = 0;
+      long long rest = u0 - at;
+      for (; rest_q0 < s.n; rest_q0 = tr_reach<kPair>(a, rest_q0)) {
+        const long long x = (long long)tr_tiles<kPair>(a, s.held, s.n, rest_q0) * a.Hk;
+        if (rest < x) break;
+        rest -= x;
+      }
+      hd->b = b; hd->q0 = rest_q0; hd->n = s.n; hd->row0 = s.row0;
+      hd->T = tr_tiles<kPair>(a, s.held, s.n, rest_q0);
+      hd->h = (int)(rest / hd->T);
+      hd->t = (int)(rest - (long long)hd->h * hd->T);
+      hd->units = u1 - u0;
+      hd->first = u0;
+      break;
+    }
+  }
+  __syncthreads();
+}
+
+template <int D, bool kPair>
+__global__ void __launch_bounds__(kTrThreads, 1)
+attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const TrArgs a) {
+  using S = Tr<D, kPair>;
+  extern __shared__ __align__(1024) char smem[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  chained_go();
+  if (smem_u32(smem) & 1023u) {                        // the swizzled tiles need 1024-byte alignment
+    if (tid == 0) report_status(a.status, DL_ERR_ALIGNMENT, -1);
+    chained_wait();
+    return;
+  }
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::BAR);
+  auto kv_full = [&](int i) { return smem_u32(bars + i); };
+  auto kv_empty = [&](int i) { return smem_u32(bars + S::SLOTS + i); };
+  // Q_*: of a Q tile (kPair: the lane's; else tile 0); the others of a lane
+  enum { Q_FULL = 0, Q_EMPTY, S_FULL, P_HALF, P_FULL, O_FULL, O_FREE, N_BAR };
+  auto bar = [&](int x, int i) { return smem_u32(bars + 2 * S::SLOTS + x * N_BAR + i); };
+  static_assert(2 * S::SLOTS + 2 * N_BAR <= 40, "barriers");
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 40);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 41);
+  volatile int* passes = reinterpret_cast<volatile int*>(bars + 42);         // [lane x][warp quad]: softmax passes behind it
+  volatile uint8_t* seen = reinterpret_cast<volatile uint8_t*>(bars + 46);   // [kTrSeen]: which 16-row parts of a tile have pages
+  TrHead* hd = reinterpret_cast<TrHead*>(bars + 48);
+  static_assert(48 * 8 + sizeof(TrHead) <= 512, "shared memory behind the barriers");
+
+  if (tid == 0) {
+    *abort_flag = 0;
+    for (int i = 0; i < 8; ++i) passes[i] = 0;
+    for (int i = 0; i < S::SLOTS; ++i) { mbar_init(kv_full(i), 1); mbar_init(kv_empty(i), kPair ? 2 : 1); }
+    for (int x = 0; x < 2; ++x)
+      for (int i = 0; i < N_BAR; ++i)
+        mbar_init(bar(x, i), i == P_HALF || i == P_FULL ? 4 : i == O_FREE ? (kPair ? 4 : 8) : i == Q_EMPTY ? (kPair ? 1 : 2) : 1);
+    fence_mbar_init();
+  }
+  if (warp == 11) { tmem_alloc(smem_u32(tmem_slot), 512); tmem_relinquish(); }
+  chained_wait();
+  tr_find<kPair>(pg, a, hd, reinterpret_cast<long long*>(smem));             // (the ring is not in use yet)
+  fence_proxy_async();
+  if (tid == 0) a.heads[blockIdx.x] = *hd;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp == 8) {
+    // ---------------------------------------------------------------- producer
+    reg_dec<kTrRegsSmall>();
+    const CUtensorMap* mq = reinterpret_cast<const CUtensorMap*>(maps.q);
+    const CUtensorMap* mkv = reinterpret_cast<const CUtensorMap*>(maps.kv);
+    if (lane == 0) { tma_prefetch_desc(mq); tma_prefetch_desc(mkv); }
+    TrWalker<kPair> W(pg, a, *hd);
+    TrItem I;
+    int n_q[2] = {0, 0}, ring[2] = {0, 0}, tiles = 0;  // Q tiles per place, tiles per ring, key tiles so far
+    bool ok = true, stop = false;
+    const int page_rows = 1 << pg.shift, ppt = kTrBN >> pg.shift;            // pages per tile
+    const uint32_t page_bytes = (uint32_t)page_rows * 128u;                  // of 64 dims
+    auto wait = [&](uint32_t b, uint32_t parity) { ok = mbar_wait_spin(b, parity & 1u, abort_flag) && ok; };
+    auto load_q = [&](int buf, int q0) {               // whole warp; true: the warp goes on
+      wait(bar(buf, Q_EMPTY), ((uint32_t)n_q[buf] & 1u) ^ 1u);
+      if (!warp_agreed(ok)) { stop = true; return; }
+      ++n_q[buf];
+      if (lane == 0) {
+        mbar_expect_tx(bar(buf, Q_FULL), (uint32_t)(D / 64) * 128u * (uint32_t)(a.box_rows * a.G));
+#pragma unroll
+        for (int hf = 0; hf < D / 64; ++hf)
+          tma_load_3d(smem_u32(smem + buf * S::TILE + hf * S::HALF), mq, 64 * hf, I.h * a.G, I.row0 + q0, bar(buf, Q_FULL));
+      }
+      __syncwarp();
+    };
+    while (!stop && W.next(I)) {
+      // page numbers of the share, 32 at a time in the warp's lanes: those of K's tile, and of the block in front for V's
+      const int32_t* row = pg.table + (size_t)I.b * pg.W;
+      const int first_page = I.t * ppt, limit = min(pg.W, (I.held + I.n + page_rows - 1) >> pg.shift);
+      auto block = [&](int k) {
+        const int i = first_page + 32 * k + lane;
+        return i < limit ? __ldcg(row + i) : -1;
+      };
+      int blk = 0, cur = block(0), before = -1, after = block(1);
+      const int rows_all = I.held + I.n;
+      auto load = [&](int kv, int j) {                 // whole warp
+        const int x = kPair ? 0 : j & 1, use = ring[x] / S::RING, slot = x * S::RING + ring[x] % S::RING;
+        wait(kv_empty(slot), ((uint32_t)use & 1u) ^ 1u);
+        if (!warp_agreed(ok)) { stop = true; return; }
+        ++ring[x];
+        const int k = (j * ppt) >> 5;
+        if (k > blk) { before = cur; cur = after; ++blk; after = block(blk + 1); }
+        const int entry = __shfl_sync(0xffffffffu, k == blk ? cur : before, ((j * ppt) & 31) + (lane < ppt ? lane : 0));
+        const int c0 = (I.t + j) * kTrBN;
+        const int pages = min(ppt, (rows_all - c0 + page_rows - 1) >> pg.shift);
+        const bool mine = lane < pages, there = (unsigned)entry < (unsigned)pg.n_pages;
+        if (kv == 0) {                                 // 16-row parts with a page, for the softmax
+          const int part = lane >> (pg.shift - 4);      // this lane's part lies in that page
+          const unsigned miss = __ballot_sync(0xffffffffu, mine && !there);
+          const unsigned parts = __ballot_sync(0xffffffffu, lane < 8 && !((miss >> part) & 1));
+          if (lane == 0) seen[tiles % kTrSeen] = (uint8_t)parts;
+          ++tiles;
+          if (mine && !there) report_status(a.status, DL_ERR_INVALID_ARG, I.b);
+        }
+        if (lane == 0) mbar_expect_tx(kv_full(slot), (uint32_t)(D / 64) * page_bytes * (uint32_t)pages);
+        __syncwarp();
+        if (mine) {
+          // (a page that is not there: rows behind the pool, which read as zero)
+          int y = there ? (int)k16_row(pg, a.Hk, entry, kv, I.h, 0) : (int)a.pool_rows;
+          if (!DL_IN_BOUNDS(a.status, KID_TREE, y, (long long)a.pool_rows + 1)) y = (int)a.pool_rows;
+#pragma unroll
+          for (int hf = 0; hf < D / 64; ++hf)
+            tma_load_2d(smem_u32(smem + S::KV + slot * S::TILE + hf * S::HALF) + (uint32_t)lane * page_bytes, mkv, 64 * hf, y, kv_full(slot));
+        }
+        __syncwarp();
+      };
+      if (kPair) {
+        if (tr_lane<kPair>(a, I, 0).n_tiles > 0) load_q(0, I.q0);
+        if (!stop) load(0, 0);
+        if (!stop && tr_lane<kPair>(a, I, 1).n_tiles > 0) load_q(1, I.q0 + a.PB);
+        for (int j = 0; j < I.nt && !stop; ++j) {
+          load(1, j);
+          if (!stop && j + 1 < I.nt) load(0, j + 1);
+        }
+      } else {
+        load_q(0, I.q0);
+        if (!stop) load(0, 0);
+        if (!stop && I.nt > 1) load(0, 1);
+        for (int j = 0; j < I.nt && !stop; ++j) {
+          load(1, j);
+          if (!stop && j + 2 < I.nt) load(0, j + 2);
+        }
+      }
+    }
+    if (stop && lane == 0) {
+      // what was requested must land before the CTA's shared memory is released
+      for (int x = 0; x < 2; ++x)
+        for (int i = max(0, ring[x] - S::RING); i < ring[x]; ++i)
+          for (int k = 0; k < kSpinLimit && !mbar_try_wait(kv_full(x * S::RING + i % S::RING), (uint32_t)(i / S::RING) & 1u); ++k) __nanosleep(40);
+      for (int x = 0; x < 2; ++x)
+        if (n_q[x] > 0)
+          for (int k = 0; k < kSpinLimit && !mbar_try_wait(bar(x, Q_FULL), (uint32_t)(n_q[x] - 1) & 1u); ++k) __nanosleep(40);
+    }
+  } else if (warp == 9 || warp == 10) {
+    // ---------------------------------------------------------------- MMA issuer of one lane
+    // The whole warp walks the loop, so that counters and descriptors stay warp-uniform, and one elected lane issues.  Its lanes
+    // wait each for itself, so the warp agrees before it goes on or stops.
+    reg_dec<kTrRegsSmall>();
+    const int x = warp - 9;
+    const uint32_t t_o = uniform32(tmem + x * kAtLaneCols + kAtColO), t_s = uniform32(tmem + x * kAtLaneCols + kAtColS);
+    constexpr uint32_t idesc_pv = idesc_bf16(kTrBM, D, 0, 1);          // B (= V) is MN-major
+    const uint64_t q_base = uniform64(smem_desc_sw128(smem_u32(smem)));
+    const uint64_t kv_desc = uniform64(smem_desc_sw128(smem_u32(smem + S::KV)));
+    const uint64_t v_desc = uniform64(smem_desc_sw128_mn(smem_u32(smem + S::KV), S::HALF));
+    TrWalker<kPair> W(pg, a, *hd);
+    TrItem I;
+    int n_item = 0, n_mine = 0, g0 = 0, ring0 = 0;     // items, those with tiles of this lane, its tiles, its ring's tiles so far
+    bool ok = true, stop = false;                      // this lane's waits so far; the warp has agreed to stop
+    auto wait = [&](uint32_t b, uint32_t parity) { ok = mbar_wait_spin(b, parity & 1u, abort_flag) && ok; };
+    while (!stop && W.next(I)) {
+      const TrLane L = tr_lane<kPair>(a, I, x);
+      const int n_sub = L.n_tiles;
+      auto full = [&](int u, int is_v) {               // waits for K or V of tile u of the ring's share; returns its slot
+        const int t = ring0 + 2 * u + is_v, slot = (kPair ? 0 : x * S::RING) + t % S::RING;
+        wait(kv_full(slot), (uint32_t)(t / S::RING));
+        return slot;
+      };
+      const int qb = kPair ? x : 0;                    // Q tile
+      const uint32_t q_use = (uint32_t)(kPair ? n_mine : n_item);
+      const uint64_t q_desc = q_base + (uint64_t)uniform32((uint32_t)qb * (S::TILE >> 4));
+      for (int u = -1; u < n_sub; ++u) {
+        if (n_sub == 0) break;
+        const bool has_pv = u >= 0, has_qk = u + 1 < n_sub;
+        const int g = g0 + u, j = tr_tile<kPair>(max(u, 0), x), jn = tr_tile<kPair>(min(u + 1, n_sub - 1), x);
+        int sv = 0, sk = 0;
+        if (!has_pv) wait(bar(qb, Q_FULL), q_use);
+        if (has_pv) sv = full(u, 1);
+        if (has_qk) sk = full(u + 1, 0);
+        if (u == 0) wait(bar(x, O_FREE), (uint32_t)n_mine ^ 1u);            // previous item's O has been read
+        if (has_pv) wait(bar(x, P_HALF), (uint32_t)g);
+        if (!warp_agreed(ok)) { stop = true; break; }
+        tc_fence_after();
+        const uint64_t vd = v_desc + (uint64_t)uniform32((uint32_t)sv * (S::TILE >> 4));
+        const uint64_t kd = kv_desc + (uint64_t)uniform32((uint32_t)sk * (S::TILE >> 4));
+        const uint32_t ksteps = has_pv ? uniform32((uint32_t)tr_cols(I, L, j) >> 4) : 0u, acc = uniform32(u != 0);
+        const uint32_t idesc_qk = uniform32(idesc_bf16(kTrBM, (uint32_t)tr_cols(I, L, jn)));
+        if (has_pv) {
+          if (pk_elect()) {
+#pragma unroll
+            for (uint32_t ks = 0; ks < 4; ++ks)
+              if (ks < ksteps) mma_ts(t_o, t_s + ks * 8, vd + ks * (2048 >> 4), idesc_pv, ks == 0 ? acc : 1u);
+          }
+          __syncwarp();
+          wait(bar(x, P_FULL), (uint32_t)g);           // (agreed on at the next turn)
+          __syncwarp();
+          tc_fence_after();
+        }
+        if (pk_elect()) {
+          if (has_pv) {
+#pragma unroll
+            for (uint32_t ks = 4; ks < 8; ++ks)
+              if (ks < ksteps) mma_ts(t_o, t_s + ks * 8, vd + ks * (2048 >> 4), idesc_pv, 1u);
+            mma_commit(kv_empty(sv));
+            if (!has_qk) mma_commit(bar(x, O_FULL));
+          }
+          if (has_qk) {
+#pragma unroll
+            for (uint32_t ks = 0; ks < D / 16; ++ks) {
+              constexpr uint64_t half = S::HALF >> 4;                  // the second 64 dims are a tile of their own
+              mma_ss(t_s, q_desc + (ks >> 2) * half + 2 * (ks & 3), kd + (ks >> 2) * half + 2 * (ks & 3), idesc_qk, ks != 0);
+            }
+            mma_commit(bar(x, S_FULL));
+            mma_commit(kv_empty(sk));
+            if (u + 2 == n_sub) mma_commit(bar(qb, Q_EMPTY));
+          }
+        }
+        __syncwarp();
+      }
+      if (!kPair && n_sub == 0) {                      // nothing of this item: its share of the Q tile's release
+        wait(bar(qb, Q_FULL), q_use);
+        stop = !warp_agreed(ok);
+        if (!stop && lane == 0) mbar_arrive(bar(qb, Q_EMPTY));
+      }
+      if (kPair)                                       // tiles that only the other lane uses, in the ring's order
+        for (int j = n_sub; j < I.nt && !stop; ++j) {
+          const int s0 = full(j, 0);
+          if (lane == 0 && ok) mbar_arrive(kv_empty(s0));
+          const int s1 = full(j, 1);
+          if (lane == 0 && ok) mbar_arrive(kv_empty(s1));
+          stop = !warp_agreed(ok);
+        }
+      ring0 += 2 * (kPair ? I.nt : n_sub);
+      g0 += n_sub;
+      ++n_item;
+      if (n_sub > 0) ++n_mine;
+    }
+  } else if (warp < 8) {
+    // ---------------------------------------------------------------- softmax / epilogue warps of one lane
+    reg_inc<kTrRegsSoftmax>();
+    const int x = warp >> 2, quad = warp & 3;
+    const int row = quad * 32 + lane;                                  // row within the tile
+    const uint32_t lane_off = (uint32_t)(quad * 32) << 16;
+    const uint32_t s_addr = tmem + lane_off + x * kAtLaneCols + kAtColS;
+    const uint32_t o_addr = tmem + lane_off + x * kAtLaneCols + kAtColO;
+    float2* exch = reinterpret_cast<float2*>(smem + S::EXCH);
+    const int my_node = row / a.G, my_head = row - my_node * a.G, warp_node = (quad * 32) / a.G;
+    constexpr int kItemRows = kPair ? 256 : 128;
+    constexpr int kPartFloats = kItemRows * (D + 2);
+    TrWalker<kPair> W(pg, a, *hd);
+    TrItem I;
+    int g0 = 0, g_twin = 0, ring0 = 0, n_mine[2] = {0, 0}, tiles = 0;  // (n_mine: of both lanes)
+    while (W.next(I)) {
+      const TrLane L = tr_lane<kPair>(a, I, x), Lt = tr_lane<kPair>(a, I, x ^ 1);
+      const int n_sub = L.n_tiles;
+      const int node = L.q0 + my_node;
+      const bool owned = my_node < a.PB && node < L.q_hi;
+      const bool active = L.q0 + warp_node < L.q_hi && warp_node < a.PB;     // some row of the warp is a node's
+      float m_used = -3.402823466e38f, l_run = 0.f;
+      const int twin0 = kPair && n_sub >= kTrTurnTiles ? g_twin : -(1 << 30);
+      const int32_t* mask_row = a.mask ? a.mask + (size_t)(I.row0 + min(node, I.n - 1)) * a.words : nullptr;
+      for (int u = 0; u < n_sub; ++u) {
+        const int j = tr_tile<kPair>(u, x), c0 = (I.t + j) * kTrBN;
+        mbar_wait_spin(bar(x, S_FULL), (uint32_t)(g0 + u) & 1u, abort_flag);
+        __syncwarp();
+        tc_fence_after();
+        auto turn = [&] {
+          if (!kPair) return;
+          if (lane == 0) {
+            const int before = twin0 + min(u + x, Lt.n_tiles);
+            for (int i = 0; i < kTrPatience && passes[4 * (x ^ 1) + quad] < before; ++i) { }
+          }
+          __syncwarp();
+        };
+        auto pass_on = [&] { if (kPair && lane == 0) passes[4 * x + quad] = g0 + u + 1; };
+        auto hand_over = [&](int which) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(x, which));
+        };
+        const uint32_t parts = seen[(tiles + j) % kTrSeen];
+        const int sees = a.mask ? I.held : I.held + L.q0 + warp_node + 1;      // keys that every row of the warp sees
+        if (active && c0 + kTrBN <= sees && parts == 0xFF) {
+          pk_softmax_full(s_addr, o_addr, owned, u > 0 ? D / 32 : 0, a.scale_log2, m_used, l_run, turn,
+                          [&] { hand_over(P_HALF); }, pass_on);
+          hand_over(P_FULL);
+          continue;
+        }
+        turn();
+        if (active) {
+          uint32_t vis[4];
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const int base = c0 + 32 * w;
+            uint32_t v;
+            if (a.mask) {
+              v = tr_low(I.held - base);
+              if (base + 32 > I.held) v |= tr_mask_bits(mask_row, a.words, base - I.held);
+              v &= tr_low(I.held + I.n - base);
+            } else {
+              v = tr_low(I.held + node + 1 - base);
+            }
+            if (!((parts >> (2 * w)) & 1)) v &= 0xFFFF0000u;
+            if (!((parts >> (2 * w + 1)) & 1)) v &= 0x0000FFFFu;
+            vis[w] = v;
+          }
+          const int n_ch = min(4, (L.keys - c0 + 31) >> 5);
+          tr_softmax_words(s_addr, o_addr, n_ch, vis, owned, u > 0 ? D / 32 : 0, a.scale_log2, m_used, l_run);
+        }
+        pass_on();
+        const int valid = I.held + I.n - c0;                           // V's rows behind them that P V covers are zeroed
+        if (tr_cols(I, L, j) > valid) {
+          const int t = ring0 + 2 * u + 1, slot = (kPair ? 0 : x * S::RING) + t % S::RING;
+          mbar_wait_spin(kv_full(slot), (uint32_t)(t / S::RING) & 1u, abort_flag);
+          char* v_s = smem + S::KV + slot * S::TILE;
+          const int pad = tr_cols(I, L, j) - valid;
+          for (int w = row; w < pad * (D / 8); w += 128) {
+            const int rr = valid + w / (D / 8), c = w % (D / 8);
+            *reinterpret_cast<uint4*>(v_s + (c >> 3) * S::HALF + rr * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+          }
+          fence_proxy_async();
+        }
+        hand_over(P_HALF);
+        hand_over(P_FULL);
+      }
+      // ---- epilogue
+      const bool whole = I.t == 0 && I.nt == I.T;                      // not cut by a border
+      const int slot = I.first ? 0 : 1;
+      float* part = a.parts + ((size_t)blockIdx.x * 2 + slot) * kPartFloats;
+      const size_t out_row = ((size_t)(I.row0 + node) * a.H + I.h * a.G + my_head) * D;
+      if (kPair) {
+        const int part_row = x * 128 + row;
+        if (n_sub > 0) {
+          mbar_wait_spin(bar(x, O_FULL), (uint32_t)n_mine[x] & 1u, abort_flag);
+          __syncwarp();
+          tc_fence_after();
+        }
+        if (!whole && owned) reinterpret_cast<float2*>(part)[part_row] = make_float2(m_used, l_run);
+        const float inv = l_run > 0.f ? 1.0f / l_run : 0.f;
+        if (n_sub > 0) {
+          if (active) {
+#pragma unroll 1
+            for (int rd = 0; rd < D / 64; ++rd) {
+              uint32_t o[64];
+              __syncwarp();
+              tmem_ld64(o_addr + rd * 64, o);
+              tmem_ld_wait();
+              if (owned && whole) {
+#pragma unroll
+                for (int i = 0; i < 64; i += 16) {
+                  uint32_t w[8];
+#pragma unroll
+                  for (int k = 0; k < 8; ++k) w[k] = cvt_bf16x2(__uint_as_float(o[i + 2 * k]) * inv, __uint_as_float(o[i + 2 * k + 1]) * inv);
+                  if (DL_IN_BOUNDS(a.status, KID_TREE, out_row + rd * 64 + i + 15, (size_t)a.total * a.H * D))
+                    tr_store32_any(a.out + out_row + rd * 64 + i, w, a.wide);
+                }
+              } else if (owned) {
+                float* po = part + 2 * kItemRows + (size_t)part_row * D + rd * 64;
+                if (DL_IN_BOUNDS(a.status, KID_TREE, po + 63 - a.parts, (long long)gridDim.x * 2 * kPartFloats)) {
+#pragma unroll
+                  for (int i = 0; i < 64; i += 8) tr_store32(po + i, o + i);
+                }
+              }
+            }
+            __syncwarp();
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(x, O_FREE));
+        }
+      } else {
+        // both lanes hold sums of the same rows: each takes half of the columns of both
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+          if (tr_lane<kPair>(a, I, y).n_tiles > 0) mbar_wait_spin(bar(y, O_FULL), (uint32_t)n_mine[y] & 1u, abort_flag);
+        __syncwarp();
+        tc_fence_after();
+        if (active) {
+          exch[x * 128 + row] = make_float2(m_used, l_run);
+          asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");
+          const float2 twin = exch[(x ^ 1) * 128 + row];
+          asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");       // read before the next item writes
+          const float m = fmaxf(m_used, twin.x);
+          const float w_me = l_run > 0.f ? fast_exp2(m_used - m) : 0.f, w_tw = twin.y > 0.f ? fast_exp2(twin.x - m) : 0.f;
+          const float l = l_run * w_me + twin.y * w_tw;
+          const float inv = whole ? (l > 0.f ? 1.0f / l : 0.f) : 1.f;
+          const float f_me = w_me * inv, f_tw = w_tw * inv;
+          const uint32_t base = tmem + lane_off + kAtColO + x * (D / 2);
+          if (!whole && owned && x == 0) reinterpret_cast<float2*>(part)[row] = make_float2(m, l);
+#pragma unroll 1
+          for (int c = 0; c < D / 2; c += 32) {
+            uint32_t p[32], q[32];
+            __syncwarp();
+            tmem_ld32(base + x * kAtLaneCols + c, p);
+            tmem_ld32(base + (x ^ 1) * kAtLaneCols + c, q);
+            tmem_ld_wait();
+            // (a lane without a sum has left whatever was in tensor memory: not 0 times that, but nothing)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              const float u0 = w_me > 0.f ? __uint_as_float(p[i]) * f_me : 0.f, u1 = w_tw > 0.f ? __uint_as_float(q[i]) * f_tw : 0.f;
+              p[i] = __float_as_uint(u0 + u1);
+            }
+            if (owned && whole) {
+#pragma unroll
+              for (int i = 0; i < 32; i += 16) {
+                uint32_t w[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) w[k] = cvt_bf16x2(__uint_as_float(p[i + 2 * k]), __uint_as_float(p[i + 2 * k + 1]));
+                if (DL_IN_BOUNDS(a.status, KID_TREE, out_row + x * (D / 2) + c + i + 15, (size_t)a.total * a.H * D))
+                  tr_store32_any(a.out + out_row + x * (D / 2) + c + i, w, a.wide);
+              }
+            } else if (owned) {
+              float* po = part + 2 * kItemRows + (size_t)row * D + x * (D / 2) + c;
+              if (DL_IN_BOUNDS(a.status, KID_TREE, po + 31 - a.parts, (long long)gridDim.x * 2 * kPartFloats)) {
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) tr_store32(po + i, p + i);
+              }
+            }
+          }
+          __syncwarp();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0)
+          for (int y = 0; y < 2; ++y)
+            if (tr_lane<kPair>(a, I, y).n_tiles > 0) mbar_arrive(bar(y, O_FREE));
+      }
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+        if (tr_lane<kPair>(a, I, y).n_tiles > 0) ++n_mine[y];
+      g0 += n_sub;
+      g_twin += Lt.n_tiles;
+      ring0 += 2 * (kPair ? I.nt : n_sub);
+      tiles += I.nt;
+    }
+    if (*abort_flag && row == 0) report_status(a.status, DL_ERR_TIMEOUT, blockIdx.x);
+  } else {
+    reg_dec<kTrRegsSmall>();                             // same budget as the rest of its warpgroup
+    // starts that lead out of the tensors (they are clamped wherever they are used) and sequences with more nodes than were
+    // said (cut off there) are reported
+    if (blockIdx.x == 0)
+      for (int b = lane; b < pg.B; b += 32) {
+        const int s0 = __ldcg(a.starts + b), s1 = __ldcg(a.starts + b + 1);
+        if (s0 < 0 || s1 < s0 || s1 > a.total || s1 - s0 > a.said_rows) report_status(a.status, DL_ERR_INVALID_ARG, b);
+      }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 11) { tc_fence_after(); tmem_dealloc(tmem, 512); }
+}
+
+// Joins the parts of an item that borders of ranges cut: CTA (c, y) those of the item that the border in front of CTA c cuts first,
+// every gridDim.y-th group of 8 rows.  A warp takes a row, a lane its D / 32 dims.
+constexpr int kTrJoinThreads = 256;
+template <int D, bool kPair>
+__global__ void __launch_bounds__(kTrJoinThreads)
+attn_tree_join_kernel(const K16Pages pg, const TrArgs a, int32_t ranges) {
+  chained_go();
+  chained_wait();
+  constexpr int kItemRows = kPair ? 256 : 128;
+  constexpr int kPartFloats = kItemRows * (D + 2);
+  constexpr int E = D / 32;
+  extern __shared__ int list[];                                    // the ranges that hold parts of the item, and their slots
+  __shared__ int n_list;
+  const int c = blockIdx.x + 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const TrHead hd = a.heads[c];
+  if (hd.units == 0 || hd.t == 0) return;                          // the border falls between items (or there is none)
+  const long long item = hd.first - hd.t, end = item + hd.T;       // the item's key tiles among all
+  if (warp == 0) {
+    int n = 0;
+    for (int p0 = 0; p0 < ranges; p0 += 32) {
+      const int p = p0 + lane;
+      bool in = false;
+      long long first = 0;
+      if (p < ranges) {
+        const long long units = a.heads[p].units;
+        first = a.heads[p].first;
+        in = units > 0 && first < end && first + units > item;
+      }
+      const unsigned m = __ballot_sync(0xffffffffu, in);
+      if (in) list[n + __popc(m & ((1u << lane) - 1u))] = 2 * p + (first < item ? 1 : 0);
+      n += __popc(m);
+    }
+    if (lane == 0) n_list = n;
+  }
+  __syncthreads();
+  const int n_parts = n_list;
+  if (list[1] >> 1 != c) return;                                   // a border in front of this one has cut the item already
+  const int nodes = min(hd.n - hd.q0, (kPair ? 2 : 1) * a.PB);
+  for (int r = blockIdx.y * (kTrJoinThreads / 32) + warp; r < nodes * a.G; r += gridDim.y * (kTrJoinThreads / 32)) {
+    const int node = r / a.G, head = r - node * a.G;
+    const int part_row = kPair && node >= a.PB ? 128 + r - a.PB * a.G : r;
+    auto part = [&](int i) { return a.parts + (size_t)list[i] * kPartFloats; };
+    float m = -3.402823466e38f;
+    for (int i = 0; i < n_parts; ++i) {
+      const float2 ml = __ldcg(reinterpret_cast<const float2*>(part(i)) + part_row);
+      if (ml.y > 0.f) m = fmaxf(m, ml.x);
+    }
+    float l = 0.f, o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    for (int i = 0; i < n_parts; ++i) {
+      const float2 ml = __ldcg(reinterpret_cast<const float2*>(part(i)) + part_row);
+      if (!(ml.y > 0.f)) continue;
+      const float w = exp2f(ml.x - m);
+      l += ml.y * w;
+      const float* po = part(i) + 2 * kItemRows + (size_t)part_row * D + lane * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] += w * __ldcg(po + e);
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const size_t at = ((size_t)(hd.row0 + hd.q0 + node) * a.H + hd.h * a.G + head) * D + lane * E;
+    if (!DL_IN_BOUNDS(a.status, KID_TREE, at + E - 1, (size_t)a.total * a.H * D)) continue;
+#pragma unroll
+    for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t*>(a.out + at + e) = cvt_bf16x2(o[e] * inv, o[e + 1] * inv);
+  }
+}
+
+static int64_t tr_head_floats(int32_t sm_count) { return ((int64_t)sm_count * (sizeof(TrHead) / 4) + 63) & ~(int64_t)63; }
+
+// Scratch: the ranges' heads, two parts a range of up to 256 rows.
+int64_t attn_tree_scratch_floats(int32_t sm_count, const dl_model_desc& d) {
+  return tr_head_floats(sm_count) + (int64_t)sm_count * 2 * 256 * (d.head_dim + 2);
+}
+
+bool attn_tree_supported(const dl_ctx* ctx) {
+  return ctx->desc.dtype == DL_BF16 && ctx->tmap_encode != nullptr && (size_t)ctx->smem_optin >= (size_t)std::max({Tr<128, true>::SMEM, Tr<128, false>::SMEM, Tr<64, true>::SMEM, Tr<64, false>::SMEM});
+}
+
+template <int D, bool kPair>
+static cudaError_t tr_launch(dl_ctx* ctx, const TrMaps& maps, const K16Pages& pg, const TrArgs& a, cudaStream_t s) {
+  static int attr_set[64];                             // (all calls ask for the same: two threads may)
+  if (!attr_set[ctx->device & 63]) {
+    const cudaError_t e = cudaFuncSetAttribute(attn_tree_kernel<D, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tr<D, kPair>::SMEM);
+    if (e != cudaSuccess) return e;
+    attr_set[ctx->device & 63] = 1;
+  }
+  // no more ranges than key tiles there can be
+  const long long row_tiles = std::min<long long>((long long)pg.B * ((a.max_rows + a.PB - 1) / a.PB), (long long)a.total);
+  const long long key_tiles = (((long long)pg.W << pg.shift) + a.max_rows + kTrBN - 1) / kTrBN;
+  const int ranges = (int)std::min<long long>(ctx->sm_count, std::max(1LL, std::min(row_tiles, 1LL << 20) * key_tiles * a.Hk));
+  cudaError_t e = launch_chained(attn_tree_kernel<D, kPair>, dim3(ranges), dim3(kTrThreads), Tr<D, kPair>::SMEM, s, maps, pg, a);
+  if (e != cudaSuccess || ranges == 1) return e;
+  const int rows = std::min((kPair ? 2 : 1) * a.PB, a.max_rows) * a.G;
+  return launch_chained(attn_tree_join_kernel<D, kPair>, dim3(ranges - 1, std::min(8, (rows + 7) / 8)), dim3(kTrJoinThreads),
+                        (size_t)(ranges + 1) * 4, s, pg, a, ranges);
+}
+
+cudaError_t launch_attn_tree(dl_ctx* ctx, const dl_pages* p, int32_t Hk, const void* pool, const void* q, int64_t q_stride,
+                             const int32_t* starts, int32_t total, int32_t max_rows, const int32_t* mask, int32_t words,
+                             float scale, void* out, cudaStream_t s) {
+  const K16Pages pg = k16_pages(p);
+  const int D = ctx->desc.head_dim, H = ctx->desc.n_heads;
+  TrArgs a = {};
+  a.starts = starts; a.mask = mask; a.out = static_cast<__nv_bfloat16*>(out);
+  a.status = ctx->ws.status;
+  a.heads = reinterpret_cast<TrHead*>(ctx->ws.kv4_partial);
+  a.parts = ctx->ws.kv4_partial + tr_head_floats(ctx->sm_count);
+  a.H = H; a.Hk = Hk; a.G = H / Hk; a.PB = kTrBM / a.G; a.total = total; a.words = words;
+  a.said_rows = mask ? (int)std::min<long long>(max_rows, 32LL * words) : max_rows;
+  a.max_rows = std::min(a.said_rows, total);
+  a.box_rows = std::min(a.PB, a.max_rows);
+  a.scale_log2 = scale * 1.4426950408889634f;
+  const uint64_t pool_rows = (2ull * Hk * pg.n_pages) << pg.shift;
+  a.pool_rows = (uint32_t)pool_rows;
+  a.wide = (reinterpret_cast<uintptr_t>(out) & 31u) == 0;
+  TrMaps maps;
+  const uint64_t dq[3] = {(uint64_t)D, (uint64_t)H, (uint64_t)total}, sq[2] = {2ull * D, 2ull * q_stride};
+  const uint64_t dkv[2] = {(uint64_t)D, pool_rows}, skv[1] = {2ull * D};
+  const uint32_t bq[3] = {64u, (uint32_t)a.G, (uint32_t)a.box_rows}, bkv[2] = {64u, 1u << pg.shift};
+  if (!encode_bf16_map(ctx->tmap_encode, reinterpret_cast<CUtensorMap*>(maps.q), q, 3, dq, sq, bq) ||
+      !encode_bf16_map(ctx->tmap_encode, reinterpret_cast<CUtensorMap*>(maps.kv), pool, 2, dkv, skv, bkv))
+    return cudaErrorInvalidValue;
+  const bool pair = a.max_rows > a.PB;
+  if (D == 128) return pair ? tr_launch<128, true>(ctx, maps, pg, a, s) : tr_launch<128, false>(ctx, maps, pg, a, s);
+  return pair ? tr_launch<64, true>(ctx, maps, pg, a, s) : tr_launch<64, false>(ctx, maps, pg, a, s);
+}
+
+}  // namespace dl

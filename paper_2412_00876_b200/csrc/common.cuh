@@ -78,7 +78,7 @@ struct Workspace {
   float* pred_split = nullptr;        // [unit tiles][kPredKSplit][kPredRowTile][tile width] raw sums of the decode-shape predictor
   int32_t* pred_split_ticket = nullptr;   // [kPredMaxSplit]; zero between launches
   int32_t pred_rows_padded = 0;
-  float* kv4_partial = nullptr;       // parts of split pairs of the 4-bit decode attention (attn_decode_kv4.cu)
+  float* kv4_partial = nullptr;       // parts of split work of the 4-bit decode attention (attn_decode_kv4.cu) and of tree attention (attn_tree_tc.cu)
 };
 
 int64_t workspace_layout(const dl_model_desc& d, int32_t sm_count, int32_t max_batch, int32_t max_rows, int32_t cap,
@@ -236,6 +236,8 @@ cudaError_t launch_kv16_append(const dl_ctx* ctx, const dl_pages* p, int32_t Hk,
                                void* k_out, int64_t k_out_stride, int32_t commit, cudaStream_t s);
 cudaError_t launch_kv16_commit(const dl_ctx* ctx, const dl_pages* p, int32_t Hk, int32_t n_pools, void* const* pools,
                                const int32_t* starts, const uint8_t* keep, int32_t total, cudaStream_t s);
+int64_t attn_tree_scratch_floats(int32_t sm_count, const dl_model_desc& d);
+bool attn_tree_supported(const dl_ctx* ctx);
 cudaError_t launch_attn_tree(dl_ctx* ctx, const dl_pages* p, int32_t Hk, const void* pool, const void* q, int64_t q_stride,
                              const int32_t* starts, int32_t total, int32_t max_rows, const int32_t* mask, int32_t words,
                              float scale, void* out, cudaStream_t s);

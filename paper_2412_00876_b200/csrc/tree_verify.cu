@@ -21,8 +21,7 @@ namespace dl {
 constexpr int kTvThreads = 512;
 constexpr int kTvCluster = 8;
 constexpr int kTvNodes = 2048;           // most nodes of a sequence
-constexpr int kTvVocab = 1 << 18;        // 2^18 values of at most 2^44 each: sums below 2^63
-constexpr double kTvUnit = 17592186044416.0;                       // 2^44
+constexpr double kTvUnit = 17592186044416.0;                       // 2^44; up to 2^18 values of at most that: sums below 2^63
 
 struct TvArgs {
   const void* target; const float* draft; const float* u; const int32_t* tokens; const int32_t* parent; const int32_t* starts;

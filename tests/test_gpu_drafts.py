@@ -261,7 +261,7 @@ def check_attention(H, Hk, D, page, held, nodes, masked, seed=0, extra_rows=0, q
         bad = ~(np.abs(got[a:e] - ref) <= bound)
         assert not bad.any(), f"sequence {b}: {bad.sum()} off, worst {np.abs(got[a:e] - ref)[bad].max()} at {np.argwhere(bad)[:4]}"
     out2 = torch.zeros_like(out)
-    ctx.kv16_attn_tree(pages, dev_pool, up(q), i32(st), max(nodes), dev_mask, scale, out2)
+    ctx.kv16_attn_tree(pages, dev_pool, up(q), i32(st), max(nodes) + extra_rows, dev_mask, scale, out2)
     assert torch.equal(out[:total], out2[:total])                              # dense rows, and the same bits again
     ctx.close()
 
@@ -468,4 +468,21 @@ def test_commit_leaves_a_sequence_that_lacks_pages():
     assert torch.equal(pool[p], before[p]) and torch.equal(pool[table[1, 0], :, :, 10], before[table[1, 0], :, :, 13])
     ctx.kv16_commit(pages, [], i32([0, 12, 30]), u8(keep * 0))
     assert pages.cache_len.tolist() == [10, 12]
+    ctx.close()
+
+
+@pytest.mark.parametrize("H,Hk,D,page,B,held,n", [(32, 8, 128, 32, 24, 5000, 1), (16, 2, 64, 16, 16, 9000, 2), (8, 2, 128, 64, 6, 6000, 40)])
+def test_attention_launched_behind_itself_without_a_gap(H, Hk, D, page, B, held, n):
+    """Hundreds of launches in the queue, shares of many key tiles: the launches' borders overlap, loads arrive in any order."""
+    dl, ctx = context(H, D, B=B)
+    rng = np.random.default_rng(B)
+    lens = [int(x) for x in rng.integers(held // 4, held, B)]
+    pages, _ = books(dl, rng, [h + n for h in lens], lens, page)
+    pool, q = (torch.randn(*s, device=DEV).to(torch.bfloat16) for s in ((pages.n_pages, 2, Hk, page, D), (B * n, H, D)))
+    st = i32(np.arange(B + 1) * n)
+    first, out = torch.zeros_like(q), torch.zeros_like(q)
+    ctx.kv16_attn_tree(pages, pool, q, st, n, None, D ** -0.5, first)
+    for _ in range(400):
+        ctx.kv16_attn_tree(pages, pool, q, st, n, None, D ** -0.5, out)
+    assert ctx.device_status()[0] == 0 and torch.equal(first, out) and bool(first.isfinite().all())
     ctx.close()
