@@ -9,12 +9,15 @@
 // of one item, some whole ones, the start of another.  Items cut by a border leave their parts (sums, row maxima) in
 // scratch, and a second kernel joins them in order: no result depends on timing.
 //   warp 8        : the producer: Q tiles, then K and V tiles through a ring
+// (warps of a CTA with two lanes; with one, the second lane's are not there)
 //   warps 9, 10   : issue the MMAs of lane A / B: S = Q K^T into tensor memory, O += P V with P read from tensor memory
 //   warps 0-3/4-7 : softmax and epilogue of lane A / B, one row per thread
 //   warp 11       : allocates tensor memory (512 columns: O_A | S_A | O_B | S_B)
 // A lane is a chain (softmax, P V and Q K^T, softmax); two of them keep the pipes busy.  What the lanes share is the template's
-// choice.  Up to 128 rows (kPair false): both work on the same rows, lane A the even key tiles, B the odd ones, each through a ring
-// of its own, and an item's end adds the two up.  More rows (kPair true): each lane has a tile of rows, and a K/V tile serves both.
+// choice.  Up to 64 rows (kTrSingle): nothing; a CTA has one lane and half of a multiprocessor (with Q as small as that two of
+// them fit), so that one's item ends, masks and start beside the other's stream.  Up to 128 rows (kTrSplit): both work on the
+// same rows, lane A the even key tiles, B the odd ones, each through a ring of its own, and an item's end adds the two up.
+// More rows (kTrPair): each lane has a tile of rows, and a K/V tile serves both.
 // Every wait is bounded (pipeline.cuh); an abort leaves DL_ERR_TIMEOUT in the status word.
 #include <algorithm>
 
@@ -25,24 +28,35 @@
 
 namespace dl {
 
-constexpr int kTrThreads = 384;
 constexpr int kTrBM = 128, kTrBN = 128;
-constexpr int kTrRegsSmall = 40, kTrRegsSoftmax = 232;             // as in attn_packed_tc.cu
+// What a CTA's lanes share, see above
+enum TrForm { kTrSingle = 0, kTrSplit = 1, kTrPair = 2 };
 constexpr int kTrPatience = 4000, kTrTurnTiles = 4;                // as there: polls for a turn, tiles from which lanes take turns
 constexpr int kTrSeen = 16;                                        // key tiles whose page flags are kept
 
-template <int D, bool kPair> struct Tr {
+template <int D, int F> struct Tr {
+  static constexpr bool kPair = F == kTrPair;
+  static constexpr int LANES = F == kTrSingle ? 1 : 2;
+  static constexpr int THREADS = LANES * 128 + 128;
+  // registers per thread: the kernel starts every thread at 128 (kTrSingle) or 168
+  static constexpr int REGS_SMALL = F == kTrSingle ? 32 : 40, REGS_SOFTMAX = F == kTrSingle ? 224 : 232;
+  static_assert(128 * REGS_SMALL + LANES * 128 * REGS_SOFTMAX <= THREADS * (F == kTrSingle ? 128 : 168), "more registers than the launch has");
   static constexpr int HALF = 128 * 128;               // 128 rows of 64 dims
   static constexpr int TILE = (D / 64) * HALF;         // one operand tile
+  static constexpr int ROWS = F == kTrSingle ? 64 : 128;   // rows of a Q tile (MMAs read 128; what lies behind them goes nowhere)
+  static constexpr int Q_HALF = ROWS * 128, Q_TILE = (D / 64) * Q_HALF;
   static constexpr int Q_TILES = kPair ? 2 : 1;
-  static constexpr int SLOTS = D == 128 ? 7 - Q_TILES : 12;
+  static constexpr int SLOTS = F == kTrSingle ? (D == 128 ? 3 : 6) : D == 128 ? 7 - Q_TILES : 12;
   // Slots of a ring.  A wait by parity only tells one use of a slot from the next: whoever waits for a slot's uses has to wait for
   // every one of them.  So lanes that take different tiles have a ring each.
-  static constexpr int RING = kPair ? SLOTS : SLOTS / 2;
-  static constexpr int KV = Q_TILES * TILE;            // offset of the rings (behind the Q tiles)
+  static constexpr int RING = F == kTrSplit ? SLOTS / 2 : SLOTS;
+  static constexpr int KV = Q_TILES * Q_TILE;          // offset of the rings (behind the Q tiles)
   static constexpr int EXCH = KV + SLOTS * TILE;       // [2][128] row maximum and sum of the lanes
-  static constexpr int BAR = EXCH + 2 * 128 * 8;
+  static constexpr int BAR = EXCH + (F == kTrSplit ? 2 * 128 * 8 : 0);
   static constexpr int SMEM = BAR + 512;
+  static constexpr int ITEM_ROWS = kPair ? 256 : ROWS;
+  static constexpr int PART_FLOATS = ITEM_ROWS * (D + 2);
+  static constexpr int TMEM_COLS = 256 * LANES;
 };
 
 struct TrMaps { alignas(64) unsigned char q[128]; alignas(64) unsigned char kv[128]; };
@@ -61,11 +75,11 @@ struct TrArgs {
 };
 
 // Key tiles of an item: nodes [q0, ...) of a sequence.
-template <bool kPair>
-__device__ __forceinline__ int tr_reach(const TrArgs& a, int q0) { return q0 + (kPair ? 2 : 1) * a.PB; }
-template <bool kPair>
+template <int F>
+__device__ __forceinline__ int tr_reach(const TrArgs& a, int q0) { return q0 + (F == kTrPair ? 2 : 1) * a.PB; }
+template <int F>
 __device__ __forceinline__ int tr_tiles(const TrArgs& a, int held, int n, int q0) {
-  return (held + (a.mask ? n : min(n, tr_reach<kPair>(a, q0))) + kTrBN - 1) / kTrBN;
+  return (held + (a.mask ? n : min(n, tr_reach<F>(a, q0))) + kTrBN - 1) / kTrBN;
 }
 
 struct TrSeq { int row0, n, held; };
@@ -82,24 +96,25 @@ struct TrItem { int b, h, row0, n, held, q0, T, t, nt; bool first; };
 // One lane's share of that: rows of nodes [q0, q_hi), `keys` of which it may see, tiles j = lane's first, + step, ...
 struct TrLane { int q0, q_hi, keys, n_tiles; };
 
-template <bool kPair>
+template <int F>
 __device__ __forceinline__ TrLane tr_lane(const TrArgs& a, const TrItem& I, int x) {
   TrLane L;
-  L.q0 = I.q0 + (kPair ? x * a.PB : 0);
+  L.q0 = I.q0 + (F == kTrPair ? x * a.PB : 0);
   L.q_hi = min(I.n, L.q0 + a.PB);
   L.keys = I.held + (a.mask ? I.n : L.q_hi);
-  if (kPair) L.n_tiles = L.q0 < I.n ? min(max((L.keys + kTrBN - 1) / kTrBN - I.t, 0), I.nt) : 0;
-  else L.n_tiles = (I.nt + 1 - x) >> 1;
+  if (F == kTrPair) L.n_tiles = L.q0 < I.n ? min(max((L.keys + kTrBN - 1) / kTrBN - I.t, 0), I.nt) : 0;
+  else if (F == kTrSplit) L.n_tiles = (I.nt + 1 - x) >> 1;
+  else L.n_tiles = x == 0 ? I.nt : 0;
   return L;
 }
 // the lane's i-th tile, counted from the share's first
-template <bool kPair> __device__ __forceinline__ int tr_tile(int i, int x) { return kPair ? i : 2 * i + x; }
+template <int F> __device__ __forceinline__ int tr_tile(int i, int x) { return F == kTrSplit ? 2 * i + x : i; }
 // keys of the share's tile j that a lane's MMAs cover
 __device__ __forceinline__ int tr_cols(const TrItem& I, const TrLane& L, int j) {
   return min(kTrBN, (L.keys - (I.t + j) * kTrBN + 15) & ~15);
 }
 // Walks a CTA's items; every role does so for itself.
-template <bool kPair>
+template <int F>
 struct TrWalker {
   const K16Pages& pg; const TrArgs& a;
   TrSeq s, ahead;                                      // the sequence, the one behind it (requested early)
@@ -115,14 +130,14 @@ struct TrWalker {
   __device__ __forceinline__ bool next(TrItem& I) {
     if (left <= 0) return false;
     I.b = b; I.h = h; I.row0 = s.row0; I.n = s.n; I.held = s.held; I.q0 = q0; I.t = t; I.first = first;
-    I.T = tr_tiles<kPair>(a, s.held, s.n, q0);
+    I.T = tr_tiles<F>(a, s.held, s.n, q0);
     I.nt = (int)min((long long)(I.T - t), left);
     left -= I.nt;
     first = false;
     t = 0;
     if (left > 0 && ++h == a.Hk) {
       h = 0;
-      q0 = tr_reach<kPair>(a, q0);
+      q0 = tr_reach<F>(a, q0);
       if (q0 >= s.n) {
         q0 = 0;
         do { ++b; s = ahead; fetch(); } while (s.n == 0 && b + 1 < pg.B);
@@ -133,12 +148,11 @@ struct TrWalker {
   }
 };
 
-// 32 bits of a row's mask from bit j0 on (j0 > -32 or lower: zeros come in front and behind).
-__device__ __forceinline__ uint32_t tr_mask_bits(const int32_t* row, int words, int j0) {
+// 32 bits of a row's mask from bit j0 on (zeros come in front and behind); m0, m1: its first two words.
+__device__ __forceinline__ uint32_t tr_mask_bits(const int32_t* row, int words, uint32_t m0, uint32_t m1, int j0) {
   const int w = j0 >> 5;
-  const uint32_t lo = w >= 0 && w < words ? (uint32_t)__ldcg(row + w) : 0u;
-  const uint32_t hi = w + 1 >= 0 && w + 1 < words ? (uint32_t)__ldcg(row + w + 1) : 0u;
-  return __funnelshift_r(lo, hi, j0 & 31);
+  auto word = [&](int i) { return i == 0 ? m0 : i == 1 ? m1 : i > 0 && i < words ? (uint32_t)__ldcg(row + i) : 0u; };
+  return __funnelshift_r(word(w), word(w + 1), j0 & 31);
 }
 __device__ __forceinline__ uint32_t tr_low(int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u; }
 
@@ -209,13 +223,14 @@ __device__ __forceinline__ void tr_store32_any(void* p, const uint32_t* r, int w
 }
 
 // Where the CTA's even range of all key tiles begins: found by the whole CTA, left in *hd (shared); scratch: shared.
-template <bool kPair>
+template <int F>
 __device__ __forceinline__ void tr_find(const K16Pages& pg, const TrArgs& a, TrHead* hd, long long* scratch) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int per = (pg.B + kTrThreads - 1) / kTrThreads, b0 = min(pg.B, tid * per), b1 = min(pg.B, b0 + per);
+  constexpr int T = Tr<64, F>::THREADS;
+  const int per = (pg.B + T - 1) / T, b0 = min(pg.B, tid * per), b1 = min(pg.B, b0 + per);
   auto units = [&](const TrSeq& s) {
     long long u = 0;
-    for (int q0 = 0; q0 < s.n; q0 = tr_reach<kPair>(a, q0)) u += tr_tiles<kPair>(a, s.held, s.n, q0);
+    for (int q0 = 0; q0 < s.n; q0 = tr_reach<F>(a, q0)) u += tr_tiles<F>(a, s.held, s.n, q0);
     return u * a.Hk;
   };
   long long mine = 0;
@@ -231,7 +246,7 @@ __device__ __forceinline__ void tr_find(const K16Pages& pg, const TrArgs& a, TrH
   __syncthreads();
   long long front = 0, all = 0;
 #pragma unroll
-  for (int w = 0; w < kTrThreads / 32; ++w) {
+  for (int w = 0; w < T / 32; ++w) {
     if (w < warp) front += scratch[w];
     all += scratch[w];
   }
@@ -244,13 +259,13 @@ __device__ __forceinline__ void tr_find(const K16Pages& pg, const TrArgs& a, TrH
       if (u0 >= at + u) { at += u; continue; }
       int rest_q0 = 0;
       long long rest = u0 - at;
-      for (; rest_q0 < s.n; rest_q0 = tr_reach<kPair>(a, rest_q0)) {
-        const long long x = (long long)tr_tiles<kPair>(a, s.held, s.n, rest_q0) * a.Hk;
+      for (; rest_q0 < s.n; rest_q0 = tr_reach<F>(a, rest_q0)) {
+        const long long x = (long long)tr_tiles<F>(a, s.held, s.n, rest_q0) * a.Hk;
         if (rest < x) break;
         rest -= x;
       }
       hd->b = b; hd->q0 = rest_q0; hd->n = s.n; hd->row0 = s.row0;
-      hd->T = tr_tiles<kPair>(a, s.held, s.n, rest_q0);
+      hd->T = tr_tiles<F>(a, s.held, s.n, rest_q0);
       hd->h = (int)(rest / hd->T);
       hd->t = (int)(rest - (long long)hd->h * hd->T);
       hd->units = u1 - u0;
@@ -261,13 +276,14 @@ __device__ __forceinline__ void tr_find(const K16Pages& pg, const TrArgs& a, TrH
   __syncthreads();
 }
 
-template <int D, bool kPair>
-__global__ void __launch_bounds__(kTrThreads, 1)
+template <int D, int F>
+__global__ void __launch_bounds__(Tr<D, F>::THREADS, F == kTrSingle ? 2 : 1)
 attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const TrArgs a) {
-  using S = Tr<D, kPair>;
+  using S = Tr<D, F>;
+  constexpr bool kPair = S::kPair;
+  constexpr int kProducer = 4 * S::LANES, kIssuer = kProducer + 1, kLast = kProducer + 3;
   extern __shared__ __align__(1024) char smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  chained_go();
   if (smem_u32(smem) & 1023u) {                        // the swizzled tiles need 1024-byte alignment
     if (tid == 0) report_status(a.status, DL_ERR_ALIGNMENT, -1);
     chained_wait();
@@ -293,26 +309,29 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
     for (int i = 0; i < S::SLOTS; ++i) { mbar_init(kv_full(i), 1); mbar_init(kv_empty(i), kPair ? 2 : 1); }
     for (int x = 0; x < 2; ++x)
       for (int i = 0; i < N_BAR; ++i)
-        mbar_init(bar(x, i), i == P_HALF || i == P_FULL ? 4 : i == O_FREE ? (kPair ? 4 : 8) : i == Q_EMPTY ? (kPair ? 1 : 2) : 1);
+        mbar_init(bar(x, i), i == P_HALF || i == P_FULL ? 4 : i == O_FREE ? (F == kTrSplit ? 8 : 4) : i == Q_EMPTY ? (F == kTrSplit ? 2 : 1) : 1);
     fence_mbar_init();
   }
-  if (warp == 11) { tmem_alloc(smem_u32(tmem_slot), 512); tmem_relinquish(); }
+  // Tensor memory is only asked for when the kernels in front are done, and nothing behind comes up before it is there: none
+  // of them can wait for the other's with tensor memory in hand.
   chained_wait();
-  tr_find<kPair>(pg, a, hd, reinterpret_cast<long long*>(smem));             // (the ring is not in use yet)
+  if (warp == kLast) { tmem_alloc(smem_u32(tmem_slot), S::TMEM_COLS); tmem_relinquish(); }
+  tr_find<F>(pg, a, hd, reinterpret_cast<long long*>(smem));             // (the ring is not in use yet)
   fence_proxy_async();
   if (tid == 0) a.heads[blockIdx.x] = *hd;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  chained_go();
   const uint32_t tmem = *tmem_slot;
 
-  if (warp == 8) {
+  if (warp == kProducer) {
     // ---------------------------------------------------------------- producer
-    reg_dec<kTrRegsSmall>();
+    reg_dec<S::REGS_SMALL>();
     const CUtensorMap* mq = reinterpret_cast<const CUtensorMap*>(maps.q);
     const CUtensorMap* mkv = reinterpret_cast<const CUtensorMap*>(maps.kv);
     if (lane == 0) { tma_prefetch_desc(mq); tma_prefetch_desc(mkv); }
-    TrWalker<kPair> W(pg, a, *hd);
+    TrWalker<F> W(pg, a, *hd);
     TrItem I;
     int n_q[2] = {0, 0}, ring[2] = {0, 0}, tiles = 0;  // Q tiles per place, tiles per ring, key tiles so far
     bool ok = true, stop = false;
@@ -327,7 +346,7 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
         mbar_expect_tx(bar(buf, Q_FULL), (uint32_t)(D / 64) * 128u * (uint32_t)(a.box_rows * a.G));
 #pragma unroll
         for (int hf = 0; hf < D / 64; ++hf)
-          tma_load_3d(smem_u32(smem + buf * S::TILE + hf * S::HALF), mq, 64 * hf, I.h * a.G, I.row0 + q0, bar(buf, Q_FULL));
+          tma_load_3d(smem_u32(smem + buf * S::Q_TILE + hf * S::Q_HALF), mq, 64 * hf, I.h * a.G, I.row0 + q0, bar(buf, Q_FULL));
       }
       __syncwarp();
     };
@@ -342,7 +361,7 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
       int blk = 0, cur = block(0), before = -1, after = block(1);
       const int rows_all = I.held + I.n;
       auto load = [&](int kv, int j) {                 // whole warp
-        const int x = kPair ? 0 : j & 1, use = ring[x] / S::RING, slot = x * S::RING + ring[x] % S::RING;
+        const int x = F == kTrSplit ? j & 1 : 0, use = ring[x] / S::RING, slot = x * S::RING + ring[x] % S::RING;
         wait(kv_empty(slot), ((uint32_t)use & 1u) ^ 1u);
         if (!warp_agreed(ok)) { stop = true; return; }
         ++ring[x];
@@ -372,10 +391,10 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
         }
         __syncwarp();
       };
-      if (kPair) {
-        if (tr_lane<kPair>(a, I, 0).n_tiles > 0) load_q(0, I.q0);
+      if (F != kTrSplit) {
+        if (tr_lane<F>(a, I, 0).n_tiles > 0) load_q(0, I.q0);
         if (!stop) load(0, 0);
-        if (!stop && tr_lane<kPair>(a, I, 1).n_tiles > 0) load_q(1, I.q0 + a.PB);
+        if (kPair && !stop && tr_lane<F>(a, I, 1).n_tiles > 0) load_q(1, I.q0 + a.PB);
         for (int j = 0; j < I.nt && !stop; ++j) {
           load(1, j);
           if (!stop && j + 1 < I.nt) load(0, j + 1);
@@ -399,37 +418,37 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
         if (n_q[x] > 0)
           for (int k = 0; k < kSpinLimit && !mbar_try_wait(bar(x, Q_FULL), (uint32_t)(n_q[x] - 1) & 1u); ++k) __nanosleep(40);
     }
-  } else if (warp == 9 || warp == 10) {
+  } else if (warp >= kIssuer && warp < kIssuer + S::LANES) {
     // ---------------------------------------------------------------- MMA issuer of one lane
     // The whole warp walks the loop, so that counters and descriptors stay warp-uniform, and one elected lane issues.  Its lanes
     // wait each for itself, so the warp agrees before it goes on or stops.
-    reg_dec<kTrRegsSmall>();
-    const int x = warp - 9;
+    reg_dec<S::REGS_SMALL>();
+    const int x = warp - kIssuer;
     const uint32_t t_o = uniform32(tmem + x * kAtLaneCols + kAtColO), t_s = uniform32(tmem + x * kAtLaneCols + kAtColS);
     constexpr uint32_t idesc_pv = idesc_bf16(kTrBM, D, 0, 1);          // B (= V) is MN-major
     const uint64_t q_base = uniform64(smem_desc_sw128(smem_u32(smem)));
     const uint64_t kv_desc = uniform64(smem_desc_sw128(smem_u32(smem + S::KV)));
     const uint64_t v_desc = uniform64(smem_desc_sw128_mn(smem_u32(smem + S::KV), S::HALF));
-    TrWalker<kPair> W(pg, a, *hd);
+    TrWalker<F> W(pg, a, *hd);
     TrItem I;
     int n_item = 0, n_mine = 0, g0 = 0, ring0 = 0;     // items, those with tiles of this lane, its tiles, its ring's tiles so far
     bool ok = true, stop = false;                      // this lane's waits so far; the warp has agreed to stop
     auto wait = [&](uint32_t b, uint32_t parity) { ok = mbar_wait_spin(b, parity & 1u, abort_flag) && ok; };
     while (!stop && W.next(I)) {
-      const TrLane L = tr_lane<kPair>(a, I, x);
+      const TrLane L = tr_lane<F>(a, I, x);
       const int n_sub = L.n_tiles;
       auto full = [&](int u, int is_v) {               // waits for K or V of tile u of the ring's share; returns its slot
-        const int t = ring0 + 2 * u + is_v, slot = (kPair ? 0 : x * S::RING) + t % S::RING;
+        const int t = ring0 + 2 * u + is_v, slot = (F == kTrSplit ? x * S::RING : 0) + t % S::RING;
         wait(kv_full(slot), (uint32_t)(t / S::RING));
         return slot;
       };
       const int qb = kPair ? x : 0;                    // Q tile
       const uint32_t q_use = (uint32_t)(kPair ? n_mine : n_item);
-      const uint64_t q_desc = q_base + (uint64_t)uniform32((uint32_t)qb * (S::TILE >> 4));
+      const uint64_t q_desc = q_base + (uint64_t)uniform32((uint32_t)qb * (S::Q_TILE >> 4));
       for (int u = -1; u < n_sub; ++u) {
         if (n_sub == 0) break;
         const bool has_pv = u >= 0, has_qk = u + 1 < n_sub;
-        const int g = g0 + u, j = tr_tile<kPair>(max(u, 0), x), jn = tr_tile<kPair>(min(u + 1, n_sub - 1), x);
+        const int g = g0 + u, j = tr_tile<F>(max(u, 0), x), jn = tr_tile<F>(min(u + 1, n_sub - 1), x);
         int sv = 0, sk = 0;
         if (!has_pv) wait(bar(qb, Q_FULL), q_use);
         if (has_pv) sv = full(u, 1);
@@ -464,8 +483,8 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
           if (has_qk) {
 #pragma unroll
             for (uint32_t ks = 0; ks < D / 16; ++ks) {
-              constexpr uint64_t half = S::HALF >> 4;                  // the second 64 dims are a tile of their own
-              mma_ss(t_s, q_desc + (ks >> 2) * half + 2 * (ks & 3), kd + (ks >> 2) * half + 2 * (ks & 3), idesc_qk, ks != 0);
+              constexpr uint64_t half = S::HALF >> 4, q_half = S::Q_HALF >> 4;   // the second 64 dims are a tile of their own
+              mma_ss(t_s, q_desc + (ks >> 2) * q_half + 2 * (ks & 3), kd + (ks >> 2) * half + 2 * (ks & 3), idesc_qk, ks != 0);
             }
             mma_commit(bar(x, S_FULL));
             mma_commit(kv_empty(sk));
@@ -474,7 +493,7 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
         }
         __syncwarp();
       }
-      if (!kPair && n_sub == 0) {                      // nothing of this item: its share of the Q tile's release
+      if (F == kTrSplit && n_sub == 0) {                      // nothing of this item: its share of the Q tile's release
         wait(bar(qb, Q_FULL), q_use);
         stop = !warp_agreed(ok);
         if (!stop && lane == 0) mbar_arrive(bar(qb, Q_EMPTY));
@@ -487,14 +506,14 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
           if (lane == 0 && ok) mbar_arrive(kv_empty(s1));
           stop = !warp_agreed(ok);
         }
-      ring0 += 2 * (kPair ? I.nt : n_sub);
+      ring0 += 2 * (F == kTrSplit ? n_sub : I.nt);
       g0 += n_sub;
       ++n_item;
       if (n_sub > 0) ++n_mine;
     }
-  } else if (warp < 8) {
+  } else if (warp < kProducer) {
     // ---------------------------------------------------------------- softmax / epilogue warps of one lane
-    reg_inc<kTrRegsSoftmax>();
+    reg_inc<S::REGS_SOFTMAX>();
     const int x = warp >> 2, quad = warp & 3;
     const int row = quad * 32 + lane;                                  // row within the tile
     const uint32_t lane_off = (uint32_t)(quad * 32) << 16;
@@ -502,13 +521,12 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
     const uint32_t o_addr = tmem + lane_off + x * kAtLaneCols + kAtColO;
     float2* exch = reinterpret_cast<float2*>(smem + S::EXCH);
     const int my_node = row / a.G, my_head = row - my_node * a.G, warp_node = (quad * 32) / a.G;
-    constexpr int kItemRows = kPair ? 256 : 128;
-    constexpr int kPartFloats = kItemRows * (D + 2);
-    TrWalker<kPair> W(pg, a, *hd);
+    constexpr int kItemRows = S::ITEM_ROWS, kPartFloats = S::PART_FLOATS;
+    TrWalker<F> W(pg, a, *hd);
     TrItem I;
     int g0 = 0, g_twin = 0, ring0 = 0, n_mine[2] = {0, 0}, tiles = 0;  // (n_mine: of both lanes)
     while (W.next(I)) {
-      const TrLane L = tr_lane<kPair>(a, I, x), Lt = tr_lane<kPair>(a, I, x ^ 1);
+      const TrLane L = tr_lane<F>(a, I, x), Lt = tr_lane<F>(a, I, x ^ 1);
       const int n_sub = L.n_tiles;
       const int node = L.q0 + my_node;
       const bool owned = my_node < a.PB && node < L.q_hi;
@@ -516,8 +534,13 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
       float m_used = -3.402823466e38f, l_run = 0.f;
       const int twin0 = kPair && n_sub >= kTrTurnTiles ? g_twin : -(1 << 30);
       const int32_t* mask_row = a.mask ? a.mask + (size_t)(I.row0 + min(node, I.n - 1)) * a.words : nullptr;
+      uint32_t m0 = 0, m1 = 0;
+      if (a.mask && active) {
+        m0 = (uint32_t)__ldcg(mask_row);
+        if (a.words > 1) m1 = (uint32_t)__ldcg(mask_row + 1);
+      }
       for (int u = 0; u < n_sub; ++u) {
-        const int j = tr_tile<kPair>(u, x), c0 = (I.t + j) * kTrBN;
+        const int j = tr_tile<F>(u, x), c0 = (I.t + j) * kTrBN;
         mbar_wait_spin(bar(x, S_FULL), (uint32_t)(g0 + u) & 1u, abort_flag);
         __syncwarp();
         tc_fence_after();
@@ -552,7 +575,7 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
             uint32_t v;
             if (a.mask) {
               v = tr_low(I.held - base);
-              if (base + 32 > I.held) v |= tr_mask_bits(mask_row, a.words, base - I.held);
+              if (base + 32 > I.held) v |= tr_mask_bits(mask_row, a.words, m0, m1, base - I.held);
               v &= tr_low(I.held + I.n - base);
             } else {
               v = tr_low(I.held + node + 1 - base);
@@ -567,7 +590,7 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
         pass_on();
         const int valid = I.held + I.n - c0;                           // V's rows behind them that P V covers are zeroed
         if (tr_cols(I, L, j) > valid) {
-          const int t = ring0 + 2 * u + 1, slot = (kPair ? 0 : x * S::RING) + t % S::RING;
+          const int t = ring0 + 2 * u + 1, slot = (F == kTrSplit ? x * S::RING : 0) + t % S::RING;
           mbar_wait_spin(kv_full(slot), (uint32_t)(t / S::RING) & 1u, abort_flag);
           char* v_s = smem + S::KV + slot * S::TILE;
           const int pad = tr_cols(I, L, j) - valid;
@@ -585,7 +608,7 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
       const int slot = I.first ? 0 : 1;
       float* part = a.parts + ((size_t)blockIdx.x * 2 + slot) * kPartFloats;
       const size_t out_row = ((size_t)(I.row0 + node) * a.H + I.h * a.G + my_head) * D;
-      if (kPair) {
+      if (F != kTrSplit) {
         const int part_row = x * 128 + row;
         if (n_sub > 0) {
           mbar_wait_spin(bar(x, O_FULL), (uint32_t)n_mine[x] & 1u, abort_flag);
@@ -629,7 +652,7 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
         // both lanes hold sums of the same rows: each takes half of the columns of both
 #pragma unroll
         for (int y = 0; y < 2; ++y)
-          if (tr_lane<kPair>(a, I, y).n_tiles > 0) mbar_wait_spin(bar(y, O_FULL), (uint32_t)n_mine[y] & 1u, abort_flag);
+          if (tr_lane<F>(a, I, y).n_tiles > 0) mbar_wait_spin(bar(y, O_FULL), (uint32_t)n_mine[y] & 1u, abort_flag);
         __syncwarp();
         tc_fence_after();
         if (active) {
@@ -680,19 +703,19 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
         __syncwarp();
         if (lane == 0)
           for (int y = 0; y < 2; ++y)
-            if (tr_lane<kPair>(a, I, y).n_tiles > 0) mbar_arrive(bar(y, O_FREE));
+            if (tr_lane<F>(a, I, y).n_tiles > 0) mbar_arrive(bar(y, O_FREE));
       }
 #pragma unroll
       for (int y = 0; y < 2; ++y)
-        if (tr_lane<kPair>(a, I, y).n_tiles > 0) ++n_mine[y];
+        if (tr_lane<F>(a, I, y).n_tiles > 0) ++n_mine[y];
       g0 += n_sub;
       g_twin += Lt.n_tiles;
-      ring0 += 2 * (kPair ? I.nt : n_sub);
+      ring0 += 2 * (F == kTrSplit ? n_sub : I.nt);
       tiles += I.nt;
     }
     if (*abort_flag && row == 0) report_status(a.status, DL_ERR_TIMEOUT, blockIdx.x);
   } else {
-    reg_dec<kTrRegsSmall>();                             // same budget as the rest of its warpgroup
+    reg_dec<S::REGS_SMALL>();                             // same budget as the rest of its warpgroup
     // starts that lead out of the tensors (they are clamped wherever they are used) and sequences with more nodes than were
     // said (cut off there) are reported
     if (blockIdx.x == 0)
@@ -703,19 +726,19 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 11) { tc_fence_after(); tmem_dealloc(tmem, 512); }
+  if (warp == kLast) { tc_fence_after(); tmem_dealloc(tmem, S::TMEM_COLS); }
 }
 
 // Joins the parts of an item that borders of ranges cut: CTA (c, y) those of the item that the border in front of CTA c cuts first,
 // every gridDim.y-th group of 8 rows.  A warp takes a row, a lane its D / 32 dims.
 constexpr int kTrJoinThreads = 256;
-template <int D, bool kPair>
+template <int D, int F>
 __global__ void __launch_bounds__(kTrJoinThreads)
 attn_tree_join_kernel(const K16Pages pg, const TrArgs a, int32_t ranges) {
   chained_go();
   chained_wait();
-  constexpr int kItemRows = kPair ? 256 : 128;
-  constexpr int kPartFloats = kItemRows * (D + 2);
+  constexpr bool kPair = F == kTrPair;
+  constexpr int kItemRows = Tr<D, F>::ITEM_ROWS, kPartFloats = Tr<D, F>::PART_FLOATS;
   constexpr int E = D / 32;
   extern __shared__ int list[];                                    // the ranges that hold parts of the item, and their slots
   __shared__ int n_list;
@@ -773,33 +796,36 @@ attn_tree_join_kernel(const K16Pages pg, const TrArgs a, int32_t ranges) {
   }
 }
 
-static int64_t tr_head_floats(int32_t sm_count) { return ((int64_t)sm_count * (sizeof(TrHead) / 4) + 63) & ~(int64_t)63; }
+static int64_t tr_head_floats(int32_t sm_count) { return ((int64_t)2 * sm_count * (sizeof(TrHead) / 4) + 63) & ~(int64_t)63; }
 
-// Scratch: the ranges' heads, two parts a range of up to 256 rows.
+// Scratch: the ranges' heads (two ranges a multiprocessor at most), two parts a range: up to 256 rows of one range or 64 of two.
 int64_t attn_tree_scratch_floats(int32_t sm_count, const dl_model_desc& d) {
   return tr_head_floats(sm_count) + (int64_t)sm_count * 2 * 256 * (d.head_dim + 2);
 }
 
+template <int D> static constexpr int tr_smem() { return std::max({Tr<D, kTrSingle>::SMEM, Tr<D, kTrSplit>::SMEM, Tr<D, kTrPair>::SMEM}); }
+static_assert(2 * (Tr<128, kTrSingle>::SMEM + 1024) <= 228 * 1024 && 2 * (Tr<64, kTrSingle>::SMEM + 1024) <= 228 * 1024, "two CTAs a multiprocessor");
+
 bool attn_tree_supported(const dl_ctx* ctx) {
-  return ctx->desc.dtype == DL_BF16 && ctx->tmap_encode != nullptr && (size_t)ctx->smem_optin >= (size_t)std::max({Tr<128, true>::SMEM, Tr<128, false>::SMEM, Tr<64, true>::SMEM, Tr<64, false>::SMEM});
+  return ctx->desc.dtype == DL_BF16 && ctx->tmap_encode != nullptr && ctx->smem_optin >= std::max(tr_smem<128>(), tr_smem<64>());
 }
 
-template <int D, bool kPair>
+template <int D, int F>
 static cudaError_t tr_launch(dl_ctx* ctx, const TrMaps& maps, const K16Pages& pg, const TrArgs& a, cudaStream_t s) {
   static int attr_set[64];                             // (all calls ask for the same: two threads may)
   if (!attr_set[ctx->device & 63]) {
-    const cudaError_t e = cudaFuncSetAttribute(attn_tree_kernel<D, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tr<D, kPair>::SMEM);
+    const cudaError_t e = cudaFuncSetAttribute(attn_tree_kernel<D, F>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tr<D, F>::SMEM);
     if (e != cudaSuccess) return e;
     attr_set[ctx->device & 63] = 1;
   }
   // no more ranges than key tiles there can be
   const long long row_tiles = std::min<long long>((long long)pg.B * ((a.max_rows + a.PB - 1) / a.PB), (long long)a.total);
   const long long key_tiles = (((long long)pg.W << pg.shift) + a.max_rows + kTrBN - 1) / kTrBN;
-  const int ranges = (int)std::min<long long>(ctx->sm_count, std::max(1LL, std::min(row_tiles, 1LL << 20) * key_tiles * a.Hk));
-  cudaError_t e = launch_chained(attn_tree_kernel<D, kPair>, dim3(ranges), dim3(kTrThreads), Tr<D, kPair>::SMEM, s, maps, pg, a);
+  const int ranges = (int)std::min<long long>((F == kTrSingle ? 2 : 1) * ctx->sm_count, std::max(1LL, std::min(row_tiles, 1LL << 20) * key_tiles * a.Hk));
+  cudaError_t e = launch_chained(attn_tree_kernel<D, F>, dim3(ranges), dim3(Tr<D, F>::THREADS), Tr<D, F>::SMEM, s, maps, pg, a);
   if (e != cudaSuccess || ranges == 1) return e;
-  const int rows = std::min((kPair ? 2 : 1) * a.PB, a.max_rows) * a.G;
-  return launch_chained(attn_tree_join_kernel<D, kPair>, dim3(ranges - 1, std::min(8, (rows + 7) / 8)), dim3(kTrJoinThreads),
+  const int rows = std::min((F == kTrPair ? 2 : 1) * a.PB, a.max_rows) * a.G;
+  return launch_chained(attn_tree_join_kernel<D, F>, dim3(ranges - 1, std::min(8, (rows + 7) / 8)), dim3(kTrJoinThreads),
                         (size_t)(ranges + 1) * 4, s, pg, a, ranges);
 }
 
@@ -813,9 +839,12 @@ cudaError_t launch_attn_tree(dl_ctx* ctx, const dl_pages* p, int32_t Hk, const v
   a.status = ctx->ws.status;
   a.heads = reinterpret_cast<TrHead*>(ctx->ws.kv4_partial);
   a.parts = ctx->ws.kv4_partial + tr_head_floats(ctx->sm_count);
-  a.H = H; a.Hk = Hk; a.G = H / Hk; a.PB = kTrBM / a.G; a.total = total; a.words = words;
+  a.H = H; a.Hk = Hk; a.G = H / Hk; a.total = total; a.words = words;
   a.said_rows = mask ? (int)std::min<long long>(max_rows, 32LL * words) : max_rows;
   a.max_rows = std::min(a.said_rows, total);
+  const int rows = (int)std::min<long long>((long long)a.max_rows * a.G, 1 << 20);
+  const int form = rows <= Tr<128, kTrSingle>::ROWS ? kTrSingle : a.max_rows <= kTrBM / a.G ? kTrSplit : kTrPair;
+  a.PB = (form == kTrSingle ? Tr<128, kTrSingle>::ROWS : kTrBM) / a.G;
   a.box_rows = std::min(a.PB, a.max_rows);
   a.scale_log2 = scale * 1.4426950408889634f;
   const uint64_t pool_rows = (2ull * Hk * pg.n_pages) << pg.shift;
@@ -828,9 +857,9 @@ cudaError_t launch_attn_tree(dl_ctx* ctx, const dl_pages* p, int32_t Hk, const v
   if (!encode_bf16_map(ctx->tmap_encode, reinterpret_cast<CUtensorMap*>(maps.q), q, 3, dq, sq, bq) ||
       !encode_bf16_map(ctx->tmap_encode, reinterpret_cast<CUtensorMap*>(maps.kv), pool, 2, dkv, skv, bkv))
     return cudaErrorInvalidValue;
-  const bool pair = a.max_rows > a.PB;
-  if (D == 128) return pair ? tr_launch<128, true>(ctx, maps, pg, a, s) : tr_launch<128, false>(ctx, maps, pg, a, s);
-  return pair ? tr_launch<64, true>(ctx, maps, pg, a, s) : tr_launch<64, false>(ctx, maps, pg, a, s);
+  auto launch = D == 128 ? (form == kTrSingle ? tr_launch<128, kTrSingle> : form == kTrSplit ? tr_launch<128, kTrSplit> : tr_launch<128, kTrPair>)
+                         : (form == kTrSingle ? tr_launch<64, kTrSingle> : form == kTrSplit ? tr_launch<64, kTrSplit> : tr_launch<64, kTrPair>);
+  return launch(ctx, maps, pg, a, s);
 }
 
 }  // namespace dl
