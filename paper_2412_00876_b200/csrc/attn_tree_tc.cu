@@ -62,7 +62,7 @@ template <int D, int F> struct Tr {
 struct TrMaps { alignas(64) unsigned char q[128]; alignas(64) unsigned char kv[128]; };
 
 // What a CTA's range begins with, for the joining kernel.
-struct TrHead { int b, q0, h, t; int T, n, row0, pad; long long units, first; };
+struct TrHead { int b, q0, h, t; int T, n, row0, held; long long units, first, all; };
 
 struct TrArgs {
   const int32_t* starts; const int32_t* mask; __nv_bfloat16* out; DeviceStatus* status;
@@ -121,7 +121,8 @@ struct TrWalker {
   int b, h, q0, t; long long left; bool first;
   __device__ __forceinline__ TrWalker(const K16Pages& pg_, const TrArgs& a_, const TrHead& hd) : pg(pg_), a(a_) {
     b = hd.b; h = hd.h; q0 = hd.q0; t = hd.t; left = hd.units; first = true;
-    if (left > 0) { s = tr_seq(pg, a, b); fetch(); }
+    s.row0 = hd.row0; s.n = hd.n; s.held = hd.held;
+    if (left > 0) fetch();
   }
   __device__ __forceinline__ void fetch() {
     ahead.row0 = ahead.n = ahead.held = 0;
@@ -264,12 +265,13 @@ __device__ __forceinline__ void tr_find(const K16Pages& pg, const TrArgs& a, TrH
         if (rest < x) break;
         rest -= x;
       }
-      hd->b = b; hd->q0 = rest_q0; hd->n = s.n; hd->row0 = s.row0;
+      hd->b = b; hd->q0 = rest_q0; hd->n = s.n; hd->row0 = s.row0; hd->held = s.held;
       hd->T = tr_tiles<F>(a, s.held, s.n, rest_q0);
       hd->h = (int)(rest / hd->T);
       hd->t = (int)(rest - (long long)hd->h * hd->T);
       hd->units = u1 - u0;
       hd->first = u0;
+      hd->all = all;
       break;
     }
   }
@@ -391,22 +393,15 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
         }
         __syncwarp();
       };
-      if (F != kTrSplit) {
-        if (tr_lane<F>(a, I, 0).n_tiles > 0) load_q(0, I.q0);
-        if (!stop) load(0, 0);
-        if (kPair && !stop && tr_lane<F>(a, I, 1).n_tiles > 0) load_q(1, I.q0 + a.PB);
-        for (int j = 0; j < I.nt && !stop; ++j) {
-          load(1, j);
-          if (!stop && j + 1 < I.nt) load(0, j + 1);
-        }
-      } else {
-        load_q(0, I.q0);
-        if (!stop) load(0, 0);
-        if (!stop && I.nt > 1) load(0, 1);
-        for (int j = 0; j < I.nt && !stop; ++j) {
-          load(1, j);
-          if (!stop && j + 2 < I.nt) load(0, j + 2);
-        }
+      // (the first K tiles in front of Q, whose place is the last item's until that one's last Q K^T)
+      load(0, 0);
+      if (F == kTrSplit && !stop && I.nt > 1) load(0, 1);
+      if (!stop && tr_lane<F>(a, I, 0).n_tiles > 0) load_q(0, I.q0);
+      if (kPair && !stop && tr_lane<F>(a, I, 1).n_tiles > 0) load_q(1, I.q0 + a.PB);
+      constexpr int kAhead = F == kTrSplit ? 2 : 1;    // K runs ahead of V by the tiles that the ring's users work on
+      for (int j = 0; j < I.nt && !stop; ++j) {
+        load(1, j);
+        if (!stop && j + kAhead < I.nt) load(0, j + kAhead);
       }
     }
     if (stop && lane == 0) {
@@ -729,70 +724,135 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
   if (warp == kLast) { tc_fence_after(); tmem_dealloc(tmem, S::TMEM_COLS); }
 }
 
-// Joins the parts of an item that borders of ranges cut: CTA (c, y) those of the item that the border in front of CTA c cuts first,
-// every gridDim.y-th group of 8 rows.  A warp takes a row, a lane its D / 32 dims.
-constexpr int kTrJoinThreads = 256;
+// Joins the parts of items that borders of ranges cut.  CTA (c, y) belongs to the border in front of range c; the CTAs of all
+// borders that cut an item share its rows out between them, so that an item of many parts has many CTAs.  A warp takes two rows
+// at a time, a lane D / 32 dims of each, with four parts of both in flight; where there are many parts a CTA takes a row at a
+// time, and its warps share the parts.
+constexpr int kTrJoinThreads = 256, kTrJoinWarps = kTrJoinThreads / 32;
+constexpr int kTrJoinMany = 16;                                    // parts from which on a CTA takes a row at a time
+
+// Sums of a row: relative to the maximum m, over parts.
+template <int E> struct TrSum { float m, l, o[E]; };
+template <int E> __device__ __forceinline__ void tr_add(TrSum<E>& s, float m, float l, const float* o) {
+  if (!(l > 0.f)) return;                                          // (a part without a sum has no values either)
+  const float top = fmaxf(s.m, m), c = exp2f(s.m - top), w = exp2f(m - top);
+  s.m = top;
+  s.l = s.l * c + l * w;
+#pragma unroll
+  for (int e = 0; e < E; ++e) s.o[e] = s.o[e] * c + o[e] * w;
+}
+template <int E> __device__ __forceinline__ void tr_load(const float* p, float (&o)[E]) {
+  if (E == 4) {
+    const float4 v = __ldcg(reinterpret_cast<const float4*>(p));
+    o[0] = v.x; o[1] = v.y; o[2 % E] = v.z; o[3 % E] = v.w;
+  } else {
+    const float2 v = __ldcg(reinterpret_cast<const float2*>(p));
+    o[0] = v.x; o[1] = v.y;
+  }
+}
+
 template <int D, int F>
 __global__ void __launch_bounds__(kTrJoinThreads)
-attn_tree_join_kernel(const K16Pages pg, const TrArgs a, int32_t ranges) {
-  chained_go();
-  chained_wait();
+attn_tree_join_kernel(const TrArgs a, int32_t ranges) {
   constexpr bool kPair = F == kTrPair;
   constexpr int kItemRows = Tr<D, F>::ITEM_ROWS, kPartFloats = Tr<D, F>::PART_FLOATS;
   constexpr int E = D / 32;
-  extern __shared__ int list[];                                    // the ranges that hold parts of the item, and their slots
-  __shared__ int n_list;
+  __shared__ float far_m[kTrJoinWarps], far_l[kTrJoinWarps], far_o[kTrJoinWarps][D];
   const int c = blockIdx.x + 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  chained_go();
+  chained_wait();
   const TrHead hd = a.heads[c];
   if (hd.units == 0 || hd.t == 0) return;                          // the border falls between items (or there is none)
-  const long long item = hd.first - hd.t, end = item + hd.T;       // the item's key tiles among all
-  if (warp == 0) {
-    int n = 0;
-    for (int p0 = 0; p0 < ranges; p0 += 32) {
-      const int p = p0 + lane;
-      bool in = false;
-      long long first = 0;
-      if (p < ranges) {
-        const long long units = a.heads[p].units;
-        first = a.heads[p].first;
-        in = units > 0 && first < end && first + units > item;
-      }
-      const unsigned m = __ballot_sync(0xffffffffu, in);
-      if (in) list[n + __popc(m & ((1u << lane) - 1u))] = 2 * p + (first < item ? 1 : 0);
-      n += __popc(m);
-    }
-    if (lane == 0) n_list = n;
-  }
-  __syncthreads();
-  const int n_parts = n_list;
-  if (list[1] >> 1 != c) return;                                   // a border in front of this one has cut the item already
-  const int nodes = min(hd.n - hd.q0, (kPair ? 2 : 1) * a.PB);
-  for (int r = blockIdx.y * (kTrJoinThreads / 32) + warp; r < nodes * a.G; r += gridDim.y * (kTrJoinThreads / 32)) {
+  const long long W = hd.all, item = hd.first - hd.t, end = item + hd.T;     // the item's key tiles among all
+  // Range c holds key tiles [W c / ranges, W (c + 1) / ranges), so key tile u is range_of(u)'s; with fewer key tiles than ranges
+  // each is a range of its own, and others are empty between them.
+  auto range_of = [&](long long u) { return (int)(((u + 1) * ranges - 1) / W); };
+  const bool dense = W >= ranges;
+  const int c_lo = range_of(item);
+  const int n_parts = dense ? range_of(end - 1) - c_lo + 1 : hd.T;
+  const int group = dense ? c - c_lo - 1 : (int)(hd.first - item) - 1, groups = n_parts - 1;   // this border among the item's
+  const int slot0 = W * c_lo / ranges < item ? 1 : 0;              // where the first part lies
+  const int rows = min(hd.n - hd.q0, (kPair ? 2 : 1) * a.PB) * a.G;
+  const int me = blockIdx.y * groups + group, all = gridDim.y * groups;      // this CTA among the item's
+  auto part = [&](int i) {
+    const int r = dense ? c_lo + i : range_of(item + i);
+    return a.parts + (size_t)(2 * r + (i == 0 ? slot0 : 0)) * kPartFloats;
+  };
+  auto row_in_part = [&](int r) { return kPair && r >= a.PB * a.G ? 128 + r - a.PB * a.G : r; };
+  auto store = [&](int r, const TrSum<E>& s) {
     const int node = r / a.G, head = r - node * a.G;
-    const int part_row = kPair && node >= a.PB ? 128 + r - a.PB * a.G : r;
-    auto part = [&](int i) { return a.parts + (size_t)list[i] * kPartFloats; };
-    float m = -3.402823466e38f;
-    for (int i = 0; i < n_parts; ++i) {
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(part(i)) + part_row);
-      if (ml.y > 0.f) m = fmaxf(m, ml.x);
-    }
-    float l = 0.f, o[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = 0.f;
-    for (int i = 0; i < n_parts; ++i) {
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(part(i)) + part_row);
-      if (!(ml.y > 0.f)) continue;
-      const float w = exp2f(ml.x - m);
-      l += ml.y * w;
-      const float* po = part(i) + 2 * kItemRows + (size_t)part_row * D + lane * E;
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[e] += w * __ldcg(po + e);
-    }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = s.l > 0.f ? 1.f / s.l : 0.f;
     const size_t at = ((size_t)(hd.row0 + hd.q0 + node) * a.H + hd.h * a.G + head) * D + lane * E;
-    if (!DL_IN_BOUNDS(a.status, KID_TREE, at + E - 1, (size_t)a.total * a.H * D)) continue;
+    if (!DL_IN_BOUNDS(a.status, KID_TREE, at + E - 1, (size_t)a.total * a.H * D)) return;
 #pragma unroll
-    for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t*>(a.out + at + e) = cvt_bf16x2(o[e] * inv, o[e + 1] * inv);
+    for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t*>(a.out + at + e) = cvt_bf16x2(s.o[e] * inv, s.o[e + 1] * inv);
+  };
+  auto none = [] {
+    TrSum<E> s;
+    s.m = -3.402823466e38f;
+    s.l = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) s.o[e] = 0.f;
+    return s;
+  };
+  if (n_parts >= kTrJoinMany) {
+    for (int r = me; r < rows; r += all) {
+      const int pr = row_in_part(r);
+      TrSum<E> s = none();
+      for (int i0 = warp; i0 < n_parts; i0 += 4 * kTrJoinWarps) {
+        float2 ml[4];
+        float o[4][E];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int i = i0 + k * kTrJoinWarps;
+          if (i >= n_parts) continue;
+          ml[k] = __ldcg(reinterpret_cast<const float2*>(part(i)) + pr);
+          tr_load<E>(part(i) + 2 * kItemRows + (size_t)pr * D + lane * E, o[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (i0 + k * kTrJoinWarps < n_parts) tr_add<E>(s, ml[k].x, ml[k].y, o[k]);
+      }
+      if (lane == 0) { far_m[warp] = s.m; far_l[warp] = s.l; }
+#pragma unroll
+      for (int e = 0; e < E; ++e) far_o[warp][lane * E + e] = s.o[e];
+      __syncthreads();
+      if (warp == 0) {
+        TrSum<E> all = none();
+#pragma unroll
+        for (int w = 0; w < kTrJoinWarps; ++w) tr_add<E>(all, far_m[w], far_l[w], &far_o[w][lane * E]);
+        store(r, all);
+      }
+      __syncthreads();
+    }
+    return;
+  }
+  for (int r = 2 * (me * kTrJoinWarps + warp); r < rows; r += 2 * all * kTrJoinWarps) {
+    TrSum<E> s[2] = {none(), none()};
+    const bool two = r + 1 < rows;
+    const int pr[2] = {row_in_part(r), row_in_part(two ? r + 1 : r)};
+    for (int i0 = 0; i0 < n_parts; i0 += 4) {
+      float2 ml[4][2];
+      float o[4][2][E];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (i0 + k >= n_parts) continue;
+        const float* p = part(i0 + k);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          ml[k][y] = __ldcg(reinterpret_cast<const float2*>(p) + pr[y]);
+          tr_load<E>(p + 2 * kItemRows + (size_t)pr[y] * D + lane * E, o[k][y]);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (i0 + k < n_parts) {
+          tr_add<E>(s[0], ml[k][0].x, ml[k][0].y, o[k][0]);
+          tr_add<E>(s[1], ml[k][1].x, ml[k][1].y, o[k][1]);
+        }
+    }
+    store(r, s[0]);
+    if (two) store(r + 1, s[1]);
   }
 }
 
@@ -825,8 +885,8 @@ static cudaError_t tr_launch(dl_ctx* ctx, const TrMaps& maps, const K16Pages& pg
   cudaError_t e = launch_chained(attn_tree_kernel<D, F>, dim3(ranges), dim3(Tr<D, F>::THREADS), Tr<D, F>::SMEM, s, maps, pg, a);
   if (e != cudaSuccess || ranges == 1) return e;
   const int rows = std::min((F == kTrPair ? 2 : 1) * a.PB, a.max_rows) * a.G;
-  return launch_chained(attn_tree_join_kernel<D, F>, dim3(ranges - 1, std::min(8, (rows + 7) / 8)), dim3(kTrJoinThreads),
-                        (size_t)(ranges + 1) * 4, s, pg, a, ranges);
+  return launch_chained(attn_tree_join_kernel<D, F>, dim3(ranges - 1, (rows + 2 * kTrJoinWarps - 1) / (2 * kTrJoinWarps)),
+                        dim3(kTrJoinThreads), 0, s, a, ranges);
 }
 
 cudaError_t launch_attn_tree(dl_ctx* ctx, const dl_pages* p, int32_t Hk, const void* pool, const void* q, int64_t q_stride,
