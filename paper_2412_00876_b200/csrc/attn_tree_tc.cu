@@ -1,98 +1,44 @@
 // Attention of new rows (trees of drafted tokens, chunks of a prompt, single tokens) over a paged cache in 16 bits, on the tensor
-// cores.  An extension, not in the paper.  bf16, head_dim 64 or 128.
+// cores: more than 64 rows an item, the joining of parts, and the launcher.  An extension, not in the paper.  bf16, head_dim 64 or 128.
 //
 // Sequence b's n new rows (nodes) attend the cache's rows [0, held) and, by a mask or causally, the n rows behind them, which hold
 // the nodes' own K and V.  The G query heads of a K/V head and the nodes make one matrix: row = (node, head), 128 / G nodes a
 // tile of 128 rows (one TMA box [nodes][G heads][64 dims] is just that).  Keys come in tiles of 128 rows, a TMA box per page.
-// Few rows and many keys is the usual shape, so the work is (sequence, tile of rows, K/V head) items of T key tiles each, and ALL
-// key tiles of a call are cut into as many even ranges as there are CTAs, whatever the lengths are: a CTA's range covers the end
-// of one item, some whole ones, the start of another.  Items cut by a border leave their parts (sums, row maxima) in
-// scratch, and a second kernel joins them in order: no result depends on timing.
+// How the work is cut into ranges: attn_tree.cuh.
 //   warp 8        : the producer: Q tiles, then K and V tiles through a ring
-// (warps of a CTA with two lanes; with one, the second lane's are not there)
 //   warps 9, 10   : issue the MMAs of lane A / B: S = Q K^T into tensor memory, O += P V with P read from tensor memory
 //   warps 0-3/4-7 : softmax and epilogue of lane A / B, one row per thread
 //   warp 11       : allocates tensor memory (512 columns: O_A | S_A | O_B | S_B)
 // A lane is a chain (softmax, P V and Q K^T, softmax); two of them keep the pipes busy.  What the lanes share is the template's
-// choice.  Up to 64 rows (kTrSingle): nothing; a CTA has one lane and half of a multiprocessor (with Q as small as that two of
-// them fit), so that one's item ends, masks and start beside the other's stream.  Up to 128 rows (kTrSplit): both work on the
-// same rows, lane A the even key tiles, B the odd ones, each through a ring of its own, and an item's end adds the two up.
-// More rows (kTrPair): each lane has a tile of rows, and a K/V tile serves both.
+// choice.  Up to 128 rows (kTrSplit): both work on the same rows, lane A the even key tiles, B the odd ones, each through a ring
+// of its own, and an item's end adds the two up.  More rows (kTrPair): each lane has a tile of rows, and a K/V tile serves both.
+// Up to 64 rows go the other way round, keys across the matrix unit's rows: attn_tree_rows.cu.
 // Every wait is bounded (pipeline.cuh); an abort leaves DL_ERR_TIMEOUT in the status word.
 #include <algorithm>
 
 #include "attn_packed_softmax.cuh"
-#include "attn_prefill.cuh"
-#include "kv16.cuh"
-#include "tc05.cuh"
+#include "attn_tree.cuh"
 
 namespace dl {
 
-constexpr int kTrBM = 128, kTrBN = 128;
-// What a CTA's lanes share, see above
-enum TrForm { kTrSingle = 0, kTrSplit = 1, kTrPair = 2 };
-constexpr int kTrPatience = 4000, kTrTurnTiles = 4;                // as there: polls for a turn, tiles from which lanes take turns
-constexpr int kTrSeen = 16;                                        // key tiles whose page flags are kept
+constexpr int kTrPatience = 4000, kTrTurnTiles = 4;                // polls for a turn, tiles from which lanes take turns (attn_packed_tc.cu)
+constexpr int kTrRegsSmall = 40, kTrRegsSoftmax = 232;             // as there
 
 template <int D, int F> struct Tr {
   static constexpr bool kPair = F == kTrPair;
-  static constexpr int LANES = F == kTrSingle ? 1 : 2;
-  static constexpr int THREADS = LANES * 128 + 128;
-  // registers per thread: the kernel starts every thread at 128 (kTrSingle) or 168
-  static constexpr int REGS_SMALL = F == kTrSingle ? 32 : 40, REGS_SOFTMAX = F == kTrSingle ? 224 : 232;
-  static_assert(128 * REGS_SMALL + LANES * 128 * REGS_SOFTMAX <= THREADS * (F == kTrSingle ? 128 : 168), "more registers than the launch has");
   static constexpr int HALF = 128 * 128;               // 128 rows of 64 dims
   static constexpr int TILE = (D / 64) * HALF;         // one operand tile
-  static constexpr int ROWS = F == kTrSingle ? 64 : 128;   // rows of a Q tile (MMAs read 128; what lies behind them goes nowhere)
-  static constexpr int Q_HALF = ROWS * 128, Q_TILE = (D / 64) * Q_HALF;
   static constexpr int Q_TILES = kPair ? 2 : 1;
-  static constexpr int SLOTS = F == kTrSingle ? (D == 128 ? 3 : 6) : D == 128 ? 7 - Q_TILES : 12;
+  static constexpr int SLOTS = D == 128 ? 7 - Q_TILES : 12;
   // Slots of a ring.  A wait by parity only tells one use of a slot from the next: whoever waits for a slot's uses has to wait for
   // every one of them.  So lanes that take different tiles have a ring each.
-  static constexpr int RING = F == kTrSplit ? SLOTS / 2 : SLOTS;
-  static constexpr int KV = Q_TILES * Q_TILE;          // offset of the rings (behind the Q tiles)
+  static constexpr int RING = kPair ? SLOTS : SLOTS / 2;
+  static constexpr int KV = Q_TILES * TILE;            // offset of the rings (behind the Q tiles)
   static constexpr int EXCH = KV + SLOTS * TILE;       // [2][128] row maximum and sum of the lanes
-  static constexpr int BAR = EXCH + (F == kTrSplit ? 2 * 128 * 8 : 0);
+  static constexpr int BAR = EXCH + (kPair ? 0 : 2 * 128 * 8);
   static constexpr int SMEM = BAR + 512;
-  static constexpr int ITEM_ROWS = kPair ? 256 : ROWS;
-  static constexpr int PART_FLOATS = ITEM_ROWS * (D + 2);
-  static constexpr int TMEM_COLS = 256 * LANES;
 };
 
-struct TrMaps { alignas(64) unsigned char q[128]; alignas(64) unsigned char kv[128]; };
-
-// What a CTA's range begins with, for the joining kernel.
-struct TrHead { int b, q0, h, t; int T, n, row0, held; long long units, first, all; };
-
-struct TrArgs {
-  const int32_t* starts; const int32_t* mask; __nv_bfloat16* out; DeviceStatus* status;
-  TrHead* heads; float* parts;                         // [grid], [grid][2 slots][rows of an item][D + 2]
-  int32_t H, Hk, G, PB, total, max_rows, said_rows, words;   // PB: nodes per tile of rows
-  int32_t box_rows;                                    // nodes per Q box
-  uint32_t pool_rows;                                  // rows of the pool's tensor map
-  int32_t wide;                                        // out is 32-byte aligned
-  float scale_log2;
-};
-
-// Key tiles of an item: nodes [q0, ...) of a sequence.
-template <int F>
-__device__ __forceinline__ int tr_reach(const TrArgs& a, int q0) { return q0 + (F == kTrPair ? 2 : 1) * a.PB; }
-template <int F>
-__device__ __forceinline__ int tr_tiles(const TrArgs& a, int held, int n, int q0) {
-  return (held + (a.mask ? n : min(n, tr_reach<F>(a, q0))) + kTrBN - 1) / kTrBN;
-}
-
-struct TrSeq { int row0, n, held; };
-__device__ __forceinline__ TrSeq tr_seq(const K16Pages& pg, const TrArgs& a, int b) {
-  TrSeq s;
-  s.row0 = k16_start(a.starts, b, a.total);
-  s.n = min(max(k16_start(a.starts, b + 1, a.total) - s.row0, 0), a.max_rows);
-  s.held = (int)min((long long)max(__ldcg(pg.len + b), 0), (long long)pg.W << pg.shift);
-  return s;
-}
-
-// A CTA's share of an item: key tiles [t, t + nt) of T.
-struct TrItem { int b, h, row0, n, held, q0, T, t, nt; bool first; };
 // One lane's share of that: rows of nodes [q0, q_hi), `keys` of which it may see, tiles j = lane's first, + step, ...
 struct TrLane { int q0, q_hi, keys, n_tiles; };
 
@@ -103,8 +49,7 @@ __device__ __forceinline__ TrLane tr_lane(const TrArgs& a, const TrItem& I, int 
   L.q_hi = min(I.n, L.q0 + a.PB);
   L.keys = I.held + (a.mask ? I.n : L.q_hi);
   if (F == kTrPair) L.n_tiles = L.q0 < I.n ? min(max((L.keys + kTrBN - 1) / kTrBN - I.t, 0), I.nt) : 0;
-  else if (F == kTrSplit) L.n_tiles = (I.nt + 1 - x) >> 1;
-  else L.n_tiles = x == 0 ? I.nt : 0;
+  else L.n_tiles = (I.nt + 1 - x) >> 1;
   return L;
 }
 // the lane's i-th tile, counted from the share's first
@@ -113,42 +58,6 @@ template <int F> __device__ __forceinline__ int tr_tile(int i, int x) { return F
 __device__ __forceinline__ int tr_cols(const TrItem& I, const TrLane& L, int j) {
   return min(kTrBN, (L.keys - (I.t + j) * kTrBN + 15) & ~15);
 }
-// Walks a CTA's items; every role does so for itself.
-template <int F>
-struct TrWalker {
-  const K16Pages& pg; const TrArgs& a;
-  TrSeq s, ahead;                                      // the sequence, the one behind it (requested early)
-  int b, h, q0, t; long long left; bool first;
-  __device__ __forceinline__ TrWalker(const K16Pages& pg_, const TrArgs& a_, const TrHead& hd) : pg(pg_), a(a_) {
-    b = hd.b; h = hd.h; q0 = hd.q0; t = hd.t; left = hd.units; first = true;
-    s.row0 = hd.row0; s.n = hd.n; s.held = hd.held;
-    if (left > 0) fetch();
-  }
-  __device__ __forceinline__ void fetch() {
-    ahead.row0 = ahead.n = ahead.held = 0;
-    if (b + 1 < pg.B) ahead = tr_seq(pg, a, b + 1);
-  }
-  __device__ __forceinline__ bool next(TrItem& I) {
-    if (left <= 0) return false;
-    I.b = b; I.h = h; I.row0 = s.row0; I.n = s.n; I.held = s.held; I.q0 = q0; I.t = t; I.first = first;
-    I.T = tr_tiles<F>(a, s.held, s.n, q0);
-    I.nt = (int)min((long long)(I.T - t), left);
-    left -= I.nt;
-    first = false;
-    t = 0;
-    if (left > 0 && ++h == a.Hk) {
-      h = 0;
-      q0 = tr_reach<F>(a, q0);
-      if (q0 >= s.n) {
-        q0 = 0;
-        do { ++b; s = ahead; fetch(); } while (s.n == 0 && b + 1 < pg.B);
-        if (s.n == 0) left = 0;                        // (the ranges end with the last sequence that has nodes)
-      }
-    }
-    return true;
-  }
-};
-
 // 32 bits of a row's mask from bit j0 on (zeros come in front and behind); m0, m1: its first two words.
 __device__ __forceinline__ uint32_t tr_mask_bits(const int32_t* row, int words, uint32_t m0, uint32_t m1, int j0) {
   const int w = j0 >> 5;
@@ -211,79 +120,12 @@ __device__ __forceinline__ void tr_softmax_words(uint32_t s_addr, uint32_t o_add
   tmem_st_wait();
 }
 
-// 32 bytes from registers; where the address is a multiple of 32, in one access
-__device__ __forceinline__ void tr_store32(void* p, const uint32_t* r) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-               :: "l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
-}
-
-__device__ __forceinline__ void tr_store32_any(void* p, const uint32_t* r, int wide) {
-  if (wide) { tr_store32(p, r); return; }
-  static_cast<uint4*>(p)[0] = make_uint4(r[0], r[1], r[2], r[3]);
-  static_cast<uint4*>(p)[1] = make_uint4(r[4], r[5], r[6], r[7]);
-}
-
-// Where the CTA's even range of all key tiles begins: found by the whole CTA, left in *hd (shared); scratch: shared.
-template <int F>
-__device__ __forceinline__ void tr_find(const K16Pages& pg, const TrArgs& a, TrHead* hd, long long* scratch) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  constexpr int T = Tr<64, F>::THREADS;
-  const int per = (pg.B + T - 1) / T, b0 = min(pg.B, tid * per), b1 = min(pg.B, b0 + per);
-  auto units = [&](const TrSeq& s) {
-    long long u = 0;
-    for (int q0 = 0; q0 < s.n; q0 = tr_reach<F>(a, q0)) u += tr_tiles<F>(a, s.held, s.n, q0);
-    return u * a.Hk;
-  };
-  long long mine = 0;
-  for (int b = b0; b < b1; ++b) mine += units(tr_seq(pg, a, b));
-  long long run = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long v = __shfl_up_sync(0xffffffffu, run, o);
-    if (lane >= o) run += v;
-  }
-  if (lane == 31) scratch[warp] = run;
-  if (tid == 0) hd->units = 0;
-  __syncthreads();
-  long long front = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < T / 32; ++w) {
-    if (w < warp) front += scratch[w];
-    all += scratch[w];
-  }
-  const long long u0 = all * blockIdx.x / gridDim.x, u1 = all * (blockIdx.x + 1) / gridDim.x;
-  long long at = front + run - mine;                   // units in front of this thread's sequences
-  if (u0 < u1 && at <= u0 && u0 < at + mine) {
-    for (int b = b0; b < b1; ++b) {
-      const TrSeq s = tr_seq(pg, a, b);
-      const long long u = units(s);
-      if (u0 >= at + u) { at += u; continue; }
-      int rest_q0 = 0;
-      long long rest = u0 - at;
-      for (; rest_q0 < s.n; rest_q0 = tr_reach<F>(a, rest_q0)) {
-        const long long x = (long long)tr_tiles<F>(a, s.held, s.n, rest_q0) * a.Hk;
-        if (rest < x) break;
-        rest -= x;
-      }
-      hd->b = b; hd->q0 = rest_q0; hd->n = s.n; hd->row0 = s.row0; hd->held = s.held;
-      hd->T = tr_tiles<F>(a, s.held, s.n, rest_q0);
-      hd->h = (int)(rest / hd->T);
-      hd->t = (int)(rest - (long long)hd->h * hd->T);
-      hd->units = u1 - u0;
-      hd->first = u0;
-      hd->all = all;
-      break;
-    }
-  }
-  __syncthreads();
-}
-
 template <int D, int F>
-__global__ void __launch_bounds__(Tr<D, F>::THREADS, F == kTrSingle ? 2 : 1)
+__global__ void __launch_bounds__(kTrThreads, 1)
 attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const TrArgs a) {
   using S = Tr<D, F>;
   constexpr bool kPair = S::kPair;
-  constexpr int kProducer = 4 * S::LANES, kIssuer = kProducer + 1, kLast = kProducer + 3;
+  constexpr int kProducer = 8, kIssuer = 9, kLast = 11;
   extern __shared__ __align__(1024) char smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (smem_u32(smem) & 1023u) {                        // the swizzled tiles need 1024-byte alignment
@@ -317,7 +159,7 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
   // Tensor memory is only asked for when the kernels in front are done, and nothing behind comes up before it is there: none
   // of them can wait for the other's with tensor memory in hand.
   chained_wait();
-  if (warp == kLast) { tmem_alloc(smem_u32(tmem_slot), S::TMEM_COLS); tmem_relinquish(); }
+  if (warp == kLast) { tmem_alloc(smem_u32(tmem_slot), 512); tmem_relinquish(); }
   tr_find<F>(pg, a, hd, reinterpret_cast<long long*>(smem));             // (the ring is not in use yet)
   fence_proxy_async();
   if (tid == 0) a.heads[blockIdx.x] = *hd;
@@ -329,7 +171,7 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
 
   if (warp == kProducer) {
     // ---------------------------------------------------------------- producer
-    reg_dec<S::REGS_SMALL>();
+    reg_dec<kTrRegsSmall>();
     const CUtensorMap* mq = reinterpret_cast<const CUtensorMap*>(maps.q);
     const CUtensorMap* mkv = reinterpret_cast<const CUtensorMap*>(maps.kv);
     if (lane == 0) { tma_prefetch_desc(mq); tma_prefetch_desc(mkv); }
@@ -348,7 +190,7 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
         mbar_expect_tx(bar(buf, Q_FULL), (uint32_t)(D / 64) * 128u * (uint32_t)(a.box_rows * a.G));
 #pragma unroll
         for (int hf = 0; hf < D / 64; ++hf)
-          tma_load_3d(smem_u32(smem + buf * S::Q_TILE + hf * S::Q_HALF), mq, 64 * hf, I.h * a.G, I.row0 + q0, bar(buf, Q_FULL));
+          tma_load_3d(smem_u32(smem + buf * S::TILE + hf * S::HALF), mq, 64 * hf, I.h * a.G, I.row0 + q0, bar(buf, Q_FULL));
       }
       __syncwarp();
     };
@@ -413,11 +255,11 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
         if (n_q[x] > 0)
           for (int k = 0; k < kSpinLimit && !mbar_try_wait(bar(x, Q_FULL), (uint32_t)(n_q[x] - 1) & 1u); ++k) __nanosleep(40);
     }
-  } else if (warp >= kIssuer && warp < kIssuer + S::LANES) {
+  } else if (warp >= kIssuer && warp < kIssuer + 2) {
     // ---------------------------------------------------------------- MMA issuer of one lane
     // The whole warp walks the loop, so that counters and descriptors stay warp-uniform, and one elected lane issues.  Its lanes
     // wait each for itself, so the warp agrees before it goes on or stops.
-    reg_dec<S::REGS_SMALL>();
+    reg_dec<kTrRegsSmall>();
     const int x = warp - kIssuer;
     const uint32_t t_o = uniform32(tmem + x * kAtLaneCols + kAtColO), t_s = uniform32(tmem + x * kAtLaneCols + kAtColS);
     constexpr uint32_t idesc_pv = idesc_bf16(kTrBM, D, 0, 1);          // B (= V) is MN-major
@@ -439,7 +281,7 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
       };
       const int qb = kPair ? x : 0;                    // Q tile
       const uint32_t q_use = (uint32_t)(kPair ? n_mine : n_item);
-      const uint64_t q_desc = q_base + (uint64_t)uniform32((uint32_t)qb * (S::Q_TILE >> 4));
+      const uint64_t q_desc = q_base + (uint64_t)uniform32((uint32_t)qb * (S::TILE >> 4));
       for (int u = -1; u < n_sub; ++u) {
         if (n_sub == 0) break;
         const bool has_pv = u >= 0, has_qk = u + 1 < n_sub;
@@ -478,8 +320,8 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
           if (has_qk) {
 #pragma unroll
             for (uint32_t ks = 0; ks < D / 16; ++ks) {
-              constexpr uint64_t half = S::HALF >> 4, q_half = S::Q_HALF >> 4;   // the second 64 dims are a tile of their own
-              mma_ss(t_s, q_desc + (ks >> 2) * q_half + 2 * (ks & 3), kd + (ks >> 2) * half + 2 * (ks & 3), idesc_qk, ks != 0);
+              constexpr uint64_t half = S::HALF >> 4;                  // the second 64 dims are a tile of their own
+              mma_ss(t_s, q_desc + (ks >> 2) * half + 2 * (ks & 3), kd + (ks >> 2) * half + 2 * (ks & 3), idesc_qk, ks != 0);
             }
             mma_commit(bar(x, S_FULL));
             mma_commit(kv_empty(sk));
@@ -508,7 +350,7 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
     }
   } else if (warp < kProducer) {
     // ---------------------------------------------------------------- softmax / epilogue warps of one lane
-    reg_inc<S::REGS_SOFTMAX>();
+    reg_inc<kTrRegsSoftmax>();
     const int x = warp >> 2, quad = warp & 3;
     const int row = quad * 32 + lane;                                  // row within the tile
     const uint32_t lane_off = (uint32_t)(quad * 32) << 16;
@@ -516,7 +358,7 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
     const uint32_t o_addr = tmem + lane_off + x * kAtLaneCols + kAtColO;
     float2* exch = reinterpret_cast<float2*>(smem + S::EXCH);
     const int my_node = row / a.G, my_head = row - my_node * a.G, warp_node = (quad * 32) / a.G;
-    constexpr int kItemRows = S::ITEM_ROWS, kPartFloats = S::PART_FLOATS;
+    constexpr int kItemRows = TrPart<D, F>::ROWS, kPartFloats = TrPart<D, F>::FLOATS;
     TrWalker<F> W(pg, a, *hd);
     TrItem I;
     int g0 = 0, g_twin = 0, ring0 = 0, n_mine[2] = {0, 0}, tiles = 0;  // (n_mine: of both lanes)
@@ -710,7 +552,7 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
     }
     if (*abort_flag && row == 0) report_status(a.status, DL_ERR_TIMEOUT, blockIdx.x);
   } else {
-    reg_dec<S::REGS_SMALL>();                             // same budget as the rest of its warpgroup
+    reg_dec<kTrRegsSmall>();                             // same budget as the rest of its warpgroup
     // starts that lead out of the tensors (they are clamped wherever they are used) and sequences with more nodes than were
     // said (cut off there) are reported
     if (blockIdx.x == 0)
@@ -721,7 +563,7 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == kLast) { tc_fence_after(); tmem_dealloc(tmem, S::TMEM_COLS); }
+  if (warp == kLast) { tc_fence_after(); tmem_dealloc(tmem, 512); }
 }
 
 // Joins the parts of items that borders of ranges cut.  CTA (c, y) belongs to the border in front of range c; the CTAs of all
@@ -755,7 +597,7 @@ template <int D, int F>
 __global__ void __launch_bounds__(kTrJoinThreads)
 attn_tree_join_kernel(const TrArgs a, int32_t ranges) {
   constexpr bool kPair = F == kTrPair;
-  constexpr int kItemRows = Tr<D, F>::ITEM_ROWS, kPartFloats = Tr<D, F>::PART_FLOATS;
+  constexpr int kItemRows = TrPart<D, F>::ROWS, kPartFloats = TrPart<D, F>::FLOATS;
   constexpr int E = D / 32;
   __shared__ float far_m[kTrJoinWarps], far_l[kTrJoinWarps], far_o[kTrJoinWarps][D];
   const int c = blockIdx.x + 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -856,33 +698,38 @@ attn_tree_join_kernel(const TrArgs a, int32_t ranges) {
   }
 }
 
-static int64_t tr_head_floats(int32_t sm_count) { return ((int64_t)2 * sm_count * (sizeof(TrHead) / 4) + 63) & ~(int64_t)63; }
+static int64_t tr_head_floats(int32_t sm_count) { return ((int64_t)sm_count * (sizeof(TrHead) / 4) + 63) & ~(int64_t)63; }
 
-// Scratch: the ranges' heads (two ranges a multiprocessor at most), two parts a range: up to 256 rows of one range or 64 of two.
+// Scratch: the ranges' heads, two parts a range of up to 256 rows.
 int64_t attn_tree_scratch_floats(int32_t sm_count, const dl_model_desc& d) {
   return tr_head_floats(sm_count) + (int64_t)sm_count * 2 * 256 * (d.head_dim + 2);
 }
 
-template <int D> static constexpr int tr_smem() { return std::max({Tr<D, kTrSingle>::SMEM, Tr<D, kTrSplit>::SMEM, Tr<D, kTrPair>::SMEM}); }
-static_assert(2 * (Tr<128, kTrSingle>::SMEM + 1024) <= 228 * 1024 && 2 * (Tr<64, kTrSingle>::SMEM + 1024) <= 228 * 1024, "two CTAs a multiprocessor");
+template <int D> static constexpr int tr_smem() { return std::max(Tr<D, kTrSplit>::SMEM, Tr<D, kTrPair>::SMEM); }
 
 bool attn_tree_supported(const dl_ctx* ctx) {
-  return ctx->desc.dtype == DL_BF16 && ctx->tmap_encode != nullptr && ctx->smem_optin >= std::max(tr_smem<128>(), tr_smem<64>());
+  return ctx->desc.dtype == DL_BF16 && ctx->tmap_encode != nullptr && ctx->smem_optin >= std::max(tr_smem<128>(), tr_smem<64>()) &&
+         attn_tree_rows_supported(ctx);
 }
 
 template <int D, int F>
 static cudaError_t tr_launch(dl_ctx* ctx, const TrMaps& maps, const K16Pages& pg, const TrArgs& a, cudaStream_t s) {
-  static int attr_set[64];                             // (all calls ask for the same: two threads may)
-  if (!attr_set[ctx->device & 63]) {
-    const cudaError_t e = cudaFuncSetAttribute(attn_tree_kernel<D, F>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tr<D, F>::SMEM);
-    if (e != cudaSuccess) return e;
-    attr_set[ctx->device & 63] = 1;
-  }
   // no more ranges than key tiles there can be
   const long long row_tiles = std::min<long long>((long long)pg.B * ((a.max_rows + a.PB - 1) / a.PB), (long long)a.total);
   const long long key_tiles = (((long long)pg.W << pg.shift) + a.max_rows + kTrBN - 1) / kTrBN;
-  const int ranges = (int)std::min<long long>((F == kTrSingle ? 2 : 1) * ctx->sm_count, std::max(1LL, std::min(row_tiles, 1LL << 20) * key_tiles * a.Hk));
-  cudaError_t e = launch_chained(attn_tree_kernel<D, F>, dim3(ranges), dim3(Tr<D, F>::THREADS), Tr<D, F>::SMEM, s, maps, pg, a);
+  const int ranges = (int)std::min<long long>(ctx->sm_count, std::max(1LL, std::min(row_tiles, 1LL << 20) * key_tiles * a.Hk));
+  cudaError_t e;
+  if constexpr (F == kTrRows) {
+    e = launch_attn_tree_rows(ctx, maps, pg, a, ranges, s);
+  } else {
+    static int attr_set[64];                           // (all calls ask for the same: two threads may)
+    if (!attr_set[ctx->device & 63]) {
+      e = cudaFuncSetAttribute(attn_tree_kernel<D, F>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tr<D, F>::SMEM);
+      if (e != cudaSuccess) return e;
+      attr_set[ctx->device & 63] = 1;
+    }
+    e = launch_chained(attn_tree_kernel<D, F>, dim3(ranges), dim3(kTrThreads), Tr<D, F>::SMEM, s, maps, pg, a);
+  }
   if (e != cudaSuccess || ranges == 1) return e;
   const int rows = std::min((F == kTrPair ? 2 : 1) * a.PB, a.max_rows) * a.G;
   return launch_chained(attn_tree_join_kernel<D, F>, dim3(ranges - 1, (rows + 2 * kTrJoinWarps - 1) / (2 * kTrJoinWarps)),
@@ -903,8 +750,8 @@ cudaError_t launch_attn_tree(dl_ctx* ctx, const dl_pages* p, int32_t Hk, const v
   a.said_rows = mask ? (int)std::min<long long>(max_rows, 32LL * words) : max_rows;
   a.max_rows = std::min(a.said_rows, total);
   const int rows = (int)std::min<long long>((long long)a.max_rows * a.G, 1 << 20);
-  const int form = rows <= Tr<128, kTrSingle>::ROWS ? kTrSingle : a.max_rows <= kTrBM / a.G ? kTrSplit : kTrPair;
-  a.PB = (form == kTrSingle ? Tr<128, kTrSingle>::ROWS : kTrBM) / a.G;
+  const int form = rows <= kTrFewRows ? kTrRows : a.max_rows <= kTrBM / a.G ? kTrSplit : kTrPair;
+  a.PB = (form == kTrRows ? kTrFewRows : kTrBM) / a.G;
   a.box_rows = std::min(a.PB, a.max_rows);
   a.scale_log2 = scale * 1.4426950408889634f;
   const uint64_t pool_rows = (2ull * Hk * pg.n_pages) << pg.shift;
@@ -917,8 +764,8 @@ cudaError_t launch_attn_tree(dl_ctx* ctx, const dl_pages* p, int32_t Hk, const v
   if (!encode_bf16_map(ctx->tmap_encode, reinterpret_cast<CUtensorMap*>(maps.q), q, 3, dq, sq, bq) ||
       !encode_bf16_map(ctx->tmap_encode, reinterpret_cast<CUtensorMap*>(maps.kv), pool, 2, dkv, skv, bkv))
     return cudaErrorInvalidValue;
-  auto launch = D == 128 ? (form == kTrSingle ? tr_launch<128, kTrSingle> : form == kTrSplit ? tr_launch<128, kTrSplit> : tr_launch<128, kTrPair>)
-                         : (form == kTrSingle ? tr_launch<64, kTrSingle> : form == kTrSplit ? tr_launch<64, kTrSplit> : tr_launch<64, kTrPair>);
+  auto launch = D == 128 ? (form == kTrRows ? tr_launch<128, kTrRows> : form == kTrSplit ? tr_launch<128, kTrSplit> : tr_launch<128, kTrPair>)
+                         : (form == kTrRows ? tr_launch<64, kTrRows> : form == kTrSplit ? tr_launch<64, kTrSplit> : tr_launch<64, kTrPair>);
   return launch(ctx, maps, pg, a, s);
 }
 
