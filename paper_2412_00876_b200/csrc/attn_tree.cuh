@@ -5,6 +5,8 @@
 // key tiles of a call are cut into as many even ranges as there are CTAs, whatever the lengths are: a CTA's range covers the end
 // of one item, some whole ones, the start of another.  Items cut by a border leave their parts (sums, row maxima) in
 // scratch, and a second kernel joins them in order: no result depends on timing.
+// An item costs more than its key tiles (its masked tile, the hand-over to the next one, its outputs): it counts tr_extra() units
+// more, in front of its tiles, so that a range of many short items holds fewer tiles.
 #pragma once
 
 #include "attn_prefill.cuh"
@@ -29,6 +31,8 @@ template <int F> __host__ __device__ constexpr int tr_threads() { return F == kT
 struct TrMaps { alignas(64) unsigned char q[128]; alignas(64) unsigned char kv[128]; };
 
 // What a CTA's range begins with, for the joining kernel.
+//   (b, q0, h), t: its first item and key tile; units: what the walk has left, without extra units in front of the first tile
+//   (0: no tile); first, all: its first unit among all units, and their number
 struct TrHead { int b, q0, h, t; int T, n, row0, held; long long units, first, all; };
 
 struct TrArgs {
@@ -48,6 +52,9 @@ template <int F>
 __device__ __forceinline__ int tr_tiles(const TrArgs& a, int held, int n, int q0) {
   return (held + (a.mask ? n : min(n, tr_reach<F>(a, q0))) + kTrBN - 1) / kTrBN;
 }
+
+// extra units of an item
+template <int F> __host__ __device__ constexpr int tr_extra() { return F == kTrRows ? 2 : 2; }
 
 struct TrSeq { int row0, n, held; };
 __device__ __forceinline__ TrSeq tr_seq(const K16Pages& pg, const TrArgs& a, int b) {
@@ -83,6 +90,7 @@ struct TrWalker {
     left -= I.nt;
     first = false;
     t = 0;
+    if (left > 0) left = max(left - tr_extra<F>(), 0ll);   // the next item's extra units
     if (left > 0 && ++h == a.Hk) {
       h = 0;
       q0 = tr_reach<F>(a, q0);
@@ -116,7 +124,7 @@ __device__ __forceinline__ void tr_find(const K16Pages& pg, const TrArgs& a, TrH
   const int per = (pg.B + T - 1) / T, b0 = min(pg.B, tid * per), b1 = min(pg.B, b0 + per);
   auto units = [&](const TrSeq& s) {
     long long u = 0;
-    for (int q0 = 0; q0 < s.n; q0 = tr_reach<F>(a, q0)) u += tr_tiles<F>(a, s.held, s.n, q0);
+    for (int q0 = 0; q0 < s.n; q0 = tr_reach<F>(a, q0)) u += tr_tiles<F>(a, s.held, s.n, q0) + tr_extra<F>();
     return u * a.Hk;
   };
   long long mine = 0;
@@ -148,15 +156,17 @@ __device__ __forceinline__ void tr_find(const K16Pages& pg, const TrArgs& a, TrH
       int rest_q0 = 0;
       long long rest = u0 - at;
       for (; rest_q0 < s.n; rest_q0 = tr_reach<F>(a, rest_q0)) {
-        const long long x = (long long)tr_tiles<F>(a, s.held, s.n, rest_q0) * a.Hk;
+        const long long x = (long long)(tr_tiles<F>(a, s.held, s.n, rest_q0) + tr_extra<F>()) * a.Hk;
         if (rest < x) break;
         rest -= x;
       }
       hd->b = b; hd->q0 = rest_q0; hd->n = s.n; hd->row0 = s.row0; hd->held = s.held;
       hd->T = tr_tiles<F>(a, s.held, s.n, rest_q0);
-      hd->h = (int)(rest / hd->T);
-      hd->t = (int)(rest - (long long)hd->h * hd->T);
-      hd->units = u1 - u0;
+      const int cost = hd->T + tr_extra<F>();
+      hd->h = (int)(rest / cost);
+      const int x = (int)(rest - (long long)hd->h * cost);
+      hd->t = max(x - tr_extra<F>(), 0);
+      hd->units = max(u1 - u0 - max(tr_extra<F>() - x, 0), 0ll);
       hd->first = u0;
       hd->all = all;
       break;

@@ -157,10 +157,9 @@ attn_tree_rows_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, co
   tc_fence_after();
   chained_go();
   const uint32_t tmem = *tmem_slot;
-  const int n_tiles = (int)hd->units;                  // key tiles of this CTA
-  // Places of the g-th K and V in the order through the ring: K_0, K_1, V_0, K_2, V_1, ...
+  // Places of the g-th K and V in the order through the ring: K_0, K_1, V_0, K_2, V_1, ...; last: there is no next tile
   auto pos_k = [&](int g) { return g == 0 ? 0 : 2 * g - 1; };
-  auto pos_v = [&](int g) { return g == n_tiles - 1 ? 2 * g + 1 : 2 * g + 2; };
+  auto pos_v = [&](int g, bool last) { return last ? 2 * g + 1 : 2 * g + 2; };
 
   if (warp == kRwProducer) {
     // ---------------------------------------------------------------- producer
@@ -266,8 +265,8 @@ attn_tree_rows_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, co
     auto wait = [&](uint32_t b, uint32_t parity) { ok = mbar_wait_spin(b, parity & 1u, abort_flag) && ok; };
     auto full = [&](int pos) { wait(kv_full(pos % S::SLOTS), (uint32_t)(pos / S::SLOTS)); return pos % S::SLOTS; };
     struct { int ksteps, run; bool first, last; } v = {0, 0, false, false};  // the tile whose P V is still to come
-    auto issue_o = [&](int t) {                        // O^T += V^T P^T of tile t
-      const int sv = full(pos_v(t)), pb = t % S::P_BUFS, ob = v.run & 1;
+    auto issue_o = [&](int t, bool at_end) {           // O^T += V^T P^T of tile t
+      const int sv = full(pos_v(t, at_end)), pb = t % S::P_BUFS, ob = v.run & 1;
       if (v.first) wait(bar(O_FREE, ob), ((uint32_t)(v.run >> 1) & 1u) ^ 1u);
       wait(bar(P_FULL, pb), (uint32_t)(t / S::P_BUFS));
       if (!warp_agreed(ok)) { stop = true; return; }
@@ -290,7 +289,7 @@ attn_tree_rows_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, co
       for (int j = 0; j < I.nt && !stop; ++j) {
         // (with one place for Q the last item's P V does not wait for this one's Q)
         const bool before = j == 0 && S::Q_PLACES == 1;
-        if (before && g > 0) issue_o(g - 1);
+        if (before && g > 0) issue_o(g - 1, false);
         if (stop) break;
         const int place = run % S::Q_PLACES, sb = g & 1;
         if (j == 0) wait(bar(Q_FULL, place), (uint32_t)(run / S::Q_PLACES));
@@ -311,7 +310,7 @@ attn_tree_rows_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, co
           if (last) mma_commit(bar(Q_EMPTY, place));
         }
         __syncwarp();
-        if (!before && g > 0) issue_o(g - 1);
+        if (!before && g > 0) issue_o(g - 1, false);
         v.ksteps = (min(kTrBN, I.held + I.n - (I.t + j) * kTrBN) + 15) >> 4;
         v.run = run;
         v.first = j == 0;
@@ -320,7 +319,7 @@ attn_tree_rows_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, co
       }
       ++run;
     }
-    if (!stop && g > 0) issue_o(g - 1);
+    if (!stop && g > 0) issue_o(g - 1, true);
   } else if (warp < 8) {
     // ---------------------------------------------------------------- exponentials, epilogue
     constexpr int kW = N / 2;                                                // rows of one half
@@ -470,7 +469,7 @@ attn_tree_rows_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, co
         }
         if (half == 0 && key >= keys && t < ((keys - c0 + 15) & ~15)) {
           // a row behind the sequence's last that V^T P^T covers: 0 * x must stay 0 for any bit pattern of it
-          const int pos = pos_v(g), slot = pos % S::SLOTS;
+          const int pos = pos_v(g, j == I.nt - 1 && W.left <= 0), slot = pos % S::SLOTS;
           mbar_wait_spin(kv_full(slot), (uint32_t)(pos / S::SLOTS) & 1u, abort_flag);
 #pragma unroll
           for (int u = 0; u < D / 8; ++u)

@@ -605,19 +605,21 @@ attn_tree_join_kernel(const TrArgs a, int32_t ranges) {
   chained_wait();
   const TrHead hd = a.heads[c];
   if (hd.units == 0 || hd.t == 0) return;                          // the border falls between items (or there is none)
-  const long long W = hd.all, item = hd.first - hd.t, end = item + hd.T;     // the item's key tiles among all
-  // Range c holds key tiles [W c / ranges, W (c + 1) / ranges), so key tile u is range_of(u)'s; with fewer key tiles than ranges
-  // each is a range of its own, and others are empty between them.
+  constexpr int kExtra = tr_extra<F>();
+  const long long W = hd.all, item = hd.first - hd.t - kExtra;     // the item's units begin there, its key tiles at tiles
+  const long long tiles = item + kExtra, end = tiles + hd.T;
+  // Range c holds units [W c / ranges, W (c + 1) / ranges), so unit u is range_of(u)'s; with fewer units than ranges each is a
+  // range of its own, and others are empty between them.
   auto range_of = [&](long long u) { return (int)(((u + 1) * ranges - 1) / W); };
   const bool dense = W >= ranges;
-  const int c_lo = range_of(item);
+  const int c_lo = range_of(tiles);
   const int n_parts = dense ? range_of(end - 1) - c_lo + 1 : hd.T;
-  const int group = dense ? c - c_lo - 1 : (int)(hd.first - item) - 1, groups = n_parts - 1;   // this border among the item's
+  const int group = dense ? c - c_lo - 1 : (int)(hd.first - tiles) - 1, groups = n_parts - 1;  // this border among the item's
   const int slot0 = W * c_lo / ranges < item ? 1 : 0;              // where the first part lies
   const int rows = min(hd.n - hd.q0, (kPair ? 2 : 1) * a.PB) * a.G;
   const int me = blockIdx.y * groups + group, all = gridDim.y * groups;      // this CTA among the item's
   auto part = [&](int i) {
-    const int r = dense ? c_lo + i : range_of(item + i);
+    const int r = dense ? c_lo + i : range_of(tiles + i);
     return a.parts + (size_t)(2 * r + (i == 0 ? slot0 : 0)) * kPartFloats;
   };
   auto row_in_part = [&](int r) { return kPair && r >= a.PB * a.G ? 128 + r - a.PB * a.G : r; };
@@ -717,7 +719,7 @@ static cudaError_t tr_launch(dl_ctx* ctx, const TrMaps& maps, const K16Pages& pg
   // no more ranges than key tiles there can be
   const long long row_tiles = std::min<long long>((long long)pg.B * ((a.max_rows + a.PB - 1) / a.PB), (long long)a.total);
   const long long key_tiles = (((long long)pg.W << pg.shift) + a.max_rows + kTrBN - 1) / kTrBN;
-  const int ranges = (int)std::min<long long>(ctx->sm_count, std::max(1LL, std::min(row_tiles, 1LL << 20) * key_tiles * a.Hk));
+  const int ranges = (int)std::min<long long>(ctx->sm_count, std::max(1LL, std::min(row_tiles, 1LL << 20) * (key_tiles + tr_extra<F>()) * a.Hk));
   cudaError_t e;
   if constexpr (F == kTrRows) {
     e = launch_attn_tree_rows(ctx, maps, pg, a, ranges, s);
