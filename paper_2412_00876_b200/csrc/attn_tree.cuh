@@ -54,7 +54,7 @@ __device__ __forceinline__ int tr_tiles(const TrArgs& a, int held, int n, int q0
 }
 
 // extra units of an item
-template <int F> __host__ __device__ constexpr int tr_extra() { return F == kTrRows ? 2 : 2; }
+template <int F> __host__ __device__ constexpr int tr_extra() { return F == kTrRows ? 3 : 4; }
 
 struct TrSeq { int row0, n, held; };
 __device__ __forceinline__ TrSeq tr_seq(const K16Pages& pg, const TrArgs& a, int b) {
