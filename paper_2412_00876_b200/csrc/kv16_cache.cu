@@ -3,8 +3,9 @@
 //
 //   plan   : (with a keep mask or a commit) per sequence, count the kept rows, check that their pages are there, note the first
 //            destination row, advance the length: one CTA per sequence;
-//   append : a CTA takes a few packed rows; their cos and sin go to shared memory once and serve all heads; then every thread
-//            moves 32 bytes at a time (both halves of 8 pairs), q to q_out, k to k_out and the cache, v to the cache;
+//   append : a CTA takes a few packed rows; cos and sin of those that are kept or asked for go to shared memory once and serve all
+//            heads; then every thread moves 32 bytes at a time (both halves of 8 pairs), four such units in flight, q to q_out, k to
+//            k_out and the cache, v to the cache;
 //   commit : accepted rows move up; a thread stays at one 16-byte column of one pool, tensor and head and walks the rows in
 //            order, so that no row is overwritten before it has been read;
 //   tree   : ancestors' bits and depths of tree nodes.
@@ -15,7 +16,8 @@
 namespace dl {
 
 constexpr int kK16Threads = 256;
-constexpr int kK16Rows = 8;              // most packed rows per CTA of the append
+constexpr int kK16Rows = 16;             // most packed rows per CTA of the append
+constexpr int kK16Batch = 4;             // units of 32 bytes a thread has in flight
 
 __device__ __forceinline__ int k16_block_sum(int v, int* sh) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -74,6 +76,7 @@ struct K16Append {
   const int32_t* pos; const double* freqs; const int32_t* starts; const uint8_t* keep;
   const int32_t* plan_base; const int32_t* plan_count;             // NULL: lengths as they are, nothing dropped
   int32_t H, Hk, total, rows, rot, interleaved;
+  uint32_t per_row, per_row_inv;                                   // units of a row, 2^32 / units rounded up
   float amplitude;
   DeviceStatus* status;
 };
@@ -125,12 +128,19 @@ __global__ void __launch_bounds__(kK16Threads)
 kv16_append_kernel(const K16Pages pg, const K16Append a) {
   extern __shared__ int seq_start[];
   __shared__ int sh[kK16Threads / 32];
+  __shared__ uint64_t step[D / 2];                                 // turns per position, 64 bits of the fraction
   __shared__ float2 cs[kK16Rows][D / 2];
-  __shared__ int row_page[kK16Rows], row_in[kK16Rows];            // page (-1: not cached) and row in it
-  __shared__ int row_there[kK16Rows];                              // the row belongs to a sequence
+  __shared__ int row_of[kK16Rows];                                 // rows that have something to do (counted from the CTA's first)
+  __shared__ long long row_at[kK16Rows];                           // K row of head 0 in the pool; -1: not cached
+  __shared__ int n_rows;
   chained_go();
   chained_wait();
-  const int t0 = blockIdx.x * a.rows, n = min(a.rows, a.total - t0);
+  const int t0 = blockIdx.x * a.rows, n = min(a.rows, a.total - t0), half = a.rot >> 1;
+  if ((int)threadIdx.x < half) {
+    double turns = __ldcg(a.freqs + threadIdx.x) * 0.15915494309189533577;
+    turns -= floor(turns);
+    step[threadIdx.x] = (uint64_t)__double2ull_rn(turns * 18446744073709551616.0);
+  }
   int b0 = -1, before = 0;                                         // the first row's sequence, its kept rows in front
   if (a.pool) {
     for (int b = threadIdx.x; b <= pg.B; b += kK16Threads) seq_start[b] = k16_start(a.starts, b, a.total);
@@ -144,7 +154,7 @@ kv16_append_kernel(const K16Pages pg, const K16Append a) {
     const int b = in && a.pool ? k16_sequence(seq_start, pg.B, r) : -1;
     const bool f = b >= 0 && (a.keep == nullptr || __ldcg(a.keep + r) != 0);
     const unsigned m = __ballot_sync(0xffffffffu, f);
-    int page = -1, at = 0;
+    long long at = -1;
     if (b >= 0) {
       const int base = a.plan_base ? __ldcg(a.plan_base + b) : __ldcg(pg.len + b);
       const bool fits = a.plan_count ? __ldcg(a.plan_count + b) >= 0 : k16_fits(pg, b, base, seq_start[b + 1] - seq_start[b]);
@@ -152,55 +162,74 @@ kv16_append_kernel(const K16Pages pg, const K16Append a) {
       if (fits && f) {
         const int head = max(seq_start[b] - t0, 0);                // first lane of this sequence
         const long long dst = (long long)base + (b == b0 ? before : 0) + __popc(m & ((1u << t) - 1u) & ~((1u << head) - 1u));
-        page = k16_page(pg, b, dst);
-        at = (int)(dst & ((1 << pg.shift) - 1));
+        const int page = k16_page(pg, b, dst);
+        if (page >= 0) at = k16_row(pg, a.Hk, page, 0, 0, dst);
       }
     }
-    if (in) {
-      row_page[t] = page;
-      row_in[t] = at;
-      row_there[t] = b >= 0 || a.pool == nullptr;
+    const bool work = in && (at >= 0 || ((b >= 0 || a.pool == nullptr) && (a.q_out || a.k_out)));
+    const unsigned w = __ballot_sync(0xffffffffu, work);
+    if (work) {
+      const int i = __popc(w & ((1u << t) - 1u));
+      row_of[i] = t;
+      row_at[i] = at;
     }
-  }
-  const int half = a.rot >> 1;
-  for (int i = threadIdx.x; i < n * half; i += kK16Threads) {
-    const int t = i / half, f = i - t * half;
-    // the angle as a fraction of a turn, 64 bits of it: products with positions wrap around by themselves
-    double turns = __ldcg(a.freqs + f) * 0.15915494309189533577;
-    turns -= floor(turns);
-    const uint64_t step = (uint64_t)__double2ull_rn(turns * 18446744073709551616.0);
-    const int64_t angle = (int64_t)((uint64_t)(int64_t)__ldcg(a.pos + t0 + t) * step);
-    float s, c;
-    sincospif((float)angle * 1.0842021724855044e-19f, &s, &c);     // half turns: 2^-63
-    cs[t][f] = make_float2(c * a.amplitude, s * a.amplitude);
+    if (t == 0) n_rows = __popc(w);
   }
   __syncthreads();
+  const int n_work = n_rows;
+  for (int i = threadIdx.x; i < n_work * half; i += kK16Threads) {
+    const int w = i / half, f = i - w * half;
+    // the angle as a fraction of a turn, 64 bits of it: products with positions wrap around by themselves
+    const int64_t angle = (int64_t)((uint64_t)(int64_t)__ldcg(a.pos + t0 + row_of[w]) * step[f]);
+    float s, c;
+    sincospif((float)angle * 1.0842021724855044e-19f, &s, &c);     // half turns: 2^-63
+    cs[w][f] = make_float2(c * a.amplitude, s * a.amplitude);
+  }
+  __syncthreads();
+  // All units of all rows in one row of indices, kK16Batch of them per thread in flight (a thread writes what it has read alone, so
+  // in-place outputs are safe).
   constexpr int C = D / 16;                                        // units of 32 bytes per head
-  const int uq = a.q_out ? a.H * C : 0, uk = a.Hk * C, U = uq + uk + (a.pool ? uk : 0);
-  const int rot_units = a.rot >> 4;
-  for (int t = 0; t < n; ++t) {
-    if (!row_there[t]) continue;
-    const int page = row_page[t];
-    const long long r = t0 + t;
-    for (int u = blockIdx.y * kK16Threads + threadIdx.x; u < U; u += gridDim.y * kK16Threads) {
-      const int part = u < uq ? 0 : u < uq + uk ? 1 : 2;
-      const int x = u - (part == 0 ? 0 : part == 1 ? uq : uq + uk), h = x / C, c = x % C;
-      if (part > 0 && page < 0 && !(part == 1 && a.k_out)) continue;
-      const __nv_bfloat16* src = (part == 0 ? a.q + r * a.q_stride : (part == 1 ? a.k : a.v) + r * a.kv_stride) + h * D;
-      const bool turn = part < 2 && c < rot_units;
-      const int d0 = turn && !a.interleaved ? 8 * c : 16 * c, d1 = turn && !a.interleaved ? 8 * c + half : 16 * c + 8;
-      uint4 w0 = *reinterpret_cast<const uint4*>(src + d0), w1 = *reinterpret_cast<const uint4*>(src + d1);
-      if (turn) k16_rotate(w0, w1, a.interleaved != 0, &cs[t][8 * c]);
-      if (part == 0 || (part == 1 && a.k_out)) {
-        __nv_bfloat16* o = (part == 0 ? a.q_out + r * a.q_out_stride : a.k_out + r * a.k_out_stride) + h * D;
-        *reinterpret_cast<uint4*>(o + d0) = w0;
-        *reinterpret_cast<uint4*>(o + d1) = w1;
+  const int uq = a.q_out ? a.H * C : 0, uk = a.Hk * C;
+  const int rot_units = a.rot >> 4, all = n_work * (int)a.per_row;
+  const long long v_rows = (long long)a.Hk << pg.shift;            // rows from K to V of a page
+  for (int i0 = (blockIdx.y * kK16Threads) * kK16Batch + threadIdx.x; i0 < all; i0 += gridDim.y * kK16Threads * kK16Batch) {
+    uint4 w0[kK16Batch], w1[kK16Batch];
+    int row[kK16Batch], part[kK16Batch], d0[kK16Batch], d1[kK16Batch], head[kK16Batch];
+#pragma unroll
+    for (int k = 0; k < kK16Batch; ++k) {
+      const int i = i0 + k * kK16Threads;
+      part[k] = -1;
+      if (i >= all) continue;
+      row[k] = (int)__umulhi((uint32_t)i, a.per_row_inv);
+      const int u = i - row[k] * (int)a.per_row, p = u < uq ? 0 : u < uq + uk ? 1 : 2;
+      const int x = u - (p == 0 ? 0 : p == 1 ? uq : uq + uk), c = x % C;
+      head[k] = x / C;
+      if (p > 0 && row_at[row[k]] < 0 && !(p == 1 && a.k_out)) continue;
+      part[k] = p;
+      const bool pairs = p < 2 && c < rot_units && !a.interleaved;  // halves apart
+      d0[k] = pairs ? 8 * c : 16 * c;
+      d1[k] = pairs ? 8 * c + half : 16 * c + 8;
+      const long long r = t0 + row_of[row[k]];
+      const __nv_bfloat16* src = (p == 0 ? a.q + r * a.q_stride : (p == 1 ? a.k : a.v) + r * a.kv_stride) + head[k] * D;
+      w0[k] = *reinterpret_cast<const uint4*>(src + d0[k]);
+      w1[k] = *reinterpret_cast<const uint4*>(src + d1[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kK16Batch; ++k) {
+      if (part[k] < 0) continue;
+      const int c = (i0 + k * kK16Threads - row[k] * (int)a.per_row - (part[k] == 0 ? 0 : part[k] == 1 ? uq : uq + uk)) % C;
+      if (part[k] < 2 && c < rot_units) k16_rotate(w0[k], w1[k], a.interleaved != 0, &cs[row[k]][8 * c]);
+      const long long r = t0 + row_of[row[k]], at = row_at[row[k]];
+      if (part[k] == 0 || (part[k] == 1 && a.k_out)) {
+        __nv_bfloat16* o = (part[k] == 0 ? a.q_out + r * a.q_out_stride : a.k_out + r * a.k_out_stride) + head[k] * D;
+        *reinterpret_cast<uint4*>(o + d0[k]) = w0[k];
+        *reinterpret_cast<uint4*>(o + d1[k]) = w1[k];
       }
-      if (part > 0 && page >= 0) {
-        const long long at = k16_row(pg, a.Hk, page, part - 1, h, row_in[t]) * D;
-        if (DL_IN_BOUNDS(a.status, KID_KV16, at + D - 1, (((long long)pg.n_pages * 2 * a.Hk) << pg.shift) * D)) {
-          *reinterpret_cast<uint4*>(a.pool + at + d0) = w0;
-          *reinterpret_cast<uint4*>(a.pool + at + d1) = w1;
+      if (part[k] > 0 && at >= 0) {
+        const long long dst = (at + (part[k] == 2 ? v_rows : 0) + ((long long)head[k] << pg.shift)) * D;
+        if (DL_IN_BOUNDS(a.status, KID_KV16, dst + D - 1, (((long long)pg.n_pages * 2 * a.Hk) << pg.shift) * D)) {
+          *reinterpret_cast<uint4*>(a.pool + dst + d0[k]) = w0[k];
+          *reinterpret_cast<uint4*>(a.pool + dst + d1[k]) = w1[k];
         }
       }
     }
@@ -358,7 +387,10 @@ cudaError_t launch_kv16_append(const dl_ctx* ctx, const dl_pages* p, int32_t Hk,
     if (e != cudaSuccess) return e;
   }
   const int units = ((q_out ? H : 0) + (pool ? 2 : 1) * Hk) * (D / 16);
-  a.rows = std::min(kK16Rows, std::max(1, total / (8 * ctx->sm_count)));
+  a.per_row = (uint32_t)units;
+  a.per_row_inv = (uint32_t)(((1ull << 32) + units - 1) / units);
+  // Rows per CTA: as many as leave four CTAs a multiprocessor; fewer rows than that are shared by several CTAs (grid y).
+  a.rows = std::min(kK16Rows, std::max(1, total / (4 * ctx->sm_count)));
   const int slices = a.rows > 1 ? 1 : std::min((units + kK16Threads - 1) / kK16Threads, std::max(1, 8 * ctx->sm_count / total));
   const dim3 grid((total + a.rows - 1) / a.rows, slices);
   const size_t smem = pool ? (size_t)(pg.B + 1) * 4 : 0;
