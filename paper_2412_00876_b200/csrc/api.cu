@@ -945,7 +945,10 @@ int32_t dl_kv16_append(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, v
   }
   if ((q && q_out == q && q_out_stride != q_stride) || (k_out == k && k_out_stride != kv_stride)) return DL_ERR_INVALID_ARG;
   if (!pages && !q_out && !k_out) return DL_OK;
-  // units of 32 bytes are counted in 32 bits, 16 rows of them at a time
+  // the list of rows with a mask lies in the scratch of the attention calls
+  if (pages && keep && total > std::max(kv4_scratch_floats(ctx->sm_count, ctx->desc), attn_tree_scratch_floats(ctx->sm_count, ctx->desc)))
+    return DL_ERR_WORKSPACE;
+  // units of 32 bytes are counted in 32 bits, a few rows of them at a time
   if ((qw + 2 * kw) >= (1 << 15)) return DL_ERR_UNSUPPORTED;
   DeviceGuard g(ctx->device);
   return cuda_status(ctx, launch_kv16_append(ctx, pages, n_kv_heads, pool, q, q_stride, k, v, kv_stride, pos, rope, starts, keep,

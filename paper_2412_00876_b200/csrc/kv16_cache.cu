@@ -1,8 +1,8 @@
 // Rows into the paged 16-bit K/V cache: appended with the position rotation on the way, and kept or dropped once drafts are
 // verified.  An extension, not in the paper: the append of Eq. 6 for rows that are not position-encoded yet.
 //
-//   plan   : (with a keep mask or a commit) per sequence, count the kept rows, check that their pages are there, note the first
-//            destination row, advance the length: one CTA per sequence;
+//   plan   : (with a keep mask or a commit) per sequence, count the kept rows and list them in front of the others, check that
+//            their pages are there, note the first destination row, advance the length: one CTA per sequence;
 //   append : a CTA takes a few packed rows; cos and sin of those that are kept or asked for go to shared memory once and serve all
 //            heads; then every thread moves 32 bytes at a time (both halves of 8 pairs), four such units in flight, q to q_out, k to
 //            k_out and the cache, v to the cache;
@@ -16,34 +16,28 @@
 namespace dl {
 
 constexpr int kK16Threads = 256;
-constexpr int kK16Rows = 16;             // most packed rows per CTA of the append
-constexpr int kK16Batch = 4;             // units of 32 bytes a thread has in flight
+constexpr int kK16Rows = 8;              // most packed rows per CTA of the append
+constexpr int kK16Batch = 2;             // units of 32 bytes a thread has in flight
+constexpr int kK16Ctas = 6;              // CTAs of it a multiprocessor holds
+constexpr int kK16PlanThreads = 1024;
 
-__device__ __forceinline__ int k16_block_sum(int v, int* sh) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+// 16 flags of keep[from, to) that thread x of a CTA looks at, as bits; flags behind `to` are 0.
+__device__ __forceinline__ uint32_t k16_flags(const uint8_t* keep, int at, int to) {
+  uint32_t m = 0;
+  if (at + 16 <= to && (reinterpret_cast<uintptr_t>(keep + at) & 15) == 0) {
+    const uint4 w = __ldcg(reinterpret_cast<const uint4*>(keep + at));
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  if (lane == 0) sh[warp] = v;
-  __syncthreads();
-  int t = 0;
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t b = __vcmpne4(v[i], 0) & 0x01010101u;
+      m |= ((b * 0x01020408u) >> 24 & 0xFu) << (4 * i);            // the four bytes' lowest bits side by side
+    }
+  } else {
 #pragma unroll
-  for (int w = 0; w < kK16Threads / 32; ++w) t += sh[w];
-  __syncthreads();
-  return t;
-}
-
-// flags that are not 0 among keep[from, to), counted by the whole CTA, 16 at a time
-__device__ __forceinline__ int k16_count(const uint8_t* keep, int from, int to, int* sh) {
-  int c = 0;
-  const int head = min(to, from + (int)((16 - (reinterpret_cast<uintptr_t>(keep + from) & 15)) & 15));
-  const int units = max(0, to - head) / 16;
-  for (int i = from + threadIdx.x; i < head; i += kK16Threads) c += __ldcg(keep + i) != 0;
-  for (int i = threadIdx.x; i < units; i += kK16Threads) {
-    const uint4 w = __ldcg(reinterpret_cast<const uint4*>(keep + head) + i);
-    c += (__popc(__vcmpne4(w.x, 0)) + __popc(__vcmpne4(w.y, 0)) + __popc(__vcmpne4(w.z, 0)) + __popc(__vcmpne4(w.w, 0))) >> 3;
+    for (int i = 0; i < 16; ++i)
+      if (at + i < to && __ldcg(keep + at + i) != 0) m |= 1u << i;
   }
-  for (int i = head + 16 * units + threadIdx.x; i < to; i += kK16Threads) c += __ldcg(keep + i) != 0;
-  return k16_block_sum(c, sh);
+  return m;
 }
 
 // Whether rows [base, base + count) of sequence b have pages: a sequence's pages come first in its table row, so the last one
@@ -52,19 +46,66 @@ __device__ __forceinline__ bool k16_fits(const K16Pages& pg, int b, int base, in
   return base >= 0 && (count == 0 || k16_page(pg, b, (long long)base + count - 1) >= 0);
 }
 
-__global__ void __launch_bounds__(kK16Threads)
+// With a mask: order[starts[b] ..] gets the sequence's rows, the kept ones first, both kinds in their order.
+__global__ void __launch_bounds__(kK16PlanThreads)
 kv16_plan_kernel(const K16Pages pg, const int32_t* starts, const uint8_t* keep, int32_t total, int32_t commit,
-                 int32_t* plan_base, int32_t* plan_count) {
-  __shared__ int sh[kK16Threads / 32];
+                 int32_t* plan_base, int32_t* plan_count, int32_t* order) {
+  __shared__ int sh[2][kK16PlanThreads / 32];
   chained_go();
   chained_wait();
-  const int b = blockIdx.x, base = __ldcg(pg.len + b);
+  const int b = blockIdx.x, base = __ldcg(pg.len + b), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int from = k16_start(starts, b, total), to = max(from, k16_start(starts, b + 1, total));
-  const int count = keep ? k16_count(keep, from, to, sh) : to - from;
+  int count = to - from;
+  if (keep) {
+    // flags from a 16-byte boundary on, 16 a thread
+    const int first = from - (int)(reinterpret_cast<uintptr_t>(keep + from) & 15), step = 16 * kK16PlanThreads;
+    auto flags = [&](int at) { return at < to ? k16_flags(keep, max(at, 0), to) << (at < 0 ? -at : 0) : 0u; };
+    // (a thread's 16 may begin in front of the sequence, or of the tensor)
+    auto mine = [&](int i0) {
+      const int at = first + i0 + 16 * (int)threadIdx.x;
+      uint32_t m = at < 0 ? flags(at) : at < to ? k16_flags(keep, at, to) : 0u;
+      if (at < from) m &= 0xFFFFFFFFu << min(from - at, 31);
+      return m & 0xFFFFu;
+    };
+    int c = 0;
+    for (int i0 = 0; first + i0 < to; i0 += step) c += __popc(mine(i0));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+    if (lane == 0) sh[0][warp] = c;
+    __syncthreads();
+    count = 0;
+#pragma unroll
+    for (int w = 0; w < kK16PlanThreads / 32; ++w) count += sh[0][w];
+    int kept = from, turn = 1;                                     // place of the next kept row
+    for (int i0 = 0; first + i0 < to; i0 += step, turn ^= 1) {
+      const uint32_t m = mine(i0);
+      const int at = first + i0 + 16 * (int)threadIdx.x, n = __popc(m);
+      int run = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, run, o);
+        if (lane >= o) run += v;
+      }
+      if (lane == 31) sh[turn][warp] = run;
+      __syncthreads();
+      int front = kept + run - n, all = 0;
+      for (int w = 0; w < kK16PlanThreads / 32; ++w) {
+        const int v = sh[turn][w];
+        if (w < warp) front += v;
+        all += v;
+      }
+      for (int i = max(0, from - at); i < 16 && at + i < to; ++i) {
+        const bool f = (m >> i) & 1;
+        order[f ? front : from + count + (at + i - from) - (front - from)] = at + i;
+        front += f;
+      }
+      kept += all;
+    }
+  }
   if (threadIdx.x == 0) {
     const bool ok = k16_fits(pg, b, base, count);
     plan_base[b] = base;
-    plan_count[b] = ok ? count : -1;
+    plan_count[b] = ok ? count : -1 - count;
     if (ok && commit) pg.len[b] = base + count;
   }
 }
@@ -73,8 +114,9 @@ struct K16Append {
   const __nv_bfloat16* q; const __nv_bfloat16* k; const __nv_bfloat16* v;
   __nv_bfloat16* q_out; __nv_bfloat16* k_out; __nv_bfloat16* pool;
   long long q_stride, kv_stride, q_out_stride, k_out_stride;
-  const int32_t* pos; const double* freqs; const int32_t* starts; const uint8_t* keep;
-  const int32_t* plan_base; const int32_t* plan_count;             // NULL: lengths as they are, nothing dropped
+  const int32_t* pos; const double* freqs; const int32_t* starts;
+  const int32_t* plan_base; const int32_t* plan_count;             // NULL: lengths as they are; count: -1 - it where pages lack
+  const int32_t* order;                                            // NULL: nothing is dropped
   int32_t H, Hk, total, rows, rot, interleaved;
   uint32_t per_row, per_row_inv;                                   // units of a row, 2^32 / units rounded up
   float amplitude;
@@ -124,13 +166,12 @@ __device__ __forceinline__ void k16_rotate(uint4& a, uint4& b, bool interleaved,
 }
 
 template <int D>
-__global__ void __launch_bounds__(kK16Threads)
+__global__ void __launch_bounds__(kK16Threads, kK16Ctas)
 kv16_append_kernel(const K16Pages pg, const K16Append a) {
   extern __shared__ int seq_start[];
-  __shared__ int sh[kK16Threads / 32];
   __shared__ uint64_t step[D / 2];                                 // turns per position, 64 bits of the fraction
   __shared__ float2 cs[kK16Rows][D / 2];
-  __shared__ int row_of[kK16Rows];                                 // rows that have something to do (counted from the CTA's first)
+  __shared__ int row_of[kK16Rows];                                 // rows that have something to do
   __shared__ long long row_at[kK16Rows];                           // K row of head 0 in the pool; -1: not cached
   __shared__ int n_rows;
   chained_go();
@@ -141,36 +182,33 @@ kv16_append_kernel(const K16Pages pg, const K16Append a) {
     turns -= floor(turns);
     step[threadIdx.x] = (uint64_t)__double2ull_rn(turns * 18446744073709551616.0);
   }
-  int b0 = -1, before = 0;                                         // the first row's sequence, its kept rows in front
   if (a.pool) {
     for (int b = threadIdx.x; b <= pg.B; b += kK16Threads) seq_start[b] = k16_start(a.starts, b, a.total);
     __syncthreads();
-    b0 = k16_sequence(seq_start, pg.B, t0);
-    if (b0 >= 0) before = a.keep ? k16_count(a.keep, seq_start[b0], t0, sh) : t0 - seq_start[b0];
   }
   if (threadIdx.x < 32) {
-    const int t = threadIdx.x, r = t0 + t;
+    const int t = threadIdx.x, x = t0 + t;                         // place in the order of rows
     const bool in = t < n;
-    const int b = in && a.pool ? k16_sequence(seq_start, pg.B, r) : -1;
-    const bool f = b >= 0 && (a.keep == nullptr || __ldcg(a.keep + r) != 0);
-    const unsigned m = __ballot_sync(0xffffffffu, f);
+    const int b = in && a.pool ? k16_sequence(seq_start, pg.B, x) : -1;
+    int r = x;
     long long at = -1;
     if (b >= 0) {
+      const int rank = x - seq_start[b], number = seq_start[b + 1] - seq_start[b];
       const int base = a.plan_base ? __ldcg(a.plan_base + b) : __ldcg(pg.len + b);
-      const bool fits = a.plan_count ? __ldcg(a.plan_count + b) >= 0 : k16_fits(pg, b, base, seq_start[b + 1] - seq_start[b]);
-      if (!fits && r == seq_start[b] && blockIdx.y == 0) report_status(a.status, DL_ERR_CAPACITY, b);
-      if (fits && f) {
-        const int head = max(seq_start[b] - t0, 0);                // first lane of this sequence
-        const long long dst = (long long)base + (b == b0 ? before : 0) + __popc(m & ((1u << t) - 1u) & ~((1u << head) - 1u));
-        const int page = k16_page(pg, b, dst);
-        if (page >= 0) at = k16_row(pg, a.Hk, page, 0, 0, dst);
+      const int planned = a.plan_count ? __ldcg(a.plan_count + b) : 0;
+      if (a.order) r = min(max(__ldcg(a.order + x), 0), a.total - 1);
+      const bool fits = a.plan_count ? planned >= 0 : k16_fits(pg, b, base, number);
+      if (!fits && rank == 0 && blockIdx.y == 0) report_status(a.status, DL_ERR_CAPACITY, b);
+      if (fits && rank < (a.order ? planned : number)) {
+        const int page = k16_page(pg, b, (long long)base + rank);
+        if (page >= 0) at = k16_row(pg, a.Hk, page, 0, 0, (long long)base + rank);
       }
     }
     const bool work = in && (at >= 0 || ((b >= 0 || a.pool == nullptr) && (a.q_out || a.k_out)));
     const unsigned w = __ballot_sync(0xffffffffu, work);
     if (work) {
       const int i = __popc(w & ((1u << t) - 1u));
-      row_of[i] = t;
+      row_of[i] = r;
       row_at[i] = at;
     }
     if (t == 0) n_rows = __popc(w);
@@ -180,7 +218,7 @@ kv16_append_kernel(const K16Pages pg, const K16Append a) {
   for (int i = threadIdx.x; i < n_work * half; i += kK16Threads) {
     const int w = i / half, f = i - w * half;
     // the angle as a fraction of a turn, 64 bits of it: products with positions wrap around by themselves
-    const int64_t angle = (int64_t)((uint64_t)(int64_t)__ldcg(a.pos + t0 + row_of[w]) * step[f]);
+    const int64_t angle = (int64_t)((uint64_t)(int64_t)__ldcg(a.pos + row_of[w]) * step[f]);
     float s, c;
     sincospif((float)angle * 1.0842021724855044e-19f, &s, &c);     // half turns: 2^-63
     cs[w][f] = make_float2(c * a.amplitude, s * a.amplitude);
@@ -209,7 +247,7 @@ kv16_append_kernel(const K16Pages pg, const K16Append a) {
       const bool pairs = p < 2 && c < rot_units && !a.interleaved;  // halves apart
       d0[k] = pairs ? 8 * c : 16 * c;
       d1[k] = pairs ? 8 * c + half : 16 * c + 8;
-      const long long r = t0 + row_of[row[k]];
+      const long long r = row_of[row[k]];
       const __nv_bfloat16* src = (p == 0 ? a.q + r * a.q_stride : (p == 1 ? a.k : a.v) + r * a.kv_stride) + head[k] * D;
       w0[k] = *reinterpret_cast<const uint4*>(src + d0[k]);
       w1[k] = *reinterpret_cast<const uint4*>(src + d1[k]);
@@ -219,7 +257,7 @@ kv16_append_kernel(const K16Pages pg, const K16Append a) {
       if (part[k] < 0) continue;
       const int c = (i0 + k * kK16Threads - row[k] * (int)a.per_row - (part[k] == 0 ? 0 : part[k] == 1 ? uq : uq + uk)) % C;
       if (part[k] < 2 && c < rot_units) k16_rotate(w0[k], w1[k], a.interleaved != 0, &cs[row[k]][8 * c]);
-      const long long r = t0 + row_of[row[k]], at = row_at[row[k]];
+      const long long r = row_of[row[k]], at = row_at[row[k]];
       if (part[k] == 0 || (part[k] == 1 && a.k_out)) {
         __nv_bfloat16* o = (part[k] == 0 ? a.q_out + r * a.q_out_stride : a.k_out + r * a.k_out_stride) + head[k] * D;
         *reinterpret_cast<uint4*>(o + d0[k]) = w0[k];
@@ -374,7 +412,7 @@ cudaError_t launch_kv16_append(const dl_ctx* ctx, const dl_pages* p, int32_t Hk,
   a.q = static_cast<const __nv_bfloat16*>(q); a.k = static_cast<const __nv_bfloat16*>(k); a.v = static_cast<const __nv_bfloat16*>(v);
   a.q_out = static_cast<__nv_bfloat16*>(q_out); a.k_out = static_cast<__nv_bfloat16*>(k_out); a.pool = static_cast<__nv_bfloat16*>(pool);
   a.q_stride = q_stride; a.kv_stride = kv_stride; a.q_out_stride = q_out_stride; a.k_out_stride = k_out_stride;
-  a.pos = pos; a.starts = starts; a.keep = pool ? keep : nullptr;
+  a.pos = pos; a.starts = starts;
   a.H = H; a.Hk = Hk; a.total = total;
   a.amplitude = 1.f;
   if (rope) { a.freqs = rope->freqs; a.rot = rope->rot_dim; a.interleaved = rope->interleaved; a.amplitude = rope->amplitude; }
@@ -382,8 +420,10 @@ cudaError_t launch_kv16_append(const dl_ctx* ctx, const dl_pages* p, int32_t Hk,
   if (pool && (keep || commit)) {
     a.plan_base = ctx->ws.plan_base;
     a.plan_count = ctx->ws.plan_count;
-    const cudaError_t e = launch_chained(kv16_plan_kernel, dim3(pg.B), dim3(kK16Threads), 0, s, pg, starts, keep, total, commit,
-                                         ctx->ws.plan_base, ctx->ws.plan_count);
+    int32_t* order = reinterpret_cast<int32_t*>(ctx->ws.kv4_partial);
+    if (keep) a.order = order;
+    const cudaError_t e = launch_chained(kv16_plan_kernel, dim3(pg.B), dim3(kK16PlanThreads), 0, s, pg, starts, keep, total, commit,
+                                         ctx->ws.plan_base, ctx->ws.plan_count, order);
     if (e != cudaSuccess) return e;
   }
   const int units = ((q_out ? H : 0) + (pool ? 2 : 1) * Hk) * (D / 16);
