@@ -21,25 +21,6 @@ constexpr int kK16Batch = 2;             // units of 32 bytes a thread has in fl
 constexpr int kK16Ctas = 6;              // CTAs of it a multiprocessor holds
 constexpr int kK16PlanThreads = 1024;
 
-// 16 flags of keep[from, to) that thread x of a CTA looks at, as bits; flags behind `to` are 0.
-__device__ __forceinline__ uint32_t k16_flags(const uint8_t* keep, int at, int to) {
-  uint32_t m = 0;
-  if (at + 16 <= to && (reinterpret_cast<uintptr_t>(keep + at) & 15) == 0) {
-    const uint4 w = __ldcg(reinterpret_cast<const uint4*>(keep + at));
-    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t b = __vcmpne4(v[i], 0) & 0x01010101u;
-      m |= ((b * 0x01020408u) >> 24 & 0xFu) << (4 * i);            // the four bytes' lowest bits side by side
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (at + i < to && __ldcg(keep + at + i) != 0) m |= 1u << i;
-  }
-  return m;
-}
-
 // Whether rows [base, base + count) of sequence b have pages: a sequence's pages come first in its table row, so the last one
 // tells.  (Every row's own page is looked at again where it is written.)
 __device__ __forceinline__ bool k16_fits(const K16Pages& pg, int b, int base, int count) {
@@ -50,36 +31,44 @@ __device__ __forceinline__ bool k16_fits(const K16Pages& pg, int b, int base, in
 __global__ void __launch_bounds__(kK16PlanThreads)
 kv16_plan_kernel(const K16Pages pg, const int32_t* starts, const uint8_t* keep, int32_t total, int32_t commit,
                  int32_t* plan_base, int32_t* plan_count, int32_t* order) {
-  __shared__ int sh[2][kK16PlanThreads / 32];
+  static_assert(kK16PlanThreads == 32 * 32, "a lane per warp");
+  __shared__ int sh[2][32];
   chained_go();
   chained_wait();
   const int b = blockIdx.x, base = __ldcg(pg.len + b), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int from = k16_start(starts, b, total), to = max(from, k16_start(starts, b + 1, total));
   int count = to - from;
   if (keep) {
-    // flags from a 16-byte boundary on, 16 a thread
-    const int first = from - (int)(reinterpret_cast<uintptr_t>(keep + from) & 15), step = 16 * kK16PlanThreads;
-    auto flags = [&](int at) { return at < to ? k16_flags(keep, max(at, 0), to) << (at < 0 ? -at : 0) : 0u; };
-    // (a thread's 16 may begin in front of the sequence, or of the tensor)
-    auto mine = [&](int i0) {
-      const int at = first + i0 + 16 * (int)threadIdx.x;
-      uint32_t m = at < 0 ? flags(at) : at < to ? k16_flags(keep, at, to) : 0u;
-      if (at < from) m &= 0xFFFFFFFFu << min(from - at, 31);
-      return m & 0xFFFFu;
+    // four flags a thread, from a 4-byte boundary on; those of other rows are 0
+    constexpr int kStep = 4 * kK16PlanThreads;
+    const int first = from - (int)(reinterpret_cast<uintptr_t>(keep + from) & 3);
+    auto flags = [&](int at) {
+      uint32_t m = 0;
+      if (at >= from && at + 4 <= to) {
+        const uint32_t b = __vcmpne4(__ldcg(reinterpret_cast<const uint32_t*>(keep + at)), 0) & 0x01010101u;
+        m = (b * 0x01020408u) >> 24;                               // the four bytes' lowest bits side by side
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (at + i >= from && at + i < to && __ldcg(keep + at + i) != 0) m |= 1u << i;
+      }
+      return m;
     };
     int c = 0;
-    for (int i0 = 0; first + i0 < to; i0 += step) c += __popc(mine(i0));
+    for (int at = first + 4 * (int)threadIdx.x; at < to; at += kStep) c += __popc(flags(at));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
     if (lane == 0) sh[0][warp] = c;
     __syncthreads();
-    count = 0;
+    c = sh[0][lane];
 #pragma unroll
-    for (int w = 0; w < kK16PlanThreads / 32; ++w) count += sh[0][w];
+    for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+    count = c;
     int kept = from, turn = 1;                                     // place of the next kept row
-    for (int i0 = 0; first + i0 < to; i0 += step, turn ^= 1) {
-      const uint32_t m = mine(i0);
-      const int at = first + i0 + 16 * (int)threadIdx.x, n = __popc(m);
+    for (int i0 = first; i0 < to; i0 += kStep, turn ^= 1) {
+      const int at = i0 + 4 * (int)threadIdx.x;
+      const uint32_t m = flags(at);
+      const int n = __popc(m);
       int run = n;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -88,18 +77,23 @@ kv16_plan_kernel(const K16Pages pg, const int32_t* starts, const uint8_t* keep, 
       }
       if (lane == 31) sh[turn][warp] = run;
       __syncthreads();
-      int front = kept + run - n, all = 0;
-      for (int w = 0; w < kK16PlanThreads / 32; ++w) {
-        const int v = sh[turn][w];
-        if (w < warp) front += v;
-        all += v;
+      // every warp adds up the warps' totals for itself
+      const int mine = sh[turn][lane];
+      int all = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, all, o);
+        if (lane >= o) all += v;
       }
-      for (int i = max(0, from - at); i < 16 && at + i < to; ++i) {
+      int front = kept + run - n + __shfl_sync(0xffffffffu, all - mine, warp);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (at + i < from || at + i >= to) continue;
         const bool f = (m >> i) & 1;
         order[f ? front : from + count + (at + i - from) - (front - from)] = at + i;
         front += f;
       }
-      kept += all;
+      kept += __shfl_sync(0xffffffffu, all, 31);
     }
   }
   if (threadIdx.x == 0) {
