@@ -272,11 +272,12 @@ kv16_append_kernel(const K16Pages pg, const K16Append a) {
 constexpr int kK16Pools = 64;            // pools per launch
 struct K16Pools { char* p[kK16Pools]; };
 
-// grid: (sequence, slices of the pools' 16-byte columns).  Moves only; lengths follow in a launch of their own.
+// grid: (sequence, slices of the pools' 16-byte columns).  `ticket` (one per sequence, zero between launches; NULL: lengths stay): the
+// last of a sequence's CTAs, all of which have read its length by then, advances it.
 template <int D>
 __global__ void __launch_bounds__(kK16Threads)
 kv16_move_kernel(const K16Pages pg, const __grid_constant__ K16Pools pools, int32_t n_pools, int32_t Hk, const int32_t* starts,
-                 const uint8_t* keep, int32_t total, DeviceStatus* st) {
+                 const uint8_t* keep, int32_t total, int32_t* ticket, DeviceStatus* st) {
   __shared__ int sh[kK16Threads / 32], warp_sum[kK16Threads / 32];
   __shared__ long long src_row[kK16Threads], dst_row[kK16Threads];  // K row of head 0 in the pool; -1: no page
   chained_go();
@@ -341,25 +342,10 @@ kv16_move_kernel(const K16Pages pg, const __grid_constant__ K16Pools pools, int3
     rank0 += count;
     __syncthreads();
   }
-}
-
-__global__ void __launch_bounds__(kK16Threads)
-kv16_advance_kernel(const K16Pages pg, const int32_t* starts, const uint8_t* keep, int32_t total) {
-  chained_go();
-  chained_wait();
-  const int b = blockIdx.x * (kK16Threads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (b >= pg.B) return;
-  const int base = __ldcg(pg.len + b);
-  const int from = k16_start(starts, b, total), to = max(from, k16_start(starts, b + 1, total));
-  int count = 0, last = -1;
-  for (int i = from + lane; i < to; i += 32)
-    if (__ldcg(keep + i) != 0) { ++count; last = i - from; }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    count += __shfl_xor_sync(0xffffffffu, count, o);
-    last = max(last, __shfl_xor_sync(0xffffffffu, last, o));
+  if (ticket && threadIdx.x == 0 && atomicAdd(ticket + b, 1) == (int)gridDim.y - 1) {
+    ticket[b] = 0;
+    pg.len[b] = base + rank0;
   }
-  if (lane == 0 && count > 0 && k16_fits(pg, b, base, last + 1)) pg.len[b] = base + count;
 }
 
 // ---- trees ------------------------------------------------------------------------------------------------------------
@@ -437,18 +423,18 @@ cudaError_t launch_kv16_commit(const dl_ctx* ctx, const dl_pages* p, int32_t Hk,
   const K16Pages pg = k16_pages(p);
   DeviceStatus* st = ctx->ws.base ? ctx->ws.status : nullptr;
   const int D = ctx->desc.head_dim;
-  for (int at = 0; at < n_pools; at += kK16Pools) {
+  for (int at = 0; at < n_pools || at == 0; at += kK16Pools) {
     K16Pools pp = {};
     const int n = std::min(kK16Pools, n_pools - at);
     for (int i = 0; i < n; ++i) pp.p[i] = static_cast<char*>(pools[at + i]);
-    const int slices = (int)std::min<long long>(((long long)n * 2 * Hk * (D / 8) + kK16Threads - 1) / kK16Threads, 4096);
+    const int slices = (int)std::min<long long>(std::max(1LL, ((long long)n * 2 * Hk * (D / 8) + kK16Threads - 1) / kK16Threads), 4096);
+    int32_t* ticket = at + kK16Pools >= n_pools ? ctx->ws.dec_ticket : nullptr;        // with the last pools
     const dim3 grid(pg.B, slices);
-    const cudaError_t e = D == 128 ? launch_chained(kv16_move_kernel<128>, grid, dim3(kK16Threads), 0, s, pg, pp, n, Hk, starts, keep, total, st)
-                                   : launch_chained(kv16_move_kernel<64>, grid, dim3(kK16Threads), 0, s, pg, pp, n, Hk, starts, keep, total, st);
+    const cudaError_t e = D == 128 ? launch_chained(kv16_move_kernel<128>, grid, dim3(kK16Threads), 0, s, pg, pp, n, Hk, starts, keep, total, ticket, st)
+                                   : launch_chained(kv16_move_kernel<64>, grid, dim3(kK16Threads), 0, s, pg, pp, n, Hk, starts, keep, total, ticket, st);
     if (e != cudaSuccess) return e;
   }
-  return launch_chained(kv16_advance_kernel, dim3((pg.B + kK16Threads / 32 - 1) / (kK16Threads / 32)), dim3(kK16Threads), 0, s,
-                        pg, starts, keep, total);
+  return cudaSuccess;
 }
 
 cudaError_t launch_tree_plan(const dl_ctx* ctx, const int32_t* parent, const int32_t* starts, const int32_t* pos0, int32_t B,
