@@ -11,10 +11,11 @@
 // the token drawn at the end is the same bit for bit wherever it is computed.
 //
 // A cluster of eight CTAs shares a sequence: each walks the tree on its own (same numbers, same decisions) and sums its part of a
-// row; a warp tells its sum to all CTAs through distributed shared memory, then the cluster's barrier, and all of them know it.  Vocabularies
-// of up to 32768 leave 8 values a thread, which stay in registers (as 64-bit floats, p times 2^44) as long as the node is the one
-// reached: what bounds a call is the chain of passes of its unluckiest sequence, and a further pass over a row costs two
-// multiplications and a conversion a value, and the barrier.
+// row; a warp tells its sum to all CTAs through distributed shared memory, then the cluster's barrier, and all of them know it.
+// Vocabularies of up to 32768 leave 8 values a thread, which stay in registers as long as the node is the one reached.  What bounds a
+// call is the chain of passes of its unluckiest sequence; 40 registers let three CTAs share a multiprocessor, so that 55 sequences
+// go at once (48 trees of 40-64 nodes: 24 us; with 69 registers, the values kept as 64-bit floats, 34 us; with 64 26 us).
+// Measured and not better: bringing rows into L2 when a node is reached (26 us), or those of its children (greedily 15.4 -> 19.7).
 #include <algorithm>
 
 #include "kv16.cuh"
@@ -156,7 +157,7 @@ template <typename T> __device__ __forceinline__ void tv_load(const T* row, int 
 
 // kNear: a thread's part of a row is one block.
 template <int MODE, typename T, bool kNear>
-__global__ void __launch_bounds__(kTvThreads)
+__global__ void __launch_bounds__(kTvThreads, 3)
 tree_verify_kernel(const TvArgs a) {
   extern __shared__ int nodes[];
   __shared__ TvShared sh;
@@ -231,9 +232,9 @@ tree_verify_kernel(const TvArgs a) {
     return (int)(0xFFFFFFFFu - (uint32_t)tv_all<true>(((unsigned long long)top << 32) | (0xFFFFFFFFu - first), &sh, rank, round));
   };
   // the row of the node reached: p 2^44 and q of this thread's block, if it has one only
-  double pr[kTvBlock], qr[kTvBlock];
+  float pr[kTvBlock], qr[kTvBlock];
   bool here = false;
-  auto fetch = [&](int v, double (&p)[kTvBlock], double (&q)[kTvBlock]) {
+  auto fetch = [&](int v, float (&p)[kTvBlock], float (&q)[kTvBlock]) {
     float x[kTvBlock], y[kTvBlock];
     if (v < a.vocab) {
       tv_load<T>(target + (long long)(from + at) * a.target_stride, v, a.vocab, wide_p, 0.f, x);
@@ -241,15 +242,15 @@ tree_verify_kernel(const TvArgs a) {
     }
 #pragma unroll
     for (int i = 0; i < kTvBlock; ++i) {
-      p[i] = v < a.vocab ? (double)x[i] * kTvUnit : 0.0;
-      q[i] = kDraft && v < a.vocab ? (double)y[i] : 0.0;
+      p[i] = v < a.vocab ? x[i] : 0.f;
+      q[i] = kDraft && v < a.vocab ? y[i] : 0.f;
     }
     if (kPoint)                                                    // tokens that this node's children have had rejected count 0
       for (int j = next_child(at); j < n; j = next_child(j)) {
         const int d = tok[j] - v;
 #pragma unroll
         for (int i = 0; i < kTvBlock; ++i)
-          if (d == i) p[i] = 0.0;
+          if (d == i) p[i] = 0.f;
       }
   };
   // weights of the thread's values, in their order: f(value's index, its weight); true ends it
@@ -270,7 +271,7 @@ tree_verify_kernel(const TvArgs a) {
       here = kNear;
 #pragma unroll
       for (int i = 0; i < kTvBlock; ++i)
-        if (f(v + i, tv_units(pr[i], qr[i], s44))) return;
+        if (f(v + i, tv_units((double)pr[i] * kTvUnit, (double)qr[i], s44))) return;
     }
   };
   auto sum_of = [&](bool plain) {
