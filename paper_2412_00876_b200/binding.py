@@ -281,6 +281,8 @@ def _rows(t, dtype, shape, what: str, index: int):
     if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
         _refuse(t, dtype, shape, what, index)
     s0, s1, s2 = t.stride()
+    if s2 == 1 and s1 == shape[2] and s0 >= shape[1] * s1 and shape[0] > 1:          # (what nearly every call passes)
+        return t.data_ptr(), s0
     if shape[0] > 0 and (s2 != 1 or (s1 != shape[2] and shape[1] > 1)):
         raise ValueError(f"{what}: want rows with dense heads, got strides {t.stride()}")
     if shape[0] > 1 and s0 < shape[1] * shape[2]:                    # (0 would mean dense rows to the library)
