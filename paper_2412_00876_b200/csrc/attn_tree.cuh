@@ -7,6 +7,10 @@
 // scratch, and a second kernel joins them in order: no result depends on timing.
 // An item costs more than its key tiles (its masked tile, the hand-over to the next one, its outputs): it counts tr_extra() units
 // more, in front of its tiles, so that a range of many short items holds fewer tiles.
+// Short contexts (TrArgs::whole) are not cut: a range holds whole items, as many as the others or one more, and nothing is
+// joined.  4 nodes with 32 heads, 8 key heads: 8 sequences of 60, 200 and 400 rows 10.3, 12.7 and 14.9 us cut, 7.8, 8.8 and
+// 10.7 whole; 32 sequences 12.4, 20.0 and 24.8 cut, 11.3, 15.3 and 20.4 whole.  40 uneven sequences of up to 400 rows with 32
+// key heads, where a CTA has nine items, lose 63.5 -> 67.6, those of up to 200 win 54.5 -> 51.4.
 #pragma once
 
 #include "attn_prefill.cuh"
@@ -42,6 +46,7 @@ struct TrArgs {
   int32_t box_rows;                                    // nodes per Q box
   uint32_t pool_rows;                                  // rows of the pool's tensor map
   int32_t wide;                                        // out is 32-byte aligned
+  int32_t whole;                                       // ranges are of whole items, each of them a unit
   float scale_log2;
 };
 
@@ -86,11 +91,11 @@ struct TrWalker {
     if (left <= 0) return false;
     I.b = b; I.h = h; I.row0 = s.row0; I.n = s.n; I.held = s.held; I.q0 = q0; I.t = t; I.first = first;
     I.T = tr_tiles<F>(a, s.held, s.n, q0);
-    I.nt = (int)min((long long)(I.T - t), left);
-    left -= I.nt;
+    I.nt = a.whole ? I.T : (int)min((long long)(I.T - t), left);
+    left -= a.whole ? 1 : I.nt;
     first = false;
     t = 0;
-    if (left > 0) left = max(left - tr_extra<F>(), 0ll);   // the next item's extra units
+    if (left > 0 && !a.whole) left = max(left - tr_extra<F>(), 0ll);   // the next item's extra units
     if (left > 0 && ++h == a.Hk) {
       h = 0;
       q0 = tr_reach<F>(a, q0);
@@ -124,7 +129,7 @@ __device__ __forceinline__ void tr_find(const K16Pages& pg, const TrArgs& a, TrH
   const int per = (pg.B + T - 1) / T, b0 = min(pg.B, tid * per), b1 = min(pg.B, b0 + per);
   auto units = [&](const TrSeq& s) {
     long long u = 0;
-    for (int q0 = 0; q0 < s.n; q0 = tr_reach<F>(a, q0)) u += tr_tiles<F>(a, s.held, s.n, q0) + tr_extra<F>();
+    for (int q0 = 0; q0 < s.n; q0 = tr_reach<F>(a, q0)) u += a.whole ? 1 : tr_tiles<F>(a, s.held, s.n, q0) + tr_extra<F>();
     return u * a.Hk;
   };
   long long mine = 0;
@@ -156,17 +161,17 @@ __device__ __forceinline__ void tr_find(const K16Pages& pg, const TrArgs& a, TrH
       int rest_q0 = 0;
       long long rest = u0 - at;
       for (; rest_q0 < s.n; rest_q0 = tr_reach<F>(a, rest_q0)) {
-        const long long x = (long long)(tr_tiles<F>(a, s.held, s.n, rest_q0) + tr_extra<F>()) * a.Hk;
+        const long long x = (long long)(a.whole ? 1 : tr_tiles<F>(a, s.held, s.n, rest_q0) + tr_extra<F>()) * a.Hk;
         if (rest < x) break;
         rest -= x;
       }
       hd->b = b; hd->q0 = rest_q0; hd->n = s.n; hd->row0 = s.row0; hd->held = s.held;
       hd->T = tr_tiles<F>(a, s.held, s.n, rest_q0);
-      const int cost = hd->T + tr_extra<F>();
+      const int extra = a.whole ? 0 : tr_extra<F>(), cost = a.whole ? 1 : hd->T + extra;
       hd->h = (int)(rest / cost);
       const int x = (int)(rest - (long long)hd->h * cost);
-      hd->t = max(x - tr_extra<F>(), 0);
-      hd->units = max(u1 - u0 - max(tr_extra<F>() - x, 0), 0ll);
+      hd->t = max(x - extra, 0);
+      hd->units = max(u1 - u0 - max(extra - x, 0), 0ll);
       hd->first = u0;
       hd->all = all;
       break;

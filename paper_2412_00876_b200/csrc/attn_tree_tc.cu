@@ -23,6 +23,7 @@ namespace dl {
 
 constexpr int kTrPatience = 4000, kTrTurnTiles = 4;                // polls for a turn, tiles from which lanes take turns (attn_packed_tc.cu)
 constexpr int kTrRegsSmall = 40, kTrRegsSoftmax = 232;             // as there
+constexpr int kTrWholeTiles = 6;                                   // key tiles up to which items are not cut
 
 template <int D, int F> struct Tr {
   static constexpr bool kPair = F == kTrPair;
@@ -715,11 +716,13 @@ bool attn_tree_supported(const dl_ctx* ctx) {
 }
 
 template <int D, int F>
-static cudaError_t tr_launch(dl_ctx* ctx, const TrMaps& maps, const K16Pages& pg, const TrArgs& a, cudaStream_t s) {
-  // no more ranges than key tiles there can be
-  const long long row_tiles = std::min<long long>((long long)pg.B * ((a.max_rows + a.PB - 1) / a.PB), (long long)a.total);
+static cudaError_t tr_launch(dl_ctx* ctx, const TrMaps& maps, const K16Pages& pg, TrArgs a, cudaStream_t s) {
+  // As many ranges as multiprocessors, but no more than there can be key tiles (or items, where those are not cut: where a table
+  // row's pages hold few key tiles, a join would cost more than the CTA that has a tile more than others).
+  const long long row_tiles = std::min(std::min<long long>((long long)pg.B * ((a.max_rows + a.PB - 1) / a.PB), (long long)a.total), 1LL << 20);
   const long long key_tiles = (((long long)pg.W << pg.shift) + a.max_rows + kTrBN - 1) / kTrBN;
-  const int ranges = (int)std::min<long long>(ctx->sm_count, std::max(1LL, std::min(row_tiles, 1LL << 20) * (key_tiles + tr_extra<F>()) * a.Hk));
+  a.whole = key_tiles <= kTrWholeTiles;
+  const int ranges = (int)std::min<long long>(ctx->sm_count, std::max(1LL, row_tiles * a.Hk * (a.whole ? 1 : key_tiles + tr_extra<F>())));
   cudaError_t e;
   if constexpr (F == kTrRows) {
     e = launch_attn_tree_rows(ctx, maps, pg, a, ranges, s);
@@ -732,7 +735,7 @@ static cudaError_t tr_launch(dl_ctx* ctx, const TrMaps& maps, const K16Pages& pg
     }
     e = launch_chained(attn_tree_kernel<D, F>, dim3(ranges), dim3(kTrThreads), Tr<D, F>::SMEM, s, maps, pg, a);
   }
-  if (e != cudaSuccess || ranges == 1) return e;
+  if (e != cudaSuccess || ranges == 1 || a.whole) return e;
   const int rows = std::min((F == kTrPair ? 2 : 1) * a.PB, a.max_rows) * a.G;
   return launch_chained(attn_tree_join_kernel<D, F>, dim3(ranges - 1, (rows + 2 * kTrJoinWarps - 1) / (2 * kTrJoinWarps)),
                         dim3(kTrJoinThreads), 0, s, a, ranges);
