@@ -87,8 +87,9 @@ int32_t dl_destroy(dl_ctx* ctx);
 
 /* Bytes of scratch the calls below need for up to `max_batch` sequences, `max_rows` predictor
  * rows per call (B * n_vis_max in prefill) and caches of `cap` rows.  Negative on bad args.
- * For bf16 models this includes the parts of dl_kv4_attn_decode, whatever the sizes: 32 MB with 16
- * heads of 128 or more on 148 multiprocessors, less with fewer or smaller heads. */
+ * For bf16 models this includes, whatever the sizes, a part that dl_kv4_attn_decode, dl_kv16_attn_tree
+ * (the parts of split sequences) and dl_kv16_append (its list of kept rows) use in turn: on 148
+ * multiprocessors 39.4 MB with D = 128; with D = 64 20 MB, up to 32 MB with many heads. */
 int64_t dl_workspace_bytes(const dl_ctx* ctx, int32_t max_batch, int32_t max_rows, int32_t cap);
 
 /* Hands the context its scratch (dev, 256-byte aligned, caller keeps ownership) and clears the
@@ -539,7 +540,8 @@ int64_t dl_kv16_page_bytes(const dl_ctx* ctx, int32_t n_kv_heads, int32_t page_r
  *   (with the same strides), but not lie over anything else; pos dev [total] (may be NULL without rotation); rope HOST
  *   struct or NULL (no rotation); starts dev [B + 1], ascending; keep dev [total] or NULL (all).
  * The pages must be reserved: a sequence that lacks one is left as it was and records DL_ERR_CAPACITY with its index (q_out and
- * k_out are written).  Pages that other sequences share must not be written: a fork leaves every partly filled page to one.
+ * k_out are written).  A call with `keep` lists its rows in the workspace: up to 33,000 rows a multiprocessor with D = 64, twice as
+ * many with 128 (DL_ERR_WORKSPACE).  Pages that other sequences share must not be written: a fork leaves every partly filled page to one.
  * Rows of no sequence are left as they were, in q_out and k_out, too. */
 int32_t dl_kv16_append(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, void* pool, const void* q, int64_t q_stride,
                        const void* k, const void* v, int64_t kv_stride, const int32_t* pos, const dl_rope* rope,
@@ -553,7 +555,7 @@ int32_t dl_kv16_append(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, v
  *   q dev bf16 [total][n_heads][D], rotated; q_stride as above; starts dev [B + 1]; mask dev [total][words] or NULL: node i sees
  *   nodes 0..i (a chain, the next chunk of a prompt, or the single token of a step without drafts);
  *   max_rows HOST: no sequence has more nodes (nodes behind it are not computed, and DL_ERR_INVALID_ARG is recorded), nor more
- *   than 32 * words with a mask; out dev bf16 [total][n_heads][D] dense, rows of no sequence are left as they were.
+ *   than 32 * words with a mask; out dev bf16 [total][n_heads][D] dense, not over q; rows of no sequence are left as they were.
  * Rows without a page are left out and record DL_ERR_INVALID_ARG with b.  NaN and infinities in rows that nobody may see do not
  * matter; in v of a node, they may reach every row of its tree (0 * NaN in a matrix product). */
 int32_t dl_kv16_attn_tree(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, const void* pool, const void* q,
@@ -582,7 +584,8 @@ enum {
  *   draft dev [total][vocab] fp32 or NULL; row strides in elements (0: vocab); u dev [total] in [0, 1) (outside: held to it);
  *   tokens, parent dev [total] (the root's are not read);
  *   keep_out dev [total]: 1 for the root and the accepted nodes, else 0; count_out dev [B]: their number; next_out dev [B]: the
- *   token drawn; a sequence without nodes gets 0 and -1.  vocab up to 262144, up to 2048 nodes a sequence.
+ *   token drawn; a sequence without nodes gets 0 and -1.  vocab up to 262144, up to 2048 nodes a sequence (those
+ *   behind are not reached, and DL_ERR_INVALID_ARG is recorded with the sequence).
  * A token outside the vocabulary is rejected without further effect, a parent as in dl_tree_plan is never reached; both record
  * DL_ERR_INVALID_ARG with the sequence, as a row without any positive entry does (next -1). */
 int32_t dl_tree_verify(dl_ctx* ctx, const void* target, int32_t dtype, int64_t target_stride, const float* draft,
@@ -592,7 +595,7 @@ int32_t dl_tree_verify(dl_ctx* ctx, const void* target, int32_t dtype, int64_t t
 
 /* Keeps, of every sequence's rows behind len[b] (the nodes [starts[b], starts[b + 1]) appended there), those whose keep flag is not
  * 0: they move up to row len[b] and on, in order, in all pools, and len[b] += their number.  Rows behind them stay as they are.
- *   pools HOST array of n_pools dev pointers; starts dev [B + 1]; keep dev [total].
+ *   pools HOST array of n_pools dev pointers, none of them twice; starts dev [B + 1]; keep dev [total].
  * A sequence that lacks a page of these rows is left as it was and records DL_ERR_CAPACITY with its index. */
 int32_t dl_kv16_commit(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, int32_t n_pools, void* const* pools,
                        const int32_t* starts, const uint8_t* keep, int32_t total, void* stream);

@@ -1005,6 +1005,8 @@ int32_t dl_kv16_commit(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, i
   for (int32_t i = 0; i < n_pools; ++i) {
     if (!pools[i]) return DL_ERR_INVALID_ARG;
     if (misaligned(pools[i])) return DL_ERR_ALIGNMENT;
+    for (int32_t j = 0; j < i; ++j)
+      if (pools[j] == pools[i]) return DL_ERR_INVALID_ARG;         // its rows would move up twice
   }
   if (pages->B == 0 || total == 0) return DL_OK;
   if (!starts || !keep) return DL_ERR_INVALID_ARG;

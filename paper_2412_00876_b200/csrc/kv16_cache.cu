@@ -349,7 +349,8 @@ kv16_move_kernel(const K16Pages pg, const __grid_constant__ K16Pools pools, int3
 }
 
 // ---- trees ------------------------------------------------------------------------------------------------------------
-// One CTA per sequence: parents in shared memory, a thread per (node, word) walks up.
+// One CTA per sequence: parents in shared memory, a thread per node walks up; ancestors have lower numbers, so it passes the words
+// of its mask once, from the last to the first.
 __global__ void __launch_bounds__(kK16Threads)
 tree_plan_kernel(const int32_t* parent, const int32_t* starts, const int32_t* pos0, int32_t total, int32_t words,
                  int32_t* mask, int32_t* pos, DeviceStatus* st) {
@@ -368,16 +369,17 @@ tree_plan_kernel(const int32_t* parent, const int32_t* starts, const int32_t* po
   if (bad) report_status(st, DL_ERR_INVALID_ARG, b);
   __syncthreads();
   const int first = pos0 ? __ldcg(pos0 + b) : 0;
-  for (int x = threadIdx.x; x < n * words; x += kK16Threads) {
-    const int i = x / words, w = x - i * words;
+  for (int i = threadIdx.x; i < n; i += kK16Threads) {
+    int32_t* row = mask + (size_t)(from + i) * words;
     uint32_t bits = 0;
-    int depth = -1;
+    int depth = -1, w = words - 1;
     for (int j = i; j >= 0; j = up[j]) {
       ++depth;
-      if ((j >> 5) == w) bits |= 1u << (j & 31);
+      for (; w > (j >> 5); --w) { row[w] = (int32_t)bits; bits = 0; }
+      bits |= 1u << (j & 31);
     }
-    mask[(size_t)(from + i) * words + w] = (int32_t)bits;
-    if (w == 0 && pos) pos[from + i] = (int32_t)((uint32_t)first + (uint32_t)depth);
+    for (; w >= 0; --w) { row[w] = (int32_t)bits; bits = 0; }
+    if (pos) pos[from + i] = (int32_t)((uint32_t)first + (uint32_t)depth);
   }
 }
 

@@ -196,7 +196,7 @@ tree_verify_kernel(const TvArgs a) {
   }
   if (bad && rank == 0) report_status(a.status, DL_ERR_INVALID_ARG, b);
   if (rank == 0)
-    for (int i = tid; i < n; i += kTvThreads) a.keep[from + i] = i == 0;
+    for (int i = tid; i < to - from; i += kTvThreads) a.keep[from + i] = i == 0;
   tv_cluster_sync();                                               // (and every CTA is there before anybody tells it something)
   // this thread's part of a row
   const int blocks = kNear ? 1 : (a.vocab + kTvCluster * kTvThreads * kTvBlock - 1) / (kTvCluster * kTvThreads * kTvBlock);

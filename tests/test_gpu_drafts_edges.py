@@ -328,6 +328,52 @@ def test_verify_of_many_sequences_at_once():
 
 
 # ---- refusals of the interface ------------------------------------------------------------------------------------------
+def test_nodes_beyond_what_a_call_takes_are_never_kept():
+    """2048 nodes of a sequence are verified; those behind are reported and count as rejected, whatever lay in the output."""
+    dl, ctx = context(4, 64)
+    n, vocab = 2060, 8
+    target = torch.zeros(n + 6, vocab, device=DEV)
+    target[:, 3] = 1
+    parent = np.concatenate([np.arange(-1, n - 1), np.arange(-1, 5)])
+    keep = torch.full((n + 6,), 7, dtype=torch.uint8, device=DEV)
+    count, nxt = i32([0, 0]), i32([0, 0])
+    ctx.tree_verify(target, None, None, i32(np.full(n + 6, 3)), i32(parent), i32([0, n, n + 6]), "greedy", keep, count, nxt)
+    status = ctx.device_status()
+    assert status[0] == dl.DL_ERR_INVALID_ARG and status[1] == 0
+    assert keep.tolist() == [1] * 2048 + [0] * 12 + [1] * 6
+    assert count.tolist() == [2048, 6] and nxt.tolist() == [3, 3]
+
+
+def test_plans_of_long_chains():
+    """2048 nodes in a row: every word of the mask, in front of the node and behind it."""
+    dl, ctx = context(4, 64)
+    n = 2048
+    mask, pos = torch.full((n + 3, 64), -9, dtype=torch.int32, device=DEV), torch.full((n + 3,), -9, dtype=torch.int32, device=DEV)
+    ctx.tree_plan(i32(np.concatenate([np.arange(-1, n - 1), [-1, 0, 0]])), i32([0, n, n + 3]), i32([5, 7]), mask, pos)
+    want = np.zeros((n + 3, 64), np.uint64)
+    for i in range(n):
+        want[i, :i // 32] = 0xFFFFFFFF
+        want[i, i // 32] = (1 << (i % 32 + 1)) - 1
+    want[n:, 0] = [1, 3, 5]
+    assert np.array_equal(mask.cpu().numpy().view(np.uint32), want.astype(np.uint32))
+    assert pos.tolist() == list(range(5, 5 + n)) + [7, 8, 8] and ctx.device_status()[0] == 0
+
+
+def test_no_pool_is_committed_twice():
+    """The same rows would move up twice: the call is refused, and nothing has moved."""
+    dl, ctx = context(4, 64)
+    pages = dl.Pages(1, 4, 4, 16, DEV)
+    pools = [ctx.kv16_pool(pages, 2) for _ in range(3)]
+    ctx.pages_reserve(pages, i32([8]))
+    for i, p in enumerate(pools):
+        p.copy_(torch.arange(p.numel(), device=DEV).reshape(p.shape) % 97 + i)
+    before = [p.clone() for p in pools]
+    with pytest.raises(dl.DlError) as e:
+        ctx.kv16_commit(pages, [pools[0], pools[1], pools[2], pools[0]], i32([0, 4]), u8(np.array([1, 0, 1, 1])))
+    assert e.value.code == dl.DL_ERR_INVALID_ARG
+    assert all(torch.equal(a, b) for a, b in zip(pools, before)) and pages.cache_len.tolist() == [0]
+
+
 def test_refusals():
     import ctypes as C
     dl, ctx = context(8, 64, B=4)
