@@ -22,8 +22,12 @@
 namespace dl {
 
 constexpr int kTrPatience = 4000, kTrTurnTiles = 4;                // polls for a turn, tiles from which lanes take turns (attn_packed_tc.cu)
-constexpr int kTrRegsSmall = 40, kTrRegsSoftmax = 232;             // as there
-constexpr int kTrWholeTiles = 6;                                   // key tiles up to which items are not cut
+// Registers per thread (the kernel starts every thread at 168): the warps that issue and load walk the items, for which 40 are too
+// few (spilled, they hold up every hand-over: 1024 items of five key tiles 112 us, with 72 103, with 88 101; chunks of 1000 rows
+// 432, 411, 417; four trees of 17-32 nodes with 8 heads over 95 thousand rows 225, 204, 217); the softmax warps do with 216.
+constexpr int kTrRegsSmall = 72, kTrRegsSoftmax = 216;
+static_assert(128 * kTrRegsSmall + 256 * kTrRegsSoftmax <= kTrThreads * 168, "more registers than the launch has");
+template <int F> static constexpr int tr_whole_tiles() { return F == kTrRows ? 6 : 12; }      // key tiles up to which items are not cut
 
 template <int D, int F> struct Tr {
   static constexpr bool kPair = F == kTrPair;
@@ -721,7 +725,7 @@ static cudaError_t tr_launch(dl_ctx* ctx, const TrMaps& maps, const K16Pages& pg
   // row's pages hold few key tiles, a join would cost more than the CTA that has a tile more than others).
   const long long row_tiles = std::min(std::min<long long>((long long)pg.B * ((a.max_rows + a.PB - 1) / a.PB), (long long)a.total), 1LL << 20);
   const long long key_tiles = (((long long)pg.W << pg.shift) + a.max_rows + kTrBN - 1) / kTrBN;
-  a.whole = key_tiles <= kTrWholeTiles;
+  a.whole = key_tiles <= tr_whole_tiles<F>();
   const int ranges = (int)std::min<long long>(ctx->sm_count, std::max(1LL, row_tiles * a.Hk * (a.whole ? 1 : key_tiles + tr_extra<F>())));
   cudaError_t e;
   if constexpr (F == kTrRows) {
