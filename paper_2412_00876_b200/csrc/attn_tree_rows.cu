@@ -16,6 +16,15 @@
 //   warp 9    : issues the MMAs
 //   warp 10   : allocates tensor memory (256 columns: S^T, S^T, O^T, O^T)
 // Every wait is bounded (pipeline.cuh); an abort leaves DL_ERR_TIMEOUT in the status word.
+//
+// Bound by memory where there is much of it: 48 single tokens over 500 to 9000 rows, 8 K/V heads, 137 us (6.1 TB/s in all, 7 while it
+// streams).  32 trees of 20-26 nodes, 32 heads of their own, over 272 to 1296 rows: 82 us for 396 MB; what comes on top of the
+// 61 us of copying is fixed: 6 us until the first tiles are there, the uneven end, the joining of parts (6 us cold).
+// Up to 64 rows: with 65 to 128 (N = 128) the exponentials of a tile cost as much as in attn_tree_tc.cu, without its two lanes.
+// N = 16 and 32 beside 64: a tile costs N exponentials and N columns of P^T whatever the rows are (one token with 4 heads a
+// group 139 us with N = 16).  Both rows on M, one lane and two CTAs a multiprocessor: 101 us instead of 82 for the trees.
+// Four warps of exponentials instead of eight 110 (90 then), the sums of an item's end behind the next one's first tile
+// 89 (83 then), the next item's page numbers requested early: no change.
 #include <algorithm>
 
 #include "attn_prefill_softmax.cuh"
@@ -24,7 +33,9 @@
 namespace dl {
 
 constexpr int kRwProducer = 8, kRwIssuer = 9, kRwAlloc = 10, kRwCheck = 11;
-constexpr float kRwFar = 1048576.f;      // a thread's sum of exponentials above which the maxima are looked for again
+// A thread's sum of exponentials above which the maxima are looked for again: far enough that it is rare; P in bf16 and sums in
+// fp32 keep their relative accuracy at that size as at any other.
+constexpr float kRwFar = 1048576.f;
 
 template <int D, int N> struct Rw {
   static constexpr int HALF = 128 * 128;               // 128 rows of 64 dims

@@ -14,6 +14,16 @@
 // of its own, and an item's end adds the two up.  More rows (kTrPair): each lane has a tile of rows, and a K/V tile serves both.
 // Up to 64 rows go the other way round, keys across the matrix unit's rows: attn_tree_rows.cu.
 // Every wait is bounded (pipeline.cuh); an abort leaves DL_ERR_TIMEOUT in the status word.
+//
+// Bound by a lane's chain of about 2.3 us a tile.  Chunks of 900-1100 nodes over 3000-8000 rows (32 heads, 8 of K/V): 380 GFLOP in 372 us
+// on its own, 1.03 PFLOP/s, and 22 us (cold) of joining; 395-425 among others, under the power limit.  Four trees of 32-48 nodes, 8
+// heads each, over 60-131 thousand rows: three tiles of rows in two passes over K and V, 340-385 us.
+// Two lanes through ONE ring, each waiting for its own tiles only, lose data: see Tr.  Odd last tiles of rows given to both lanes
+// inside the kernel for pairs made those trees 321-337 us, but chunks 433-474 and short contexts 5 to 15 % slower.
+// The masked form of the pass unrolled like the other one: 101 -> 119 us where it matters most (instruction cache).  Visible keys looked up
+// before the wait for scores: no gain.  Extra units of an item 1 instead of 4: 40.8 -> 42.6 us (100 nodes, 16 thousand rows), 61 -> 66.
+// Joining: by arithmetic on the ranges instead of a search through their heads 4 us less; three or four CTAs of it a
+// multiprocessor instead of two no change.
 #include <algorithm>
 
 #include "attn_packed_softmax.cuh"

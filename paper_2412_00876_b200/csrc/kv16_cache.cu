@@ -4,11 +4,19 @@
 //   plan   : (with a keep mask or a commit) per sequence, count the kept rows and list them in front of the others, check that
 //            their pages are there, note the first destination row, advance the length: one CTA per sequence;
 //   append : a CTA takes a few packed rows; cos and sin of those that are kept or asked for go to shared memory once and serve all
-//            heads; then every thread moves 32 bytes at a time (both halves of 8 pairs), four such units in flight, q to q_out, k to
+//            heads; then every thread moves 32 bytes at a time (both halves of 8 pairs), two such units in flight, q to q_out, k to
 //            k_out and the cache, v to the cache;
 //   commit : accepted rows move up; a thread stays at one 16-byte column of one pool, tensor and head and walks the rows in
 //            order, so that no row is overwritten before it has been read;
 //   tree   : ancestors' bits and depths of tree nodes.
+//
+// The append is bound by memory: 23 thousand rows of 32 + 2 x 8 heads 111 us, 5.5 TB/s moved; a batch of which a mask keeps a part
+// (22 thousand rows of 32 + 32 heads, 8 thousand kept) 65 us with its plan of 6 us, and there the rows kept are far apart.  Between
+// the first load and the last store lie the row's place, the angles and the rotation, so what counts is how many CTAs are at
+// different points of that: (rows a CTA, units in flight, CTAs a multiprocessor), both batches in us: 16, 4, 4: 78.5 and 124;
+// 4, 4, 4: 83, 122; 8, 4, 4: 74, 116; 8, 2, 8: 77, 129; 8, 2, 6 as here.  A fixed unit per thread: 64-72 and 117-137, a grid of
+// resident CTAs that take rows in turn: 70-98 and 111-122.  Flags counted by every CTA instead of listed by the plan: 77 and 120.
+// Moving accepted rows takes 7 us for 32 sequences of four layers, launch and two dependent looks at the books included.
 #include <algorithm>
 
 #include "kv16.cuh"
