@@ -62,16 +62,19 @@ kv16_plan_kernel(const K16Pages pg, const int32_t* starts, const uint8_t* keep, 
       }
       return m;
     };
-    int c = 0;
-    for (int at = first + 4 * (int)threadIdx.x; at < to; at += kStep) c += __popc(flags(at));
+    const bool once = to - first <= kStep;                         // all flags at a time: their number comes with the places
+    if (!once) {
+      int c = 0;
+      for (int at = first + 4 * (int)threadIdx.x; at < to; at += kStep) c += __popc(flags(at));
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
-    if (lane == 0) sh[0][warp] = c;
-    __syncthreads();
-    c = sh[0][lane];
+      for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+      if (lane == 0) sh[0][warp] = c;
+      __syncthreads();
+      c = sh[0][lane];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
-    count = c;
+      for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+      count = c;
+    }
     int kept = from, turn = 1;                                     // place of the next kept row
     for (int i0 = first; i0 < to; i0 += kStep, turn ^= 1) {
       const int at = i0 + 4 * (int)threadIdx.x;
@@ -93,6 +96,8 @@ kv16_plan_kernel(const K16Pages pg, const int32_t* starts, const uint8_t* keep, 
         const int v = __shfl_up_sync(0xffffffffu, all, o);
         if (lane >= o) all += v;
       }
+      const int of_step = __shfl_sync(0xffffffffu, all, 31);
+      if (once) count = of_step;
       int front = kept + run - n + __shfl_sync(0xffffffffu, all - mine, warp);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -101,7 +106,7 @@ kv16_plan_kernel(const K16Pages pg, const int32_t* starts, const uint8_t* keep, 
         order[f ? front : from + count + (at + i - from) - (front - from)] = at + i;
         front += f;
       }
-      kept += __shfl_sync(0xffffffffu, all, 31);
+      kept += of_step;
     }
   }
   if (threadIdx.x == 0) {
