@@ -10,12 +10,13 @@
 //            order, so that no row is overwritten before it has been read;
 //   tree   : ancestors' bits and depths of tree nodes.
 //
-// The append is bound by memory: 23 thousand rows of 32 + 2 x 8 heads 111 us, 5.5 TB/s moved; a batch of which a mask keeps a part
-// (22 thousand rows of 32 + 32 heads, 8 thousand kept) 65 us with its plan of 6 us, and there the rows kept are far apart.  Between
+// The append is bound by memory: 23 thousand rows of 32 + 2 x 8 heads 104.5 us, 5.8 TB/s moved; a batch of which a mask keeps a part
+// (22 thousand rows of 32 + 32 heads, 8 thousand kept) 60 us with its plan of 6 us, and there the rows kept are far apart.  Between
 // the first load and the last store lie the row's place, the angles and the rotation, so what counts is how many CTAs are at
 // different points of that: (rows a CTA, units in flight, CTAs a multiprocessor), both batches in us: 16, 4, 4: 78.5 and 124;
-// 4, 4, 4: 83, 122; 8, 4, 4: 74, 116; 8, 2, 8: 77, 129; 8, 2, 6 as here.  A fixed unit per thread: 64-72 and 117-137, a grid of
-// resident CTAs that take rows in turn: 70-98 and 111-122.  Flags counted by every CTA instead of listed by the plan: 77 and 120.
+// 8, 4, 4: 74, 116; 8, 2, 8: 77, 129; 12, 10, 8, 6, 5, 4, 3, 2 with 2, 6: 66, 64, 64.5, 62, 60, 60, 62, 67 and 117, 112, 110.5, 107,
+// 107, 104.5, 107, 111; 4, 3, 5: 66, 114; 4, 1, 8: 58.5, 106.5; 4, 2, 7 (spills): 67, 119.  A fixed unit per thread: 64-72 and 117-137, a
+// grid of resident CTAs that take rows in turn: 70-98 and 111-122.  Flags counted by every CTA instead of listed by the plan: 77, 120.
 // Moving accepted rows takes 7 us for 32 sequences of four layers, launch and two dependent looks at the books included.
 #include <algorithm>
 
@@ -24,7 +25,7 @@
 namespace dl {
 
 constexpr int kK16Threads = 256;
-constexpr int kK16Rows = 8;              // most packed rows per CTA of the append
+constexpr int kK16Rows = 4;              // most packed rows per CTA of the append
 constexpr int kK16Batch = 2;             // units of 32 bytes a thread has in flight
 constexpr int kK16Ctas = 6;              // CTAs of it a multiprocessor holds
 constexpr int kK16PlanThreads = 1024;
