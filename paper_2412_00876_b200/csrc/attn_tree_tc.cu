@@ -19,7 +19,9 @@
 // on its own, 1.03 PFLOP/s, and 22 us (cold) of joining; 395-425 among others, under the power limit.  Four trees of 32-48 nodes, 8
 // heads each, over 60-131 thousand rows: three tiles of rows in two passes over K and V, 340-385 us.
 // Two lanes through ONE ring, each waiting for its own tiles only, lose data: see Tr.  Odd last tiles of rows given to both lanes
-// inside the kernel for pairs made those trees 321-337 us, but chunks 433-474 and short contexts 5 to 15 % slower.
+// inside the kernel for pairs made those trees 321-360 us, but chunks 433-474 and short contexts 5 to 15 % slower; in a launch of their
+// own: 368 instead of 375, and trees without such a tile 3 to 5 % slower.  The producer telling the others its items instead of
+// everyone's own walk: 1 to 3 us more an item.
 // The masked form of the pass unrolled like the other one: 101 -> 119 us where it matters most (instruction cache).  Visible keys looked up
 // before the wait for scores: no gain.  Extra units of an item 1 instead of 4: 40.8 -> 42.6 us (100 nodes, 16 thousand rows), 61 -> 66.
 // Joining: by arithmetic on the ranges instead of a search through their heads 4 us less; three or four CTAs of it a
