@@ -20,9 +20,12 @@
 // Bound by memory where there is much of it: 48 single tokens over 500 to 9000 rows, 8 K/V heads, 137 us (6.1 TB/s in all, 7 while it
 // streams).  32 trees of 20-26 nodes, 32 heads of their own, over 272 to 1296 rows: 82 us for 396 MB; what comes on top of the
 // 61 us of copying is fixed: 6 us until the first tiles are there, the uneven end, the joining of parts (6 us cold).
-// Up to 64 rows: with 65 to 128 (N = 128) the exponentials of a tile cost as much as in attn_tree_tc.cu, without its two lanes.
-// N = 16 and 32 beside 64: a tile costs N exponentials and N columns of P^T whatever the rows are (one token with 4 heads a
-// group 139 us with N = 16).  Both rows on M, one lane and two CTAs a multiprocessor: 101 us instead of 82 for the trees.
+// N = 16 and 32 beside 64: a tile costs N exponentials and N columns of P^T whatever the rows are.  The trees take 83 us with N = 32
+// and 118 with 64; trees of 5-16 nodes 79 with 16, 80.5 with 32, 107 with 64; the single tokens 138, 139, 144.5.
+// Up to 64 rows: from 33 on this and attn_tree_tc.cu are even over much memory (32 trees of 33-64 nodes 121 and 118 us, 32 of 5-8 nodes
+// with 8 heads 88 both, 4 of those over 60-131 thousand rows 130 and 126), and where a few items share all CTAs this is
+// faster (2 trees of 16 nodes over 4000 rows 17.2 and 19.5, 32 tokens with 64 heads a group 32 and 35).
+// The trees with rows on M, one lane and two CTAs a multiprocessor: 101 us instead of 82.
 // Four warps of exponentials instead of eight 110 (90 then), the sums of an item's end behind the next one's first tile
 // 89 (83 then), the next item's page numbers requested early: no change.
 #include <algorithm>

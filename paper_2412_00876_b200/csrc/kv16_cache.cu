@@ -425,7 +425,9 @@ cudaError_t launch_kv16_append(const dl_ctx* ctx, const dl_pages* p, int32_t Hk,
   const int units = ((q_out ? H : 0) + (pool ? 2 : 1) * Hk) * (D / 16);
   a.per_row = (uint32_t)units;
   a.per_row_inv = (uint32_t)(((1ull << 32) + units - 1) / units);
-  // Rows per CTA: as many as leave four CTAs a multiprocessor; fewer rows than that are shared by several CTAs (grid y).
+  // Rows per CTA: as many as leave four CTAs a multiprocessor; fewer rows than that are shared by several CTAs (grid y).  With 32
+  // heads and 32 of K/V, 1280, 1600, 2000 rows: 22.6, 24.8, 28.2 us; if two or one CTA a multiprocessor are left 24.9, 26.7, 29.0;
+  // always four rows a CTA 24.9, 26.7, 29.0 (fewer rows wait for the host's call, 22 us with a plan of the tree, in every form).
   a.rows = std::min(kK16Rows, std::max(1, total / (4 * ctx->sm_count)));
   const int slices = a.rows > 1 ? 1 : std::min((units + kK16Threads - 1) / kK16Threads, std::max(1, 8 * ctx->sm_count / total));
   const dim3 grid((total + a.rows - 1) / a.rows, slices);
