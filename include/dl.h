@@ -581,7 +581,8 @@ enum {
  * written, sums over r of trunc(r * 2^44), the drawn token's bound (trunc(u * 2^31) * sum) >> 31; no result depends on timing.
  * GREEDY compares values (NaN counts as -infinity; -0 equals +0) and draws the first largest.
  *   target dev [total][vocab] fp32 probabilities, or with GREEDY fp32 or bf16 (`dtype`), probabilities or logits alike;
- *   draft dev [total][vocab] fp32 or NULL; row strides in elements (0: vocab); u dev [total] in [0, 1) (outside: held to it);
+ *   draft dev [total][vocab] fp32 or NULL; row strides in elements (0: vocab); u dev [total] in [0, 1) (outside: held
+ *   to it, below and NaN as 0, from 1 on as the last fp32 number below 1, the root's as 1 - 2^-31);
  *   tokens, parent dev [total] (the root's are not read);
  *   keep_out dev [total]: 1 for the root and the accepted nodes, else 0; count_out dev [B]: their number; next_out dev [B]: the
  *   token drawn; a sequence without nodes gets 0 and -1.  vocab up to 262144, up to 2048 nodes a sequence (those

@@ -72,6 +72,11 @@ def held01(x: float) -> float:
     return (x if x < 1.0 else 1.0) if x > 0.0 else 0.0
 
 
+def number(u, last: float = 1.0 - 2.0 ** -24) -> float:
+    """a random number held to [0, last]; NaN counts as 0"""
+    return min(max(float(u), 0.0), last) if float(u) == float(u) else 0.0
+
+
 def first_largest(row) -> int:
     best, at = -math.inf, 0
     for v, x in enumerate(row):
@@ -111,13 +116,13 @@ def verify(target, draft, u, tokens, parent, mode):
             yes = c == best
         elif mode == "point":
             p = 0.0 if c in dead else float(target[at][c])
-            yes = float(u[i]) * R < p
+            yes = number(u[i]) * R < p
             if not yes:
                 R -= p
                 dead.add(c)
         else:
             p, q = float(target[at][c]), float(draft[at][c])
-            yes = a > 0.0 and (float(u[i]) * q) * R < held01(p - s * q) * a
+            yes = a > 0.0 and (number(u[i]) * q) * R < held01(p - s * q) * a
             if not yes and a > 0.0:
                 s = s + R / a
                 R = float(sum(left(s))) / UNIT
@@ -136,7 +141,7 @@ def verify(target, draft, u, tokens, parent, mode):
     W = sum(w)
     if W == 0:
         return keep, -1
-    k = min(max(int(float(u[0]) * 2.0 ** 31), 0), 2 ** 31 - 1) if not math.isnan(float(u[0])) else 0
+    k = int(number(u[0], 1.0 - 2.0 ** -31) * 2.0 ** 31)
     bound, run = (k * W) >> 31, 0
     for v, x in enumerate(w):
         run += x

@@ -55,6 +55,8 @@ __device__ __forceinline__ void tv_tell(unsigned long long* word, uint32_t rank,
   asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(there), "l"(v) : "memory");
 }
 
+// a child's random number, held to [0, 1): below 0 and NaN as 0, from 1 on as the last number in front of it
+__device__ __forceinline__ float tv_number(float u) { return fminf(fmaxf(u, 0.f), 0x1.fffffep-1f); }
 __device__ __forceinline__ double tv_held(double x) { return x > 0.0 ? (x < 1.0 ? x : 1.0) : 0.0; }
 // (p - s q held to 0..1) in units of 2^-44, cut off: from p 2^44 and s 2^44, which round as p and s do; NaN converts to the least
 // number, what is too large to the largest
@@ -190,7 +192,7 @@ tree_verify_kernel(const TvArgs a) {
     up[i] = p;
     tok[i] = t;
     if (!kGreedy) {
-      un[i] = u;
+      un[i] = i > 0 ? tv_number(u) : u;                            // (the root's is held where the token is drawn)
       pc[i] = p >= 0 ? to_f32<T>(target[(from + p) * a.target_stride + t]) : 0.f;
       qc[i] = kDraft && p >= 0 ? __ldcg(a.draft + (from + p) * a.draft_stride + t) : 0.f;
     }
