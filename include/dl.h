@@ -556,8 +556,9 @@ int32_t dl_kv16_append(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, v
  *   nodes 0..i (a chain, the next chunk of a prompt, or the single token of a step without drafts);
  *   max_rows HOST: no sequence has more nodes (nodes behind it are not computed, and DL_ERR_INVALID_ARG is recorded), nor more
  *   than 32 * words with a mask; out dev bf16 [total][n_heads][D] dense, not over q; rows of no sequence are left as they were.
- * Rows without a page are left out and record DL_ERR_INVALID_ARG with b.  NaN and infinities in rows that nobody may see do not
- * matter; in v of a node, they may reach every row of its tree (0 * NaN in a matrix product). */
+ * Rows without a page are left out and record DL_ERR_INVALID_ARG with b.  A row whose scores hold a NaN or +infinity among
+ * what it sees is NaN.  NaN and infinities in rows that nobody may see do not matter; in v of a node, they may reach every row of
+ * its tree (0 * NaN in a matrix product). */
 int32_t dl_kv16_attn_tree(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, const void* pool, const void* q,
                           int64_t q_stride, const int32_t* starts, int32_t total, int32_t max_rows, const int32_t* mask,
                           int32_t words, float scale, void* out, void* stream);

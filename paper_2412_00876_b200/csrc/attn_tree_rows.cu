@@ -507,7 +507,7 @@ attn_tree_rows_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, co
       float* part = a.parts + ((size_t)blockIdx.x * 2 + (I.first ? 0 : 1)) * kPartFloats;
       if (t < kW) {
         const float l = (red[t] + red[64 + t]) + (red[128 + t] + red[192 + t]);
-        l_s[t] = l > 0.f ? 1.0f / l : 0.f;
+        l_s[t] = l != 0.f ? 1.0f / l : 0.f;                            // (a NaN sum is the row's)
         if (!whole && t < rows) reinterpret_cast<float2*>(part)[col0 + t] = make_float2(m_s[t], l);
       }
       rw_sync(half);

@@ -470,7 +470,7 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
           tc_fence_after();
         }
         if (!whole && owned) reinterpret_cast<float2*>(part)[part_row] = make_float2(m_used, l_run);
-        const float inv = l_run > 0.f ? 1.0f / l_run : 0.f;
+        const float inv = l_run != 0.f ? 1.0f / l_run : 0.f;             // (a NaN sum is the row's)
         if (n_sub > 0) {
           if (active) {
 #pragma unroll 1
@@ -515,9 +515,9 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
           const float2 twin = exch[(x ^ 1) * 128 + row];
           asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");       // read before the next item writes
           const float m = fmaxf(m_used, twin.x);
-          const float w_me = l_run > 0.f ? fast_exp2(m_used - m) : 0.f, w_tw = twin.y > 0.f ? fast_exp2(twin.x - m) : 0.f;
+          const float w_me = l_run != 0.f ? fast_exp2(m_used - m) : 0.f, w_tw = twin.y != 0.f ? fast_exp2(twin.x - m) : 0.f;
           const float l = l_run * w_me + twin.y * w_tw;
-          const float inv = whole ? (l > 0.f ? 1.0f / l : 0.f) : 1.f;
+          const float inv = whole ? (l != 0.f ? 1.0f / l : 0.f) : 1.f;
           const float f_me = w_me * inv, f_tw = w_tw * inv;
           const uint32_t base = tmem + lane_off + kAtColO + x * (D / 2);
           if (!whole && owned && x == 0) reinterpret_cast<float2*>(part)[row] = make_float2(m, l);
@@ -528,10 +528,10 @@ attn_tree_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, const T
             tmem_ld32(base + x * kAtLaneCols + c, p);
             tmem_ld32(base + (x ^ 1) * kAtLaneCols + c, q);
             tmem_ld_wait();
-            // (a lane without a sum has left whatever was in tensor memory: not 0 times that, but nothing)
+            // (a lane without a sum has left whatever was in tensor memory: not 0 times that, but nothing; NaN weights stay)
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
-              const float u0 = w_me > 0.f ? __uint_as_float(p[i]) * f_me : 0.f, u1 = w_tw > 0.f ? __uint_as_float(q[i]) * f_tw : 0.f;
+              const float u0 = w_me != 0.f ? __uint_as_float(p[i]) * f_me : 0.f, u1 = w_tw != 0.f ? __uint_as_float(q[i]) * f_tw : 0.f;
               p[i] = __float_as_uint(u0 + u1);
             }
             if (owned && whole) {
@@ -593,7 +593,7 @@ constexpr int kTrJoinMany = 16;                                    // parts from
 // Sums of a row: relative to the maximum m, over parts.
 template <int E> struct TrSum { float m, l, o[E]; };
 template <int E> __device__ __forceinline__ void tr_add(TrSum<E>& s, float m, float l, const float* o) {
-  if (!(l > 0.f)) return;                                          // (a part without a sum has no values either)
+  if (l == 0.f) return;                                            // (a part without a sum has no values either; a NaN stays one)
   const float top = fmaxf(s.m, m), c = exp2f(s.m - top), w = exp2f(m - top);
   s.m = top;
   s.l = s.l * c + l * w;
@@ -642,7 +642,7 @@ attn_tree_join_kernel(const TrArgs a, int32_t ranges) {
   auto row_in_part = [&](int r) { return kPair && r >= a.PB * a.G ? 128 + r - a.PB * a.G : r; };
   auto store = [&](int r, const TrSum<E>& s) {
     const int node = r / a.G, head = r - node * a.G;
-    const float inv = s.l > 0.f ? 1.f / s.l : 0.f;
+    const float inv = s.l != 0.f ? 1.f / s.l : 0.f;
     const size_t at = ((size_t)(hd.row0 + hd.q0 + node) * a.H + hd.h * a.G + head) * D + lane * E;
     if (!DL_IN_BOUNDS(a.status, KID_TREE, at + E - 1, (size_t)a.total * a.H * D)) return;
 #pragma unroll
