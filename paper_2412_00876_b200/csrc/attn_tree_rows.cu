@@ -459,7 +459,8 @@ attn_tree_rows_kernel(const __grid_constant__ TrMaps maps, const K16Pages pg, co
             s[c] = __float_as_uint(e0);
             s[c + 1] = __float_as_uint(e1);
           }
-          if (!rw_any(half, !look && sum + sum2 > kRwFar)) break;
+          // (the sum is over the half's rows, those of nobody among them: a NaN in one must not hide that another one's is too large)
+          if (!rw_any(half, !look && !(sum + sum2 <= kRwFar))) break;
           look = true;                                             // the tile is done over under its own maxima
         }
         tc_fence_before();
