@@ -539,6 +539,7 @@ int64_t dl_kv16_page_bytes(const dl_ctx* ctx, int32_t n_kv_heads, int32_t page_r
  *   *_stride: elements from one token's row to the next (0: dense), multiples of 8; q_out and k_out may be q and k themselves
  *   (with the same strides), but not lie over anything else; pos dev [total] (may be NULL without rotation); rope HOST
  *   struct or NULL (no rotation); starts dev [B + 1], ascending; keep dev [total] or NULL (all).
+ * The rows of q (if any), k and v (with a cache) of one token hold less than 2^19 values together (DL_ERR_UNSUPPORTED).
  * The pages must be reserved: a sequence that lacks one is left as it was and records DL_ERR_CAPACITY with its index (q_out and
  * k_out are written).  A call with `keep` lists its rows in the workspace: up to 33,000 rows a multiprocessor with D = 64, twice as
  * many with 128 (DL_ERR_WORKSPACE).  Pages that other sequences share must not be written: a fork leaves every partly filled page to one.

@@ -948,8 +948,9 @@ int32_t dl_kv16_append(dl_ctx* ctx, const dl_pages* pages, int32_t n_kv_heads, v
   // the list of rows with a mask lies in the scratch of the attention calls
   if (pages && keep && total > std::max(kv4_scratch_floats(ctx->sm_count, ctx->desc), attn_tree_scratch_floats(ctx->sm_count, ctx->desc)))
     return DL_ERR_WORKSPACE;
-  // units of 32 bytes are counted in 32 bits, a few rows of them at a time
-  if ((qw + 2 * kw) >= (1 << 15)) return DL_ERR_UNSUPPORTED;
+  // Units of 32 bytes of up to four rows are told apart by a product with 2^32 / units, rounded up: exact as long as
+  // 4 units^2 stays below 2^32.
+  if ((q ? qw : 0) + (pages ? 2 : 1) * kw >= (1LL << 19)) return DL_ERR_UNSUPPORTED;
   DeviceGuard g(ctx->device);
   return cuda_status(ctx, launch_kv16_append(ctx, pages, n_kv_heads, pool, q, q_stride, k, v, kv_stride, pos, rope, starts, keep,
                                              total, q_out, q_out_stride, k_out, k_out_stride, commit,

@@ -423,6 +423,7 @@ cudaError_t launch_kv16_append(const dl_ctx* ctx, const dl_pages* p, int32_t Hk,
     if (e != cudaSuccess) return e;
   }
   const int units = ((q_out ? H : 0) + (pool ? 2 : 1) * Hk) * (D / 16);
+  static_assert(kK16Rows <= 4, "units of a call's widest rows (2^15) would not be told apart: see the check of the arguments");
   a.per_row = (uint32_t)units;
   a.per_row_inv = (uint32_t)(((1ull << 32) + units - 1) / units);
   // Rows per CTA: as many as leave four CTAs a multiprocessor; fewer rows than that are shared by several CTAs (grid y).  With 32
