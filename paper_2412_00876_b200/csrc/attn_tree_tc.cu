@@ -84,7 +84,9 @@ __device__ __forceinline__ uint32_t tr_mask_bits(const int32_t* row, int words, 
 __device__ __forceinline__ uint32_t tr_low(int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u; }
 
 // The softmax of a tile of which a row sees the columns whose bits are set in vis (bit c of word q: column 32 q + c): 32 columns at a
-// time in a rolled loop; otherwise as in attn_prefill_softmax.cuh.
+// time in a rolled loop; otherwise as in attn_prefill_softmax.cuh, but for the step by which a row's maximum is raised: whole powers of
+// two, so that what the tile has stored as bf16 already keeps its bits when it is scaled down, and P is rounded once only.  (By the
+// difference itself P was rounded twice in such rows, 2.8 half steps of the output in all instead of 2.)
 __device__ __forceinline__ void tr_softmax_words(uint32_t s_addr, uint32_t o_addr, int n_ch, const uint32_t (&vis)[4], bool owned,
                                                  int o_blocks, float scale_log2, float& m_used, float& l_run) {
   const uint64_t sc2 = pack2(scale_log2, scale_log2);
@@ -109,8 +111,9 @@ __device__ __forceinline__ void tr_softmax_words(uint32_t s_addr, uint32_t o_add
       const float mc = fmax3(mx4[0], mx4[1], fmaxf(mx4[2], mx4[3])) * scale_log2;
       const bool need = owned && mc > m_used + kRescaleStep;
       if (__any_sync(0xffffffffu, need)) {
-        const float corr = need ? fast_exp2(m_used - mc) : 1.0f;
-        if (need) m_used = mc;
+        const float m_old = m_used;
+        if (need) m_used = m_old < -1e38f ? mc : m_old + ceilf(mc - m_old);              // (a first maximum has nothing in front of it)
+        const float corr = need ? fast_exp2(m_old - m_used) : 1.0f;
         l_run *= corr;
         at_rescale_row(o_addr, s_addr, q, corr, o_blocks);
       }
