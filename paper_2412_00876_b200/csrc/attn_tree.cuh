@@ -8,7 +8,8 @@
 // An item costs more than its key tiles (its masked tile, the hand-over to the next one, its outputs): it counts tr_extra() units
 // more, in front of its tiles, so that a range of many short items holds fewer tiles.
 // Short contexts (TrArgs::whole) are not cut: a range holds whole items, as many as the others or one more, and nothing is
-// joined.  With up to 64 rows an item that goes up to 6 key tiles.  4 nodes with 32 heads, 8 key heads: 8 sequences of 60, 200 and
+// joined.  The host decides, by what a row of the table has columns for: a wide table is cut whatever the lengths are.  With up to 64
+// rows an item that goes up to 6 key tiles.  4 nodes with 32 heads, 8 key heads: 8 sequences of 60, 200 and
 // 400 rows 10.3, 12.7 and 14.9 us cut, 7.8, 8.8 and 10.7 whole; 32 sequences 12.4, 20.0 and 24.8 cut, 11.3, 15.3 and 20.4 whole.
 // 40 uneven sequences of up to 400 rows with 32 key heads, where a CTA has nine items, lose 63.5 -> 67.6, those of up to 200 win
 // 54.5 -> 51.4; up to 10 tiles 85 -> 90, up to 12 82 -> 95.  More rows leave larger parts, so there it is 12: 32 heads, 50-100 nodes

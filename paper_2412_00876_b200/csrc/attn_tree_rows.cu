@@ -5,11 +5,12 @@
 // the columns.
 //   S^T [128 keys][N] = K Q^T;   P^T = 2^(S^T scale - m), one key per thread;   O^T [D dims][N] += V^T P^T
 // K and V are read from shared memory as they come (V^T is V with the roles of its indices exchanged), P^T goes through shared
-// memory as 64-byte rows of keys.  So a tile costs a thread N exponentials instead of 128, all four warps have work however few the
-// rows are, the masked form of the pass is the same code with N selects in front, S^T and O^T take so few columns of tensor
+// memory as 64-byte rows of keys.  So a tile costs a thread N / 2 exponentials instead of 128, all eight warps have work however few
+// the rows are, the masked form of the pass is the same code with N selects in front, S^T and O^T take so few columns of tensor
 // memory that both are kept twice: K Q^T of the next tile, across the ends of items, too, runs beside the exponentials.
 // What a row needs across keys is across threads here: its maximum is looked for in a share's first tile only (and again if a
-// score passes it by far: the threads vote), its sum is added up per thread and joined at the share's end.
+// score passes it by far: the threads vote), its sum is added up per thread and joined at the share's end.  P^T is rounded to bf16
+// once, as 16-bit matrix products take it (at most 2^-8 of a weight); sums are of the unrounded weights, in fp32.
 //   warps 0-7 : exponentials and epilogue; thread = key of the tile (lane of tensor memory), later = dim of the output; warps 0-3
 //               the first half of the rows, 4-7 the second: rows have nothing to do with one another
 //   warp 8    : the producer: Q tiles, then K and V tiles through one ring, K a tile ahead

@@ -15,9 +15,12 @@
 // Up to 64 rows go the other way round, keys across the matrix unit's rows: attn_tree_rows.cu.
 // Every wait is bounded (pipeline.cuh); an abort leaves DL_ERR_TIMEOUT in the status word.
 //
+// P is rounded to bf16, as 16-bit matrix products take it, and once only: at most 2^-8 of a weight.  Sums are of the unrounded weights;
+// scores, maxima, sums and the joining are fp32.
+//
 // Bound by a lane's chain of about 2.3 us a tile.  Chunks of 900-1100 nodes over 3000-8000 rows (32 heads, 8 of K/V): 380 GFLOP in 372 us
-// on its own, 1.03 PFLOP/s, and 22 us (cold) of joining; 395-425 among others, under the power limit.  Four trees of 32-48 nodes, 8
-// heads each, over 60-131 thousand rows: three tiles of rows in two passes over K and V, 340-385 us.
+// cold and on its own, 1.03 PFLOP/s, and 22 us of joining; 421-429 us a call among others, 0.89 PFLOP/s.  Four trees of 32-48 nodes, 8
+// heads each, over 60-131 thousand rows: three tiles of rows in two passes over K and V (1.45 GB), 385 us, 15 of them of joining.
 // Two lanes through ONE ring, each waiting for its own tiles only, lose data: see Tr.  Odd last tiles of rows given to both lanes
 // inside the kernel for pairs made those trees 321-360 us, but chunks 433-474 and short contexts 5 to 15 % slower; in a launch of their
 // own: 368 instead of 375, and trees without such a tile 3 to 5 % slower.  The producer telling the others its items instead of
@@ -774,6 +777,8 @@ cudaError_t launch_attn_tree(dl_ctx* ctx, const dl_pages* p, int32_t Hk, const v
   a.said_rows = mask ? (int)std::min<long long>(max_rows, 32LL * words) : max_rows;
   a.max_rows = std::min(a.said_rows, total);
   const int rows = (int)std::min<long long>((long long)a.max_rows * a.G, 1 << 20);
+  // The largest sequence decides for all (the host knows no other).  A chunk of 1000 nodes over 4000 rows (32 heads, 8 of K/V) with 47
+  // single tokens over 500-9000: 261 us, in two calls 96 + 144; with 15 tokens over 500-4000: 134, in two calls 109 + 42.
   const int form = rows <= kTrFewRows ? kTrRows : a.max_rows <= kTrBM / a.G ? kTrSplit : kTrPair;
   a.PB = (form == kTrRows ? kTrFewRows : kTrBM) / a.G;
   a.box_rows = std::min(a.PB, a.max_rows);

@@ -14,8 +14,8 @@
 // row; a warp tells its sum to all CTAs through distributed shared memory, then the cluster's barrier, and all of them know it.
 // Vocabularies of up to 32768 leave 8 values a thread, which stay in registers as long as the node is the one reached.  What bounds a
 // call is the chain of passes of its unluckiest sequence; 40 registers let three CTAs share a multiprocessor, so that 55 sequences
-// go at once (48 trees of 40-64 nodes: 24.4 us, read anew in every pass, as larger vocabularies are, 26.6; with 69 registers, the
-// values kept as 64-bit floats, 34 us; with 64 26 us).
+// go at once (48 trees of 40-64 nodes: 26 us, greedily 20-26 nodes 16; side by side 24.4, read anew in every pass, as larger vocabularies
+// are, 26.6; with 69 registers, the values kept as 64-bit floats, 34 us; with 64 26 us).
 // Measured and not better: bringing rows into L2 when a node is reached (26 us), or those of its children (greedily 15.4 -> 19.7).
 #include <algorithm>
 
